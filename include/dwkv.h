@@ -62,7 +62,7 @@ typedef enum dwkv_status {
                              dwkv_static_scratch_bytes()                           */
 } dwkv_status;
 
-typedef enum dwkv_qtype { DWKV_F16 = 0, DWKV_BF16 = 1 } dwkv_qtype;
+typedef enum dwkv_qtype { DWKV_F16 = 0, DWKV_BF16 = 1, DWKV_F32 = 2 /* dwkv_tree_verify only */ } dwkv_qtype;
 
 /* Shape of one factorized cache (all sequences packed along the token axis). */
 typedef struct dwkv_dims {
@@ -507,6 +507,129 @@ size_t dwkv_dense_workspace_bytes(const dwkv_dims* dims);
 dwkv_status dwkv_dense_decode(const dwkv_dims* dims, const void* k, const void* v, const void* q,
                               int32_t q_type, float sm_scale, float* out, void* workspace,
                               size_t ws_bytes, void* stream);
+
+/* ---- Speculative step: several drafted tokens per sequence ------------------
+ * A program that drafts tokens ahead of the model scores all of them in one
+ * pass over the cache (dwkv_tree_decode), decides which stand
+ * (dwkv_tree_verify) and lays the cache out for them (dwkv_repack, then
+ * dwkv_compress of their keys and values).  The paper decodes one position per
+ * step; these calls run its data path (Sec. 3, Eq. 1) for many. */
+#define DWKV_MAX_TREE_NODES 64    /* drafted nodes of one sequence */
+
+/* The drafted nodes of a batch, packed by sequence.  Node i of a sequence
+ * (0-based inside it) continues its parent, or the cached context. */
+typedef struct dwkv_tree {
+  int32_t n_nodes;               /* N = cu_nodes_host[B], all sequences              */
+  const int32_t* cu_nodes_host;  /* [B+1] packed node starts, host copy; at most
+                                    DWKV_MAX_TREE_NODES nodes per sequence          */
+  const int32_t* cu_nodes;       /* the same [B+1], device copy                      */
+  const int32_t* parent;         /* DEVICE [N]: the parent's index inside the sequence,
+                                    lower than the node's own, or -1 (the context).
+                                    Any other value, or an absent parent, makes the
+                                    node absent: padding of a fixed-size batch       */
+} dwkv_tree;
+
+/* Bytes of device workspace dwkv_tree_decode needs (0 when dims or tree are
+ * invalid). */
+size_t dwkv_tree_workspace_bytes(const dwkv_dims* dims, const dwkv_tree* tree);
+
+/* Attention of a tree of drafted tokens over layer `layer` of the factorized
+ * cache.  Node i of sequence b attends to the T_b cached tokens of b (K_hat,
+ * V_hat of Eq. 1, never written out) and to the dense keys and values of itself
+ * and its ancestors:
+ *   out[i][hq] = softmax(sm_scale q_i . K) V  over  cached tokens, then
+ *                nodes on the path from the context to i, i included
+ * An absent node's rows are zero, and no node sees it.  Nothing a node does not
+ * see changes its row, infinities and NaN included.
+ *   q:          [N] rows of [Hq][d] in q_type, q_stride elements apart
+ *   k_new, v_new: fp16 [N] rows of [Hkv][d], kv_stride elements apart (keys post
+ *               positional encoding, as dwkv_compress takes them)
+ *   q_stride, kv_stride: multiples of 8, 0 = rows without a gap (a fused
+ *               projection's output is read in place)
+ *   sm_scale:   <= 0 selects 1/sqrt(d)
+ *   out:        fp32 [N][Hq][d], written
+ *   workspace:  >= dwkv_tree_workspace_bytes(dims, tree), no initial contents
+ * Both coefficient formats, every basis rank, group and level table that
+ * dims allow.  Scores and value sums are accurate to about float32, as the
+ * decode's.  The coefficients' padding tokens must be finite.  Two launches
+ * (none when N = 0).  Every device pointer 16-byte aligned, parent 4-byte, the
+ * residual and block scales 2-byte. */
+dwkv_status dwkv_tree_decode(const dwkv_dims* dims, const dwkv_cache* cache, int32_t layer, const dwkv_tree* tree,
+                             const void* q, int32_t q_type, int64_t q_stride, const void* k_new, const void* v_new,
+                             int64_t kv_stride, float sm_scale, float* out, void* workspace, size_t ws_bytes,
+                             void* stream);
+
+/* Bytes of device workspace dwkv_tree_verify needs (0 when arguments are invalid). */
+size_t dwkv_tree_verify_workspace_bytes(int32_t batch, const dwkv_tree* tree, int32_t vocab, int32_t max_children);
+
+/* Verification of drafted tokens against the target's probabilities, from
+ * given random numbers, so that the tokens kept are distributed as the
+ * target's.  Node 0 of a sequence is its last known token (its parent is not
+ * read); a node whose parent is not a lower node of its sequence is never
+ * kept.  From node 0 on, the children of the node reached are tested in index
+ * order, at most max_children of them.  With p and q the target's and the
+ * draft's rows of that node, x a child's token and u its number, after k
+ * rejected children:
+ *   draft given (children drawn independently from q):
+ *     r_k = max(p - c_k q, 0),  c_0 = 0, Z_0 = 1,
+ *     Z_k = sum_v r_k(v),  c_{k+1} = c_k + Z_k      (the distribution left after
+ *     k rejections is r_k / Z_k);  the child stands if u q(x) Z_k < r_k(x)
+ *   draft NULL (children chosen without chance, e.g. the most likely tokens):
+ *     r_k = p without the rejected tokens, Z_k = 1 - the sum of their p;
+ *     the child stands if u Z_k < r_k(x)
+ * The walk ends at the node none of whose children stands; the next token is
+ * the first v with sum_{v' <= v} r(v') > u_next sum r, r that node's last r_k
+ * (the first v of largest p when the sum is 0).  All in float64.
+ *   token:  int32 [N] drafted token ids (node 0's not read; an id outside
+ *           [0, vocab) never stands)
+ *   target: [N] rows of vocab in p_type (DWKV_F32, DWKV_F16 or DWKV_BF16), row i
+ *           the target's probabilities after node i; draft: NULL, or the same,
+ *           row i what node i's children were drawn from.  What is not positive
+ *           and finite counts as 0
+ *   u, u_next: fp32 [N] and [B], each in [0, 1)
+ *   path:   out int32 [N]: from cu_nodes[b] on the kept nodes of sequence b in
+ *           order (0 first), then -1;  n_kept: out int32 [B], their count (0 for a
+ *           sequence without nodes);  next: out int32 [B] (-1 then)
+ *   workspace: >= dwkv_tree_verify_workspace_bytes, no initial contents,
+ *           16-byte aligned; the other pointers aligned to their type
+ * max_children is in [1, DWKV_MAX_TREE_NODES].  2 launches, and with a draft
+ * max_children - 1 more. */
+dwkv_status dwkv_tree_verify(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, int32_t p_type,
+                             const void* target, const void* draft, const float* u, const float* u_next,
+                             int32_t max_children, int32_t* path, int32_t* n_kept, int32_t* next, void* workspace,
+                             size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace dwkv_repack needs (0 when dims are invalid). */
+size_t dwkv_repack_workspace_bytes(const dwkv_dims* dst);
+
+/* Copies, forks, compacts, frees and grows: fills the cache `to` (sequences,
+ * lengths and res_stride of dst) with tokens of the cache `from` (of src), all
+ * layers.  Packed token t of `to` is token src_token[t] of `from`, or, when
+ * negative, a fresh slot: slot j = -1 - src_token[t] of n_new, at level
+ * new_code[m][h][j], with zero coefficients, scales and codes (entry e of it at
+ * channel e), ready for dwkv_compress.  A token may be taken more than once (a
+ * fork) or not at all (compaction; a sequence that leaves the batch).
+ *   rank_code, res_off, coefficients (padding tokens zero), block scales,
+ *   res_scale and the entries of every token are written; entries past the
+ *   last token's are left as they were
+ *   basis of sequence b is that of sequence src_seq[b] of `from`; a negative
+ *   src_seq[b] leaves it as it was.  Tokens keep their coefficients, so
+ *   src_token should take sequence b's tokens from src_seq[b]
+ *   src_token: DEVICE int32 [dst T]; src_seq: DEVICE int32 [dst B]
+ *   new_code:  DEVICE uint8 [M][Hkv][n_new], or NULL (level 0)
+ * A source index or slot out of range reads as a fresh slot of level 0, a rank
+ * code out of range as level 0.  A slab whose entries need more than
+ * dst->res_stride - 512 keeps its offsets but not the entries past that
+ * (dwkv_validate reports it).  dst and src agree in everything but the batch,
+ * the lengths, res_stride and split_tokens (else DWKV_E_DIMS), and no array of
+ * `to` overlaps one of `from`.
+ *   workspace: >= dwkv_repack_workspace_bytes(dst), no initial contents
+ * Three launches.  basis, coef_k and coef_v of both caches and workspace
+ * 16-byte aligned, the res_off arrays, src_token and src_seq 4-byte, scales,
+ * res_idx 2-byte. */
+dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_dims* src, const dwkv_cache* from,
+                        const int32_t* src_token, const int32_t* src_seq, const uint8_t* new_code, int64_t n_new,
+                        void* workspace, size_t ws_bytes, void* stream);
 
 /* Number of sink words dwkv_hbm_read writes (its block count). */
 int32_t dwkv_hbm_read_blocks(void);

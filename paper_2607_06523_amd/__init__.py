@@ -10,6 +10,14 @@ provide device memory and the current HIP stream.
     codes, offsets = cache.route(phi, u, theta)
     cache.route_range(phi, u, theta, t0, t1)      # routing of new tokens, in place
     cache.compress(layer, x_k, x_v, t0, t1)       # their Eq. 1 factors, in place
+
+Several drafted tokens per sequence:
+
+    tree = DraftTree(cu_nodes, parent)            # nodes of every sequence, packed
+    out = cache.tree_decode(layer, tree, q, k, v) # fp32 [N, Hq, d]
+    path, n_kept, nxt = tree_verify(tree, token, target, u, u_next, draft=draft)
+    new = cache.empty_like(seqlens, res_stride)   # then the tokens that stay, with room for the kept ones
+    new.repack_from(cache, src_token, src_seq, new_code=codes)
 """
 from __future__ import annotations
 
@@ -19,10 +27,10 @@ from dataclasses import dataclass
 import numpy as np
 
 from . import binding, layout
-from .binding import DwkvError, F16, BF16
+from .binding import DwkvError, F16, BF16, F32
 
-__all__ = ["DeviceCache", "ProbeRef", "DwkvError", "load", "F16", "BF16", "hbm_read", "hbm_read_blocks",
-           "probe_schedule"]
+__all__ = ["DeviceCache", "ProbeRef", "DraftTree", "DwkvError", "load", "F16", "BF16", "F32", "hbm_read",
+           "hbm_read_blocks", "probe_schedule", "tree_verify", "tree_verify_workspace"]
 
 
 def load():
@@ -85,6 +93,70 @@ class ProbeRef:
         return 1 if self.q_prev is None else 1 + int(self.q_prev.shape[0])
 
 
+class DraftTree:
+    """Drafted nodes of a batch: cu_nodes [B+1] (host) packed starts, parent int32
+    [N] (device) each node's parent inside its sequence, lower than its own
+    index, -1 for the cached context; any other value marks an absent node."""
+
+    def __init__(self, cu_nodes, parent):
+        import torch
+        if parent.dtype != torch.int32 or parent.dim() != 1 or not parent.is_contiguous():
+            raise TypeError("parent must be a contiguous int32 vector")
+        self.cu_host = np.ascontiguousarray(cu_nodes, dtype=np.int32)
+        if self.cu_host.ndim != 1 or len(self.cu_host) < 2 or int(self.cu_host[-1]) != parent.numel():
+            raise ValueError("cu_nodes must be [B+1] and end at the number of nodes")
+        self.parent = parent
+        self.cu = torch.from_numpy(self.cu_host).to(parent.device)
+        self.batch, self.n_nodes = len(self.cu_host) - 1, parent.numel()
+        t = binding.Tree()
+        t.n_nodes = self.n_nodes
+        t.cu_nodes_host = self.cu_host.ctypes.data_as(C.POINTER(C.c_int32))
+        t.cu_nodes, t.parent = self.cu.data_ptr(), parent.data_ptr()
+        self.cstruct = t
+
+
+def tree_verify_workspace(tree: DraftTree, vocab: int, max_children: int):
+    """A workspace for ``tree_verify`` of such trees."""
+    import torch
+    n = int(load().dwkv_tree_verify_workspace_bytes(tree.batch, C.byref(tree.cstruct), int(vocab), int(max_children)))
+    if n == 0:
+        raise DwkvError(2, "dwkv_tree_verify_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=tree.parent.device)
+
+
+def tree_verify(tree: DraftTree, token, target, u, u_next, draft=None, max_children: int = 1, workspace=None):
+    """dwkv_tree_verify: which drafted tokens stand against the target's
+    probabilities.  token int32 [N], target [N, vocab] (float32, float16 or
+    bfloat16), draft None or like target (row i: what node i's children were
+    drawn from), u fp32 [N] and u_next fp32 [B] in [0, 1).  Returns (path int32
+    [N], n_kept int32 [B], next int32 [B])."""
+    import torch
+    kinds = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    N, B = tree.n_nodes, tree.batch
+    if target.dtype not in kinds or target.dim() != 2 or target.shape[0] != N or not target.is_contiguous():
+        raise TypeError("target must be a contiguous [N, vocab] tensor of float32, float16 or bfloat16")
+    if draft is not None and (draft.dtype != target.dtype or draft.shape != target.shape or not draft.is_contiguous()):
+        raise TypeError("draft must be like target")
+    if token.dtype != torch.int32 or token.numel() != N or not token.is_contiguous():
+        raise TypeError("token must be contiguous int32 [N]")
+    for x, n in ((u, N), (u_next, B)):
+        if x.dtype != torch.float32 or x.numel() != n or not x.is_contiguous():
+            raise TypeError("u and u_next must be contiguous float32 [N] and [B]")
+    dev = tree.parent.device
+    if any(x is not None and x.device != dev for x in (token, target, draft, u, u_next, workspace)):
+        raise ValueError("every tensor must be on the tree's device")
+    V = target.shape[1]
+    ws = workspace if workspace is not None else tree_verify_workspace(tree, V, max_children)
+    path = torch.empty(N, dtype=torch.int32, device=dev)
+    n_kept, nxt = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2))
+    with torch.cuda.device(dev):
+        st = load().dwkv_tree_verify(B, C.byref(tree.cstruct), _ptr(token), V, kinds[target.dtype], _ptr(target),
+                                     _ptr(draft), _ptr(u), _ptr(u_next), int(max_children), _ptr(path), _ptr(n_kept),
+                                     _ptr(nxt), _ptr(ws), ws.numel(), _stream(torch, dev))
+    binding.check(st, "dwkv_tree_verify")
+    return path, n_kept, nxt
+
+
 class DeviceCache:
     """One factorized cache resident on the GPU in the C-ABI layout.
 
@@ -131,6 +203,65 @@ class DeviceCache:
         self.total_tokens = int(self.cu_host[-1])
         self.res_stride = int(host.res_stride)
         self.set_split(split_tokens)
+
+    @classmethod
+    def from_device(cls, *, basis, coef_k, coef_v, rank_code, res_off, res_idx, res_val, res_scale, cu_seqlens, window: int,
+                    n_q_heads: int, levels, coef_scale_k=None, coef_scale_v=None, coef_format: str = "f16",
+                    q_dtype: str = "bf16", split_tokens: int = 0):
+        """A cache over device tensors that are in the C ABI's layouts already
+        (include/dwkv.h, dwkv_cache); they are used in place.  res_off is int32
+        bits; cu_seqlens [B+1] is a host array.  Such a cache holds no queries."""
+        import torch
+        self = cls.__new__(cls)
+        self.torch, self.lib, self.device = torch, binding.load(), basis.device
+        self.coef_format, self.q_dtype, self.q = coef_format, q_dtype, None
+        self.cu_host = np.ascontiguousarray(cu_seqlens, dtype=np.int32)
+        self.cu = torch.from_numpy(self.cu_host).to(self.device)
+        self.batch, self.total_tokens = len(self.cu_host) - 1, int(self.cu_host[-1])
+        self.window, self.levels, self.n_q_heads = int(window), tuple(int(x) for x in levels), int(n_q_heads)
+        self.n_layers, self.n_kv_heads, self.head_dim = int(coef_k.shape[0]), int(coef_k.shape[1]), int(basis.shape[-1])
+        self.basis_rank, self.res_stride = int(basis.shape[-2]), int(res_idx.shape[-1])
+        L, H, T, rb, M = self.n_layers, self.n_kv_heads, self.total_tokens, self.basis_rank, self.n_layers // self.window
+        T16, i8 = -(-T // 16) * 16, coef_format == "int8"
+        want = {"basis": (basis, self.batch * M * H * 2 * rb * self.head_dim, 2), "coef_k": (coef_k, L * H * T16 * rb, 1 if i8 else 2),
+                "coef_v": (coef_v, L * H * T16 * rb, 1 if i8 else 2), "rank_code": (rank_code, M * H * T, 1),
+                "res_off": (res_off, M * H * (T + 1), 4), "res_idx": (res_idx, L * 2 * H * self.res_stride, 1),
+                "res_val": (res_val, L * 2 * H * (self.res_stride // 2), 1), "res_scale": (res_scale, L * 2 * H * T, 2)}
+        if i8:
+            want.update(coef_scale_k=(coef_scale_k, L * H * (rb // 16) * T, 2), coef_scale_v=(coef_scale_v, L * H * (rb // 16) * T, 2))
+        else:
+            coef_scale_k = coef_scale_v = None
+        for name, (x, n, size) in want.items():
+            if x is None or x.numel() != n or x.element_size() != size or not x.is_contiguous() or x.device != self.device:
+                raise ValueError(f"{name} must be a contiguous tensor of {n} elements of {size} bytes on {self.device}")
+        self.basis, self.coef_k, self.coef_v = basis, coef_k, coef_v
+        self.coef_scale_k, self.coef_scale_v = coef_scale_k, coef_scale_v
+        self.rank_code, self.res_off, self.res_idx, self.res_val, self.res_scale = rank_code, res_off, res_idx, res_val, res_scale
+        self.set_split(split_tokens)
+        return self
+
+    def empty_like(self, seqlens, res_stride: int | None = None):
+        """A zero-filled cache of this one's kind for other sequence lengths;
+        res_stride: residual entries per slab (a multiple of 256, 512 of them spare),
+        by default room for every token at the highest level."""
+        torch = self.torch
+        cu = np.concatenate([[0], np.cumsum(np.asarray(list(seqlens), dtype=np.int64))])
+        T, B, L, H, rb, d = int(cu[-1]), len(cu) - 1, self.n_layers, self.n_kv_heads, self.basis_rank, self.head_dim
+        M, T16 = L // self.window, -(-T // 16) * 16
+        if res_stride is None:
+            res_stride = -(-(T * self.levels[-1] + 512) // 256) * 256
+        z = lambda *s, dtype=torch.uint8: torch.zeros(s, dtype=dtype, device=self.basis.device)
+        f16, i8 = torch.float16, self.coef_format == "int8"
+        if i8:
+            k, v = z(L, H, T16 // 16, rb // 16, 16, 16, dtype=self.coef_k.dtype), z(L, H, T16 // 16, rb, 16, dtype=self.coef_v.dtype)
+        else:
+            k, v = z(L, H, T16 // 16, rb // 8, 16, 8, dtype=f16), z(L, H, T16 // 8, rb, 8, dtype=f16)
+        return DeviceCache.from_device(
+            basis=z(B, M, H, 2, rb, d, dtype=f16), coef_k=k, coef_v=v, rank_code=z(M, H, T),
+            res_off=z(M, H, T + 1, dtype=torch.int32), res_idx=z(L, 2, H, res_stride), res_val=z(L, 2, H, res_stride // 2),
+            res_scale=z(L, 2, H, T, dtype=f16), coef_scale_k=z(L, H, rb // 16, T, dtype=f16) if i8 else None,
+            coef_scale_v=z(L, H, rb // 16, T, dtype=f16) if i8 else None, cu_seqlens=cu, window=self.window,
+            n_q_heads=self.n_q_heads, levels=self.levels, coef_format=self.coef_format, q_dtype=self.q_dtype)
 
     # -- descriptors -----------------------------------------------------------------
     def set_split(self, split_tokens: int):
@@ -454,6 +585,82 @@ class DeviceCache:
                                         _stream(torch, self.device))
         binding.check(st, "dwkv_dense_decode")
         return out
+
+    def tree_workspace(self, tree: DraftTree):
+        """A workspace for ``tree_decode`` of such trees over this cache."""
+        n = int(self.lib.dwkv_tree_workspace_bytes(C.byref(self.dims), C.byref(tree.cstruct)))
+        if n == 0:
+            raise DwkvError(2, "dwkv_tree_workspace_bytes")
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.basis.device)
+
+    def tree_decode(self, layer: int, tree: DraftTree, q, k_new, v_new, sm_scale: float | None = None, out=None,
+                    workspace=None):
+        """dwkv_tree_decode: attention of the drafted nodes' queries q [N, Hq, d]
+        over the cache and their ancestors' keys and values k_new, v_new fp16
+        [N, Hkv, d] (q and k_new, v_new may be slices of wider rows); returns out
+        fp32 [N, Hq, d]."""
+        torch = self.torch
+        N, Hq, Hk, d = tree.n_nodes, self.n_q_heads, self.n_kv_heads, self.head_dim
+        if tree.batch != self.batch:
+            raise ValueError("the tree and the cache have different batches")
+        if q.dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError("q must be float16 or bfloat16")
+        if k_new.dtype != torch.float16 or v_new.dtype != torch.float16:
+            raise TypeError("k_new and v_new must be float16")
+        for x, heads in ((q, Hq), (k_new, Hk), (v_new, Hk)):
+            if tuple(x.shape) != (N, heads, d) or (N > 0 and (x.stride(2) != 1 or x.stride(1) != d)):
+                raise ValueError("q must be [N, Hq, d], k_new and v_new [N, Hkv, d], each row without gaps")
+        if N > 1 and k_new.stride(0) != v_new.stride(0):
+            raise ValueError("k_new and v_new must have the same row stride")
+        if any(x is not None and x.device != self.basis.device for x in (q, k_new, v_new, tree.parent, out, workspace)):
+            raise ValueError("every tensor must be on the cache's device")
+        if out is None:
+            out = torch.empty((N, Hq, d), dtype=torch.float32, device=self.basis.device)
+        elif out.dtype != torch.float32 or tuple(out.shape) != (N, Hq, d) or not out.is_contiguous():
+            raise TypeError("out must be contiguous float32 [N, Hq, d]")
+        if N == 0:
+            return out
+        ws = workspace if workspace is not None else self.tree_workspace(tree)
+        qs, ks = (q.stride(0), k_new.stride(0)) if N > 1 else (0, 0)
+        with torch.cuda.device(self.basis.device):
+            st = self.lib.dwkv_tree_decode(C.byref(self.dims), C.byref(self.cstruct), int(layer), C.byref(tree.cstruct),
+                                           _ptr(q), F16 if q.dtype == torch.float16 else BF16, qs, _ptr(k_new), _ptr(v_new), ks,
+                                           float(sm_scale or 0.0), _ptr(out), _ptr(ws), ws.numel(),
+                                           _stream(torch, self.basis.device))
+        binding.check(st, "dwkv_tree_decode")
+        return out
+
+    def repack_workspace(self):
+        """A workspace for ``repack_from`` into this cache."""
+        n = int(self.lib.dwkv_repack_workspace_bytes(C.byref(self.dims)))
+        if n == 0:
+            raise DwkvError(2, "dwkv_repack_workspace_bytes")
+        return self.torch.empty(n, dtype=self.torch.uint8, device=self.basis.device)
+
+    def repack_from(self, src: "DeviceCache", src_token, src_seq, new_code=None, workspace=None):
+        """dwkv_repack: fill this cache with tokens of ``src``: token t is
+        src_token[t] (int32 [T], device), or the fresh slot -1 - src_token[t] at
+        level new_code[m, h, slot] (uint8 [M, Hkv, n], None: level 0); sequence b
+        takes the bases of src_seq[b] (int32 [B], device; negative: unchanged)."""
+        torch = self.torch
+        M, H = self.n_layers // self.window, self.n_kv_heads
+        if src_token.dtype != torch.int32 or src_token.numel() != self.total_tokens or not src_token.is_contiguous():
+            raise TypeError("src_token must be contiguous int32 [T]")
+        if src_seq.dtype != torch.int32 or src_seq.numel() != self.batch or not src_seq.is_contiguous():
+            raise TypeError("src_seq must be contiguous int32 [B]")
+        n_new = 0
+        if new_code is not None:
+            n_new = int(new_code.shape[-1])
+            if new_code.dtype != torch.uint8 or tuple(new_code.shape) != (M, H, n_new) or not new_code.is_contiguous():
+                raise TypeError("new_code must be contiguous uint8 [M, Hkv, n]")
+        if any(x is not None and x.device != self.basis.device for x in (src_token, src_seq, new_code, workspace, src.basis)):
+            raise ValueError("every tensor must be on the cache's device")
+        ws = workspace if workspace is not None else self.repack_workspace()
+        with torch.cuda.device(self.basis.device):
+            st = self.lib.dwkv_repack(C.byref(self.dims), C.byref(self.cstruct), C.byref(src.dims), C.byref(src.cstruct),
+                                      _ptr(src_token), _ptr(src_seq), _ptr(new_code), n_new, _ptr(ws), ws.numel(),
+                                      _stream(torch, self.basis.device))
+        binding.check(st, "dwkv_repack")
 
     def residual_map(self, layer: int, z: int, kv_head: int, t0: int, t1: int):
         torch = self.torch

@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(HERE, "_lib", "libdwkv.so")
 
 MAX_LEVELS = 8
 MAX_PROBE_HEADS = 64
-F16, BF16 = 0, 1
+F16, BF16, F32 = 0, 1, 2
+MAX_TREE_NODES = 64
 COEF_F16, COEF_I8 = 0, 1
 
 STATUS = {0: "ok", 1: "null pointer", 2: "inconsistent dimensions", 3: "unsupported shape",
@@ -58,6 +59,11 @@ class Probe(C.Structure):
                 ("err", C.c_void_p), ("out_ref", C.c_void_p), ("n_pos", C.c_int32), ("q_prev", C.c_void_p)]
 
 
+class Tree(C.Structure):
+    _fields_ = [("n_nodes", C.c_int32), ("cu_nodes_host", C.POINTER(C.c_int32)), ("cu_nodes", C.c_void_p),
+                ("parent", C.c_void_p)]
+
+
 EXPORTS = ["dwkv_abi_version", "dwkv_status_str", "dwkv_split_tokens", "dwkv_decode_kernel", "dwkv_workspace_bytes",
            "dwkv_decode_launches", "dwkv_decode", "dwkv_decode_partials", "dwkv_decode_merge",
            "dwkv_static_scratch_bytes", "dwkv_decode_noalloc", "dwkv_route_workspace_bytes", "dwkv_route",
@@ -65,7 +71,9 @@ EXPORTS = ["dwkv_abi_version", "dwkv_status_str", "dwkv_split_tokens", "dwkv_dec
            "dwkv_decode_append_workspace_bytes", "dwkv_decode_append_launches", "dwkv_decode_append",
            "dwkv_controller_update", "dwkv_sketch_workspace_bytes", "dwkv_sketch_basis", "dwkv_materialize", "dwkv_dense_workspace_bytes",
            "dwkv_dense_decode", "dwkv_residual_map",
-           "dwkv_validate_workspace_bytes", "dwkv_validate", "dwkv_hbm_read_blocks", "dwkv_hbm_read"]
+           "dwkv_validate_workspace_bytes", "dwkv_validate", "dwkv_hbm_read_blocks", "dwkv_hbm_read",
+           "dwkv_tree_workspace_bytes", "dwkv_tree_decode", "dwkv_tree_verify_workspace_bytes", "dwkv_tree_verify",
+           "dwkv_repack_workspace_bytes", "dwkv_repack"]
 
 _lib = None
 
@@ -169,6 +177,22 @@ def load(path: str = LIB_PATH):
     lib.dwkv_validate_workspace_bytes.restype = C.c_size_t
     lib.dwkv_validate.restype = C.c_int
     lib.dwkv_validate.argtypes = [P(Dims), P(Cache), P(C.c_int64), C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.dwkv_tree_workspace_bytes.restype = C.c_size_t
+    lib.dwkv_tree_workspace_bytes.argtypes = [P(Dims), P(Tree)]
+    lib.dwkv_tree_decode.restype = C.c_int
+    lib.dwkv_tree_decode.argtypes = [P(Dims), P(Cache), C.c_int32, P(Tree), C.c_void_p, C.c_int32, C.c_int64, C.c_void_p,
+                                     C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.dwkv_tree_verify_workspace_bytes.restype = C.c_size_t
+    lib.dwkv_tree_verify_workspace_bytes.argtypes = [C.c_int32, P(Tree), C.c_int32, C.c_int32]
+    lib.dwkv_tree_verify.restype = C.c_int
+    lib.dwkv_tree_verify.argtypes = [C.c_int32, P(Tree), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                     C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                     C.c_size_t, C.c_void_p]
+    lib.dwkv_repack_workspace_bytes.restype = C.c_size_t
+    lib.dwkv_repack_workspace_bytes.argtypes = [P(Dims)]
+    lib.dwkv_repack.restype = C.c_int
+    lib.dwkv_repack.argtypes = [P(Dims), P(Cache), P(Dims), P(Cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                C.c_void_p, C.c_size_t, C.c_void_p]
     _lib = lib
     return lib
 

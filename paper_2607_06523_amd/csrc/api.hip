@@ -1217,3 +1217,285 @@ dwkv_status dwkv_validate(const dwkv_dims* d, const dwkv_cache* c, int64_t* bad_
 }
 
 }  // extern "C"
+
+namespace {
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+dwkv_status check_tree(const dwkv_tree* t, int32_t batch) {
+  if (!t) return DWKV_E_NULL;
+  if (batch < 1 || t->n_nodes < 0) return DWKV_E_DIMS;
+  if (!t->cu_nodes_host || !t->cu_nodes || (t->n_nodes > 0 && !t->parent)) return DWKV_E_NULL;
+  if (t->cu_nodes_host[0] != 0 || t->cu_nodes_host[batch] != t->n_nodes) return DWKV_E_DIMS;
+  for (int b = 0; b < batch; ++b)
+    if (t->cu_nodes_host[b + 1] < t->cu_nodes_host[b]) return DWKV_E_DIMS;
+  for (int b = 0; b < batch; ++b)
+    if (t->cu_nodes_host[b + 1] - t->cu_nodes_host[b] > DWKV_MAX_TREE_NODES) return DWKV_E_UNSUPPORTED;
+  if (!aligned4(t->cu_nodes) || !aligned4(t->parent)) return DWKV_E_ALIGN;
+  return DWKV_OK;
+}
+
+// Rows of a workgroup's block: 32, or 16 where no sequence has more or the
+// basis leaves no registers for 32.
+int tree_rows(const dwkv_dims* d, const dwkv_tree* t) {
+  int most = 0;
+  for (int b = 0; b < d->batch; ++b) most = std::max(most, t->cu_nodes_host[b + 1] - t->cu_nodes_host[b]);
+  return most * (d->n_q_heads / d->n_kv_heads) <= 16 || d->basis_rank > 64 ? 16 : 32;
+}
+
+int64_t tree_items(const dwkv_dims* d, const dwkv_tree* t, int rows, int64_t split, int b) {
+  const int64_t n = t->cu_nodes_host[b + 1] - t->cu_nodes_host[b], len = d->cu_seqlens_host[b + 1] - d->cu_seqlens_host[b];
+  return ((len + split - 1) / split + 1) * ((n * (d->n_q_heads / d->n_kv_heads) + rows - 1) / rows);
+}
+
+// Chunk size: one workgroup per compute unit, a tile per wave at least.
+int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t, int rows) {
+  constexpr int64_t q = kTreeWaves * kTreeTile;
+  if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets
+  for (int64_t c = q;; c += std::max<int64_t>(q, c / 8 / q * q)) {
+    int64_t n = 0;
+    for (int b = 0; b < d->batch; ++b) n += tree_items(d, t, rows, c, b);
+    if (n * d->n_kv_heads <= kTargetWorkgroups / 2 || c >= 65536) return c;
+  }
+}
+
+struct TreePlan {
+  int rows;
+  int64_t split, items;
+  size_t bytes;
+};
+
+TreePlan tree_plan(const dwkv_dims* d, const dwkv_tree* t) {
+  TreePlan p;
+  p.rows = tree_rows(d, t);
+  p.split = tree_split(d, t, p.rows);
+  p.items = 0;
+  for (int b = 0; b < d->batch; ++b) p.items += tree_items(d, t, p.rows, p.split, b);
+  p.bytes = std::max<size_t>(256, align_up((size_t)p.items * d->n_kv_heads * p.rows * (kHeadDim + d->basis_rank + 4) * sizeof(float), 256));
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dwkv_tree_workspace_bytes(const dwkv_dims* dims, const dwkv_tree* tree) {
+  if (check_dims(dims) != DWKV_OK || check_tree(tree, dims->batch) != DWKV_OK) return 0;
+  return tree_plan(dims, tree).bytes;
+}
+
+dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t layer, const dwkv_tree* tree,
+                             const void* q, int32_t q_type, int64_t q_stride, const void* k_new, const void* v_new,
+                             int64_t kv_stride, float sm_scale, float* out, void* workspace, size_t ws_bytes,
+                             void* stream) {
+  dwkv_status st = check_dims(d);
+  if (st != DWKV_OK) return st;
+  if ((st = check_tree(tree, d->batch)) != DWKV_OK) return st;
+  if (!c || !q || !k_new || !v_new || !out || !workspace) return DWKV_E_NULL;
+  if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(out) || !aligned16(workspace)) return DWKV_E_ALIGN;
+  const int64_t qrow = (int64_t)d->n_q_heads * kHeadDim, kvrow = (int64_t)d->n_kv_heads * kHeadDim;
+  if (q_stride == 0) q_stride = qrow;
+  if (kv_stride == 0) kv_stride = kvrow;
+  if (q_stride < qrow || kv_stride < kvrow || q_stride % 8 || kv_stride % 8) return DWKV_E_DIMS;
+  SplitArgs a;                           // checks the cache, layer and query
+  if ((st = split_args(d, c, layer, q, q_type, sm_scale, workspace, a)) != DWKV_OK) return st;
+  const TreePlan p = tree_plan(d, tree);
+  if (ws_bytes < p.bytes) return DWKV_E_WORKSPACE;
+  if (p.items * d->n_kv_heads > 0x7ffffff0) return DWKV_E_UNSUPPORTED;
+  if (tree->n_nodes == 0) return DWKV_OK;
+  TreeArgs t;
+  std::memset(&t, 0, sizeof(t));
+  t.coef_k = a.coef_k;
+  t.coef_v = a.coef_v;
+  t.cscale_k = a.cscale_k;
+  t.cscale_v = a.cscale_v;
+  t.basis = a.basis;
+  t.basis_b_stride = a.basis_b_stride;
+  t.off = a.off;
+  t.idx_k = a.idx_k;
+  t.idx_v = a.idx_v;
+  t.val_k = a.val_k;
+  t.val_v = a.val_v;
+  t.scale_k = a.scale_k;
+  t.scale_v = a.scale_v;
+  t.q = a.q;
+  t.k_new = static_cast<const uint16_t*>(k_new);
+  t.v_new = static_cast<const uint16_t*>(v_new);
+  t.q_stride = q_stride;
+  t.kv_stride = kv_stride;
+  t.cu = d->cu_seqlens;
+  t.cu_nodes = tree->cu_nodes;
+  t.parent = tree->parent;
+  t.part = static_cast<float*>(workspace);
+  t.out = out;
+  t.T = a.T;
+  t.res_stride = a.res_stride;
+  t.n_items = p.items * d->n_kv_heads;
+  t.batch = d->batch;
+  t.n_q_heads = d->n_q_heads;
+  t.n_kv_heads = d->n_kv_heads;
+  t.group = d->n_q_heads / d->n_kv_heads;
+  t.rb = d->basis_rank;
+  t.split = (int32_t)p.split;
+  t.rows = p.rows;
+  t.q_bf16 = a.q_bf16;
+  t.c8 = d->coef_format == DWKV_COEF_I8;
+  t.qscale = a.qscale;
+  int most = 0;
+  for (int b = 0; b < d->batch; ++b) most = std::max(most, tree->cu_nodes_host[b + 1] - tree->cu_nodes_host[b]);
+  if (d->batch <= kKernargSeqs) {
+    t.wt.n_seq = d->batch;
+    for (int b = 0; b <= d->batch; ++b) {
+      t.wt.tok[b] = d->cu_seqlens_host[b];
+      t.wt.node[b] = tree->cu_nodes_host[b];
+      if (b < d->batch) t.wt.work[b + 1] = t.wt.work[b] + (int32_t)tree_items(d, tree, p.rows, p.split, b);
+    }
+  }
+  return hip_status(launch_tree(t, most * t.group, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+struct VerifyWs {
+  size_t sum, end, total;
+  int zblk, nblk;
+};
+
+VerifyWs verify_ws(int32_t batch, int32_t n_nodes, int32_t vocab, int32_t max_children) {
+  VerifyWs w;
+  w.zblk = (vocab + kVerifyZChunk - 1) / kVerifyZChunk;
+  w.nblk = (vocab + kVerifyChunk - 1) / kVerifyChunk;
+  w.sum = align_up((size_t)n_nodes * (max_children - 1) * w.zblk * sizeof(double), 256);
+  w.end = w.sum + align_up((size_t)batch * w.nblk * sizeof(double), 256);
+  w.total = w.end + align_up((size_t)batch * sizeof(VerifyEnd), 256);
+  return w;
+}
+
+dwkv_status check_verify(int32_t batch, const dwkv_tree* tree, int32_t vocab, int32_t max_children) {
+  const dwkv_status st = check_tree(tree, batch);
+  if (st != DWKV_OK) return st;
+  if (vocab < 1 || max_children < 1 || max_children > DWKV_MAX_TREE_NODES) return DWKV_E_DIMS;
+  // one grid row per sequence and per node
+  if (batch > 65535 || tree->n_nodes > 65535 || vocab > 0x7fffffff - kVerifyZChunk) return DWKV_E_UNSUPPORTED;
+  return DWKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dwkv_tree_verify_workspace_bytes(int32_t batch, const dwkv_tree* tree, int32_t vocab, int32_t max_children) {
+  if (check_verify(batch, tree, vocab, max_children) != DWKV_OK) return 0;
+  return verify_ws(batch, tree->n_nodes, vocab, max_children).total;
+}
+
+dwkv_status dwkv_tree_verify(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, int32_t p_type,
+                             const void* target, const void* draft, const float* u, const float* u_next,
+                             int32_t max_children, int32_t* path, int32_t* n_kept, int32_t* next, void* workspace,
+                             size_t ws_bytes, void* stream) {
+  const dwkv_status st = check_verify(batch, tree, vocab, max_children);
+  if (st != DWKV_OK) return st;
+  if (p_type != DWKV_F32 && p_type != DWKV_F16 && p_type != DWKV_BF16) return DWKV_E_DIMS;
+  if (!u_next || !n_kept || !next || !workspace) return DWKV_E_NULL;
+  if (tree->n_nodes > 0 && (!token || !target || !u || !path)) return DWKV_E_NULL;
+  const uintptr_t size = p_type == DWKV_F32 ? 4 : 2;
+  if ((reinterpret_cast<uintptr_t>(target) | reinterpret_cast<uintptr_t>(draft)) & (size - 1)) return DWKV_E_ALIGN;
+  if (!aligned4(token) || !aligned4(u) || !aligned4(u_next) || !aligned4(path) || !aligned4(n_kept) || !aligned4(next) ||
+      !aligned16(workspace))
+    return DWKV_E_ALIGN;
+  const VerifyWs w = verify_ws(batch, tree->n_nodes, vocab, max_children);
+  if (ws_bytes < w.total) return DWKV_E_WORKSPACE;
+  char* ws = static_cast<char*>(workspace);
+  VerifyArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.cu_nodes = tree->cu_nodes;
+  a.parent = tree->parent;
+  a.token = token;
+  a.target = target;
+  a.draft = tree->n_nodes > 0 ? draft : nullptr;
+  a.u = u;
+  a.u_next = u_next;
+  a.path = path;
+  a.n_kept = n_kept;
+  a.next = next;
+  a.z = reinterpret_cast<double*>(ws);
+  a.sum = reinterpret_cast<double*>(ws + w.sum);
+  a.end = reinterpret_cast<VerifyEnd*>(ws + w.end);
+  a.batch = batch;
+  a.n_nodes = tree->n_nodes;
+  a.vocab = vocab;
+  a.p_type = p_type;
+  a.max_children = max_children;
+  a.zblk = w.zblk;
+  a.nblk = w.nblk;
+  return hip_status(launch_verify(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+size_t dwkv_repack_workspace_bytes(const dwkv_dims* dst) {
+  if (check_dims(dst) != DWKV_OK) return 0;
+  const int64_t nblk = std::max<int64_t>(1, (dst->total_tokens + kRepackBlock - 1) / kRepackBlock);
+  return align_up((size_t)nblk * (dst->n_layers / dst->window) * dst->n_kv_heads * sizeof(uint32_t), 256);
+}
+
+dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_dims* src, const dwkv_cache* from,
+                        const int32_t* src_token, const int32_t* src_seq, const uint8_t* new_code, int64_t n_new,
+                        void* workspace, size_t ws_bytes, void* stream) {
+  dwkv_status st = check_dims(dst);
+  if (st != DWKV_OK) return st;
+  if ((st = check_dims(src)) != DWKV_OK) return st;
+  if (dst->n_layers != src->n_layers || dst->window != src->window || dst->n_kv_heads != src->n_kv_heads ||
+      dst->n_q_heads != src->n_q_heads || dst->basis_rank != src->basis_rank || dst->n_levels != src->n_levels ||
+      dst->coef_format != src->coef_format || n_new < 0)
+    return DWKV_E_DIMS;
+  for (int i = 0; i < dst->n_levels; ++i)
+    if (dst->levels[i] != src->levels[i]) return DWKV_E_DIMS;
+  if (!to || !from || !src_seq || !workspace || (dst->total_tokens > 0 && !src_token)) return DWKV_E_NULL;
+  const bool c8 = dst->coef_format == DWKV_COEF_I8;
+  for (const dwkv_cache* c : {to, from}) {
+    if (!c->basis || !c->res_off || !c->res_idx || !c->res_val) return DWKV_E_NULL;
+    if ((c == to ? dst : src)->total_tokens > 0 &&      // arrays of tokens are not there without any
+        (!c->coef_k || !c->coef_v || !c->rank_code || !c->res_scale || (c8 && (!c->coef_k_scale || !c->coef_v_scale))))
+      return DWKV_E_NULL;
+    if (!aligned16(c->basis) || !aligned16(c->coef_k) || !aligned16(c->coef_v) || !aligned4(c->res_off)) return DWKV_E_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(c->res_idx) | reinterpret_cast<uintptr_t>(c->res_scale)) & 1u) return DWKV_E_ALIGN;
+    if (c8 && ((reinterpret_cast<uintptr_t>(c->coef_k_scale) | reinterpret_cast<uintptr_t>(c->coef_v_scale)) & 1u))
+      return DWKV_E_ALIGN;
+  }
+  if (!aligned4(src_token) || !aligned4(src_seq) || !aligned16(workspace)) return DWKV_E_ALIGN;
+  const void* const pairs[][2] = {{to->basis, from->basis}, {to->coef_k, from->coef_k}, {to->coef_v, from->coef_v},
+                                  {to->rank_code, from->rank_code}, {to->res_off, from->res_off}, {to->res_idx, from->res_idx},
+                                  {to->res_val, from->res_val}, {to->res_scale, from->res_scale}};
+  for (const auto& p : pairs)
+    if (p[0] && p[0] == p[1]) return DWKV_E_DIMS;        // not in place
+  if (ws_bytes < dwkv_repack_workspace_bytes(dst)) return DWKV_E_WORKSPACE;
+  // one grid row per window and head, one grid layer per layer and Z
+  if ((int64_t)(dst->n_layers / dst->window) * dst->n_kv_heads > 65535 || 2 * (int64_t)dst->n_layers > 65535) return DWKV_E_UNSUPPORTED;
+  RepackArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.to = *to;
+  a.from = *from;
+  a.src_token = src_token;
+  a.src_seq = src_seq;
+  a.new_code = new_code;
+  a.bsum = static_cast<uint32_t*>(workspace);
+  a.T = dst->total_tokens;
+  a.T0 = src->total_tokens;
+  a.stride = dst->res_stride;
+  a.stride0 = src->res_stride;
+  a.n_new = new_code ? n_new : 0;
+  a.batch = dst->batch;
+  a.batch0 = src->batch;
+  a.n_layers = dst->n_layers;
+  a.window = dst->window;
+  a.n_kv_heads = dst->n_kv_heads;
+  a.rb = dst->basis_rank;
+  a.n_levels = dst->n_levels;
+  a.c8 = c8;
+  a.nblk = (int)std::max<int64_t>(1, (a.T + kRepackBlock - 1) / kRepackBlock);
+  for (int i = 0; i < DWKV_MAX_LEVELS; ++i) a.levels[i] = i < dst->n_levels ? dst->levels[i] : 0;
+  return hip_status(launch_repack(a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

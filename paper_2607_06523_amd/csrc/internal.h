@@ -348,6 +348,95 @@ hipError_t launch_split_tl_probe(int rb, int g, bool resid, bool c8, const TLPro
 // probed heads (s, r_b rb) and its reference pass (r) in one launch.
 hipError_t launch_probe_pos(int rb, int g, bool resid, const TLProbeArgs& a, hipStream_t s);
 
+// Attention of drafted trees (tree.hip): items of every sequence with nodes,
+// (chunks + 1) x row blocks per KV head, the last chunk the drafted nodes.
+constexpr int kTreeWaves = 8;        // waves per workgroup
+constexpr int kTreeTile = 32;        // tokens per wave tile
+
+struct TreeTable {                   // up to kKernargSeqs sequences; n_seq == 0: from the device arrays
+  int32_t n_seq;
+  int32_t work[kKernargSeqs + 1];    // items of one KV head before each sequence
+  int32_t tok[kKernargSeqs + 1];
+  int32_t node[kKernargSeqs + 1];
+};
+
+struct TreeArgs {
+  const uint16_t* coef_k;      // layer's coefficients and residuals, KV head 0 (as SplitArgs)
+  const uint16_t* coef_v;
+  const uint16_t* cscale_k;
+  const uint16_t* cscale_v;
+  const uint16_t* basis;
+  int64_t basis_b_stride;
+  const uint32_t* off;
+  const uint8_t* idx_k;
+  const uint8_t* idx_v;
+  const uint8_t* val_k;
+  const uint8_t* val_v;
+  const uint16_t* scale_k;
+  const uint16_t* scale_v;
+  const uint16_t* q;           // [N] rows of [Hq][d], q_stride apart
+  const uint16_t* k_new;       // fp16 [N] rows of [Hkv][d], kv_stride apart
+  const uint16_t* v_new;
+  int64_t q_stride, kv_stride;
+  const int32_t* cu;
+  const int32_t* cu_nodes;
+  const int32_t* parent;
+  float* part;                 // [item][Hkv][rows][d + rb + 4]: r, a~, m, l
+  float* out;                  // [N][Hq][d]
+  int64_t T, res_stride;
+  int64_t n_items;             // items x Hkv
+  int32_t batch, n_q_heads, n_kv_heads, group, rb, split;
+  int32_t rows;                // rows of a block: 16 or 32
+  int32_t q_bf16, c8;
+  float qscale;                // sm_scale * log2(e)
+  TreeTable wt;
+};
+hipError_t launch_tree(const TreeArgs& a, int max_rows, hipStream_t s);
+
+// Verification of drafted tokens (verify.hip).
+struct VerifyArgs {
+  const int32_t* cu_nodes;
+  const int32_t* parent;
+  const int32_t* token;
+  const void* target;          // [N][vocab] p_type
+  const void* draft;           // null, or the same
+  const float* u;
+  const float* u_next;
+  int32_t* path;
+  int32_t* n_kept;
+  int32_t* next;
+  double* z;                   // [N][max_children][zblk] partial sums of Z_k (k >= 1)
+  double* sum;                 // [B][nblk] sums of r over chunks of the last row
+  struct VerifyEnd* end;       // [B] the node the walk ends at
+  int32_t batch, n_nodes, vocab, p_type, max_children, zblk, nblk;
+};
+// The last node of a sequence's walk and what its rejected children left.
+struct VerifyEnd {
+  double c;
+  int32_t node;                // -1: no nodes
+  int32_t n_out;               // rejected tokens to leave out (no draft)
+  int32_t out[DWKV_MAX_TREE_NODES];
+};
+constexpr int kVerifyChunk = 2048;   // vocabulary entries of a workgroup
+constexpr int kVerifyZChunk = 8192;
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
+
+// Repacking (repack.hip).
+struct RepackArgs {
+  dwkv_cache to, from;
+  const int32_t* src_token;
+  const int32_t* src_seq;
+  const uint8_t* new_code;
+  uint32_t* bsum;              // [M*Hkv][nblk]
+  int64_t T, T0;               // tokens of `to` and `from`
+  int64_t stride, stride0;     // res_stride
+  int64_t n_new;
+  int32_t batch, batch0, n_layers, window, n_kv_heads, rb, n_levels, c8, nblk;
+  int32_t levels[DWKV_MAX_LEVELS];
+};
+constexpr int kRepackBlock = 1024;   // tokens per workgroup of the offset scan
+hipError_t launch_repack(const RepackArgs& a, hipStream_t s);
+
 // Materialization of one layer's rebuilt keys and values (Eq. 1) as fp16.
 struct MatArgs {
   const uint16_t* basis;       // window m, sequence 0; sequence b adds b*basis_b_stride, (h, z) add (h*2+z)*rb*d
