@@ -1,0 +1,922 @@
+// Attention of a tree of drafted tokens over the cross-depth factorized KV
+// cache (Eq. 1 used through its linearity, as in the decode), gfx950.
+//
+// Row r of a sequence and KV head is node r / G, group member r % G.  For
+// cached token t, with q~ = B^K q (once per workgroup, float32 MFMA):
+//   S[t][r] = A^K_t . q~_r + s^K_t (R^K_t . q_r),   p = 2^(S - m_r)
+//   O_r = (sum_t p A^V_t) B^V + sum_t (p s^V_t) R^V_t,  then the drafted nodes
+// A decode has G rows; here G n of them share every byte read, so both sums
+// and the routed residuals run on the matrix cores: a wave turns the entries
+// of 32 tokens into dense code tiles in LDS (integers, exact in 16 bits) and
+// multiplies them like the coefficients.
+//
+//  * tree_split_kernel: workgroup = (chunk of a sequence's tokens, KV head,
+//    block of 16 NC rows), 8 waves taking its 32-token tiles in turn.  Scores
+//    come out transposed, tokens down the accumulator and rows across, which is
+//    the operand layout the value products read: probabilities never leave the
+//    registers.  A tile's tokens are dealt to the score rows so that a lane's
+//    eight scores are eight consecutive tokens, one value block.
+//  * one more workgroup per (sequence, KV head, row block) attends to the
+//    drafted nodes, whose masks it derives from the parents.
+//  * tree_merge_kernel joins the partials and applies B^V.
+//
+// Precision: q~ and the probabilities are fp16 pairs (hi + lo, 22 bits), the
+// codes, fp16 coefficients and queries are exact, sums and softmax statistics
+// are float32.
+#pragma once
+#include "entry.h"
+#include "internal.h"
+
+namespace dwkv {
+namespace {
+
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u2v __attribute__((ext_vector_type(2)));
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+
+constexpr int D = kHeadDim;
+constexpr int NW = kTreeWaves;           // waves per workgroup, two per SIMD
+constexpr int TT = kTreeTile;            // tokens per tile
+constexpr int kKRow = D + 8;             // halves per token row of the key code tile (16-byte pad: no bank conflicts)
+constexpr float kUp = 6.0f;              // a moved reference leaves the largest probability at 2^6,
+constexpr float kHead = 14.0f;           // and moves again when one exceeds 2^14: fp16 pairs hold both ends
+
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+__device__ __forceinline__ rsrc_t make_rsrc(const void* base, int64_t bytes) {
+  const uint32_t n = (uint32_t)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, n, 0x00020000);
+}
+
+__device__ __forceinline__ int incl_max(int v) {   // running maximum over the lanes, v >= 0
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));   // row_shr:1
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));   // row_bcast:15
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));   // row_bcast:31
+  return v;
+}
+
+__device__ __forceinline__ f4 mfma_h(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+template <bool BF>
+__device__ __forceinline__ f4 mfma_q(u4v a, u4v b, f4 c) {
+  if constexpr (BF)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+  else
+    return mfma_h(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c);
+}
+
+__device__ __forceinline__ uint16_t h_bits(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+template <bool BF>
+__device__ __forceinline__ uint16_t code_bits(float v) {   // v an int4 code: exact in both types
+  return BF ? (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16) : h_bits(v);
+}
+
+// Place of a tile's token among the rows of the key code tile: score row r of
+// token block b is token 8 (r / 4) + 4 b + r % 4, held at row 16 b + r, so that
+// 16 lanes read 16 consecutive rows.
+__device__ __forceinline__ int key_row(int t) { return 16 * ((t >> 2) & 1) + 4 * (t >> 3) + (t & 3); }
+
+struct alignas(16) WaveTile {
+  uint16_t k[TT * kKRow];                // key codes [token place][channel], zero between tiles
+  uint16_t v[D * TT];                    // value codes [channel][token]
+  float sk[TT], sv[TT];                  // residual scales of the tile's tokens (sv in units of 2^ex)
+  uint8_t mark[64];
+};
+
+// Smem of the drafted nodes' workgroups.
+template <int NC>
+struct alignas(16) DraftSmem {
+  float q[16 * NC][D];
+  uint16_t v[DWKV_MAX_TREE_NODES][D];
+};
+
+template <int NB, int NC, bool C8>
+struct alignas(16) TreeSmem {
+  static constexpr int R = 16 * NC, NK = (NB + 1) / 2;
+  u4v qf[4][NC][64];                     // query fragments: channels 32 s + 8 g + j
+  u4v qt[2][NK][NC][64];                 // q~ fragments (hi, lo)
+  float m[NW][R], l[NW][R];
+  float big;                             // largest |q~|
+  alignas(16) uint16_t vs[C8 ? NW : 1][C8 ? NB : 1][C8 ? TT : 8];   // value block scales of a tile (int8)
+  union {
+    WaveTile w[NW];
+    float acc[NW][R][D + 4];             // the waves' sums, 128 columns at a time
+    DraftSmem<NC> d;
+  };
+};
+
+// Sequence, row block, chunk and KV head of a workgroup.  Workgroups of one
+// (chunk, KV head) follow each other on one XCD (consecutive workgroups go to
+// the 8 XCDs in turn), so the row blocks share the chunk through its L2.
+struct Item {
+  int b, rb, h, c;                       // c == chunks: the drafted nodes
+  int chunks, nrb;
+  int t0, t1, n0, n;                     // tokens [t0, t1), nodes n0 .. n0 + n - 1 of the sequence
+  int64_t part;                          // partial's index
+};
+
+__device__ __forceinline__ int seq_items(int T, int n, const TreeArgs& a, int& chunks, int& nrb) {
+  chunks = T > 0 ? (T - 1) / a.split + 1 : 0;
+  nrb = (n * a.group + a.rows - 1) / a.rows;
+  return (chunks + 1) * nrb;
+}
+
+__device__ __forceinline__ Item find_item(const TreeArgs& a, int64_t x) {
+  Item it;
+  int64_t base = 0;
+  const int H = a.n_kv_heads;
+  if (a.wt.n_seq > 0) {
+    // branch-free: the table's entries are read at fixed offsets, all at once
+    int b = 0, w0 = 0, t0 = a.wt.tok[0], t1 = a.wt.tok[1], n0 = a.wt.node[0], n1 = a.wt.node[1];
+    if (a.wt.n_seq > 1) {
+#pragma unroll
+      for (int i = 1; i < kKernargSeqs; ++i) {
+        const bool here = i < a.wt.n_seq && x >= (int64_t)a.wt.work[i] * H;
+        b = here ? i : b;
+        w0 = here ? a.wt.work[i] : w0;
+        t0 = here ? a.wt.tok[i] : t0;
+        t1 = here ? a.wt.tok[i + 1] : t1;
+        n0 = here ? a.wt.node[i] : n0;
+        n1 = here ? a.wt.node[i + 1] : n1;
+      }
+    }
+    it.b = b;
+    base = w0;
+    it.t0 = t0;
+    it.t1 = t1;
+    it.n0 = n0;
+    it.n = n1 - n0;
+  } else {                               // 64 sequences at a time
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0;; b0 += 64) {
+      const int b = b0 + lane;
+      int chunks, nrb, mine = 0;
+      if (b < a.batch) mine = seq_items(a.cu[b + 1] - a.cu[b], a.cu_nodes[b + 1] - a.cu_nodes[b], a, chunks, nrb);
+      int64_t end = mine;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int64_t o = __shfl_up(end, d);
+        if (lane >= d) end += o;
+      }
+      const unsigned long long in = __ballot(x < (base + end) * H);
+      if (in) {
+        const int w = __ffsll(in) - 1;
+        base += __builtin_amdgcn_readlane((int)(end - mine), w);
+        it.b = b0 + w;
+        break;
+      }
+      base += __builtin_amdgcn_readlane((int)end, 63);
+      if (b0 + 64 >= a.batch) { it.b = a.batch - 1; break; }   // not reached: the grid ends with the items
+    }
+    it.t0 = a.cu[it.b];
+    it.t1 = a.cu[it.b + 1];
+    it.n0 = a.cu_nodes[it.b];
+    it.n = a.cu_nodes[it.b + 1] - it.n0;
+  }
+  seq_items(it.t1 - it.t0, it.n, a, it.chunks, it.nrb);
+  int64_t y = x - base * H;
+  it.rb = (int)(y % it.nrb);
+  y /= it.nrb;
+  it.h = (int)(y % H);
+  it.c = (int)(y / H);
+  it.part = (base + (int64_t)it.c * it.nrb + it.rb) * H + it.h;
+  return it;
+}
+
+// Ancestors of node `lane` of a sequence, itself included (bit j: node j), or
+// 0 when it is absent; by pointer doubling over the wave.
+__device__ __forceinline__ unsigned long long ancestors(const int32_t* parent, int n, int lane) {
+  int p = lane < n ? parent[lane] : -2;
+  bool bad = p < -1 || p >= lane;
+  if (bad) p = -1;
+  unsigned long long m = 1ull << lane;
+  for (int d = 1; d < 64; d <<= 1) {
+    const unsigned long long om = __shfl(m, max(p, 0));
+    const int op = __shfl(p, max(p, 0)), ob = __shfl((int)bad, max(p, 0));
+    if (p >= 0) {
+      m |= om;
+      bad |= ob != 0;
+      p = op;
+    }
+  }
+  return bad ? 0ull : m;
+}
+
+// 16 bytes of the query of row r (node r / G, member r % G) from channel c on.
+__device__ __forceinline__ u4v q_piece(const TreeArgs& a, const Item& it, int r, int c) {
+  return *reinterpret_cast<const u4v*>(a.q + (int64_t)(it.n0 + r / a.group) * a.q_stride + (it.h * a.group + r % a.group) * D + c);
+}
+
+// The drafted nodes: a wave takes rows w, w + 8, ... of the block, all at once; a
+// lane takes node `lane` for the scores and channels 2 lane, 2 lane + 1 for the
+// values.  Nodes a row does not see are skipped, not weighted with zero.
+template <int NC>
+__device__ __forceinline__ void draft_item(const TreeArgs& a, const Item& it, DraftSmem<NC>& sm, float* part, int stride) {
+  constexpr int R = 16 * NC, PER = R / NW;
+  const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, rows = it.n * a.group;
+  const uint16_t* k = a.k_new + (int64_t)(it.n0 + min(lane, it.n - 1)) * a.kv_stride + it.h * D;
+  const uint16_t* V = a.v_new + (int64_t)it.n0 * a.kv_stride + it.h * D;
+  u4v kw[D / 8];
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) kw[c] = *reinterpret_cast<const u4v*>(k + 8 * c);
+  for (int i = threadIdx.x; i < it.n * (D / 8); i += 64 * NW)
+    *reinterpret_cast<u4v*>(&sm.v[i / (D / 8)][8 * (i % (D / 8))]) =
+        *reinterpret_cast<const u4v*>(V + (int64_t)(i / (D / 8)) * a.kv_stride + 8 * (i % (D / 8)));
+  for (int i = threadIdx.x; i < R * (D / 8); i += 64 * NW) {
+    const int r = i / (D / 8), c = 8 * (i % (D / 8));
+    const u4v w = q_piece(a, it, min(it.rb * R + r, rows - 1), c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint16_t b = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+      sm.q[r][c + j] = a.q_bf16 ? bf16_bits_to_float(b) : half_bits_to_float(b);
+    }
+  }
+  const unsigned long long anc = ancestors(a.parent + it.n0, it.n, lane);
+  __syncthreads();
+  float s[PER] = {};
+#pragma unroll
+  for (int c = 0; c < D; c += 4) {
+    float kf[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) kf[j] = half_bits_to_float((uint16_t)(kw[c / 8][(c % 8 + j) >> 1] >> (16 * (j & 1))));
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const f4 q = *reinterpret_cast<const f4*>(&sm.q[wv + NW * u][c]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[u] = __builtin_fmaf(kf[j], q[j], s[u]);
+    }
+    __builtin_amdgcn_sched_barrier(0);   // else every query piece is read at once, into registers there are none of
+  }
+#pragma unroll
+  for (int u = 0; u < PER; ++u) asm volatile("" : "+v"(s[u]));   // nor are the sums put off until their rows are known to be there
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int row = it.rb * R + wv + NW * u;
+    if (row >= rows) continue;
+    float* o = part + (int64_t)(wv + NW * u) * stride;
+    const unsigned long long see = __shfl(anc, row / a.group);
+    const bool mine = (see >> lane) & 1;
+    const float sc = mine ? s[u] * a.qscale : -__builtin_inff();
+    float m = sc;
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if (!(m > -__builtin_inff())) m = 0.f;                    // nothing seen, or -inf alone
+    const float p = mine ? __builtin_amdgcn_exp2f(sc - m) : 0.f;
+    float l = p;
+    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+    float o0 = 0.f, o1 = 0.f;
+    unsigned long long left = ((unsigned long long)__builtin_amdgcn_readfirstlane((int)(see >> 32)) << 32) |
+                              (uint32_t)__builtin_amdgcn_readfirstlane((int)see);
+    while (left) {
+      const int j = __ffsll(left) - 1;
+      left &= left - 1;
+      const float pj = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, p), j));
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(&sm.v[j][2 * lane]);
+      o0 = __builtin_fmaf(pj, half_bits_to_float(w & 0xffff), o0);
+      o1 = __builtin_fmaf(pj, half_bits_to_float(w >> 16), o1);
+    }
+    *reinterpret_cast<float2*>(o + 2 * lane) = make_float2(o0, o1);
+    for (int i = lane; i < a.rb; i += 64) o[D + i] = 0.f;
+    if (lane == 0) {
+      o[D + a.rb] = m;
+      o[D + a.rb + 1] = see ? l : -1.f;                       // -1: the node is absent
+    }
+  }
+}
+
+// Dequantized int8 coefficients, code * scale = hi + lo exactly (18 bits).
+__device__ __forceinline__ void split8(const float (&v)[8], h8& hi, h8& lo) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    hi[j] = (_Float16)v[j];
+    lo[j] = (_Float16)(v[j] - (float)hi[j]);
+  }
+}
+
+__device__ __forceinline__ float byte_at(u2v w, int j) { return (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))); }
+
+// v rounded towards zero to an fp16 pair: two values' hi and lo halves.
+__device__ __forceinline__ void pair2(float v0, float v1, uint32_t& hi, uint32_t& lo) {
+  typedef __fp16 fp2 __attribute__((ext_vector_type(2)));
+  const fp2 h = __builtin_amdgcn_cvt_pkrtz(v0, v1);
+  const fp2 l = __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf((float)h[0], -1.f, v0), __builtin_fmaf((float)h[1], -1.f, v1));
+  hi = __builtin_bit_cast(uint32_t, h);
+  lo = __builtin_bit_cast(uint32_t, l);
+}
+
+// Streams of a chunk and KV head; offsets count from the chunk's first 16-token block.
+struct Streams {
+  rsrc_t k, v, ks, vs;                   // coefficients; int8 block scales
+  rsrc_t off, sk, sv;                    // offsets and residual scales from the chunk's first block on
+  rsrc_t idx[2], val[2];                 // entries from the chunk's first on
+};
+
+// What a wave holds of a tile ahead of its use.
+template <int NB, bool C8>
+struct Ahead {
+  static constexpr int NK = (NB + 1) / 2;
+  u4v k[2][NK], v[NB];                   // fp16 coefficients; int8: the first two words
+  uint32_t ks[C8 ? 2 : 1][C8 ? NK : 1], vs[C8 ? NB : 1];
+  uint32_t oa, ob, oa2, ob2;             // entry ranges of the lane's token, this tile and the next
+  uint32_t sk, sv;                       // residual scales
+  uint32_t ck, cv, vk, vv;               // entry pair `lane`: channel bytes and code byte, keys and values
+};
+
+template <int NB, bool C8>
+__device__ __forceinline__ void load_k(Ahead<NB, C8>& f, const Streams& x, int rel, int T, int g, int col) {
+  constexpr int NK = (NB + 1) / 2, rb = 16 * NB;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int tr = rel + 8 * (col >> 2) + 4 * b + (col & 3);           // token of score row `col`
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      const bool have = NB % 2 == 0 || s + 1 < NK || g < 2;            // past r_b: beyond the slab, which reads as zero
+      if constexpr (C8) {
+        const int blk = 2 * s + (g >> 1);
+        const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.k, have ? (((tr >> 4) * NB + blk) * 16 + (tr & 15)) * 16 + 8 * (g & 1) : 0x7ffffff0, 0, 0);
+        f.k[b][s].x = w.x;
+        f.k[b][s].y = w.y;
+        f.ks[b][s] = __builtin_amdgcn_raw_buffer_load_b16(x.ks, have ? (blk * T + tr) * 2 : 0x7ffffff0, 0, 0);
+      } else {
+        f.k[b][s] = __builtin_amdgcn_raw_buffer_load_b128(x.k, have ? (((tr >> 4) * (rb / 8) + 4 * s + g) * 128 + (tr & 15) * 8) * 2 : 0x7ffffff0, 0, 0);
+      }
+    }
+  }
+}
+
+template <int NB, bool C8>
+__device__ __forceinline__ void load_v(Ahead<NB, C8>& f, const Streams& x, int rel, int T, int g, int col, int lane) {
+  constexpr int rb = 16 * NB;
+#pragma unroll
+  for (int k = 0; k < NB; ++k) {
+    if constexpr (C8) {
+      const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.v, ((((rel >> 4) + (g >> 1)) * rb + 16 * k + col) * 16) + 8 * (g & 1), 0, 0);
+      f.v[k].x = w.x;
+      f.v[k].y = w.y;
+    } else {
+      f.v[k] = __builtin_amdgcn_raw_buffer_load_b128(x.v, (((rel >> 3) + g) * rb + 16 * k + col) * 16, 0, 0);
+    }
+  }
+}
+
+template <int NB, bool C8>
+__device__ __forceinline__ void load_vs(Ahead<NB, C8>& f, const Streams& x, int rel, int T, int lane) {
+  if constexpr (C8) {
+#pragma unroll
+    for (int k = 0; k < NB; ++k) f.vs[k] = __builtin_amdgcn_raw_buffer_load_b16(x.vs, (k * T + rel + (lane & 31)) * 2, 0, 0);
+  }
+}
+
+// Scales and the first 64 entry pairs of a tile whose first entry is e0.
+template <int NB, bool C8>
+__device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x, int rel, uint32_t e0, int lane) {
+  const uint32_t t2 = (uint32_t)(rel + (lane & 31)) * 2, e = e0 + 2 * lane;
+  f.sk = __builtin_amdgcn_raw_buffer_load_b16(x.sk, t2, 0, 0);
+  f.sv = __builtin_amdgcn_raw_buffer_load_b16(x.sv, t2, 0, 0);
+  f.ck = __builtin_amdgcn_raw_buffer_load_b16(x.idx[0], e, 0, 0);
+  f.cv = __builtin_amdgcn_raw_buffer_load_b16(x.idx[1], e, 0, 0);
+  f.vk = __builtin_amdgcn_raw_buffer_load_b8(x.val[0], e >> 1, 0, 0);
+  f.vv = __builtin_amdgcn_raw_buffer_load_b8(x.val[1], e >> 1, 0, 0);
+}
+
+template <int NB, int NC, bool BF, bool C8>
+__global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a) {
+  constexpr int R = 16 * NC, NK = (NB + 1) / 2, rb = 16 * NB, stride = D + rb + 4;
+  __shared__ TreeSmem<NB, NC, C8> sm;
+  const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+  // consecutive workgroups of an XCD take consecutive items
+  const int64_t per = (a.n_items + 7) / 8;
+  const int64_t x = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
+  if (x >= a.n_items) return;
+  const Item it = find_item(a, x);
+  const int rows_left = it.n * a.group - it.rb * R;
+  float* part = a.part + it.part * R * stride;
+  if (it.c == it.chunks) {
+    draft_item<NC>(a, it, sm.d, part, stride);
+    return;
+  }
+
+  // ---- the chunk's streams, and the wave's first tiles in flight -----------------
+  const int c0 = it.t0 + it.c * a.split, c1 = it.t1 - c0 > a.split ? c0 + a.split : it.t1, tb = c0 & ~15;
+  const int ntile = (c1 - tb + TT - 1) / TT;
+  const int64_t T = a.T, T16 = (T + 15) / 16 * 16;
+  constexpr int esz = C8 ? 1 : 2;
+  const uint32_t* off = a.off + (int64_t)it.h * (T + 1);
+  const uint32_t ec0 = off[c0];
+  const int64_t eroom = a.res_stride - (int64_t)ec0;   // entries of the slab from the chunk on (ec0 is even)
+  const int64_t es = (int64_t)it.h * a.res_stride + (eroom > 0 ? ec0 : 0);
+  Streams sx;
+  sx.k = make_rsrc(reinterpret_cast<const uint8_t*>(a.coef_k) + ((int64_t)it.h * T16 + tb) * rb * esz, (T16 - tb) * rb * esz);
+  sx.v = make_rsrc(reinterpret_cast<const uint8_t*>(a.coef_v) + ((int64_t)it.h * T16 + tb) * rb * esz, (T16 - tb) * rb * esz);
+  sx.off = make_rsrc(off + tb, (T + 1 - tb) * 4);
+  sx.sk = make_rsrc(a.scale_k + (int64_t)it.h * T + tb, (T - tb) * 2);
+  sx.sv = make_rsrc(a.scale_v + (int64_t)it.h * T + tb, (T - tb) * 2);
+  sx.idx[0] = make_rsrc(a.idx_k + es, eroom);
+  sx.idx[1] = make_rsrc(a.idx_v + es, eroom);
+  sx.val[0] = make_rsrc(a.val_k + es / 2, eroom / 2);
+  sx.val[1] = make_rsrc(a.val_v + es / 2, eroom / 2);
+  if constexpr (C8) {
+    sx.ks = make_rsrc(a.cscale_k + (int64_t)it.h * NB * T + tb, (NB * T - tb) * 2);
+    sx.vs = make_rsrc(a.cscale_v + (int64_t)it.h * NB * T + tb, (NB * T - tb) * 2);
+  }
+  const int Ti = (int)T;
+  const int last = ntile - 1, j0 = min(wv, last);      // tiles past the last are read as the last and not used
+  const auto load_off = [&](int j, uint32_t& oa, uint32_t& ob) {
+    const int t = j * TT + (lane & 31);                // tokens outside the chunk hold no entries
+    oa = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)(min(max(t + tb, c0), c1) - tb) * 4, 0, 0) - ec0;
+    ob = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)(min(max(t + tb + 1, c0), c1) - tb) * 4, 0, 0) - ec0;
+  };
+  Ahead<NB, C8> f;
+  load_off(j0, f.oa, f.ob);
+  load_off(min(j0 + NW, last), f.oa2, f.ob2);
+  load_k<NB, C8>(f, sx, j0 * TT, Ti, g, col);
+  load_v<NB, C8>(f, sx, j0 * TT, Ti, g, col, lane);
+  load_vs<NB, C8>(f, sx, j0 * TT, Ti, lane);
+
+  // ---- query fragments, and q~ = B^K q as fp16 pairs ---------------------------
+  constexpr int TILES = NB * NC, PER = (2 * NK * NC + NW - 1) / NW;
+  const uint16_t* bk = a.basis + (int64_t)it.b * a.basis_b_stride + (int64_t)(it.h * 2) * rb * D;
+  u4v bw[PER][4];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int tile = wv + NW * u;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      if (tile < TILES) bw[u][s] = *reinterpret_cast<const u4v*>(bk + (16 * (tile / NC) + col) * D + 32 * s + 8 * g);
+  }
+  for (int i = threadIdx.x; i < 4 * NC * 64; i += 64 * NW) {
+    const int ln = i & 63, n = (i >> 6) % NC, s = (i >> 6) / NC, r = 16 * n + (ln & 15);
+    u4v w = {0, 0, 0, 0};
+    if (r < rows_left) {
+      const int row = it.rb * R + r, p = a.parent[it.n0 + row / a.group];
+      w = q_piece(a, it, row, 32 * s + 8 * (ln >> 4));
+      if (p < -1 || p >= row / a.group) w = u4v{0, 0, 0, 0};           // absent: its query may be anything
+    }
+    sm.qf[s][n][ln] = w;
+  }
+  if (threadIdx.x == 0) sm.big = 0.f;
+  WaveTile& w = sm.w[wv];
+  for (int i = lane; i < (int)((sizeof(w.k) + sizeof(w.v)) / 16); i += 64) reinterpret_cast<u4v*>(&w)[i] = u4v{0, 0, 0, 0};
+  __syncthreads();
+  {
+    f4 q[PER];
+    float big = 0.f;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int tile = wv + NW * u, n = tile % NC;
+      f4 c = {0.f, 0.f, 0.f, 0.f};
+      if (tile < TILES) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const u4v qw = sm.qf[s][n][lane];            // channels 32 s + 8 g + j
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint16_t qb = (uint16_t)(qw[j >> 1] >> (16 * (j & 1))), bb = (uint16_t)(bw[u][s][j >> 1] >> (16 * (j & 1)));
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(half_bits_to_float(bb), BF ? bf16_bits_to_float(qb) : half_bits_to_float(qb), c, 0, 0, 0);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        c[i] *= a.qscale;
+        const float m = fabsf(c[i]);
+        if (m < __builtin_inff()) big = fmaxf(big, m);
+      }
+      q[u] = c;
+    }
+    // |q~| beyond fp16 is scaled down for the whole workgroup (scores stay float32)
+    for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
+    if (lane == 0) atomicMax(reinterpret_cast<int*>(&sm.big), __builtin_bit_cast(int, big));
+    __syncthreads();
+    const float dn = __builtin_ldexpf(1.f, -max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15));
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int tile = wv + NW * u, blk = tile / NC, n = tile % NC;
+      if (tile >= 2 * NK * NC) continue;
+      h4 hi, lo;                                       // basis rows 16 blk + 4 g + i, zero past r_b
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v = q[u][i] * dn;
+        hi[i] = (_Float16)v;
+        lo[i] = (_Float16)(v - (float)hi[i]);
+      }
+      const int ln = 16 * (2 * (blk & 1) + (g >> 1)) + col;
+      reinterpret_cast<h4*>(&sm.qt[0][blk >> 1][n][ln])[g & 1] = hi;
+      reinterpret_cast<h4*>(&sm.qt[1][blk >> 1][n][ln])[g & 1] = lo;
+    }
+  }
+  const int down = max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15);
+  const float up = __builtin_ldexpf(1.f, down), fdn = __builtin_ldexpf(1.f, -down);
+  uint32_t e0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.oa);
+  load_entries<NB, C8>(f, sx, j0 * TT, e0, lane);
+  __syncthreads();                       // q~ is whole
+
+  u4v qt[2][NK][NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n)
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      qt[0][s][n] = sm.qt[0][s][n][lane];
+      qt[1][s][n] = sm.qt[1][s][n][lane];
+    }
+  f4 acc_a[NB][NC], acc_r[D / 16][NC];   // a~ and the residual channels: (channel 4 g + i of the block, row col)
+  float m[NC], l[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    m[n] = l[n] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) acc_a[k][n] = f4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) acc_r[k][n] = f4{0, 0, 0, 0};
+  }
+  bool first = true;
+  int ex = -24;                          // |s^V| <= 2^ex of the tiles so far
+  float exf = __builtin_ldexpf(1.f, -24), exi = __builtin_ldexpf(1.f, 24);
+  const float inf = __builtin_inff();
+
+#pragma unroll 1
+  for (int j = wv; j < ntile; j += NW) {
+    const int t0 = tb + j * TT, jn = min(j + NW, last);
+    const bool edge = t0 < c0 || t0 + TT > c1;
+    // ---- entries of the next tile and offsets of the one after, in flight
+    const uint32_t oa = f.oa, ob = f.ob, sk = f.sk, sv = f.sv, ck = f.ck, cv = f.cv, vk = f.vk, vv = f.vv;
+    const uint32_t en = e0;
+    f.oa = f.oa2;
+    f.ob = f.ob2;
+    e0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.oa);
+    load_off(min(jn + NW, last), f.oa2, f.ob2);
+    load_entries<NB, C8>(f, sx, jn * TT, e0, lane);
+
+    // ---- scales, one lane per token
+    const bool own = ob > oa;
+    const float fk = own ? half_bits_to_float((uint16_t)sk) : 0.f, fv = own ? half_bits_to_float((uint16_t)sv) : 0.f;
+    const bool odd_k = !(fabsf(fk) < inf), odd_v = !(fabsf(fv) < inf);
+    if (__ballot(!odd_v && fabsf(fv) > exf)) {           // rare: larger value scales
+      int e = !odd_v && fv != 0.f ? __builtin_amdgcn_frexp_expf(fv) : -24;
+      for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
+      const float fall = __builtin_ldexpf(1.f, ex - e);
+      ex = e;
+      exf = __builtin_ldexpf(1.f, e);
+      exi = __builtin_ldexpf(1.f, -e);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+        for (int n = 0; n < NC; ++n) acc_r[k][n] *= fall;
+    }
+    const uint32_t odd_tokens = (uint32_t)__ballot(odd_v);   // lanes 32 .. 63 repeat the first 32
+    const bool odd = __ballot(odd_k || odd_v) != 0;
+    // a scale that is not finite goes with its entries into the code tiles
+    if (lane < 32) {
+      w.sk[lane] = odd_k ? a.qscale : fk * a.qscale;
+      w.sv[lane] = odd_v ? 1.f : fv * exi;
+    }
+    if constexpr (C8) {
+      if (lane < 32) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k) sm.vs[wv][k][lane] = (uint16_t)f.vs[k];
+      }
+      load_vs<NB, C8>(f, sx, jn * TT, Ti, lane);
+    }
+    // ---- entries into the code tiles, 64 pairs at a time (ranks are even, so a pair belongs to one token)
+    const uint32_t e1 = (uint32_t)__builtin_amdgcn_readlane((int)ob, 31);
+    const uint32_t np = e1 > en ? min(e1 - en, (uint32_t)(TT * D)) / 2 : 0u;
+    uint32_t at_k = 0xffffffffu, at_v = 0;             // places of the first batch
+    const auto scatter = [&](uint32_t b0, int carry, uint32_t pk, uint32_t pv, uint32_t qk, uint32_t qv, uint32_t& ak, uint32_t& av) {
+      w.mark[lane] = 0;
+      wave_lds_sync();
+      const uint32_t at = (oa - en) / 2 - b0;
+      if (lane < 32 && own && at < 64) w.mark[at] = (uint8_t)(lane + 1);
+      wave_lds_sync();
+      const int tok = max(incl_max((int)w.mark[lane]), carry);
+      ak = 0xffffffffu;
+      if (b0 + lane < np && tok > 0) {
+        const int t = tok - 1, kr = key_row(t) * kKRow;
+        const uint32_t k0 = kr + (pk & (D - 1)), k1 = kr + ((pk >> 8) & (D - 1));
+        const uint32_t v0 = (pv & (D - 1)) * TT + t, v1 = ((pv >> 8) & (D - 1)) * TT + t;
+        ak = k0 | k1 << 16;
+        av = v0 | v1 << 16;
+        const float a0 = (float)int4_value(qk), a1 = (float)int4_value(qk >> 4), b0f = (float)int4_value(qv), b1f = (float)int4_value(qv >> 4);
+        uint16_t wk0 = code_bits<BF>(a0), wk1 = code_bits<BF>(a1), wv0 = h_bits(b0f), wv1 = h_bits(b1f);
+        if (odd) {
+          const uint32_t t2 = (uint32_t)(j * TT + t) * 2;
+          const float tk = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sk, t2, 0, 0));
+          const float tv = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sv, t2, 0, 0));
+          if (!(fabsf(tk) < inf)) wk0 = code_bits<BF>(a0 * tk), wk1 = code_bits<BF>(a1 * tk);
+          if (!(fabsf(tv) < inf)) wv0 = h_bits(b0f * tv), wv1 = h_bits(b1f * tv);
+        }
+        w.k[k0] = wk0;
+        w.k[k1] = wk1;
+        w.v[v0] = wv0;
+        w.v[v1] = wv1;
+      }
+      return __builtin_amdgcn_readlane(tok, 63);
+    };
+    if (np > 0) {
+      int carry = scatter(0, 0, ck, cv, vk, vv, at_k, at_v);
+#pragma unroll 1
+      for (uint32_t b0 = 64; b0 < np; b0 += 64) {      // more than 128 entries: read as they come
+        const uint32_t e = en + 2 * (b0 + lane);
+        uint32_t x0, x1;
+        carry = scatter(b0, carry, __builtin_amdgcn_raw_buffer_load_b16(sx.idx[0], e, 0, 0), __builtin_amdgcn_raw_buffer_load_b16(sx.idx[1], e, 0, 0),
+                        __builtin_amdgcn_raw_buffer_load_b8(sx.val[0], e >> 1, 0, 0), __builtin_amdgcn_raw_buffer_load_b8(sx.val[1], e >> 1, 0, 0), x0, x1);
+      }
+    }
+    wave_lds_sync();
+
+    // ---- scores: (token 8 g + 4 b + i, row col)
+    float ks[8], vs[8];
+    {
+      const f4 s0 = *reinterpret_cast<const f4*>(&w.sk[8 * g]), s1 = *reinterpret_cast<const f4*>(&w.sk[8 * g + 4]);
+      const f4 v0 = *reinterpret_cast<const f4*>(&w.sv[8 * g]), v1 = *reinterpret_cast<const f4*>(&w.sv[8 * g + 4]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { ks[i] = s0[i]; ks[4 + i] = s1[i]; vs[i] = v0[i]; vs[4 + i] = v1[i]; }
+    }
+    f4 sb[2][NC], sr[2][NC];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const float c = -m[n] * fdn;
+        sb[b][n] = f4{c, c, c, c};
+        sr[b][n] = f4{0, 0, 0, 0};
+      }
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      h8 kh[2], kl[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if constexpr (C8) {
+          const float sc = half_bits_to_float((uint16_t)f.ks[b][s]);
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.k[b][s].x, f.k[b][s].y}, e) * sc;
+          split8(v, kh[b], kl[b]);
+        } else {
+          kh[b] = __builtin_bit_cast(h8, f.k[b][s]);
+        }
+      }
+#pragma unroll
+      for (int part = 0; part < (C8 ? 3 : 2); ++part)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int n = 0; n < NC; ++n)
+            sb[b][n] = mfma_h(part == 2 ? kl[b] : kh[b], __builtin_bit_cast(h8, qt[part == 1][s][n]), sb[b][n]);
+    }
+    load_k<NB, C8>(f, sx, jn * TT, Ti, g, col);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      u4v qv[NC];
+#pragma unroll
+      for (int n = 0; n < NC; ++n) qv[n] = sm.qf[s][n][lane];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const u4v kc = *reinterpret_cast<const u4v*>(&w.k[(16 * b + col) * kKRow + 32 * s + 8 * g]);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) sr[b][n] = mfma_q<BF>(kc, qv[n], sr[b][n]);
+      }
+    }
+    if (down) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int n = 0; n < NC; ++n) sb[b][n] *= up;
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int n = 0; n < NC; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sb[b][n][i] = __builtin_fmaf(ks[4 * b + i], sr[b][n][i], sb[b][n][i]);
+    if (edge) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = t0 + 8 * g + 4 * b + i;
+          if (t < c0 || t >= c1)
+#pragma unroll
+            for (int n = 0; n < NC; ++n) sb[b][n][i] = -inf;
+        }
+      // tokens outside the chunk may hold anything
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        if constexpr (!C8) {
+          h8 av = __builtin_bit_cast(h8, f.v[k]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (t0 + 8 * g + e < c0 || t0 + 8 * g + e >= c1) av[e] = (_Float16)0.f;
+          f.v[k] = __builtin_bit_cast(u4v, av);
+        }
+      }
+    }
+    // ---- the reference moves for the first tile and when a score exceeds it by far
+    float mx[NC];
+    bool move = first;
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      mx[n] = fmaxf(fmaxf(fmaxf(sb[0][n][0], sb[0][n][1]), fmaxf(sb[0][n][2], sb[0][n][3])),
+                    fmaxf(fmaxf(sb[1][n][0], sb[1][n][1]), fmaxf(sb[1][n][2], sb[1][n][3])));
+      move = move || mx[n] > kHead;
+    }
+    if (__ballot(move)) {
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        float c = fmaxf(mx[n], __shfl_xor(mx[n], 16));
+        c = fmaxf(c, __shfl_xor(c, 32));
+        const float by = (first ? c > -inf : c > kHead) ? c - kUp : 0.f;
+        const float fall = first ? 0.f : __builtin_amdgcn_exp2f(-by);
+        m[n] += by;
+        l[n] *= fall;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sb[b][n][i] -= by;
+        if (!first) {
+#pragma unroll
+          for (int k = 0; k < NB; ++k) acc_a[k][n] *= fall;
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) acc_r[k][n] *= fall;
+        }
+      }
+      first = false;
+    }
+    // ---- probabilities as fp16 pairs, plain and times the value scales
+    u4v ph[NC], pl[NC], rh[NC], rl[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float v0 = __builtin_amdgcn_exp2f(sb[e >> 2][n][e & 3]), v1 = __builtin_amdgcn_exp2f(sb[e >> 2][n][(e & 3) + 1]);
+        sum[0] += v0;
+        sum[1] += v1;
+        uint32_t h, lo;
+        pair2(v0, v1, h, lo);
+        ph[n][e >> 1] = h;
+        pl[n][e >> 1] = lo;
+        pair2(v0 * vs[e], v1 * vs[e + 1], h, lo);
+        rh[n][e >> 1] = h;
+        rl[n][e >> 1] = lo;
+      }
+      l[n] += sum[0] + sum[1];
+      if (odd_tokens) {                  // an infinite entry meets positive numbers only
+        h8 hh = __builtin_bit_cast(h8, rh[n]), ll = __builtin_bit_cast(h8, rl[n]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if ((odd_tokens >> (8 * g + e)) & 1) {
+            hh[e] = hh[e] > (_Float16)0x1p-14f ? hh[e] : (_Float16)0x1p-14f;
+            ll[e] = (_Float16)0x1p-14f;
+          }
+        rh[n] = __builtin_bit_cast(u4v, hh);
+        rl[n] = __builtin_bit_cast(u4v, ll);
+      }
+    }
+    // ---- values: channel blocks of the basis, then of the residual
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      h8 hi, lo;
+      if constexpr (C8) {
+        const u4v sw = *reinterpret_cast<const u4v*>(&sm.vs[wv][k][8 * g]);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.v[k].x, f.v[k].y}, e) * half_bits_to_float((uint16_t)(sw[e >> 1] >> (16 * (e & 1))));
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (t0 + 8 * g + e < c0 || t0 + 8 * g + e >= c1) v[e] = 0.f;
+        }
+        split8(v, hi, lo);
+      } else {
+        hi = __builtin_bit_cast(h8, f.v[k]);
+      }
+#pragma unroll
+      for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
+#pragma unroll
+      for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, pl[n]), acc_a[k][n]);
+      if constexpr (C8) {
+#pragma unroll
+        for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(lo, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
+      }
+    }
+    load_v<NB, C8>(f, sx, jn * TT, Ti, g, col, lane);
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+      const h8 av = __builtin_bit_cast(h8, *reinterpret_cast<const u4v*>(&w.v[(16 * k + col) * TT + 8 * g]));
+#pragma unroll
+      for (int n = 0; n < NC; ++n) acc_r[k][n] = mfma_h(av, __builtin_bit_cast(h8, rh[n]), acc_r[k][n]);
+#pragma unroll
+      for (int n = 0; n < NC; ++n) acc_r[k][n] = mfma_h(av, __builtin_bit_cast(h8, rl[n]), acc_r[k][n]);
+    }
+    // ---- the code tiles go back to zero
+    wave_lds_sync();
+    if (np > 64) {
+      for (int i = lane; i < (int)((sizeof(w.k) + sizeof(w.v)) / 16); i += 64) reinterpret_cast<u4v*>(&w)[i] = u4v{0, 0, 0, 0};
+    } else if (at_k != 0xffffffffu) {
+      w.k[at_k & 0xffff] = 0;
+      w.k[at_k >> 16] = 0;
+      w.v[at_v & 0xffff] = 0;
+      w.v[at_v >> 16] = 0;
+    }
+    wave_lds_sync();
+  }
+
+  // ---- join the waves: common reference per row, then sums in wave order -----------
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    l[n] += __shfl_xor(l[n], 16);
+    l[n] += __shfl_xor(l[n], 32);
+    if (g == 0) {
+      sm.m[wv][16 * n + col] = first ? -inf : m[n];
+      sm.l[wv][16 * n + col] = l[n];
+    }
+  }
+  __syncthreads();                       // the code tiles are done with
+  float mine[NC];
+#pragma unroll
+  for (int n = 0; n < NC; ++n) {
+    float ms = -inf;
+#pragma unroll
+    for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][16 * n + col]);
+    mine[n] = first ? 0.f : __builtin_amdgcn_exp2f(m[n] - ms);
+  }
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+      *reinterpret_cast<f4*>(&sm.acc[wv][16 * n + col][16 * k + 4 * g]) = acc_r[k][n] * (mine[n] * exf);
+  __syncthreads();
+  for (int i = threadIdx.x; i < R * (D / 4); i += 64 * NW) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    f4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < NW; ++u) s += *reinterpret_cast<const f4*>(&sm.acc[u][r][c]);
+    if (r < rows_left) *reinterpret_cast<f4*>(part + r * stride + c) = s;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < NB; ++k)
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+      *reinterpret_cast<f4*>(&sm.acc[wv][16 * n + col][16 * k + 4 * g]) = acc_a[k][n] * mine[n];
+  __syncthreads();
+  for (int i = threadIdx.x; i < R * (rb / 4); i += 64 * NW) {
+    const int r = i / (rb / 4), c = 4 * (i % (rb / 4));
+    f4 s = {0, 0, 0, 0};
+#pragma unroll
+    for (int u = 0; u < NW; ++u) s += *reinterpret_cast<const f4*>(&sm.acc[u][r][c]);
+    if (r < rows_left) *reinterpret_cast<f4*>(part + r * stride + D + c) = s;
+  }
+  if (threadIdx.x < R && (int)threadIdx.x < rows_left) {
+    const int r = threadIdx.x;
+    float ms = -inf, ls = 0.f;
+#pragma unroll
+    for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][r]);
+#pragma unroll
+    for (int u = 0; u < NW; ++u)
+      if (sm.m[u][r] > -inf) ls += sm.l[u][r] * __builtin_amdgcn_exp2f(sm.m[u][r] - ms);
+    part[r * stride + D + rb] = ms;
+    part[r * stride + D + rb + 1] = ls;
+  }
+}
+
+template <int NB, int NC, bool BF>
+void launch_tree_c(const TreeArgs& a, dim3 grid, hipStream_t s) {
+  if (a.c8) hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, true>), grid, dim3(64 * NW), 0, s, a);
+  else hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, false>), grid, dim3(64 * NW), 0, s, a);
+}
+
+template <int NB, bool BF>
+void launch_tree_b(const TreeArgs& a, dim3 grid, hipStream_t s) {
+  if constexpr (NB <= 4) {
+    if (a.rows == 32) return launch_tree_c<NB, 2, BF>(a, grid, s);
+  }
+  launch_tree_c<NB, 1, BF>(a, grid, s);
+}
+
+template <bool BF>
+void launch_tree_split(const TreeArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.n_items + 7) / 8 * 8));
+  switch (a.rb / 16) {
+    case 1: launch_tree_b<1, BF>(a, grid, s); break;
+    case 2: launch_tree_b<2, BF>(a, grid, s); break;
+    case 3: launch_tree_b<3, BF>(a, grid, s); break;
+    case 4: launch_tree_b<4, BF>(a, grid, s); break;
+    case 5: launch_tree_b<5, BF>(a, grid, s); break;
+    case 6: launch_tree_b<6, BF>(a, grid, s); break;
+    case 7: launch_tree_b<7, BF>(a, grid, s); break;
+    default: launch_tree_b<8, BF>(a, grid, s); break;
+  }
+}
+
+}  // namespace
+}  // namespace dwkv
