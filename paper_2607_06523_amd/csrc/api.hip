@@ -1,6 +1,7 @@
 // C ABI of the library: argument checks, split planning, launches.
 #include <algorithm>
 #include <cmath>
+#include <cstdint>
 #include <cstring>
 #include <mutex>
 
@@ -1243,34 +1244,68 @@ int tree_rows(const dwkv_dims* d, const dwkv_tree* t) {
   return most * (d->n_q_heads / d->n_kv_heads) <= 16 || d->basis_rank > 64 ? 16 : 32;
 }
 
-int64_t tree_items(const dwkv_dims* d, const dwkv_tree* t, int rows, int64_t split, int b) {
-  const int64_t n = t->cu_nodes_host[b + 1] - t->cu_nodes_host[b], len = d->cu_seqlens_host[b + 1] - d->cu_seqlens_host[b];
-  return ((len + split - 1) / split + 1) * ((n * (d->n_q_heads / d->n_kv_heads) + rows - 1) / rows);
-}
-
-// Chunk size: one workgroup per compute unit, a tile per wave at least.
-int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t, int rows) {
-  constexpr int64_t q = kTreeWaves * kTreeTile;
-  if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets
-  for (int64_t c = q;; c += std::max<int64_t>(q, c / 8 / q * q)) {
-    int64_t n = 0;
-    for (int b = 0; b < d->batch; ++b) n += tree_items(d, t, rows, c, b);
-    if (n * d->n_kv_heads <= kTargetWorkgroups / 2 || c >= 65536) return c;
-  }
-}
-
 struct TreePlan {
-  int rows;
-  int64_t split, items;
+  int rows, max_nrb;
+  int64_t split, items, pairs;           // items and pairs of one KV head
   size_t bytes;
 };
+
+// Chunks and row blocks of sequence b.
+void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int rows, int64_t split, int b, int64_t& chunks, int64_t& nrb) {
+  const int64_t n = t->cu_nodes_host[b + 1] - t->cu_nodes_host[b], len = d->cu_seqlens_host[b + 1] - d->cu_seqlens_host[b];
+  chunks = (len + split - 1) / split;
+  nrb = (n * (d->n_q_heads / d->n_kv_heads) + rows - 1) / rows;
+}
+
+// Chunk size, in rounds of a workgroup's waves over their tiles.  A workgroup
+// takes about kFixed rounds before and after them, one of the drafted nodes about
+// kDraft; a compute unit holds one.  Of the chunk sizes that give every compute unit
+// 1 to 8 workgroups, or one tile per wave more, the one whose estimated end is
+// first: full rounds of the longest workgroup, or the work shared out evenly
+// plus one workgroup's length where sequences are ragged.
+int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t, int rows) {
+  constexpr int64_t q = kTreeWaves * kTreeTile, kCU = kTargetWorkgroups / 2, kFixed = 3, kDraft = 2;
+  if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets
+  int64_t total = 0, chunks, nrb;
+  for (int b = 0; b < d->batch; ++b) {
+    tree_seq(d, t, rows, q, b, chunks, nrb);
+    total += chunks * nrb * d->n_kv_heads;
+  }
+  int64_t best = q, best_time = INT64_MAX;
+  for (int k = 2; k < 18; ++k) {
+    const int64_t cus = kCU * (k / 2), tiles = std::min<int64_t>(std::max<int64_t>((total + cus - 1) / cus, 1) + k % 2, 256), c = tiles * q;
+    int64_t wgs = 0, drafts = 0, work = 0, most = 0;
+    for (int b = 0; b < d->batch; ++b) {
+      tree_seq(d, t, rows, c, b, chunks, nrb);
+      const int64_t n = nrb * d->n_kv_heads, len = d->cu_seqlens_host[b + 1] - d->cu_seqlens_host[b];
+      if (n == 0) continue;
+      drafts += n;
+      wgs += chunks * n;
+      work += (chunks * kFixed + (len + q - 1) / q + kDraft) * n;
+      if (chunks > 0) most = std::max(most, kFixed + (std::min(len, c) + q - 1) / q);
+    }
+    const int64_t rounds = (wgs + kCU - 1) / kCU;
+    const int64_t time = std::min((rounds * most + (rounds * kCU - wgs < drafts ? kDraft : 0)) * kCU, work + most * kCU);
+    if (time < best_time) {
+      best_time = time;
+      best = c;
+    }
+  }
+  return best;
+}
 
 TreePlan tree_plan(const dwkv_dims* d, const dwkv_tree* t) {
   TreePlan p;
   p.rows = tree_rows(d, t);
   p.split = tree_split(d, t, p.rows);
-  p.items = 0;
-  for (int b = 0; b < d->batch; ++b) p.items += tree_items(d, t, p.rows, p.split, b);
+  p.items = p.pairs = p.max_nrb = 0;
+  for (int b = 0; b < d->batch; ++b) {
+    int64_t chunks, nrb;
+    tree_seq(d, t, p.rows, p.split, b, chunks, nrb);
+    p.items += (chunks + 1) * nrb;
+    p.pairs += nrb > 0 ? chunks + 1 : 0;
+    p.max_nrb = std::max<int>(p.max_nrb, (int)nrb);
+  }
   p.bytes = std::max<size_t>(256, align_up((size_t)p.items * d->n_kv_heads * p.rows * (kHeadDim + d->basis_rank + 4) * sizeof(float), 256));
   return p;
 }
@@ -1301,7 +1336,7 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
   if ((st = split_args(d, c, layer, q, q_type, sm_scale, workspace, a)) != DWKV_OK) return st;
   const TreePlan p = tree_plan(d, tree);
   if (ws_bytes < p.bytes) return DWKV_E_WORKSPACE;
-  if (p.items * d->n_kv_heads > 0x7ffffff0) return DWKV_E_UNSUPPORTED;
+  if ((p.pairs * d->n_kv_heads + 8) * p.max_nrb > 0x7fffffff) return DWKV_E_UNSUPPORTED;
   if (tree->n_nodes == 0) return DWKV_OK;
   TreeArgs t;
   std::memset(&t, 0, sizeof(t));
@@ -1330,7 +1365,8 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
   t.out = out;
   t.T = a.T;
   t.res_stride = a.res_stride;
-  t.n_items = p.items * d->n_kv_heads;
+  t.n_pairs = p.pairs * d->n_kv_heads;
+  t.max_nrb = p.max_nrb;
   t.batch = d->batch;
   t.n_q_heads = d->n_q_heads;
   t.n_kv_heads = d->n_kv_heads;
@@ -1348,7 +1384,11 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
     for (int b = 0; b <= d->batch; ++b) {
       t.wt.tok[b] = d->cu_seqlens_host[b];
       t.wt.node[b] = tree->cu_nodes_host[b];
-      if (b < d->batch) t.wt.work[b + 1] = t.wt.work[b] + (int32_t)tree_items(d, tree, p.rows, p.split, b);
+      if (b == d->batch) break;
+      int64_t chunks, nrb;
+      tree_seq(d, tree, p.rows, p.split, b, chunks, nrb);
+      t.wt.work[b + 1] = t.wt.work[b] + (int32_t)((chunks + 1) * nrb);
+      t.wt.pair[b + 1] = t.wt.pair[b] + (int32_t)(nrb > 0 ? chunks + 1 : 0);
     }
   }
   return hip_status(launch_tree(t, most * t.group, reinterpret_cast<hipStream_t>(stream)));

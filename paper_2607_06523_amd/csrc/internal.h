@@ -356,6 +356,7 @@ constexpr int kTreeTile = 32;        // tokens per wave tile
 struct TreeTable {                   // up to kKernargSeqs sequences; n_seq == 0: from the device arrays
   int32_t n_seq;
   int32_t work[kKernargSeqs + 1];    // items of one KV head before each sequence
+  int32_t pair[kKernargSeqs + 1];    // chunks (the drafted nodes counted as one) of the sequences with nodes
   int32_t tok[kKernargSeqs + 1];
   int32_t node[kKernargSeqs + 1];
 };
@@ -384,7 +385,8 @@ struct TreeArgs {
   float* part;                 // [item][Hkv][rows][d + rb + 4]: r, a~, m, l
   float* out;                  // [N][Hq][d]
   int64_t T, res_stride;
-  int64_t n_items;             // items x Hkv
+  int64_t n_pairs;             // (chunk, KV head) pairs of the sequences with nodes
+  int32_t max_nrb;             // row blocks of the sequence with most nodes
   int32_t batch, n_q_heads, n_kv_heads, group, rb, split;
   int32_t rows;                // rows of a block: 16 or 32
   int32_t q_bf16, c8;

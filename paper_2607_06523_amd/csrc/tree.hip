@@ -32,7 +32,8 @@ __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) 
   } else {
     for (int i = lane; i < b; i += 64) {
       int ch, nr;
-      base += seq_items(a.cu[i + 1] - a.cu[i], a.cu_nodes[i + 1] - a.cu_nodes[i], a, ch, nr);
+      seq_items(a.cu[i + 1] - a.cu[i], a.cu_nodes[i + 1] - a.cu_nodes[i], a, ch, nr);
+      base += (int64_t)(ch + 1) * nr;
     }
     for (int d = 32; d; d >>= 1) base += __shfl_xor(base, d);
     t0 = a.cu[b], t1 = a.cu[b + 1], n0 = a.cu_nodes[b], n = a.cu_nodes[b + 1] - n0;

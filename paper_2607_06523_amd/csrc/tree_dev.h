@@ -42,6 +42,7 @@ constexpr int D = kHeadDim;
 constexpr int NW = kTreeWaves;           // waves per workgroup, two per SIMD
 constexpr int TT = kTreeTile;            // tokens per tile
 constexpr int kKRow = D + 8;             // halves per token row of the key code tile (16-byte pad: no bank conflicts)
+constexpr int kWaitVmcnt0 = 0x0F70;      // s_waitcnt immediate: vmcnt(0) only
 constexpr float kUp = 6.0f;              // a moved reference leaves the largest probability at 2^6,
 constexpr float kHead = 14.0f;           // and moves again when one exceeds 2^14: fp16 pairs hold both ends
 
@@ -52,7 +53,7 @@ __device__ __forceinline__ void wave_lds_sync() {
 }
 
 __device__ __forceinline__ rsrc_t make_rsrc(const void* base, int64_t bytes) {
-  const uint32_t n = (uint32_t)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff);
+  const uint32_t n = (uint32_t)min(max(bytes, (int64_t)0), (int64_t)1 << 30);   // a chunk is far shorter
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, n, 0x00020000);
 }
 
@@ -116,35 +117,40 @@ struct alignas(16) TreeSmem {
   };
 };
 
-// Sequence, row block, chunk and KV head of a workgroup.  Workgroups of one
-// (chunk, KV head) follow each other on one XCD (consecutive workgroups go to
-// the 8 XCDs in turn), so the row blocks share the chunk through its L2.
+// Sequence, row block, chunk and KV head of a workgroup.
 struct Item {
   int b, rb, h, c;                       // c == chunks: the drafted nodes
-  int chunks, nrb;
+  int chunks, nrb;                       // nrb == 0: no sequence has this item
   int t0, t1, n0, n;                     // tokens [t0, t1), nodes n0 .. n0 + n - 1 of the sequence
   int64_t part;                          // partial's index
 };
 
-__device__ __forceinline__ int seq_items(int T, int n, const TreeArgs& a, int& chunks, int& nrb) {
+__device__ __forceinline__ void seq_items(int T, int n, const TreeArgs& a, int& chunks, int& nrb) {
   chunks = T > 0 ? (T - 1) / a.split + 1 : 0;
   nrb = (n * a.group + a.rows - 1) / a.rows;
-  return (chunks + 1) * nrb;
 }
 
-__device__ __forceinline__ Item find_item(const TreeArgs& a, int64_t x) {
+// Workgroups go to the 8 XCDs in turn.  The row blocks of one (chunk, KV head)
+// follow each other on one XCD, so that they share the chunk through its L2:
+// workgroup w is row block (w / 8) % max_nrb of pair w % 8 + 8 (w / 8 / max_nrb),
+// the pairs (chunk, KV head) counted over the sequences with nodes.
+__device__ __forceinline__ Item find_item(const TreeArgs& a, uint32_t w) {
   Item it;
-  int64_t base = 0;
   const int H = a.n_kv_heads;
+  const uint32_t slot = w >> 3;
+  it.rb = (int)(slot % (uint32_t)a.max_nrb);
+  int64_t y = (int64_t)(slot / (uint32_t)a.max_nrb) * 8 + (w & 7), base = 0;   // pair, items before the sequence
+  it.nrb = 0;
   if (a.wt.n_seq > 0) {
     // branch-free: the table's entries are read at fixed offsets, all at once
-    int b = 0, w0 = 0, t0 = a.wt.tok[0], t1 = a.wt.tok[1], n0 = a.wt.node[0], n1 = a.wt.node[1];
+    int b = 0, w0 = 0, p0 = 0, t0 = a.wt.tok[0], t1 = a.wt.tok[1], n0 = a.wt.node[0], n1 = a.wt.node[1];
     if (a.wt.n_seq > 1) {
 #pragma unroll
       for (int i = 1; i < kKernargSeqs; ++i) {
-        const bool here = i < a.wt.n_seq && x >= (int64_t)a.wt.work[i] * H;
+        const bool here = i < a.wt.n_seq && y >= (int64_t)a.wt.pair[i] * H;
         b = here ? i : b;
         w0 = here ? a.wt.work[i] : w0;
+        p0 = here ? a.wt.pair[i] : p0;
         t0 = here ? a.wt.tok[i] : t0;
         t1 = here ? a.wt.tok[i + 1] : t1;
         n0 = here ? a.wt.node[i] : n0;
@@ -153,6 +159,7 @@ __device__ __forceinline__ Item find_item(const TreeArgs& a, int64_t x) {
     }
     it.b = b;
     base = w0;
+    y -= (int64_t)p0 * H;
     it.t0 = t0;
     it.t1 = t1;
     it.n0 = n0;
@@ -160,23 +167,26 @@ __device__ __forceinline__ Item find_item(const TreeArgs& a, int64_t x) {
   } else {                               // 64 sequences at a time
     const int lane = threadIdx.x & 63;
     for (int b0 = 0;; b0 += 64) {
+      if (b0 >= a.batch) return it;
       const int b = b0 + lane;
-      int chunks, nrb, mine = 0;
-      if (b < a.batch) mine = seq_items(a.cu[b + 1] - a.cu[b], a.cu_nodes[b + 1] - a.cu_nodes[b], a, chunks, nrb);
-      int64_t end = mine;
+      int chunks = 0, nrb = 0;
+      if (b < a.batch) seq_items(a.cu[b + 1] - a.cu[b], a.cu_nodes[b + 1] - a.cu_nodes[b], a, chunks, nrb);
+      const int pairs = nrb > 0 ? chunks + 1 : 0, items = pairs * nrb;
+      int pe = pairs, ie = items;
       for (int d = 1; d < 64; d <<= 1) {
-        const int64_t o = __shfl_up(end, d);
-        if (lane >= d) end += o;
+        const int po = __shfl_up(pe, d), io = __shfl_up(ie, d);
+        if (lane >= d) pe += po, ie += io;
       }
-      const unsigned long long in = __ballot(x < (base + end) * H);
+      const unsigned long long in = __ballot(y < (int64_t)pe * H);
       if (in) {
-        const int w = __ffsll(in) - 1;
-        base += __builtin_amdgcn_readlane((int)(end - mine), w);
-        it.b = b0 + w;
+        const int i = __ffsll(in) - 1;
+        base += __builtin_amdgcn_readlane(ie - items, i);
+        y -= (int64_t)__builtin_amdgcn_readlane(pe - pairs, i) * H;
+        it.b = b0 + i;
         break;
       }
-      base += __builtin_amdgcn_readlane((int)end, 63);
-      if (b0 + 64 >= a.batch) { it.b = a.batch - 1; break; }   // not reached: the grid ends with the items
+      base += __builtin_amdgcn_readlane(ie, 63);
+      y -= (int64_t)__builtin_amdgcn_readlane(pe, 63) * H;
     }
     it.t0 = a.cu[it.b];
     it.t1 = a.cu[it.b + 1];
@@ -184,11 +194,9 @@ __device__ __forceinline__ Item find_item(const TreeArgs& a, int64_t x) {
     it.n = a.cu_nodes[it.b + 1] - it.n0;
   }
   seq_items(it.t1 - it.t0, it.n, a, it.chunks, it.nrb);
-  int64_t y = x - base * H;
-  it.rb = (int)(y % it.nrb);
-  y /= it.nrb;
   it.h = (int)(y % H);
   it.c = (int)(y / H);
+  if (it.c > it.chunks || it.rb >= it.nrb) it.nrb = 0;       // past the last pair, or fewer row blocks than the longest
   it.part = (base + (int64_t)it.c * it.nrb + it.rb) * H + it.h;
   return it;
 }
@@ -331,61 +339,91 @@ struct Ahead {
   uint32_t ck, cv, vk, vv;               // entry pair `lane`: channel bytes and code byte, keys and values
 };
 
+// Places of a lane in a tile's streams; a tile adds a scalar offset.
 template <int NB, bool C8>
-__device__ __forceinline__ void load_k(Ahead<NB, C8>& f, const Streams& x, int rel, int T, int g, int col) {
+struct Lane {
+  static constexpr int NK = (NB + 1) / 2;
+  uint32_t k[2][NK], v, ks[C8 ? 2 : 1][C8 ? NK : 1], vs, t2;
+};
+
+constexpr uint32_t kPast = 0x7ffffff0;   // beyond every stream: reads as zero
+
+template <int NB, bool C8>
+__device__ __forceinline__ Lane<NB, C8> make_lane(int T, int lane) {
   constexpr int NK = (NB + 1) / 2, rb = 16 * NB;
+  const int g = lane >> 4, col = lane & 15;
+  Lane<NB, C8> p;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
-    const int tr = rel + 8 * (col >> 2) + 4 * b + (col & 3);           // token of score row `col`
+    const int t = 8 * (col >> 2) + 4 * b + (col & 3);                  // token of score row `col`
 #pragma unroll
     for (int s = 0; s < NK; ++s) {
-      const bool have = NB % 2 == 0 || s + 1 < NK || g < 2;            // past r_b: beyond the slab, which reads as zero
+      const bool have = NB % 2 == 0 || s + 1 < NK || g < 2;            // else past r_b
       if constexpr (C8) {
         const int blk = 2 * s + (g >> 1);
-        const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.k, have ? (((tr >> 4) * NB + blk) * 16 + (tr & 15)) * 16 + 8 * (g & 1) : 0x7ffffff0, 0, 0);
+        p.k[b][s] = have ? (((t >> 4) * NB + blk) * 16 + (t & 15)) * 16 + 8 * (g & 1) : kPast;
+        p.ks[b][s] = have ? (uint32_t)(blk * T + t) * 2 : kPast;
+      } else {
+        p.k[b][s] = have ? (((t >> 4) * (rb / 8) + 4 * s + g) * 128 + (t & 15) * 8) * 2 : kPast;
+      }
+    }
+  }
+  p.v = C8 ? ((g >> 1) * rb + col) * 16 + 8 * (g & 1) : (g * rb + col) * 16;
+  p.t2 = 2 * (lane & 31);
+  return p;
+}
+
+template <int NB, bool C8>
+__device__ __forceinline__ void load_k(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile) {
+  constexpr int NK = (NB + 1) / 2, step = TT * 16 * NB * (C8 ? 1 : 2);
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      if constexpr (C8) {
+        const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.k, p.k[b][s], tile * step, 0);
         f.k[b][s].x = w.x;
         f.k[b][s].y = w.y;
-        f.ks[b][s] = __builtin_amdgcn_raw_buffer_load_b16(x.ks, have ? (blk * T + tr) * 2 : 0x7ffffff0, 0, 0);
+        f.ks[b][s] = __builtin_amdgcn_raw_buffer_load_b16(x.ks, p.ks[b][s], tile * (2 * TT), 0);
       } else {
-        f.k[b][s] = __builtin_amdgcn_raw_buffer_load_b128(x.k, have ? (((tr >> 4) * (rb / 8) + 4 * s + g) * 128 + (tr & 15) * 8) * 2 : 0x7ffffff0, 0, 0);
+        f.k[b][s] = __builtin_amdgcn_raw_buffer_load_b128(x.k, p.k[b][s], tile * step, 0);
       }
     }
   }
 }
 
 template <int NB, bool C8>
-__device__ __forceinline__ void load_v(Ahead<NB, C8>& f, const Streams& x, int rel, int T, int g, int col, int lane) {
-  constexpr int rb = 16 * NB;
+__device__ __forceinline__ void load_v(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile) {
+  constexpr int step = TT * 16 * NB * (C8 ? 1 : 2);
 #pragma unroll
   for (int k = 0; k < NB; ++k) {
     if constexpr (C8) {
-      const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.v, ((((rel >> 4) + (g >> 1)) * rb + 16 * k + col) * 16) + 8 * (g & 1), 0, 0);
+      const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.v, p.v + 256 * k, tile * step, 0);
       f.v[k].x = w.x;
       f.v[k].y = w.y;
     } else {
-      f.v[k] = __builtin_amdgcn_raw_buffer_load_b128(x.v, (((rel >> 3) + g) * rb + 16 * k + col) * 16, 0, 0);
+      f.v[k] = __builtin_amdgcn_raw_buffer_load_b128(x.v, p.v + 256 * k, tile * step, 0);
     }
   }
 }
 
 template <int NB, bool C8>
-__device__ __forceinline__ void load_vs(Ahead<NB, C8>& f, const Streams& x, int rel, int T, int lane) {
+__device__ __forceinline__ void load_vs(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile, int T) {
   if constexpr (C8) {
 #pragma unroll
-    for (int k = 0; k < NB; ++k) f.vs[k] = __builtin_amdgcn_raw_buffer_load_b16(x.vs, (k * T + rel + (lane & 31)) * 2, 0, 0);
+    for (int k = 0; k < NB; ++k) f.vs[k] = __builtin_amdgcn_raw_buffer_load_b16(x.vs, p.t2, tile * (2 * TT) + k * T * 2, 0);
   }
 }
 
 // Scales and the first 64 entry pairs of a tile whose first entry is e0.
 template <int NB, bool C8>
-__device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x, int rel, uint32_t e0, int lane) {
-  const uint32_t t2 = (uint32_t)(rel + (lane & 31)) * 2, e = e0 + 2 * lane;
-  f.sk = __builtin_amdgcn_raw_buffer_load_b16(x.sk, t2, 0, 0);
-  f.sv = __builtin_amdgcn_raw_buffer_load_b16(x.sv, t2, 0, 0);
-  f.ck = __builtin_amdgcn_raw_buffer_load_b16(x.idx[0], e, 0, 0);
-  f.cv = __builtin_amdgcn_raw_buffer_load_b16(x.idx[1], e, 0, 0);
-  f.vk = __builtin_amdgcn_raw_buffer_load_b8(x.val[0], e >> 1, 0, 0);
-  f.vv = __builtin_amdgcn_raw_buffer_load_b8(x.val[1], e >> 1, 0, 0);
+__device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile, uint32_t e0, int lane) {
+  f.sk = __builtin_amdgcn_raw_buffer_load_b16(x.sk, p.t2, tile * (2 * TT), 0);
+  f.sv = __builtin_amdgcn_raw_buffer_load_b16(x.sv, p.t2, tile * (2 * TT), 0);
+  f.ck = __builtin_amdgcn_raw_buffer_load_b16(x.idx[0], 2 * lane, e0, 0);
+  f.cv = __builtin_amdgcn_raw_buffer_load_b16(x.idx[1], 2 * lane, e0, 0);
+  f.vk = __builtin_amdgcn_raw_buffer_load_b8(x.val[0], lane, e0 >> 1, 0);
+  f.vv = __builtin_amdgcn_raw_buffer_load_b8(x.val[1], lane, e0 >> 1, 0);
 }
 
 template <int NB, int NC, bool BF, bool C8>
@@ -393,11 +431,8 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
   constexpr int R = 16 * NC, NK = (NB + 1) / 2, rb = 16 * NB, stride = D + rb + 4;
   __shared__ TreeSmem<NB, NC, C8> sm;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
-  // consecutive workgroups of an XCD take consecutive items
-  const int64_t per = (a.n_items + 7) / 8;
-  const int64_t x = (int64_t)(blockIdx.x & 7) * per + (blockIdx.x >> 3);
-  if (x >= a.n_items) return;
-  const Item it = find_item(a, x);
+  const Item it = find_item(a, blockIdx.x);
+  if (it.nrb == 0) return;
   const int rows_left = it.n * a.group - it.rb * R;
   float* part = a.part + it.part * R * stride;
   if (it.c == it.chunks) {
@@ -429,18 +464,18 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
     sx.vs = make_rsrc(a.cscale_v + (int64_t)it.h * NB * T + tb, (NB * T - tb) * 2);
   }
   const int Ti = (int)T;
-  const int last = ntile - 1, j0 = min(wv, last);      // tiles past the last are read as the last and not used
+  const int wvu = __builtin_amdgcn_readfirstlane(wv);
+  const int last = ntile - 1, j0 = min(wvu, last);      // tiles past the last are read as the last and not used
   const auto load_off = [&](int j, uint32_t& oa, uint32_t& ob) {
     const int t = j * TT + (lane & 31);                // tokens outside the chunk hold no entries
-    oa = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)(min(max(t + tb, c0), c1) - tb) * 4, 0, 0) - ec0;
-    ob = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)(min(max(t + tb + 1, c0), c1) - tb) * 4, 0, 0) - ec0;
+    oa = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)min(max(t, c0 - tb), c1 - tb) * 4, 0, 0) - ec0;
+    ob = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)min(max(t + 1, c0 - tb), c1 - tb) * 4, 0, 0) - ec0;
   };
+  const Lane<NB, C8> lp = make_lane<NB, C8>(Ti, lane);
   Ahead<NB, C8> f;
   load_off(j0, f.oa, f.ob);
   load_off(min(j0 + NW, last), f.oa2, f.ob2);
-  load_k<NB, C8>(f, sx, j0 * TT, Ti, g, col);
-  load_v<NB, C8>(f, sx, j0 * TT, Ti, g, col, lane);
-  load_vs<NB, C8>(f, sx, j0 * TT, Ti, lane);
+  load_k<NB, C8>(f, sx, lp, j0);
 
   // ---- query fragments, and q~ = B^K q as fp16 pairs ---------------------------
   constexpr int TILES = NB * NC, PER = (2 * NK * NC + NW - 1) / NW;
@@ -514,20 +549,27 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
       reinterpret_cast<h4*>(&sm.qt[1][blk >> 1][n][ln])[g & 1] = lo;
     }
   }
-  const int down = max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15);
+  const int down = __builtin_amdgcn_readfirstlane(max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15));
   const float up = __builtin_ldexpf(1.f, down), fdn = __builtin_ldexpf(1.f, -down);
   uint32_t e0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.oa);
-  load_entries<NB, C8>(f, sx, j0 * TT, e0, lane);
+  load_entries<NB, C8>(f, sx, lp, j0, e0, lane);
+  load_vs<NB, C8>(f, sx, lp, j0, Ti);
+  load_v<NB, C8>(f, sx, lp, j0);
   __syncthreads();                       // q~ is whole
 
-  u4v qt[2][NK][NC];
+  // the q~ fragments stay in registers where those hold them beside the sums;
+  // a spill in the loop would wait for the loads in flight
+  constexpr bool kQReg = NK * NC < 4;
+  u4v qt[2][kQReg ? NK : 1][kQReg ? NC : 1];
+  if constexpr (kQReg) {
 #pragma unroll
-  for (int n = 0; n < NC; ++n)
+    for (int n = 0; n < NC; ++n)
 #pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      qt[0][s][n] = sm.qt[0][s][n][lane];
-      qt[1][s][n] = sm.qt[1][s][n][lane];
-    }
+      for (int s = 0; s < NK; ++s) {
+        qt[0][s][n] = sm.qt[0][s][n][lane];
+        qt[1][s][n] = sm.qt[1][s][n][lane];
+      }
+  }
   f4 acc_a[NB][NC], acc_r[D / 16][NC];   // a~ and the residual channels: (channel 4 g + i of the block, row col)
   float m[NC], l[NC];
 #pragma unroll
@@ -544,17 +586,72 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
   const float inf = __builtin_inff();
 
 #pragma unroll 1
-  for (int j = wv; j < ntile; j += NW) {
+  for (int j = wvu; j < ntile; j += NW) {
     const int t0 = tb + j * TT, jn = min(j + NW, last);
     const bool edge = t0 < c0 || t0 + TT > c1;
-    // ---- entries of the next tile and offsets of the one after, in flight
+    // Loads return in order, and a wait for one is a wait for those before it.  A
+    // tile's key coefficients, entries and value coefficients are requested
+    // in that order, each once its predecessor's registers are free.
+    // ---- basis part of the scores: (token 8 g + 4 b + i, row col)
+    f4 sb[2][NC], sr[2][NC];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const float c = -m[n] * fdn;
+        sb[b][n] = f4{c, c, c, c};
+        sr[b][n] = f4{0, 0, 0, 0};
+      }
+#pragma unroll
+    for (int s = 0; s < NK; ++s) {
+      h8 kh[2], kl[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if constexpr (C8) {
+          const float sc = half_bits_to_float((uint16_t)f.ks[b][s]);
+          float v[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.k[b][s].x, f.k[b][s].y}, e) * sc;
+          split8(v, kh[b], kl[b]);
+        } else {
+          kh[b] = __builtin_bit_cast(h8, f.k[b][s]);
+        }
+      }
+      u4v qh[NC], ql[NC];
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        if constexpr (kQReg) {
+          qh[n] = qt[0][s][n];
+          ql[n] = qt[1][s][n];
+        } else {
+          qh[n] = sm.qt[0][s][n][lane];
+          ql[n] = sm.qt[1][s][n][lane];
+        }
+      }
+#pragma unroll
+      for (int part = 0; part < (C8 ? 3 : 2); ++part)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int n = 0; n < NC; ++n)
+            sb[b][n] = mfma_h(part == 2 ? kl[b] : kh[b], __builtin_bit_cast(h8, part == 1 ? ql[n] : qh[n]), sb[b][n]);
+    }
+    load_k<NB, C8>(f, sx, lp, jn);
+    // ---- entries of the next tile and offsets of the one after
     const uint32_t oa = f.oa, ob = f.ob, sk = f.sk, sv = f.sv, ck = f.ck, cv = f.cv, vk = f.vk, vv = f.vv;
     const uint32_t en = e0;
     f.oa = f.oa2;
     f.ob = f.ob2;
     e0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.oa);
+    if constexpr (C8) {
+      if (lane < 32) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k) sm.vs[wv][k][lane] = (uint16_t)f.vs[k];
+      }
+    }
     load_off(min(jn + NW, last), f.oa2, f.ob2);
-    load_entries<NB, C8>(f, sx, jn * TT, e0, lane);
+    load_entries<NB, C8>(f, sx, lp, jn, e0, lane);
+    load_vs<NB, C8>(f, sx, lp, jn, Ti);
 
     // ---- scales, one lane per token
     const bool own = ob > oa;
@@ -578,13 +675,6 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
     if (lane < 32) {
       w.sk[lane] = odd_k ? a.qscale : fk * a.qscale;
       w.sv[lane] = odd_v ? 1.f : fv * exi;
-    }
-    if constexpr (C8) {
-      if (lane < 32) {
-#pragma unroll
-        for (int k = 0; k < NB; ++k) sm.vs[wv][k][lane] = (uint16_t)f.vs[k];
-      }
-      load_vs<NB, C8>(f, sx, jn * TT, Ti, lane);
     }
     // ---- entries into the code tiles, 64 pairs at a time (ranks are even, so a pair belongs to one token)
     const uint32_t e1 = (uint32_t)__builtin_amdgcn_readlane((int)ob, 31);
@@ -610,6 +700,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
           const uint32_t t2 = (uint32_t)(j * TT + t) * 2;
           const float tk = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sk, t2, 0, 0));
           const float tv = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sv, t2, 0, 0));
+          __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
           if (!(fabsf(tk) < inf)) wk0 = code_bits<BF>(a0 * tk), wk1 = code_bits<BF>(a1 * tk);
           if (!(fabsf(tv) < inf)) wv0 = h_bits(b0f * tv), wv1 = h_bits(b1f * tv);
         }
@@ -628,11 +719,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
         uint32_t x0, x1;
         carry = scatter(b0, carry, __builtin_amdgcn_raw_buffer_load_b16(sx.idx[0], e, 0, 0), __builtin_amdgcn_raw_buffer_load_b16(sx.idx[1], e, 0, 0),
                         __builtin_amdgcn_raw_buffer_load_b8(sx.val[0], e >> 1, 0, 0), __builtin_amdgcn_raw_buffer_load_b8(sx.val[1], e >> 1, 0, 0), x0, x1);
+        // nothing of this rare path may look pending after it: the compiler would
+        // have every tile wait for all its loads
+        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
       }
     }
     wave_lds_sync();
 
-    // ---- scores: (token 8 g + 4 b + i, row col)
+    // ---- residual part of the scores
     float ks[8], vs[8];
     {
       const f4 s0 = *reinterpret_cast<const f4*>(&w.sk[8 * g]), s1 = *reinterpret_cast<const f4*>(&w.sk[8 * g + 4]);
@@ -640,39 +734,6 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
 #pragma unroll
       for (int i = 0; i < 4; ++i) { ks[i] = s0[i]; ks[4 + i] = s1[i]; vs[i] = v0[i]; vs[4 + i] = v1[i]; }
     }
-    f4 sb[2][NC], sr[2][NC];
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const float c = -m[n] * fdn;
-        sb[b][n] = f4{c, c, c, c};
-        sr[b][n] = f4{0, 0, 0, 0};
-      }
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      h8 kh[2], kl[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if constexpr (C8) {
-          const float sc = half_bits_to_float((uint16_t)f.ks[b][s]);
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.k[b][s].x, f.k[b][s].y}, e) * sc;
-          split8(v, kh[b], kl[b]);
-        } else {
-          kh[b] = __builtin_bit_cast(h8, f.k[b][s]);
-        }
-      }
-#pragma unroll
-      for (int part = 0; part < (C8 ? 3 : 2); ++part)
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int n = 0; n < NC; ++n)
-            sb[b][n] = mfma_h(part == 2 ? kl[b] : kh[b], __builtin_bit_cast(h8, qt[part == 1][s][n]), sb[b][n]);
-    }
-    load_k<NB, C8>(f, sx, jn * TT, Ti, g, col);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       u4v qv[NC];
@@ -808,7 +869,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
         for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(lo, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
       }
     }
-    load_v<NB, C8>(f, sx, jn * TT, Ti, g, col, lane);
+    load_v<NB, C8>(f, sx, lp, jn);
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       const h8 av = __builtin_bit_cast(h8, *reinterpret_cast<const u4v*>(&w.v[(16 * k + col) * TT + 8 * g]));
@@ -905,7 +966,7 @@ void launch_tree_b(const TreeArgs& a, dim3 grid, hipStream_t s) {
 
 template <bool BF>
 void launch_tree_split(const TreeArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n_items + 7) / 8 * 8));
+  const dim3 grid((unsigned)((a.n_pairs + 7) / 8 * 8 * a.max_nrb));
   switch (a.rb / 16) {
     case 1: launch_tree_b<1, BF>(a, grid, s); break;
     case 2: launch_tree_b<2, BF>(a, grid, s); break;
