@@ -9,21 +9,26 @@ void launch_tree_split_bf16(const TreeArgs& a, hipStream_t s);
 namespace {
 
 // Joins the partials of kMR rows and applies B^V.  The four waves take every
-// fourth chunk, a lane four columns (residual channels, then a~), so a row's
-// partials are read with independent loads; sums in a fixed order.
-// grid (row pairs of the longest sequence, Hkv, B)
+// fourth chunk with a running maximum and sum of their own, a lane four columns
+// (residual channels, then a~): no load waits for another's value.  Sums in a
+// fixed order.  grid (row pairs of the longest sequence, Hkv, B)
 constexpr int kMR = 2, kMW = 4;
 struct alignas(16) MergeSmem {
   float part[kMW][kMR][2 * D];
   float m[kMW][kMR], l[kMW][kMR];
   float as[kMR][D];
-  uint16_t basis[128 * D];
+  u4v basis[128 * D / 8];
 };
 
 __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) {
   __shared__ MergeSmem sm;
   const int b = blockIdx.z, h = blockIdx.y, H = a.n_kv_heads, rb = a.rb;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const u4v* bv = reinterpret_cast<const u4v*>(a.basis + (int64_t)b * a.basis_b_stride + (int64_t)(h * 2 + 1) * rb * D);
+  u4v bw[8];                             // B^V on its way to LDS
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i * 16 < rb) bw[i] = bv[threadIdx.x + 256 * i];
   int64_t base = 0;
   int t0, t1, n0, n;
   if (a.wt.n_seq > 0) {
@@ -42,69 +47,77 @@ __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) 
   seq_items(t1 - t0, n, a, chunks, nrb);
   const int r0 = blockIdx.x * kMR, rows = n * a.group;
   if (r0 >= rows) return;
-  const uint16_t* bv = a.basis + (int64_t)b * a.basis_b_stride + (int64_t)(h * 2 + 1) * rb * D;
-  for (int i = threadIdx.x; i < rb * (D / 8); i += 64 * kMW) reinterpret_cast<u4v*>(sm.basis)[i] = reinterpret_cast<const u4v*>(bv)[i];
   const int stride = D + rb + 4, block = r0 / a.rows;         // a.rows is a multiple of kMR
   const float* p0 = a.part + ((base + block) * H + h) * a.rows * stride + (int64_t)(r0 % a.rows) * stride;
   const int64_t step = (int64_t)nrb * H * a.rows * stride;    // to the next chunk's partial
   const float inf = __builtin_inff();
-  // the rows' statistics: the largest reference, then every chunk's weight
-  float ms[kMR], ls[kMR];
-  bool absent[kMR];
+  const int cols = (D + rb) / 4, mycol = 4 * min(lane, cols - 1);
+  f4 o[kMR] = {};
+  float m[kMR], l[kMR];
 #pragma unroll
-  for (int r = 0; r < kMR; ++r) {
-    ms[r] = -inf;
-    bool gone = r0 + r >= rows;
-    for (int s = lane; s <= chunks && r0 + r < rows; s += 64) {
-      const float2 ml = *reinterpret_cast<const float2*>(p0 + r * stride + s * step + D + rb);
-      gone = gone || ml.y < 0.f;
-      if (!(ml.y == 0.f)) ms[r] = fmaxf(ms[r], ml.x);
-    }
-    for (int d = 32; d; d >>= 1) ms[r] = fmaxf(ms[r], __shfl_xor(ms[r], d));
-    absent[r] = __ballot(gone) != 0;
-    ls[r] = 0.f;
-  }
-  const int cols = (D + rb) / 4;
-  f4 o[kMR][2] = {};
+  for (int r = 0; r < kMR; ++r) m[r] = -inf, l[r] = 0.f;
+  constexpr int kAt = 4;                 // chunks of a wave read at once
+  const int last_row = rows - 1 - r0;
+  for (int s0 = wv; s0 <= chunks; s0 += kMW * kAt) {
+    float2 ml[kAt][kMR];
+    f4 x[kAt][kMR];
 #pragma unroll
-  for (int r = 0; r < kMR; ++r) {
-    if (absent[r]) continue;
-    const float* p = p0 + r * stride;
-#pragma unroll 4
-    for (int s = wv; s <= chunks; s += kMW) {
-      const float2 ml = *reinterpret_cast<const float2*>(p + s * step + D + rb);
-      const f4 x = *reinterpret_cast<const f4*>(p + s * step + 4 * min(lane, cols - 1));
-      const float wt = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - ms[r]);
-      ls[r] = __builtin_fmaf(wt, ml.y, ls[r]);
-      if (ml.y == 0.f) continue;         // nothing there, and its sums may be anything
-      o[r][0] += x * wt;
+    for (int k = 0; k < kAt; ++k)
+#pragma unroll
+      for (int r = 0; r < kMR; ++r) {
+        const float* p = p0 + min(r, last_row) * stride + min(s0 + kMW * k, chunks) * step;
+        ml[k][r] = *reinterpret_cast<const float2*>(p + D + rb);
+        x[k][r] = *reinterpret_cast<const f4*>(p + mycol);
+      }
+#pragma unroll
+    for (int k = 0; k < kAt; ++k) {
+      if (s0 + kMW * k > chunks) continue;
+#pragma unroll
+      for (int r = 0; r < kMR; ++r) {
+        if (ml[k][r].y == 0.f) continue;   // nothing there
+        const float mn = fmaxf(m[r], ml[k][r].x), was = m[r] > -inf ? __builtin_amdgcn_exp2f(m[r] - mn) : 0.f;
+        const float wt = __builtin_amdgcn_exp2f(ml[k][r].x - mn);
+        l[r] = ml[k][r].y < 0.f ? -inf : __builtin_fmaf(wt, ml[k][r].y, l[r] * was);   // absent: stays -inf
+        o[r] = o[r] * was + x[k][r] * wt;
+        m[r] = mn;
+      }
     }
   }
   if (lane < cols) {
 #pragma unroll
-    for (int r = 0; r < kMR; ++r) *reinterpret_cast<f4*>(&sm.part[wv][r][4 * lane]) = o[r][0];
+    for (int r = 0; r < kMR; ++r) *reinterpret_cast<f4*>(&sm.part[wv][r][4 * lane]) = o[r];
   }
   if (lane == 0) {
 #pragma unroll
-    for (int r = 0; r < kMR; ++r) sm.l[wv][r] = ls[r];
+    for (int r = 0; r < kMR; ++r) sm.m[wv][r] = m[r], sm.l[wv][r] = l[r];
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (i * 16 < rb) sm.basis[threadIdx.x + 256 * i] = bw[i];
   __syncthreads();
   const int r = threadIdx.x >> 7, c = threadIdx.x & 127;     // a thread per output
-  float l = 0.f, out = 0.f, av = 0.f;
+  float ms = -inf, ls = 0.f, out = 0.f, av = 0.f;
+  bool absent = false;
+#pragma unroll
+  for (int u = 0; u < kMW; ++u) ms = fmaxf(ms, sm.m[u][r]);
 #pragma unroll
   for (int u = 0; u < kMW; ++u) {
-    l += sm.l[u][r];
-    out += sm.part[u][r][c];
-    if (c < rb) av += sm.part[u][r][D + c];
+    if (sm.l[u][r] == 0.f) continue;
+    absent = absent || sm.l[u][r] == -inf;
+    const float wt = __builtin_amdgcn_exp2f(sm.m[u][r] - ms);
+    ls = __builtin_fmaf(wt, sm.l[u][r], ls);
+    out = __builtin_fmaf(wt, sm.part[u][r][c], out);
+    if (c < rb) av = __builtin_fmaf(wt, sm.part[u][r][D + c], av);
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = ls == 0.f ? 0.f : 1.f / ls;
   out *= inv;
   sm.as[r][c] = c < rb ? av * inv : 0.f;
   __syncthreads();
+  const uint16_t* bas = reinterpret_cast<const uint16_t*>(sm.basis);
 #pragma unroll 8
-  for (int i = 0; i < rb; ++i) out = __builtin_fmaf(sm.as[r][i], half_bits_to_float(sm.basis[i * D + c]), out);
+  for (int i = 0; i < rb; ++i) out = __builtin_fmaf(sm.as[r][i], half_bits_to_float(bas[i * D + c]), out);
   if (r0 + r < rows)
-    a.out[((int64_t)(n0 + (r0 + r) / a.group) * a.n_q_heads + h * a.group + (r0 + r) % a.group) * D + c] = absent[r] ? 0.f : out;
+    a.out[((int64_t)(n0 + (r0 + r) / a.group) * a.n_q_heads + h * a.group + (r0 + r) % a.group) * D + c] = absent ? 0.f : out;
 }
 
 }  // namespace

@@ -39,7 +39,6 @@ typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
 constexpr int D = kHeadDim;
-constexpr int NW = kTreeWaves;           // waves per workgroup, two per SIMD
 constexpr int TT = kTreeTile;            // tokens per tile
 constexpr int kKRow = D + 8;             // halves per token row of the key code tile (16-byte pad: no bank conflicts)
 constexpr int kWaitVmcnt0 = 0x0F70;      // s_waitcnt immediate: vmcnt(0) only
@@ -88,12 +87,15 @@ __device__ __forceinline__ uint16_t code_bits(float v) {   // v an int4 code: ex
 // 16 lanes read 16 consecutive rows.
 __device__ __forceinline__ int key_row(int t) { return 16 * ((t >> 2) & 1) + 4 * (t >> 3) + (t & 3); }
 
+// Lanes without an entry write past the ends of k and v and of mark's first half:
+// no branch keeps them out.
 struct alignas(16) WaveTile {
-  uint16_t k[TT * kKRow];                // key codes [token place][channel], zero between tiles
-  uint16_t v[D * TT];                    // value codes [channel][token]
+  uint16_t k[TT * kKRow + 8];            // key codes [token place][channel], zero between tiles
+  uint16_t v[D * TT + 8];                // value codes [channel][token]
   float sk[TT], sv[TT];                  // residual scales of the tile's tokens (sv in units of 2^ex)
-  uint8_t mark[64];
+  uint8_t mark[128];
 };
+constexpr uint32_t kNoKey = TT * kKRow, kNoValue = D * TT;
 
 // Smem of the drafted nodes' workgroups.
 template <int NC>
@@ -102,16 +104,22 @@ struct alignas(16) DraftSmem {
   uint16_t v[DWKV_MAX_TREE_NODES][D];
 };
 
+// Waves of a workgroup: two per SIMD, or one where it holds the sums of 64 rows.
+template <int NC>
+constexpr int kWaves = NC > 2 ? 4 : 8;
+
 template <int NB, int NC, bool C8>
 struct alignas(16) TreeSmem {
-  static constexpr int R = 16 * NC, NK = (NB + 1) / 2;
-  u4v qf[4][NC][64];                     // query fragments: channels 32 s + 8 g + j
-  u4v qt[2][NK][NC][64];                 // q~ fragments (hi, lo)
+  static constexpr int R = 16 * NC, NK = (NB + 1) / 2, NW = kWaves<NC>;
   float m[NW][R], l[NW][R];
   float big;                             // largest |q~|
   alignas(16) uint16_t vs[C8 ? NW : 1][C8 ? NB : 1][C8 ? TT : 8];   // value block scales of a tile (int8)
   union {
-    WaveTile w[NW];
+    struct {
+      WaveTile w[NW];
+      u4v qf[4][NC][64];                 // query fragments: channels 32 s + 8 g + j
+      u4v qt[2][NK][NC][64];             // q~ fragments (hi, lo)
+    };
     float acc[NW][R][D + 4];             // the waves' sums, 128 columns at a time
     DraftSmem<NC> d;
   };
@@ -230,7 +238,7 @@ __device__ __forceinline__ u4v q_piece(const TreeArgs& a, const Item& it, int r,
 // values.  Nodes a row does not see are skipped, not weighted with zero.
 template <int NC>
 __device__ __forceinline__ void draft_item(const TreeArgs& a, const Item& it, DraftSmem<NC>& sm, float* part, int stride) {
-  constexpr int R = 16 * NC, PER = R / NW;
+  constexpr int R = 16 * NC, NW = kWaves<NC>, PER = R / NW;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, rows = it.n * a.group;
   const uint16_t* k = a.k_new + (int64_t)(it.n0 + min(lane, it.n - 1)) * a.kv_stride + it.h * D;
   const uint16_t* V = a.v_new + (int64_t)it.n0 * a.kv_stride + it.h * D;
@@ -312,13 +320,14 @@ __device__ __forceinline__ void split8(const float (&v)[8], h8& hi, h8& lo) {
 
 __device__ __forceinline__ float byte_at(u2v w, int j) { return (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))); }
 
-// v rounded towards zero to an fp16 pair: two values' hi and lo halves.
+// Two values as fp16 pairs, rounded towards zero: hi and lo halves.  v - hi is
+// exact; the mixed-precision fma takes hi as it is packed.
 __device__ __forceinline__ void pair2(float v0, float v1, uint32_t& hi, uint32_t& lo) {
-  typedef __fp16 fp2 __attribute__((ext_vector_type(2)));
-  const fp2 h = __builtin_amdgcn_cvt_pkrtz(v0, v1);
-  const fp2 l = __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf((float)h[0], -1.f, v0), __builtin_fmaf((float)h[1], -1.f, v1));
-  hi = __builtin_bit_cast(uint32_t, h);
-  lo = __builtin_bit_cast(uint32_t, l);
+  hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(v0, v1));
+  float d0, d1;
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d0) : "v"(hi), "v"(v0));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d1) : "v"(hi), "v"(v1));
+  lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(d0, d1));
 }
 
 // Streams of a chunk and KV head; offsets count from the chunk's first 16-token block.
@@ -327,6 +336,18 @@ struct Streams {
   rsrc_t off, sk, sv;                    // offsets and residual scales from the chunk's first block on
   rsrc_t idx[2], val[2];                 // entries from the chunk's first on
 };
+
+// Asks for the vector instructions since the last such request to be spread
+// between N matrix products: a wave issues in order, and behind a run of
+// products they would wait for the matrix core.
+template <int N>
+__device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
+  }
+}
 
 // What a wave holds of a tile ahead of its use.
 template <int NB, bool C8>
@@ -427,8 +448,8 @@ __device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x,
 }
 
 template <int NB, int NC, bool BF, bool C8>
-__global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a) {
-  constexpr int R = 16 * NC, NK = (NB + 1) / 2, rb = 16 * NB, stride = D + rb + 4;
+__global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_kernel(const TreeArgs a) {
+  constexpr int NW = kWaves<NC>, R = 16 * NC, NK = (NB + 1) / 2, rb = 16 * NB, stride = D + rb + 4;
   __shared__ TreeSmem<NB, NC, C8> sm;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const Item it = find_item(a, blockIdx.x);
@@ -559,7 +580,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
 
   // the q~ fragments stay in registers where those hold them beside the sums;
   // a spill in the loop would wait for the loads in flight
-  constexpr bool kQReg = NK * NC < 4;
+  constexpr bool kQReg = NC <= 2 && NK * NC < 4;
   u4v qt[2][kQReg ? NK : 1][kQReg ? NC : 1];
   if constexpr (kQReg) {
 #pragma unroll
@@ -672,57 +693,51 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
     const uint32_t odd_tokens = (uint32_t)__ballot(odd_v);   // lanes 32 .. 63 repeat the first 32
     const bool odd = __ballot(odd_k || odd_v) != 0;
     // a scale that is not finite goes with its entries into the code tiles
-    if (lane < 32) {
-      w.sk[lane] = odd_k ? a.qscale : fk * a.qscale;
-      w.sv[lane] = odd_v ? 1.f : fv * exi;
-    }
+    w.sk[lane & 31] = odd_k ? a.qscale : fk * a.qscale;
+    w.sv[lane & 31] = odd_v ? 0.f : fv * exi;
     // ---- entries into the code tiles, 64 pairs at a time (ranks are even, so a pair belongs to one token)
     const uint32_t e1 = (uint32_t)__builtin_amdgcn_readlane((int)ob, 31);
     const uint32_t np = e1 > en ? min(e1 - en, (uint32_t)(TT * D)) / 2 : 0u;
-    uint32_t at_k = 0xffffffffu, at_v = 0;             // places of the first batch
+    uint32_t at_k, at_v;                               // places of the first batch
     const auto scatter = [&](uint32_t b0, int carry, uint32_t pk, uint32_t pv, uint32_t qk, uint32_t qv, uint32_t& ak, uint32_t& av) {
       w.mark[lane] = 0;
       wave_lds_sync();
       const uint32_t at = (oa - en) / 2 - b0;
-      if (lane < 32 && own && at < 64) w.mark[at] = (uint8_t)(lane + 1);
+      w.mark[lane < 32 && own && at < 64 ? at : 64 + lane] = (uint8_t)(lane + 1);
       wave_lds_sync();
       const int tok = max(incl_max((int)w.mark[lane]), carry);
-      ak = 0xffffffffu;
-      if (b0 + lane < np && tok > 0) {
-        const int t = tok - 1, kr = key_row(t) * kKRow;
-        const uint32_t k0 = kr + (pk & (D - 1)), k1 = kr + ((pk >> 8) & (D - 1));
-        const uint32_t v0 = (pv & (D - 1)) * TT + t, v1 = ((pv >> 8) & (D - 1)) * TT + t;
-        ak = k0 | k1 << 16;
-        av = v0 | v1 << 16;
-        const float a0 = (float)int4_value(qk), a1 = (float)int4_value(qk >> 4), b0f = (float)int4_value(qv), b1f = (float)int4_value(qv >> 4);
-        uint16_t wk0 = code_bits<BF>(a0), wk1 = code_bits<BF>(a1), wv0 = h_bits(b0f), wv1 = h_bits(b1f);
-        if (odd) {
-          const uint32_t t2 = (uint32_t)(j * TT + t) * 2;
-          const float tk = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sk, t2, 0, 0));
-          const float tv = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sv, t2, 0, 0));
-          __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-          if (!(fabsf(tk) < inf)) wk0 = code_bits<BF>(a0 * tk), wk1 = code_bits<BF>(a1 * tk);
-          if (!(fabsf(tv) < inf)) wv0 = h_bits(b0f * tv), wv1 = h_bits(b1f * tv);
-        }
-        w.k[k0] = wk0;
-        w.k[k1] = wk1;
-        w.v[v0] = wv0;
-        w.v[v1] = wv1;
+      const bool live = b0 + lane < np && tok > 0;
+      const int t = (tok - 1) & (TT - 1), kr = key_row(t) * kKRow;
+      const uint32_t k0 = live ? kr + (pk & (D - 1)) : kNoKey, k1 = live ? kr + ((pk >> 8) & (D - 1)) : kNoKey;
+      const uint32_t v0 = live ? (pv & (D - 1)) * TT + t : kNoValue, v1 = live ? ((pv >> 8) & (D - 1)) * TT + t : kNoValue;
+      ak = k0 | k1 << 16;
+      av = v0 | v1 << 16;
+      const float a0 = (float)int4_value(qk), a1 = (float)int4_value(qk >> 4), b0f = (float)int4_value(qv), b1f = (float)int4_value(qv >> 4);
+      uint16_t wk0 = code_bits<BF>(a0), wk1 = code_bits<BF>(a1), wv0 = h_bits(b0f), wv1 = h_bits(b1f);
+      if (odd) {
+        const uint32_t t2 = (uint32_t)(j * TT + t) * 2;
+        const float tk = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sk, t2, 0, 0));
+        const float tv = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sv, t2, 0, 0));
+        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
+        if (!(fabsf(tk) < inf)) wk0 = code_bits<BF>(a0 * tk), wk1 = code_bits<BF>(a1 * tk);
+        if (!(fabsf(tv) < inf)) wv0 = h_bits(b0f * tv), wv1 = h_bits(b1f * tv);
       }
+      w.k[k0] = wk0;
+      w.k[k1] = wk1;
+      w.v[v0] = wv0;
+      w.v[v1] = wv1;
       return __builtin_amdgcn_readlane(tok, 63);
     };
-    if (np > 0) {
-      int carry = scatter(0, 0, ck, cv, vk, vv, at_k, at_v);
+    int carry = scatter(0, 0, ck, cv, vk, vv, at_k, at_v);
 #pragma unroll 1
-      for (uint32_t b0 = 64; b0 < np; b0 += 64) {      // more than 128 entries: read as they come
-        const uint32_t e = en + 2 * (b0 + lane);
-        uint32_t x0, x1;
-        carry = scatter(b0, carry, __builtin_amdgcn_raw_buffer_load_b16(sx.idx[0], e, 0, 0), __builtin_amdgcn_raw_buffer_load_b16(sx.idx[1], e, 0, 0),
-                        __builtin_amdgcn_raw_buffer_load_b8(sx.val[0], e >> 1, 0, 0), __builtin_amdgcn_raw_buffer_load_b8(sx.val[1], e >> 1, 0, 0), x0, x1);
-        // nothing of this rare path may look pending after it: the compiler would
-        // have every tile wait for all its loads
-        __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
-      }
+    for (uint32_t b0 = 64; b0 < np; b0 += 64) {        // more than 128 entries: read as they come
+      const uint32_t e = en + 2 * (b0 + lane);
+      uint32_t x0, x1;
+      carry = scatter(b0, carry, __builtin_amdgcn_raw_buffer_load_b16(sx.idx[0], e, 0, 0), __builtin_amdgcn_raw_buffer_load_b16(sx.idx[1], e, 0, 0),
+                      __builtin_amdgcn_raw_buffer_load_b8(sx.val[0], e >> 1, 0, 0), __builtin_amdgcn_raw_buffer_load_b8(sx.val[1], e >> 1, 0, 0), x0, x1);
+      // nothing of this rare path may look pending after it: the compiler would
+      // have every tile wait for all its loads
+      __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
     }
     wave_lds_sync();
 
@@ -811,10 +826,17 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
       }
       first = false;
     }
-    // ---- probabilities as fp16 pairs, plain and times the value scales
-    u4v ph[NC], pl[NC], rh[NC], rl[NC];
+    // ---- probabilities as fp16 pairs, plain and times the value scales; values:
+    // channel blocks of the basis, then of the residual.  One block of 16 rows is
+    // prepared while the products of the one before it run.
+    float vo[8] = {};                    // an infinite entry meets two positive halves
+    if (odd_tokens) {
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
+      for (int e = 0; e < 8; ++e)
+        if ((odd_tokens >> (8 * g + e)) & 1) vo[e] = 1.f + 0x1p-13f;
+    }
+    u4v ph[NC], pl[NC], rh[2], rl[2];
+    const auto prepare = [&](int n) {
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
@@ -825,28 +847,38 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
         pair2(v0, v1, h, lo);
         ph[n][e >> 1] = h;
         pl[n][e >> 1] = lo;
-        pair2(v0 * vs[e], v1 * vs[e + 1], h, lo);
-        rh[n][e >> 1] = h;
-        rl[n][e >> 1] = lo;
+        pair2(__builtin_fmaf(v0, vs[e], vo[e]), __builtin_fmaf(v1, vs[e + 1], vo[e + 1]), h, lo);
+        rh[n & 1][e >> 1] = h;
+        rl[n & 1][e >> 1] = lo;
       }
       l[n] += sum[0] + sum[1];
-      if (odd_tokens) {                  // an infinite entry meets positive numbers only
-        h8 hh = __builtin_bit_cast(h8, rh[n]), ll = __builtin_bit_cast(h8, rl[n]);
+    };
+    h8 vc[D / 16];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if ((odd_tokens >> (8 * g + e)) & 1) {
-            hh[e] = hh[e] > (_Float16)0x1p-14f ? hh[e] : (_Float16)0x1p-14f;
-            ll[e] = (_Float16)0x1p-14f;
-          }
-        rh[n] = __builtin_bit_cast(u4v, hh);
-        rl[n] = __builtin_bit_cast(u4v, ll);
+    for (int k = 0; k < D / 16; ++k) vc[k] = __builtin_bit_cast(h8, *reinterpret_cast<const u4v*>(&w.v[(16 * k + col) * TT + 8 * g]));
+    prepare(0);
+#pragma unroll
+    for (int n = 0; n < NC; ++n) {
+      const h8 r0 = __builtin_bit_cast(h8, rh[n & 1]), r1 = __builtin_bit_cast(h8, rl[n & 1]);
+      if constexpr (!C8) {
+        const h8 p0 = __builtin_bit_cast(h8, ph[n]), p1 = __builtin_bit_cast(h8, pl[n]);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) acc_a[k][n] = mfma_h(__builtin_bit_cast(h8, f.v[k]), p0, acc_a[k][n]);
+#pragma unroll
+        for (int k = 0; k < NB; ++k) acc_a[k][n] = mfma_h(__builtin_bit_cast(h8, f.v[k]), p1, acc_a[k][n]);
+      }
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) acc_r[k][n] = mfma_h(vc[k], r0, acc_r[k][n]);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) acc_r[k][n] = mfma_h(vc[k], r1, acc_r[k][n]);
+      if (n + 1 < NC) {
+        prepare(n + 1);
+        interleave<(C8 ? 0 : 2) * NB + D / 8>();
       }
     }
-    // ---- values: channel blocks of the basis, then of the residual
+    if constexpr (C8) {                  // one block dequantized at a time
 #pragma unroll
-    for (int k = 0; k < NB; ++k) {
-      h8 hi, lo;
-      if constexpr (C8) {
+      for (int k = 0; k < NB; ++k) {
         const u4v sw = *reinterpret_cast<const u4v*>(&sm.vs[wv][k][8 * g]);
         float v[8];
 #pragma unroll
@@ -856,33 +888,22 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
           for (int e = 0; e < 8; ++e)
             if (t0 + 8 * g + e < c0 || t0 + 8 * g + e >= c1) v[e] = 0.f;
         }
+        h8 hi, lo;
         split8(v, hi, lo);
-      } else {
-        hi = __builtin_bit_cast(h8, f.v[k]);
-      }
 #pragma unroll
-      for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
+        for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
 #pragma unroll
-      for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, pl[n]), acc_a[k][n]);
-      if constexpr (C8) {
+        for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, pl[n]), acc_a[k][n]);
 #pragma unroll
         for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(lo, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
       }
     }
     load_v<NB, C8>(f, sx, lp, jn);
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      const h8 av = __builtin_bit_cast(h8, *reinterpret_cast<const u4v*>(&w.v[(16 * k + col) * TT + 8 * g]));
-#pragma unroll
-      for (int n = 0; n < NC; ++n) acc_r[k][n] = mfma_h(av, __builtin_bit_cast(h8, rh[n]), acc_r[k][n]);
-#pragma unroll
-      for (int n = 0; n < NC; ++n) acc_r[k][n] = mfma_h(av, __builtin_bit_cast(h8, rl[n]), acc_r[k][n]);
-    }
     // ---- the code tiles go back to zero
     wave_lds_sync();
     if (np > 64) {
       for (int i = lane; i < (int)((sizeof(w.k) + sizeof(w.v)) / 16); i += 64) reinterpret_cast<u4v*>(&w)[i] = u4v{0, 0, 0, 0};
-    } else if (at_k != 0xffffffffu) {
+    } else {
       w.k[at_k & 0xffff] = 0;
       w.k[at_k >> 16] = 0;
       w.v[at_v & 0xffff] = 0;
@@ -952,13 +973,14 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_split_kernel(const TreeArgs a
 
 template <int NB, int NC, bool BF>
 void launch_tree_c(const TreeArgs& a, dim3 grid, hipStream_t s) {
-  if (a.c8) hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, true>), grid, dim3(64 * NW), 0, s, a);
-  else hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, false>), grid, dim3(64 * NW), 0, s, a);
+  if (a.c8) hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, true>), grid, dim3(64 * kWaves<NC>), 0, s, a);
+  else hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, false>), grid, dim3(64 * kWaves<NC>), 0, s, a);
 }
 
 template <int NB, bool BF>
 void launch_tree_b(const TreeArgs& a, dim3 grid, hipStream_t s) {
   if constexpr (NB <= 4) {
+    if (a.rows == 64) return launch_tree_c<NB, 4, BF>(a, grid, s);
     if (a.rows == 32) return launch_tree_c<NB, 2, BF>(a, grid, s);
   }
   launch_tree_c<NB, 1, BF>(a, grid, s);
