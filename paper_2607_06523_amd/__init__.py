@@ -45,6 +45,29 @@ def _stream(torch, device):
     return C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 
+class _on:
+    """``with _on(torch, index)``: the device current, left alone when it is already."""
+
+    def __init__(self, torch, index):
+        self.torch, self.index, self.was = torch, index, torch.cuda.current_device()
+
+    def __enter__(self):
+        if self.was != self.index:
+            self.torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.was != self.index:
+            self.torch.cuda.set_device(self.was)
+
+
+def _all_on(index, *tensors):
+    """Whether every tensor (None aside) is on GPU ``index``."""
+    for x in tensors:
+        if x is not None and x.get_device() != index:
+            return False
+    return True
+
+
 def probe_schedule(step: int, period: int, n_heads: int, n_kv_heads: int, n_pos: int = 1):
     """dwkv_probe_schedule: (probed KV heads, positions) at decode step
     `step`, ([], 0) on a step that does not probe."""
@@ -112,7 +135,7 @@ class DraftTree:
         t.n_nodes = self.n_nodes
         t.cu_nodes_host = self.cu_host.ctypes.data_as(C.POINTER(C.c_int32))
         t.cu_nodes, t.parent = self.cu.data_ptr(), parent.data_ptr()
-        self.cstruct = t
+        self.cstruct, self.ref, self.index = t, C.byref(t), parent.get_device()
 
 
 def tree_verify_workspace(tree: DraftTree, vocab: int, max_children: int):
@@ -143,16 +166,16 @@ def tree_verify(tree: DraftTree, token, target, u, u_next, draft=None, max_child
         if x.dtype != torch.float32 or x.numel() != n or not x.is_contiguous():
             raise TypeError("u and u_next must be contiguous float32 [N] and [B]")
     dev = tree.parent.device
-    if any(x is not None and x.device != dev for x in (token, target, draft, u, u_next, workspace)):
+    if not _all_on(tree.index, token, target, draft, u, u_next, workspace):
         raise ValueError("every tensor must be on the tree's device")
     V = target.shape[1]
     ws = workspace if workspace is not None else tree_verify_workspace(tree, V, max_children)
-    path = torch.empty(N, dtype=torch.int32, device=dev)
-    n_kept, nxt = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2))
-    with torch.cuda.device(dev):
-        st = load().dwkv_tree_verify(B, C.byref(tree.cstruct), _ptr(token), V, kinds[target.dtype], _ptr(target),
-                                     _ptr(draft), _ptr(u), _ptr(u_next), int(max_children), _ptr(path), _ptr(n_kept),
-                                     _ptr(nxt), _ptr(ws), ws.numel(), _stream(torch, dev))
+    path, n_kept, nxt = torch.empty(N + 2 * B, dtype=torch.int32, device=dev).split((N, B, B))
+    with _on(torch, tree.index):
+        st = load().dwkv_tree_verify(B, tree.ref, token.data_ptr(), V, kinds[target.dtype], target.data_ptr(),
+                                     draft.data_ptr() if draft is not None else None, u.data_ptr(), u_next.data_ptr(),
+                                     int(max_children), path.data_ptr(), n_kept.data_ptr(), nxt.data_ptr(), ws.data_ptr(),
+                                     ws.numel(), torch.cuda.current_stream(tree.index).cuda_stream)
     binding.check(st, "dwkv_tree_verify")
     return path, n_kept, nxt
 
@@ -607,26 +630,28 @@ class DeviceCache:
             raise TypeError("q must be float16 or bfloat16")
         if k_new.dtype != torch.float16 or v_new.dtype != torch.float16:
             raise TypeError("k_new and v_new must be float16")
-        for x, heads in ((q, Hq), (k_new, Hk), (v_new, Hk)):
-            if tuple(x.shape) != (N, heads, d) or (N > 0 and (x.stride(2) != 1 or x.stride(1) != d)):
-                raise ValueError("q must be [N, Hq, d], k_new and v_new [N, Hkv, d], each row without gaps")
-        if N > 1 and k_new.stride(0) != v_new.stride(0):
+        if q.shape != (N, Hq, d) or k_new.shape != (N, Hk, d) or v_new.shape != (N, Hk, d):
+            raise ValueError("q must be [N, Hq, d], k_new and v_new [N, Hkv, d]")
+        qs, ks, vs = q.stride(), k_new.stride(), v_new.stride()
+        if N > 0 and not qs[1:] == ks[1:] == vs[1:] == (d, 1):
+            raise ValueError("the rows of q, k_new and v_new must have no gaps inside")
+        if N > 1 and ks[0] != vs[0]:
             raise ValueError("k_new and v_new must have the same row stride")
-        if any(x is not None and x.device != self.basis.device for x in (q, k_new, v_new, tree.parent, out, workspace)):
+        index = self.basis.get_device()
+        if tree.index != index or not _all_on(index, q, k_new, v_new, out, workspace):
             raise ValueError("every tensor must be on the cache's device")
         if out is None:
             out = torch.empty((N, Hq, d), dtype=torch.float32, device=self.basis.device)
-        elif out.dtype != torch.float32 or tuple(out.shape) != (N, Hq, d) or not out.is_contiguous():
+        elif out.dtype != torch.float32 or out.shape != (N, Hq, d) or not out.is_contiguous():
             raise TypeError("out must be contiguous float32 [N, Hq, d]")
         if N == 0:
             return out
         ws = workspace if workspace is not None else self.tree_workspace(tree)
-        qs, ks = (q.stride(0), k_new.stride(0)) if N > 1 else (0, 0)
-        with torch.cuda.device(self.basis.device):
-            st = self.lib.dwkv_tree_decode(C.byref(self.dims), C.byref(self.cstruct), int(layer), C.byref(tree.cstruct),
-                                           _ptr(q), F16 if q.dtype == torch.float16 else BF16, qs, _ptr(k_new), _ptr(v_new), ks,
-                                           float(sm_scale or 0.0), _ptr(out), _ptr(ws), ws.numel(),
-                                           _stream(torch, self.basis.device))
+        with _on(torch, index):
+            st = self.lib.dwkv_tree_decode(C.byref(self.dims), C.byref(self.cstruct), int(layer), tree.ref, q.data_ptr(),
+                                           F16 if q.dtype == torch.float16 else BF16, qs[0] if N > 1 else 0, k_new.data_ptr(),
+                                           v_new.data_ptr(), ks[0] if N > 1 else 0, float(sm_scale or 0.0), out.data_ptr(),
+                                           ws.data_ptr(), ws.numel(), torch.cuda.current_stream(index).cuda_stream)
         binding.check(st, "dwkv_tree_decode")
         return out
 
@@ -653,13 +678,14 @@ class DeviceCache:
             n_new = int(new_code.shape[-1])
             if new_code.dtype != torch.uint8 or tuple(new_code.shape) != (M, H, n_new) or not new_code.is_contiguous():
                 raise TypeError("new_code must be contiguous uint8 [M, Hkv, n]")
-        if any(x is not None and x.device != self.basis.device for x in (src_token, src_seq, new_code, workspace, src.basis)):
+        index = self.basis.get_device()
+        if not _all_on(index, src_token, src_seq, new_code, workspace, src.basis):
             raise ValueError("every tensor must be on the cache's device")
         ws = workspace if workspace is not None else self.repack_workspace()
-        with torch.cuda.device(self.basis.device):
+        with _on(torch, index):
             st = self.lib.dwkv_repack(C.byref(self.dims), C.byref(self.cstruct), C.byref(src.dims), C.byref(src.cstruct),
-                                      _ptr(src_token), _ptr(src_seq), _ptr(new_code), n_new, _ptr(ws), ws.numel(),
-                                      _stream(torch, self.basis.device))
+                                      src_token.data_ptr() or None, src_seq.data_ptr(), None if new_code is None else new_code.data_ptr(),
+                                      n_new, ws.data_ptr(), ws.numel(), torch.cuda.current_stream(index).cuda_stream)
         binding.check(st, "dwkv_repack")
 
     def residual_map(self, layer: int, z: int, kv_head: int, t0: int, t1: int):

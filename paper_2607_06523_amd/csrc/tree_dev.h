@@ -112,6 +112,7 @@ template <int NB, int NC, bool C8>
 struct alignas(16) TreeSmem {
   static constexpr int R = 16 * NC, NK = (NB + 1) / 2, NW = kWaves<NC>;
   float m[NW][R], l[NW][R];
+  uint32_t odd[D];                       // channels with entries of value scales that are not finite: bits +inf, -inf, NaN
   float big;                             // largest |q~|
   alignas(16) uint16_t vs[C8 ? NW : 1][C8 ? NB : 1][C8 ? TT : 8];   // value block scales of a tile (int8)
   union {
@@ -520,6 +521,7 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     sm.qf[s][n][ln] = w;
   }
   if (threadIdx.x == 0) sm.big = 0.f;
+  if (threadIdx.x < D) sm.odd[threadIdx.x] = 0;
   WaveTile& w = sm.w[wv];
   for (int i = lane; i < (int)((sizeof(w.k) + sizeof(w.v)) / 16); i += 64) reinterpret_cast<u4v*>(&w)[i] = u4v{0, 0, 0, 0};
   __syncthreads();
@@ -690,9 +692,11 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
 #pragma unroll
         for (int n = 0; n < NC; ++n) acc_r[k][n] *= fall;
     }
-    const uint32_t odd_tokens = (uint32_t)__ballot(odd_v);   // lanes 32 .. 63 repeat the first 32
     const bool odd = __ballot(odd_k || odd_v) != 0;
-    // a scale that is not finite goes with its entries into the code tiles
+    // A key scale that is not finite goes with its entries into the code tile.  A
+    // value scale that is not: every row sees its token, so its entries'
+    // channels end as infinities of their sign or NaN whatever the rest is; they
+    // are noted, and left out here.
     w.sk[lane & 31] = odd_k ? a.qscale : fk * a.qscale;
     w.sv[lane & 31] = odd_v ? 0.f : fv * exi;
     // ---- entries into the code tiles, 64 pairs at a time (ranks are even, so a pair belongs to one token)
@@ -720,7 +724,11 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
         const float tv = half_bits_to_float(__builtin_amdgcn_raw_buffer_load_b16(sx.sv, t2, 0, 0));
         __builtin_amdgcn_s_waitcnt(kWaitVmcnt0);
         if (!(fabsf(tk) < inf)) wk0 = code_bits<BF>(a0 * tk), wk1 = code_bits<BF>(a1 * tk);
-        if (!(fabsf(tv) < inf)) wv0 = h_bits(b0f * tv), wv1 = h_bits(b1f * tv);
+        if (!(fabsf(tv) < inf) && live) {
+          const float x0 = b0f * tv, x1 = b1f * tv;
+          atomicOr(&sm.odd[pv & (D - 1)], x0 > 0.f ? 1u : x0 < 0.f ? 2u : 4u);
+          atomicOr(&sm.odd[(pv >> 8) & (D - 1)], x1 > 0.f ? 1u : x1 < 0.f ? 2u : 4u);
+        }
       }
       w.k[k0] = wk0;
       w.k[k1] = wk1;
@@ -829,13 +837,7 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     // ---- probabilities as fp16 pairs, plain and times the value scales; values:
     // channel blocks of the basis, then of the residual.  One block of 16 rows is
     // prepared while the products of the one before it run.
-    float vo[8] = {};                    // an infinite entry meets two positive halves
-    if (odd_tokens) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if ((odd_tokens >> (8 * g + e)) & 1) vo[e] = 1.f + 0x1p-13f;
-    }
-    u4v ph[NC], pl[NC], rh[2], rl[2];
+    u4v ph[C8 ? NC : 2], pl[C8 ? NC : 2], rh[2], rl[2];
     const auto prepare = [&](int n) {
       float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -845,9 +847,9 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
         sum[1] += v1;
         uint32_t h, lo;
         pair2(v0, v1, h, lo);
-        ph[n][e >> 1] = h;
-        pl[n][e >> 1] = lo;
-        pair2(__builtin_fmaf(v0, vs[e], vo[e]), __builtin_fmaf(v1, vs[e + 1], vo[e + 1]), h, lo);
+        ph[C8 ? n : n & 1][e >> 1] = h;
+        pl[C8 ? n : n & 1][e >> 1] = lo;
+        pair2(v0 * vs[e], v1 * vs[e + 1], h, lo);
         rh[n & 1][e >> 1] = h;
         rl[n & 1][e >> 1] = lo;
       }
@@ -861,7 +863,7 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     for (int n = 0; n < NC; ++n) {
       const h8 r0 = __builtin_bit_cast(h8, rh[n & 1]), r1 = __builtin_bit_cast(h8, rl[n & 1]);
       if constexpr (!C8) {
-        const h8 p0 = __builtin_bit_cast(h8, ph[n]), p1 = __builtin_bit_cast(h8, pl[n]);
+        const h8 p0 = __builtin_bit_cast(h8, ph[n & 1]), p1 = __builtin_bit_cast(h8, pl[n & 1]);
 #pragma unroll
         for (int k = 0; k < NB; ++k) acc_a[k][n] = mfma_h(__builtin_bit_cast(h8, f.v[k]), p0, acc_a[k][n]);
 #pragma unroll
@@ -942,6 +944,9 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     f4 s = {0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < NW; ++u) s += *reinterpret_cast<const f4*>(&sm.acc[u][r][c]);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (const uint32_t o = sm.odd[c + k]) s[k] = o == 1 ? inf : o == 2 ? -inf : __builtin_nanf("");
     if (r < rows_left) *reinterpret_cast<f4*>(part + r * stride + c) = s;
   }
   __syncthreads();
