@@ -420,7 +420,7 @@ struct VerifyEnd {
   int32_t out[DWKV_MAX_TREE_NODES];
 };
 constexpr int kVerifyChunk = 2048;   // vocabulary entries of a workgroup
-constexpr int kVerifyZChunk = 8192;
+constexpr int kVerifyZChunk = 4096;
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t s);
 
 // Repacking (repack.hip).
