@@ -624,7 +624,7 @@ size_t dwkv_repack_workspace_bytes(const dwkv_dims* dst);
  * the lengths, res_stride and split_tokens (else DWKV_E_DIMS), and no array of
  * `to` overlaps one of `from`.
  *   workspace: >= dwkv_repack_workspace_bytes(dst), no initial contents
- * Three launches.  basis, coef_k and coef_v of both caches and workspace
+ * Up to three launches.  basis, coef_k and coef_v of both caches and workspace
  * 16-byte aligned, the res_off arrays, src_token and src_seq 4-byte, scales,
  * res_idx 2-byte. */
 dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_dims* src, const dwkv_cache* from,

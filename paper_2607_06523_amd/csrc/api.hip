@@ -1510,8 +1510,8 @@ dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_d
   for (const auto& p : pairs)
     if (p[0] && p[0] == p[1]) return DWKV_E_DIMS;        // not in place
   if (ws_bytes < dwkv_repack_workspace_bytes(dst)) return DWKV_E_WORKSPACE;
-  // one grid row per window and head, one grid layer per layer and Z
-  if ((int64_t)(dst->n_layers / dst->window) * dst->n_kv_heads > 65535 || 2 * (int64_t)dst->n_layers > 65535) return DWKV_E_UNSUPPORTED;
+  // one grid row per window and head, one grid layer per layer
+  if ((int64_t)(dst->n_layers / dst->window) * dst->n_kv_heads > 65535 || dst->n_layers > 65535) return DWKV_E_UNSUPPORTED;
   RepackArgs a;
   std::memset(&a, 0, sizeof(a));
   a.to = *to;

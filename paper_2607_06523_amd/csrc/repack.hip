@@ -2,9 +2,11 @@
 // sequences (gfx950).  Nothing is computed but the offsets; every byte of the
 // destination is written once, from where its token lay in the source:
 //  * repack_code_kernel: the tokens' rank codes, and the block sums of their ranks
-//  * repack_offset_kernel: the offsets, each block adding the sums before it
-//  * repack_copy_kernel: coefficients, scales and entries of 64 tokens of one
-//    (layer, Z, KV head) per workgroup.
+//  * repack_offset_kernel: the offsets, each block adding the sums before it (a
+//    cache of one block has them from the first kernel)
+//  * repack_copy_kernel: coefficients, scales and entries of 256 tokens of one
+//    (layer, KV head) per workgroup, keys and values.
+// Bound by HBM, reading and writing.
 #include "entry.h"
 #include "internal.h"
 
@@ -14,7 +16,8 @@ namespace {
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 
 constexpr int kRT = 256;
-constexpr int kTok = 64;                 // tokens per copy workgroup
+constexpr int kTok = kRT;                // tokens per copy workgroup, one per thread
+constexpr int kPer = kRepackBlock / kRT; // tokens per thread of the offset scan
 constexpr int D = kHeadDim;
 
 // Source token of slot t, or -1 for a fresh slot.
@@ -53,51 +56,28 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* red, uint32
   return before + inc - v;
 }
 
-// grid (nblk, M*Hkv)
-__global__ __launch_bounds__(kRT) void repack_code_kernel(const RepackArgs a) {
-  __shared__ uint32_t red[kRT / 64];
-  const int mh = blockIdx.y;
-  uint8_t* code = const_cast<uint8_t*>(a.to.rank_code) + (int64_t)mh * a.T;
-  uint32_t sum = 0;
-  for (int i = 0; i < kRepackBlock / kRT; ++i) {
-    const int64_t t = (int64_t)blockIdx.x * kRepackBlock + i * kRT + threadIdx.x;
-    if (t < a.T) {
-      const int c = code_of(a, mh, t);
-      code[t] = (uint8_t)c;
-      sum += (uint32_t)a.levels[c];
-    }
+// Offsets of a block whose tokens' ranks come after `run` entries, four
+// consecutive tokens per thread; the block's total.
+__device__ __forceinline__ uint32_t write_offsets(const RepackArgs& a, int mh, const int (&code)[kPer], uint32_t run, uint32_t* red) {
+  uint32_t* off = const_cast<uint32_t*>(a.to.res_off) + (int64_t)mh * (a.T + 1);
+  const int64_t t0 = (int64_t)blockIdx.x * kRepackBlock + kPer * threadIdx.x;
+  uint32_t mine = 0, total;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) mine += t0 + i < a.T ? (uint32_t)a.levels[code[i]] : 0u;
+  uint32_t at = run + block_scan(mine, red, total);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    if (t0 + i >= a.T) break;
+    off[t0 + i] = at;
+    at += (uint32_t)a.levels[code[i]];
+    if (t0 + i == a.T - 1) off[a.T] = at;
   }
-  uint32_t total;
-  block_scan(sum, red, total);
-  if (threadIdx.x == 0) a.bsum[(int64_t)mh * a.nblk + blockIdx.x] = total;
+  if (a.T == 0 && blockIdx.x == 0 && threadIdx.x == 0) off[0] = 0;
+  return total;
 }
 
-// grid (nblk, M*Hkv); also the bases, spread over the workgroups
-__global__ __launch_bounds__(kRT) void repack_offset_kernel(const RepackArgs a) {
-  __shared__ uint32_t red[kRT / 64];
-  const int mh = blockIdx.y;
-  const uint8_t* code = a.to.rank_code + (int64_t)mh * a.T;
-  uint32_t* off = const_cast<uint32_t*>(a.to.res_off) + (int64_t)mh * (a.T + 1);
-  uint32_t run = 0;
-  {
-    uint32_t sum = 0, total;
-    for (int i = threadIdx.x; i < (int)blockIdx.x; i += kRT) sum += a.bsum[(int64_t)mh * a.nblk + i];
-    block_scan(sum, red, total);
-    run = total;
-  }
-  for (int i = 0; i < kRepackBlock / kRT; ++i) {
-    const int64_t t = (int64_t)blockIdx.x * kRepackBlock + i * kRT + threadIdx.x;
-    const uint32_t r = t < a.T ? (uint32_t)a.levels[code[t]] : 0u;
-    uint32_t total;
-    const uint32_t at = run + block_scan(r, red, total);
-    if (t < a.T) {
-      off[t] = at;
-      if (t == a.T - 1) off[a.T] = at + r;
-    }
-    run += total;
-  }
-  if (a.T == 0 && threadIdx.x == 0 && blockIdx.x == 0) off[0] = 0;
-  // bases of this window and head, both Z
+// Bases of a window and head, both Z, spread over the blocks.
+__device__ __forceinline__ void copy_bases(const RepackArgs& a, int mh) {
   const int M = a.n_layers / a.window, n16 = 2 * a.rb * D / 8;
   for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
     const int sb = a.src_seq[b];
@@ -105,81 +85,182 @@ __global__ __launch_bounds__(kRT) void repack_offset_kernel(const RepackArgs a) 
     const int64_t mhs = (int64_t)M * a.n_kv_heads;
     const u4v* s = static_cast<const u4v*>(a.from.basis) + ((int64_t)sb * mhs + mh) * n16;
     u4v* d = static_cast<u4v*>(const_cast<void*>(a.to.basis)) + ((int64_t)b * mhs + mh) * n16;
+#pragma unroll 4
     for (int i = threadIdx.x; i < n16; i += kRT) d[i] = s[i];
   }
 }
 
-// grid (ceil(T16 / 64), Hkv, 2 L)
+// grid (nblk, M*Hkv)
+__global__ __launch_bounds__(kRT) void repack_code_kernel(const RepackArgs a) {
+  __shared__ uint32_t red[kRT / 64];
+  const int mh = blockIdx.y;
+  uint8_t* to = const_cast<uint8_t*>(a.to.rank_code) + (int64_t)mh * a.T;
+  const int64_t t0 = (int64_t)blockIdx.x * kRepackBlock + kPer * threadIdx.x;
+  int code[kPer];
+  uint32_t sum = 0, total;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) code[i] = t0 + i < a.T ? code_of(a, mh, t0 + i) : 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (t0 + i < a.T) {
+      to[t0 + i] = (uint8_t)code[i];
+      sum += (uint32_t)a.levels[code[i]];
+    }
+  if (a.nblk == 1) {
+    write_offsets(a, mh, code, 0, red);
+    copy_bases(a, mh);
+    return;
+  }
+  block_scan(sum, red, total);
+  if (threadIdx.x == 0) a.bsum[(int64_t)mh * a.nblk + blockIdx.x] = total;
+}
+
+// grid (nblk, M*Hkv)
+__global__ __launch_bounds__(kRT) void repack_offset_kernel(const RepackArgs a) {
+  __shared__ uint32_t red[kRT / 64];
+  const int mh = blockIdx.y;
+  const uint8_t* from = a.to.rank_code + (int64_t)mh * a.T;
+  const int64_t t0 = (int64_t)blockIdx.x * kRepackBlock + kPer * threadIdx.x;
+  int code[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) code[i] = t0 + i < a.T ? from[t0 + i] : 0;
+  uint32_t sum = 0, before;
+  for (int i = threadIdx.x; i < (int)blockIdx.x; i += kRT) sum += a.bsum[(int64_t)mh * a.nblk + i];
+  block_scan(sum, red, before);
+  write_offsets(a, mh, code, before, red);
+  copy_bases(a, mh);
+}
+
+// 16 bytes from byte `sh` (0 .. 15) of the 32 bytes lo, hi.
+__device__ __forceinline__ u4v funnel(u4v lo, u4v hi, int sh) {
+  typedef unsigned long long u64;
+  const u64 w0 = lo.x | (u64)lo.y << 32, w1 = lo.z | (u64)lo.w << 32, w2 = hi.x | (u64)hi.y << 32, w3 = hi.z | (u64)hi.w << 32;
+  const u64 a0 = sh & 8 ? w1 : w0, a1 = sh & 8 ? w2 : w1, a2 = sh & 8 ? w3 : w2;
+  const int r = 8 * (sh & 7);
+  const u64 o0 = r ? a0 >> r | a1 << (64 - r) : a0, o1 = r ? a1 >> r | a2 << (64 - r) : a1;
+  return u4v{(uint32_t)o0, (uint32_t)(o0 >> 32), (uint32_t)o1, (uint32_t)(o1 >> 32)};
+}
+
+// grid (ceil(T16 / 256), Hkv, L)
+template <bool C8>
 __global__ __launch_bounds__(kRT) void repack_copy_kernel(const RepackArgs a) {
-  __shared__ int src[kTok];
-  const int h = blockIdx.y, l = blockIdx.z >> 1, z = blockIdx.z & 1, H = a.n_kv_heads, rb = a.rb;
+  constexpr int esz = C8 ? 1 : 2, tb = 16 / esz;       // bytes of a coefficient; tokens of a value block
+  __shared__ int src[kTok], run[kTok / tb];            // run: first source token of a block of consecutive ones, else -1
+  __shared__ uint32_t off[kTok + 1], from[kTok];       // first entries here and there
+  const int h = blockIdx.y, l = blockIdx.z, H = a.n_kv_heads, rb = a.rb, tid = threadIdx.x;
   const int64_t t0 = (int64_t)blockIdx.x * kTok, T16 = (a.T + 15) / 16 * 16, T160 = (a.T0 + 15) / 16 * 16;
   const int nt = (int)min((int64_t)kTok, T16 - t0), nr = (int)min((int64_t)kTok, a.T - t0);
-  if (threadIdx.x < kTok) src[threadIdx.x] = (int)threadIdx.x < nr ? source(a, t0 + threadIdx.x) : -1;
-  __syncthreads();
-  const int64_t slab = (int64_t)l * H + h, zslab = ((int64_t)l * 2 + z) * H + h;
-  const int esz = a.c8 ? 1 : 2;
-  const uint8_t* cs = static_cast<const uint8_t*>(z ? a.from.coef_v : a.from.coef_k) + slab * T160 * rb * esz;
-  uint8_t* cd = static_cast<uint8_t*>(const_cast<void*>(z ? a.to.coef_v : a.to.coef_k)) + slab * T16 * rb * esz;
-  if (z == 0) {                          // key tiles: 16 bytes of one token
-    const int per = rb * esz / 16;
-    for (int i = threadIdx.x; i < nt * per; i += kRT) {
-      const int tile = i / (16 * per), piece = i / 16 % per, k = tile * 16 + (i & 15), s = src[k];
-      u4v w = {0, 0, 0, 0};
-      if (s >= 0) w = *reinterpret_cast<const u4v*>(cs + (((int64_t)(s >> 4) * per + piece) * 16 + (s & 15)) * 16);
-      *reinterpret_cast<u4v*>(cd + (((t0 >> 4) + tile) * per + piece) * 256 + (i & 15) * 16) = w;
-    }
-  } else {                               // value blocks: 16 bytes of one coefficient, 8 or 16 tokens
-    const int tb = 16 / esz;
-    for (int i = threadIdx.x; i < nt / tb * rb; i += kRT) {
-      const int blk = i / rb, c = i % rb;
-      u4v w = {0, 0, 0, 0};
-      for (int j = 0; j < tb; ++j) {
-        const int s = src[blk * tb + j];
-        if (s < 0) continue;
-        const uint8_t* p = cs + ((int64_t)(s / tb) * rb + c) * 16 + (s % tb) * esz;
-        const uint32_t v = a.c8 ? *p : *reinterpret_cast<const uint16_t*>(p);
-        w[j * esz / 4] |= v << (8 * (j * esz % 4));
-      }
-      *reinterpret_cast<u4v*>(cd + ((t0 / tb + blk) * rb + c) * 16) = w;
-    }
-  }
-  const uint16_t* ss = static_cast<const uint16_t*>(a.from.res_scale) + zslab * a.T0;
-  uint16_t* sd = static_cast<uint16_t*>(const_cast<void*>(a.to.res_scale)) + zslab * a.T;
-  if ((int)threadIdx.x < nr) sd[t0 + threadIdx.x] = src[threadIdx.x] >= 0 ? ss[src[threadIdx.x]] : 0;
-  if (a.c8) {
-    const int nb = rb / 16;
-    const uint16_t* bs = static_cast<const uint16_t*>(z ? a.from.coef_v_scale : a.from.coef_k_scale) + slab * nb * a.T0;
-    uint16_t* bd = static_cast<uint16_t*>(const_cast<void*>(z ? a.to.coef_v_scale : a.to.coef_k_scale)) + slab * nb * a.T;
-    for (int i = threadIdx.x; i < nb * kTok; i += kRT) {
-      const int k = i % kTok, s = i / kTok;
-      if (k < nr) bd[s * a.T + t0 + k] = src[k] >= 0 ? bs[s * a.T0 + src[k]] : 0;
-    }
-  }
-  // entries: four lanes per token, two entries (one code byte) each in turn
   const int mh = (l / a.window) * H + h;
-  const uint32_t* off = a.to.res_off + (int64_t)mh * (a.T + 1);
-  const uint32_t* off0 = a.from.res_off + (int64_t)mh * (a.T0 + 1);
-  const uint8_t* is = a.from.res_idx + zslab * a.stride0;
-  const uint8_t* vs = a.from.res_val + zslab * (a.stride0 / 2);
-  uint8_t* id = const_cast<uint8_t*>(a.to.res_idx) + zslab * a.stride;
-  uint8_t* vd = const_cast<uint8_t*>(a.to.res_val) + zslab * (a.stride / 2);
-  const int k = threadIdx.x >> 2;
-  if (k < nr) {
-    const uint32_t d0 = off[t0 + k], n = off[t0 + k + 1] - d0;
-    const int s = src[k];
-    const uint32_t s0 = s >= 0 ? off0[s] : 0;
-    for (uint32_t e = 2 * (threadIdx.x & 3); e < n; e += 8) {
-      if ((int64_t)d0 + e + 2 > a.stride - kResTailPad) break;
-      uint16_t ch = (uint16_t)(e | (e + 1) << 8);
-      uint8_t v = 0;
-      if (s >= 0) {
-        if ((int64_t)s0 + e + 2 > a.stride0) break;
-        ch = *reinterpret_cast<const uint16_t*>(is + s0 + e);
-        v = vs[(s0 + e) >> 1];
+  const uint32_t* off_to = a.to.res_off + (int64_t)mh * (a.T + 1) + t0;
+  const int s = tid < nr ? source(a, t0 + tid) : -1;
+  const uint32_t o = off_to[min(tid, nr)];
+  if (tid == 0) off[kTok] = off_to[nr];
+  src[tid] = s;
+  off[tid] = o;
+  from[tid] = s >= 0 ? a.from.res_off[(int64_t)mh * (a.T0 + 1) + s] : 0u;
+  {
+    int ok = s >= 0;                     // consecutive tokens of a value block, looked for with lane shifts
+    const int first = __shfl(s, (tid & 63) & ~(tb - 1));
+    ok = ok && s == first + (tid & (tb - 1));
+    const unsigned long long all = __ballot(ok);
+    if ((tid & (tb - 1)) == 0) run[tid / tb] = ((all >> (tid & 63)) & ((1ull << tb) - 1)) == (1ull << tb) - 1 ? s : -1;
+  }
+  __syncthreads();
+  const int64_t slab = (int64_t)l * H + h;
+  // ---- key tiles: a thread's token, 16 bytes at a time
+  {
+    const int per = rb * esz / 16;
+    const uint8_t* cs = static_cast<const uint8_t*>(a.from.coef_k) + slab * T160 * rb * esz + ((int64_t)(max(s, 0) >> 4) * per * 16 + (max(s, 0) & 15)) * 16;
+    uint8_t* cd = static_cast<uint8_t*>(const_cast<void*>(a.to.coef_k)) + slab * T16 * rb * esz + (((t0 + tid) >> 4) * per * 16 + (tid & 15)) * 16;
+    if (tid < nt) {
+#pragma unroll 8
+      for (int p = 0; p < per; ++p) {
+        u4v w = {0, 0, 0, 0};
+        if (s >= 0) w = *reinterpret_cast<const u4v*>(cs + p * 256);
+        *reinterpret_cast<u4v*>(cd + p * 256) = w;
       }
-      *reinterpret_cast<uint16_t*>(id + d0 + e) = ch;
-      vd[(d0 + e) >> 1] = v;
+    }
+  }
+  // ---- value blocks: 16 bytes of one coefficient, the block's tokens
+  {
+    const uint8_t* cs = static_cast<const uint8_t*>(a.from.coef_v) + slab * T160 * rb * esz;
+    uint8_t* cd = static_cast<uint8_t*>(const_cast<void*>(a.to.coef_v)) + slab * T16 * rb * esz + t0 * rb * esz;
+    const int n = nt / tb * rb;
+    int blk = tid / rb, c = tid % rb;
+    const int dblk = kRT / rb, dc = kRT % rb;
+#pragma unroll 4
+    for (int i = tid; i < n; i += kRT) {
+      const int s0 = run[blk];
+      u4v w = {0, 0, 0, 0};
+      if (s0 >= 0) {
+        const int sh = s0 % tb * esz;
+        const uint8_t* p = cs + ((int64_t)(s0 / tb) * rb + c) * 16;
+        w = *reinterpret_cast<const u4v*>(p);
+        if (sh) w = funnel(w, *reinterpret_cast<const u4v*>(p + rb * 16), sh);
+      } else {
+        for (int j = 0; j < tb; ++j) {
+          const int t = src[blk * tb + j];
+          if (t < 0) continue;
+          const uint8_t* p = cs + ((int64_t)(t / tb) * rb + c) * 16 + (t % tb) * esz;
+          const uint32_t v = C8 ? *p : *reinterpret_cast<const uint16_t*>(p);
+          w[j * esz / 4] |= v << (8 * (j * esz % 4));
+        }
+      }
+      *reinterpret_cast<u4v*>(cd + (int64_t)i * 16) = w;
+      c += dc;
+      blk += dblk;
+      if (c >= rb) c -= rb, ++blk;
+    }
+  }
+  // ---- scales
+  if (tid < nr) {
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int64_t zslab = ((int64_t)l * 2 + z) * H + h;
+      const uint16_t* ss = static_cast<const uint16_t*>(a.from.res_scale) + zslab * a.T0;
+      uint16_t* sd = static_cast<uint16_t*>(const_cast<void*>(a.to.res_scale)) + zslab * a.T;
+      sd[t0 + tid] = s >= 0 ? ss[s] : 0;
+      if constexpr (C8) {
+        const int nb = rb / 16;
+        const uint16_t* bs = static_cast<const uint16_t*>(z ? a.from.coef_v_scale : a.from.coef_k_scale) + slab * nb * a.T0;
+        uint16_t* bd = static_cast<uint16_t*>(const_cast<void*>(z ? a.to.coef_v_scale : a.to.coef_k_scale)) + slab * nb * a.T;
+#pragma unroll 4
+        for (int k = 0; k < nb; ++k) bd[k * a.T + t0 + tid] = s >= 0 ? bs[k * a.T0 + s] : 0;
+      }
+    }
+  }
+  // ---- entries, a pair of one token (ranks are even) per thread: two channel
+  // bytes and one code byte, keys and values at the same place
+  const int64_t zs = H * a.stride, zs0 = H * a.stride0;       // from keys to values
+  const uint8_t* is = a.from.res_idx + ((int64_t)l * 2 * H + h) * a.stride0;
+  const uint8_t* vs = a.from.res_val + ((int64_t)l * 2 * H + h) * (a.stride0 / 2);
+  uint8_t* id = const_cast<uint8_t*>(a.to.res_idx) + ((int64_t)l * 2 * H + h) * a.stride;
+  uint8_t* vd = const_cast<uint8_t*>(a.to.res_val) + ((int64_t)l * 2 * H + h) * (a.stride / 2);
+  const uint32_t e0 = off[0];
+  const int64_t room = min((int64_t)off[kTok], a.stride - kResTailPad) - e0;
+  for (int64_t x = 2 * tid; x + 2 <= room; x += 2 * kRT) {
+    const uint32_t e = e0 + (uint32_t)x;
+    int k = 0;                           // the last token with off[k] <= e
+#pragma unroll
+    for (int d = kTok / 2; d; d >>= 1)
+      if (off[k + d] <= e) k += d;
+    const uint32_t j = e - off[k];
+    uint16_t ch[2];
+    uint8_t v[2] = {0, 0};
+    ch[0] = ch[1] = (uint16_t)(j | (j + 1) << 8);
+    if (src[k] >= 0) {
+      const int64_t f = (int64_t)from[k] + j;
+      if (f + 2 > a.stride0) continue;   // past the source's slab: its offsets are not its own
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        ch[z] = *reinterpret_cast<const uint16_t*>(is + z * zs0 + f);
+        v[z] = vs[z * (zs0 / 2) + (f >> 1)];
+      }
+    }
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      *reinterpret_cast<uint16_t*>(id + z * zs + e) = ch[z];
+      vd[z * (zs / 2) + (e >> 1)] = v[z];
     }
   }
 }
@@ -189,9 +270,13 @@ __global__ __launch_bounds__(kRT) void repack_copy_kernel(const RepackArgs a) {
 hipError_t launch_repack(const RepackArgs& a, hipStream_t s) {
   const dim3 scan(a.nblk, a.n_layers / a.window * a.n_kv_heads);
   hipLaunchKernelGGL(repack_code_kernel, scan, dim3(kRT), 0, s, a);
-  hipLaunchKernelGGL(repack_offset_kernel, scan, dim3(kRT), 0, s, a);
+  if (a.nblk > 1) hipLaunchKernelGGL(repack_offset_kernel, scan, dim3(kRT), 0, s, a);
   const unsigned tiles = (unsigned)((a.T + kTok - 1) / kTok);
-  if (tiles > 0) hipLaunchKernelGGL(repack_copy_kernel, dim3(tiles, a.n_kv_heads, 2 * a.n_layers), dim3(kRT), 0, s, a);
+  const dim3 grid(tiles, a.n_kv_heads, a.n_layers);
+  if (tiles > 0) {
+    if (a.c8) hipLaunchKernelGGL(repack_copy_kernel<true>, grid, dim3(kRT), 0, s, a);
+    else hipLaunchKernelGGL(repack_copy_kernel<false>, grid, dim3(kRT), 0, s, a);
+  }
   return hipGetLastError();
 }
 
