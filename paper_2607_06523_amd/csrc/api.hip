@@ -1236,25 +1236,17 @@ dwkv_status check_tree(const dwkv_tree* t, int32_t batch) {
   return DWKV_OK;
 }
 
-// Rows of a workgroup's block: 32, or 16 where no sequence has more or the
-// basis leaves no registers for 32.
-int tree_rows(const dwkv_dims* d, const dwkv_tree* t) {
-  int most = 0;
-  for (int b = 0; b < d->batch; ++b) most = std::max(most, t->cu_nodes_host[b + 1] - t->cu_nodes_host[b]);
-  return most * (d->n_q_heads / d->n_kv_heads) <= 16 || d->basis_rank > 64 ? 16 : 32;
-}
-
 struct TreePlan {
-  int rows, max_nrb;
+  int max_nrb;
   int64_t split, items, pairs;           // items and pairs of one KV head
   size_t bytes;
 };
 
 // Chunks and row blocks of sequence b.
-void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int rows, int64_t split, int b, int64_t& chunks, int64_t& nrb) {
+void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int64_t split, int b, int64_t& chunks, int64_t& nrb) {
   const int64_t n = t->cu_nodes_host[b + 1] - t->cu_nodes_host[b], len = d->cu_seqlens_host[b + 1] - d->cu_seqlens_host[b];
   chunks = (len + split - 1) / split;
-  nrb = (n * (d->n_q_heads / d->n_kv_heads) + rows - 1) / rows;
+  nrb = (n * (d->n_q_heads / d->n_kv_heads) + kTreeRows - 1) / kTreeRows;
 }
 
 // Chunk size, in rounds of a workgroup's waves over their tiles.  A workgroup
@@ -1263,12 +1255,12 @@ void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int rows, int64_t split, i
 // 1 to 8 workgroups, or one tile per wave more, the one whose estimated end is
 // first: full rounds of the longest workgroup, or the work shared out evenly
 // plus one workgroup's length where sequences are ragged.
-int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t, int rows) {
+int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t) {
   constexpr int64_t q = kTreeWaves * kTreeTile, kCU = kTargetWorkgroups / 2, kFixed = 3, kDraft = 2;
   if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets
   int64_t total = 0, chunks, nrb;
   for (int b = 0; b < d->batch; ++b) {
-    tree_seq(d, t, rows, q, b, chunks, nrb);
+    tree_seq(d, t, q, b, chunks, nrb);
     total += chunks * nrb * d->n_kv_heads;
   }
   int64_t best = q, best_time = INT64_MAX;
@@ -1276,7 +1268,7 @@ int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t, int rows) {
     const int64_t cus = kCU * (k / 2), tiles = std::min<int64_t>(std::max<int64_t>((total + cus - 1) / cus, 1) + k % 2, 256), c = tiles * q;
     int64_t wgs = 0, drafts = 0, work = 0, most = 0;
     for (int b = 0; b < d->batch; ++b) {
-      tree_seq(d, t, rows, c, b, chunks, nrb);
+      tree_seq(d, t, c, b, chunks, nrb);
       const int64_t n = nrb * d->n_kv_heads, len = d->cu_seqlens_host[b + 1] - d->cu_seqlens_host[b];
       if (n == 0) continue;
       drafts += n;
@@ -1296,17 +1288,16 @@ int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t, int rows) {
 
 TreePlan tree_plan(const dwkv_dims* d, const dwkv_tree* t) {
   TreePlan p;
-  p.rows = tree_rows(d, t);
-  p.split = tree_split(d, t, p.rows);
+  p.split = tree_split(d, t);
   p.items = p.pairs = p.max_nrb = 0;
   for (int b = 0; b < d->batch; ++b) {
     int64_t chunks, nrb;
-    tree_seq(d, t, p.rows, p.split, b, chunks, nrb);
+    tree_seq(d, t, p.split, b, chunks, nrb);
     p.items += (chunks + 1) * nrb;
     p.pairs += nrb > 0 ? chunks + 1 : 0;
     p.max_nrb = std::max<int>(p.max_nrb, (int)nrb);
   }
-  p.bytes = std::max<size_t>(256, align_up((size_t)p.items * d->n_kv_heads * p.rows * (kHeadDim + d->basis_rank + 4) * sizeof(float), 256));
+  p.bytes = std::max<size_t>(256, align_up((size_t)p.items * d->n_kv_heads * kTreeRows * (kHeadDim + d->basis_rank + 4) * sizeof(float), 256));
   return p;
 }
 
@@ -1373,7 +1364,6 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
   t.group = d->n_q_heads / d->n_kv_heads;
   t.rb = d->basis_rank;
   t.split = (int32_t)p.split;
-  t.rows = p.rows;
   t.q_bf16 = a.q_bf16;
   t.c8 = d->coef_format == DWKV_COEF_I8;
   t.qscale = a.qscale;
@@ -1386,7 +1376,7 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
       t.wt.node[b] = tree->cu_nodes_host[b];
       if (b == d->batch) break;
       int64_t chunks, nrb;
-      tree_seq(d, tree, p.rows, p.split, b, chunks, nrb);
+      tree_seq(d, tree, p.split, b, chunks, nrb);
       t.wt.work[b + 1] = t.wt.work[b] + (int32_t)((chunks + 1) * nrb);
       t.wt.pair[b + 1] = t.wt.pair[b] + (int32_t)(nrb > 0 ? chunks + 1 : 0);
     }

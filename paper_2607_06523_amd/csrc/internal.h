@@ -350,7 +350,8 @@ hipError_t launch_probe_pos(int rb, int g, bool resid, const TLProbeArgs& a, hip
 
 // Attention of drafted trees (tree.hip): items of every sequence with nodes,
 // (chunks + 1) x row blocks per KV head, the last chunk the drafted nodes.
-constexpr int kTreeWaves = 8;        // waves per workgroup
+constexpr int kTreeRows = 32;        // rows (node, group member) of a workgroup
+constexpr int kTreeWaves = 8;        // waves per workgroup (4 at r_b above 64)
 constexpr int kTreeTile = 32;        // tokens per wave tile
 
 struct TreeTable {                   // up to kKernargSeqs sequences; n_seq == 0: from the device arrays
@@ -382,13 +383,12 @@ struct TreeArgs {
   const int32_t* cu;
   const int32_t* cu_nodes;
   const int32_t* parent;
-  float* part;                 // [item][Hkv][rows][d + rb + 4]: r, a~, m, l
+  float* part;                 // [item][Hkv][kTreeRows][d + rb + 4]: r, a~, m, l
   float* out;                  // [N][Hq][d]
   int64_t T, res_stride;
   int64_t n_pairs;             // (chunk, KV head) pairs of the sequences with nodes
   int32_t max_nrb;             // row blocks of the sequence with most nodes
   int32_t batch, n_q_heads, n_kv_heads, group, rb, split;
-  int32_t rows;                // rows of a block: 16 or 32
   int32_t q_bf16, c8;
   float qscale;                // sm_scale * log2(e)
   TreeTable wt;

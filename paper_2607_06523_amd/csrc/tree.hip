@@ -47,9 +47,9 @@ __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) 
   seq_items(t1 - t0, n, a, chunks, nrb);
   const int r0 = blockIdx.x * kMR, rows = n * a.group;
   if (r0 >= rows) return;
-  const int stride = D + rb + 4, block = r0 / a.rows;         // a.rows is a multiple of kMR
-  const float* p0 = a.part + ((base + block) * H + h) * a.rows * stride + (int64_t)(r0 % a.rows) * stride;
-  const int64_t step = (int64_t)nrb * H * a.rows * stride;    // to the next chunk's partial
+  const int stride = D + rb + 4, block = r0 / R;              // R is a multiple of kMR
+  const float* p0 = a.part + ((base + block) * H + h) * R * stride + (int64_t)(r0 % R) * stride;
+  const int64_t step = (int64_t)nrb * H * R * stride;    // to the next chunk's partial
   const float inf = __builtin_inff();
   const int cols = (D + rb) / 4, mycol = 4 * min(lane, cols - 1);
   f4 o[kMR] = {};

@@ -11,11 +11,15 @@
 // multiplies them like the coefficients.
 //
 //  * tree_split_kernel: workgroup = (chunk of a sequence's tokens, KV head,
-//    block of 16 NC rows), 8 waves taking its 32-token tiles in turn.  Scores
-//    come out transposed, tokens down the accumulator and rows across, which is
-//    the operand layout the value products read: probabilities never leave the
-//    registers.  A tile's tokens are dealt to the score rows so that a lane's
-//    eight scores are eight consecutive tokens, one value block.
+//    block of 32 rows), its waves taking the chunk's 32-token tiles in turn.
+//    Scores come out transposed, tokens down the accumulator and rows across,
+//    which is the operand layout the value products read: probabilities never
+//    leave the registers.  A tile's tokens are dealt to the score rows so that
+//    eight consecutive scores of a lane are eight consecutive tokens, one
+//    value block.  All products are 32x32x16: beside one of them, unlike a pair
+//    of 16x16x32, the vector unit goes on (four 16x16x32 and twelve vector
+//    instructions of each of two waves take 93 ns, the same work in two 32x32x16
+//    69, the products alone 72 and 71).
 //  * one more workgroup per (sequence, KV head, row block) attends to the
 //    drafted nodes, whose masks it derives from the parents.
 //  * tree_merge_kernel joins the partials and applies B^V.
@@ -34,12 +38,14 @@ typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u2v __attribute__((ext_vector_type(2)));
 typedef __amdgpu_buffer_rsrc_t rsrc_t;
 
 constexpr int D = kHeadDim;
 constexpr int TT = kTreeTile;            // tokens per tile
+constexpr int R = kTreeRows;             // rows of a workgroup
 constexpr int kKRow = D + 8;             // halves per token row of the key code tile (16-byte pad: no bank conflicts)
 constexpr int kWaitVmcnt0 = 0x0F70;      // s_waitcnt immediate: vmcnt(0) only
 constexpr float kUp = 6.0f;              // a moved reference leaves the largest probability at 2^6,
@@ -66,12 +72,12 @@ __device__ __forceinline__ int incl_max(int v) {   // running maximum over the l
   return v;
 }
 
-__device__ __forceinline__ f4 mfma_h(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f16v mfma_h(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 template <bool BF>
-__device__ __forceinline__ f4 mfma_q(u4v a, u4v b, f4 c) {
+__device__ __forceinline__ f16v mfma_q(u4v a, u4v b, f16v c) {
   if constexpr (BF)
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
   else
     return mfma_h(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c);
 }
@@ -82,35 +88,42 @@ __device__ __forceinline__ uint16_t code_bits(float v) {   // v an int4 code: ex
   return BF ? (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16) : h_bits(v);
 }
 
-// Place of a tile's token among the rows of the key code tile: score row r of
-// token block b is token 8 (r / 4) + 4 b + r % 4, held at row 16 b + r, so that
-// 16 lanes read 16 consecutive rows.
-__device__ __forceinline__ int key_row(int t) { return 16 * ((t >> 2) & 1) + 4 * (t >> 3) + (t & 3); }
+// Score row of a tile's token.  Accumulator register 4 a + i of lane half h is score
+// row 8 a + 4 h + i; with these rows it is token 16 (a / 2) + 8 h + 4 (a % 2) + i, so
+// that registers 8 u .. 8 u + 7 are tokens 16 u + 8 h .. + 7, the u-th 16-deep step of
+// the value products.
+__device__ __forceinline__ int key_row(int t) { return 16 * (t >> 4) + 8 * ((t >> 2) & 1) + 4 * ((t >> 3) & 1) + (t & 3); }
+__device__ __forceinline__ int row_token(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
+
+// Place of (channel, token) in the value code tile: a channel's four 8-token
+// pieces are dealt by channel, so that 16 lanes reading the same piece of 16
+// channels touch every bank once.
+__device__ __forceinline__ uint32_t value_place(uint32_t c, uint32_t t) { return c * TT + (((t >> 3) ^ ((c >> 2) & 3)) << 3) + (t & 7); }
 
 // Lanes without an entry write past the ends of k and v and of mark's first half:
 // no branch keeps them out.
 struct alignas(16) WaveTile {
   uint16_t k[TT * kKRow + 8];            // key codes [token place][channel], zero between tiles
-  uint16_t v[D * TT + 8];                // value codes [channel][token]
+  uint16_t v[D * TT + 8];                // value codes (value_place)
   float sk[TT], sv[TT];                  // residual scales of the tile's tokens (sv in units of 2^ex)
   uint8_t mark[128];
 };
 constexpr uint32_t kNoKey = TT * kKRow, kNoValue = D * TT;
 
 // Smem of the drafted nodes' workgroups.
-template <int NC>
 struct alignas(16) DraftSmem {
-  float q[16 * NC][D];
+  float q[R][D];
   uint16_t v[DWKV_MAX_TREE_NODES][D];
 };
 
-// Waves of a workgroup: two per SIMD, or one where it holds the sums of 64 rows.
-template <int NC>
-constexpr int kWaves = NC > 2 ? 4 : 8;
+// Waves of a workgroup: two per SIMD, or one where the sums and fragments of wide
+// bases take more than half its registers.
+template <int NB>
+constexpr int kWaves = NB > 4 ? 4 : 8;
 
-template <int NB, int NC, bool C8>
+template <int NB, bool C8>
 struct alignas(16) TreeSmem {
-  static constexpr int R = 16 * NC, NK = (NB + 1) / 2, NW = kWaves<NC>;
+  static constexpr int NW = kWaves<NB>;
   float m[NW][R], l[NW][R];
   uint32_t odd[D];                       // channels with entries of value scales that are not finite: bits +inf, -inf, NaN
   float big;                             // largest |q~|
@@ -118,11 +131,11 @@ struct alignas(16) TreeSmem {
   union {
     struct {
       WaveTile w[NW];
-      u4v qf[4][NC][64];                 // query fragments: channels 32 s + 8 g + j
-      u4v qt[2][NK][NC][64];             // q~ fragments (hi, lo)
+      u4v qf[8][64];                     // query fragments: channels 16 s + 8 h + j of row lane % 32
+      u4v qt[2][NB][64];                 // q~ fragments (hi, lo)
     };
     float acc[NW][R][D + 4];             // the waves' sums, 128 columns at a time
-    DraftSmem<NC> d;
+    DraftSmem d;
   };
 };
 
@@ -136,7 +149,7 @@ struct Item {
 
 __device__ __forceinline__ void seq_items(int T, int n, const TreeArgs& a, int& chunks, int& nrb) {
   chunks = T > 0 ? (T - 1) / a.split + 1 : 0;
-  nrb = (n * a.group + a.rows - 1) / a.rows;
+  nrb = (n * a.group + R - 1) / R;
 }
 
 // Workgroups go to the 8 XCDs in turn.  The row blocks of one (chunk, KV head)
@@ -234,12 +247,12 @@ __device__ __forceinline__ u4v q_piece(const TreeArgs& a, const Item& it, int r,
   return *reinterpret_cast<const u4v*>(a.q + (int64_t)(it.n0 + r / a.group) * a.q_stride + (it.h * a.group + r % a.group) * D + c);
 }
 
-// The drafted nodes: a wave takes rows w, w + 8, ... of the block, all at once; a
+// The drafted nodes: a wave takes rows w, w + NW, ... of the block, all at once; a
 // lane takes node `lane` for the scores and channels 2 lane, 2 lane + 1 for the
 // values.  Nodes a row does not see are skipped, not weighted with zero.
-template <int NC>
-__device__ __forceinline__ void draft_item(const TreeArgs& a, const Item& it, DraftSmem<NC>& sm, float* part, int stride) {
-  constexpr int R = 16 * NC, NW = kWaves<NC>, PER = R / NW;
+template <int NW>
+__device__ __forceinline__ void draft_item(const TreeArgs& a, const Item& it, DraftSmem& sm, float* part, int stride) {
+  constexpr int PER = R / NW;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, rows = it.n * a.group;
   const uint16_t* k = a.k_new + (int64_t)(it.n0 + min(lane, it.n - 1)) * a.kv_stride + it.h * D;
   const uint16_t* V = a.v_new + (int64_t)it.n0 * a.kv_stride + it.h * D;
@@ -338,99 +351,76 @@ struct Streams {
   rsrc_t idx[2], val[2];                 // entries from the chunk's first on
 };
 
-// Asks for the vector instructions since the last such request to be spread
-// between N matrix products: a wave issues in order, and behind a run of
-// products they would wait for the matrix core.
-template <int N>
-__device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
-  }
-}
-
 // What a wave holds of a tile ahead of its use.
 template <int NB, bool C8>
 struct Ahead {
-  static constexpr int NK = (NB + 1) / 2;
-  u4v k[2][NK], v[NB];                   // fp16 coefficients; int8: the first two words
-  uint32_t ks[C8 ? 2 : 1][C8 ? NK : 1], vs[C8 ? NB : 1];
+  static constexpr int NV = (NB + 1) / 2;
+  u4v k[NB], v[NV][2];                   // fp16 coefficients; int8: the first two words
+  uint32_t ks[C8 ? NB : 1], vs[C8 ? NB : 1];
   uint32_t oa, ob, oa2, ob2;             // entry ranges of the lane's token, this tile and the next
   uint32_t sk, sv;                       // residual scales
   uint32_t ck, cv, vk, vv;               // entry pair `lane`: channel bytes and code byte, keys and values
 };
 
-// Places of a lane in a tile's streams; a tile adds a scalar offset.
-template <int NB, bool C8>
+// Places of a lane in a tile's streams; a tile, a 16-deep step and a block add constants.
 struct Lane {
-  static constexpr int NK = (NB + 1) / 2;
-  uint32_t k[2][NK], v, ks[C8 ? 2 : 1][C8 ? NK : 1], vs, t2;
+  uint32_t k, v, ks, t2;
 };
 
-constexpr uint32_t kPast = 0x7ffffff0;   // beyond every stream: reads as zero
-
 template <int NB, bool C8>
-__device__ __forceinline__ Lane<NB, C8> make_lane(int T, int lane) {
-  constexpr int NK = (NB + 1) / 2, rb = 16 * NB;
-  const int g = lane >> 4, col = lane & 15;
-  Lane<NB, C8> p;
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int t = 8 * (col >> 2) + 4 * b + (col & 3);                  // token of score row `col`
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      const bool have = NB % 2 == 0 || s + 1 < NK || g < 2;            // else past r_b
-      if constexpr (C8) {
-        const int blk = 2 * s + (g >> 1);
-        p.k[b][s] = have ? (((t >> 4) * NB + blk) * 16 + (t & 15)) * 16 + 8 * (g & 1) : kPast;
-        p.ks[b][s] = have ? (uint32_t)(blk * T + t) * 2 : kPast;
-      } else {
-        p.k[b][s] = have ? (((t >> 4) * (rb / 8) + 4 * s + g) * 128 + (t & 15) * 8) * 2 : kPast;
-      }
-    }
+__device__ __forceinline__ Lane make_lane(int lane) {
+  constexpr int rb = 16 * NB;
+  const int h = lane >> 5, c = lane & 31, t = row_token(c);
+  Lane p;
+  if constexpr (C8) {
+    p.k = ((t >> 4) * NB * 16 + (t & 15)) * 16 + 8 * h;
+    p.v = c * 16 + 8 * h;
+  } else {
+    p.k = (((t >> 4) * (rb / 8) + h) * 128 + (t & 15) * 8) * 2;
+    p.v = (h * rb + c) * 16;
   }
-  p.v = C8 ? ((g >> 1) * rb + col) * 16 + 8 * (g & 1) : (g * rb + col) * 16;
-  p.t2 = 2 * (lane & 31);
+  p.ks = 2 * t;
+  p.t2 = 2 * c;
   return p;
 }
 
 template <int NB, bool C8>
-__device__ __forceinline__ void load_k(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile) {
-  constexpr int NK = (NB + 1) / 2, step = TT * 16 * NB * (C8 ? 1 : 2);
+__device__ __forceinline__ void load_k(Ahead<NB, C8>& f, const Streams& x, const Lane& p, int tile, int T) {
+  constexpr int step = TT * 16 * NB * (C8 ? 1 : 2);
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int s = 0; s < NB; ++s) {
+    if constexpr (C8) {
+      const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.k, p.k + 256 * s, tile * step, 0);
+      f.k[s].x = w.x;
+      f.k[s].y = w.y;
+      f.ks[s] = __builtin_amdgcn_raw_buffer_load_b16(x.ks, p.ks, tile * (2 * TT) + s * T * 2, 0);
+    } else {
+      f.k[s] = __builtin_amdgcn_raw_buffer_load_b128(x.k, p.k + 512 * s, tile * step, 0);
+    }
+  }
+}
+
+// Channels past r_b read whatever follows; their sums are not used.
+template <int NB, bool C8>
+__device__ __forceinline__ void load_v(Ahead<NB, C8>& f, const Streams& x, const Lane& p, int tile) {
+  constexpr int rb = 16 * NB, step = TT * rb * (C8 ? 1 : 2);
 #pragma unroll
-    for (int s = 0; s < NK; ++s) {
+  for (int k = 0; k < (NB + 1) / 2; ++k) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
       if constexpr (C8) {
-        const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.k, p.k[b][s], tile * step, 0);
-        f.k[b][s].x = w.x;
-        f.k[b][s].y = w.y;
-        f.ks[b][s] = __builtin_amdgcn_raw_buffer_load_b16(x.ks, p.ks[b][s], tile * (2 * TT), 0);
+        const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.v, p.v + 512 * k + u * rb * 16, tile * step, 0);
+        f.v[k][u].x = w.x;
+        f.v[k][u].y = w.y;
       } else {
-        f.k[b][s] = __builtin_amdgcn_raw_buffer_load_b128(x.k, p.k[b][s], tile * step, 0);
+        f.v[k][u] = __builtin_amdgcn_raw_buffer_load_b128(x.v, p.v + 512 * k + u * 2 * rb * 16, tile * step, 0);
       }
     }
   }
 }
 
 template <int NB, bool C8>
-__device__ __forceinline__ void load_v(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile) {
-  constexpr int step = TT * 16 * NB * (C8 ? 1 : 2);
-#pragma unroll
-  for (int k = 0; k < NB; ++k) {
-    if constexpr (C8) {
-      const u2v w = __builtin_amdgcn_raw_buffer_load_b64(x.v, p.v + 256 * k, tile * step, 0);
-      f.v[k].x = w.x;
-      f.v[k].y = w.y;
-    } else {
-      f.v[k] = __builtin_amdgcn_raw_buffer_load_b128(x.v, p.v + 256 * k, tile * step, 0);
-    }
-  }
-}
-
-template <int NB, bool C8>
-__device__ __forceinline__ void load_vs(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile, int T) {
+__device__ __forceinline__ void load_vs(Ahead<NB, C8>& f, const Streams& x, const Lane& p, int tile, int T) {
   if constexpr (C8) {
 #pragma unroll
     for (int k = 0; k < NB; ++k) f.vs[k] = __builtin_amdgcn_raw_buffer_load_b16(x.vs, p.t2, tile * (2 * TT) + k * T * 2, 0);
@@ -439,7 +429,7 @@ __device__ __forceinline__ void load_vs(Ahead<NB, C8>& f, const Streams& x, cons
 
 // Scales and the first 64 entry pairs of a tile whose first entry is e0.
 template <int NB, bool C8>
-__device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x, const Lane<NB, C8>& p, int tile, uint32_t e0, int lane) {
+__device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x, const Lane& p, int tile, uint32_t e0, int lane) {
   f.sk = __builtin_amdgcn_raw_buffer_load_b16(x.sk, p.t2, tile * (2 * TT), 0);
   f.sv = __builtin_amdgcn_raw_buffer_load_b16(x.sv, p.t2, tile * (2 * TT), 0);
   f.ck = __builtin_amdgcn_raw_buffer_load_b16(x.idx[0], 2 * lane, e0, 0);
@@ -448,17 +438,17 @@ __device__ __forceinline__ void load_entries(Ahead<NB, C8>& f, const Streams& x,
   f.vv = __builtin_amdgcn_raw_buffer_load_b8(x.val[1], lane, e0 >> 1, 0);
 }
 
-template <int NB, int NC, bool BF, bool C8>
-__global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_kernel(const TreeArgs a) {
-  constexpr int NW = kWaves<NC>, R = 16 * NC, NK = (NB + 1) / 2, rb = 16 * NB, stride = D + rb + 4;
-  __shared__ TreeSmem<NB, NC, C8> sm;
-  const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+template <int NB, bool BF, bool C8>
+__global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_kernel(const TreeArgs a) {
+  constexpr int NW = kWaves<NB>, NV = (NB + 1) / 2, rb = 16 * NB, stride = D + rb + 4;
+  __shared__ TreeSmem<NB, C8> sm;
+  const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, h = lane >> 5, col = lane & 31;
   const Item it = find_item(a, blockIdx.x);
   if (it.nrb == 0) return;
   const int rows_left = it.n * a.group - it.rb * R;
   float* part = a.part + it.part * R * stride;
   if (it.c == it.chunks) {
-    draft_item<NC>(a, it, sm.d, part, stride);
+    draft_item<NW>(a, it, sm.d, part, stride);
     return;
   }
 
@@ -493,14 +483,15 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     oa = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)min(max(t, c0 - tb), c1 - tb) * 4, 0, 0) - ec0;
     ob = __builtin_amdgcn_raw_buffer_load_b32(sx.off, (uint32_t)min(max(t + 1, c0 - tb), c1 - tb) * 4, 0, 0) - ec0;
   };
-  const Lane<NB, C8> lp = make_lane<NB, C8>(Ti, lane);
+  const Lane lp = make_lane<NB, C8>(lane);
   Ahead<NB, C8> f;
   load_off(j0, f.oa, f.ob);
   load_off(min(j0 + NW, last), f.oa2, f.ob2);
-  load_k<NB, C8>(f, sx, lp, j0);
+  load_k<NB, C8>(f, sx, lp, j0, Ti);
 
-  // ---- query fragments, and q~ = B^K q as fp16 pairs ---------------------------
-  constexpr int TILES = NB * NC, PER = (2 * NK * NC + NW - 1) / NW;
+  // ---- query fragments, and q~ = B^K q as fp16 pairs (16x16x4 float32 products) ---
+  constexpr int TILES = 2 * NB, PER = (TILES + NW - 1) / NW;
+  const int g = lane >> 4, c16 = lane & 15;
   const uint16_t* bk = a.basis + (int64_t)it.b * a.basis_b_stride + (int64_t)(it.h * 2) * rb * D;
   u4v bw[PER][4];
 #pragma unroll
@@ -508,17 +499,17 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     const int tile = wv + NW * u;
 #pragma unroll
     for (int s = 0; s < 4; ++s)
-      if (tile < TILES) bw[u][s] = *reinterpret_cast<const u4v*>(bk + (16 * (tile / NC) + col) * D + 32 * s + 8 * g);
+      if (tile < TILES) bw[u][s] = *reinterpret_cast<const u4v*>(bk + (16 * (tile / 2) + c16) * D + 32 * s + 8 * g);
   }
-  for (int i = threadIdx.x; i < 4 * NC * 64; i += 64 * NW) {
-    const int ln = i & 63, n = (i >> 6) % NC, s = (i >> 6) / NC, r = 16 * n + (ln & 15);
+  for (int i = threadIdx.x; i < 8 * 64; i += 64 * NW) {
+    const int ln = i & 63, s = i >> 6, r = ln & 31;
     u4v w = {0, 0, 0, 0};
     if (r < rows_left) {
       const int row = it.rb * R + r, p = a.parent[it.n0 + row / a.group];
-      w = q_piece(a, it, row, 32 * s + 8 * (ln >> 4));
+      w = q_piece(a, it, row, 16 * s + 8 * (ln >> 5));
       if (p < -1 || p >= row / a.group) w = u4v{0, 0, 0, 0};           // absent: its query may be anything
     }
-    sm.qf[s][n][ln] = w;
+    sm.qf[s][ln] = w;
   }
   if (threadIdx.x == 0) sm.big = 0.f;
   if (threadIdx.x < D) sm.odd[threadIdx.x] = 0;
@@ -530,12 +521,12 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     float big = 0.f;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const int tile = wv + NW * u, n = tile % NC;
+      const int tile = wv + NW * u, n = tile % 2;
       f4 c = {0.f, 0.f, 0.f, 0.f};
       if (tile < TILES) {
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-          const u4v qw = sm.qf[s][n][lane];            // channels 32 s + 8 g + j
+          const u4v qw = sm.qf[2 * s + (g >> 1)][32 * (g & 1) + 16 * n + c16];   // channels 32 s + 8 g + j
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const uint16_t qb = (uint16_t)(qw[j >> 1] >> (16 * (j & 1))), bb = (uint16_t)(bw[u][s][j >> 1] >> (16 * (j & 1)));
@@ -558,18 +549,18 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     const float dn = __builtin_ldexpf(1.f, -max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15));
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const int tile = wv + NW * u, blk = tile / NC, n = tile % NC;
-      if (tile >= 2 * NK * NC) continue;
-      h4 hi, lo;                                       // basis rows 16 blk + 4 g + i, zero past r_b
+      const int tile = wv + NW * u;
+      if (tile >= TILES) continue;
+      h4 hi, lo;                                       // basis rows 16 (tile / 2) + 4 g + i, row 16 (tile % 2) + c16
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float v = q[u][i] * dn;
         hi[i] = (_Float16)v;
         lo[i] = (_Float16)(v - (float)hi[i]);
       }
-      const int ln = 16 * (2 * (blk & 1) + (g >> 1)) + col;
-      reinterpret_cast<h4*>(&sm.qt[0][blk >> 1][n][ln])[g & 1] = hi;
-      reinterpret_cast<h4*>(&sm.qt[1][blk >> 1][n][ln])[g & 1] = lo;
+      const int ln = 32 * (g >> 1) + 16 * (tile % 2) + c16;
+      reinterpret_cast<h4*>(&sm.qt[0][tile / 2][ln])[g & 1] = hi;
+      reinterpret_cast<h4*>(&sm.qt[1][tile / 2][ln])[g & 1] = lo;
     }
   }
   const int down = __builtin_amdgcn_readfirstlane(max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15));
@@ -580,29 +571,12 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
   load_v<NB, C8>(f, sx, lp, j0);
   __syncthreads();                       // q~ is whole
 
-  // the q~ fragments stay in registers where those hold them beside the sums;
-  // a spill in the loop would wait for the loads in flight
-  constexpr bool kQReg = NC <= 2 && NK * NC < 4;
-  u4v qt[2][kQReg ? NK : 1][kQReg ? NC : 1];
-  if constexpr (kQReg) {
+  f16v acc_a[NV], acc_r[D / 32];         // a~ and the residual channels: (channel 8 a + 4 h + i of the block, row col)
+  float m = 0.f, l = 0.f;
 #pragma unroll
-    for (int n = 0; n < NC; ++n)
+  for (int k = 0; k < NV; ++k) acc_a[k] = f16v{};
 #pragma unroll
-      for (int s = 0; s < NK; ++s) {
-        qt[0][s][n] = sm.qt[0][s][n][lane];
-        qt[1][s][n] = sm.qt[1][s][n][lane];
-      }
-  }
-  f4 acc_a[NB][NC], acc_r[D / 16][NC];   // a~ and the residual channels: (channel 4 g + i of the block, row col)
-  float m[NC], l[NC];
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    m[n] = l[n] = 0.f;
-#pragma unroll
-    for (int k = 0; k < NB; ++k) acc_a[k][n] = f4{0, 0, 0, 0};
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) acc_r[k][n] = f4{0, 0, 0, 0};
-  }
+  for (int k = 0; k < D / 32; ++k) acc_r[k] = f16v{};
   bool first = true;
   int ex = -24;                          // |s^V| <= 2^ex of the tiles so far
   float exf = __builtin_ldexpf(1.f, -24), exi = __builtin_ldexpf(1.f, 24);
@@ -615,51 +589,32 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     // Loads return in order, and a wait for one is a wait for those before it.  A
     // tile's key coefficients, entries and value coefficients are requested
     // in that order, each once its predecessor's registers are free.
-    // ---- basis part of the scores: (token 8 g + 4 b + i, row col)
-    f4 sb[2][NC], sr[2][NC];
+    // ---- basis part of the scores: register 8 u + e is token 16 u + 8 h + e, row col
+    f16v sb, sr = {};
+    {
+      const float c = -m * fdn;
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const float c = -m[n] * fdn;
-        sb[b][n] = f4{c, c, c, c};
-        sr[b][n] = f4{0, 0, 0, 0};
-      }
-#pragma unroll
-    for (int s = 0; s < NK; ++s) {
-      h8 kh[2], kl[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if constexpr (C8) {
-          const float sc = half_bits_to_float((uint16_t)f.ks[b][s]);
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.k[b][s].x, f.k[b][s].y}, e) * sc;
-          split8(v, kh[b], kl[b]);
-        } else {
-          kh[b] = __builtin_bit_cast(h8, f.k[b][s]);
-        }
-      }
-      u4v qh[NC], ql[NC];
-#pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        if constexpr (kQReg) {
-          qh[n] = qt[0][s][n];
-          ql[n] = qt[1][s][n];
-        } else {
-          qh[n] = sm.qt[0][s][n][lane];
-          ql[n] = sm.qt[1][s][n][lane];
-        }
-      }
-#pragma unroll
-      for (int part = 0; part < (C8 ? 3 : 2); ++part)
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int n = 0; n < NC; ++n)
-            sb[b][n] = mfma_h(part == 2 ? kl[b] : kh[b], __builtin_bit_cast(h8, part == 1 ? ql[n] : qh[n]), sb[b][n]);
+      for (int i = 0; i < 16; ++i) sb[i] = c;
     }
-    load_k<NB, C8>(f, sx, lp, jn);
+#pragma unroll
+    for (int s = 0; s < NB; ++s) {
+      const h8 qh = __builtin_bit_cast(h8, sm.qt[0][s][lane]), ql = __builtin_bit_cast(h8, sm.qt[1][s][lane]);
+      if constexpr (C8) {
+        const float sc = half_bits_to_float((uint16_t)f.ks[s]);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.k[s].x, f.k[s].y}, e) * sc;
+        h8 kh, kl;
+        split8(v, kh, kl);
+        sb = mfma_h(kh, qh, sb);
+        sb = mfma_h(kh, ql, sb);
+        sb = mfma_h(kl, qh, sb);
+      } else {
+        sb = mfma_h(__builtin_bit_cast(h8, f.k[s]), qh, sb);
+        sb = mfma_h(__builtin_bit_cast(h8, f.k[s]), ql, sb);
+      }
+    }
+    load_k<NB, C8>(f, sx, lp, jn, Ti);
     // ---- entries of the next tile and offsets of the one after
     const uint32_t oa = f.oa, ob = f.ob, sk = f.sk, sv = f.sv, ck = f.ck, cv = f.cv, vk = f.vk, vv = f.vv;
     const uint32_t en = e0;
@@ -688,9 +643,7 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
       exf = __builtin_ldexpf(1.f, e);
       exi = __builtin_ldexpf(1.f, -e);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-        for (int n = 0; n < NC; ++n) acc_r[k][n] *= fall;
+      for (int k = 0; k < D / 32; ++k) acc_r[k] *= fall;
     }
     const bool odd = __ballot(odd_k || odd_v) != 0;
     // A key scale that is not finite goes with its entries into the code tile.  A
@@ -713,7 +666,7 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
       const bool live = b0 + lane < np && tok > 0;
       const int t = (tok - 1) & (TT - 1), kr = key_row(t) * kKRow;
       const uint32_t k0 = live ? kr + (pk & (D - 1)) : kNoKey, k1 = live ? kr + ((pk >> 8) & (D - 1)) : kNoKey;
-      const uint32_t v0 = live ? (pv & (D - 1)) * TT + t : kNoValue, v1 = live ? ((pv >> 8) & (D - 1)) * TT + t : kNoValue;
+      const uint32_t v0 = live ? value_place(pv & (D - 1), t) : kNoValue, v1 = live ? value_place((pv >> 8) & (D - 1), t) : kNoValue;
       ak = k0 | k1 << 16;
       av = v0 | v1 << 16;
       const float a0 = (float)int4_value(qk), a1 = (float)int4_value(qk >> 4), b0f = (float)int4_value(qv), b1f = (float)int4_value(qv >> 4);
@@ -750,154 +703,114 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
     wave_lds_sync();
 
     // ---- residual part of the scores
-    float ks[8], vs[8];
-    {
-      const f4 s0 = *reinterpret_cast<const f4*>(&w.sk[8 * g]), s1 = *reinterpret_cast<const f4*>(&w.sk[8 * g + 4]);
-      const f4 v0 = *reinterpret_cast<const f4*>(&w.sv[8 * g]), v1 = *reinterpret_cast<const f4*>(&w.sv[8 * g + 4]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { ks[i] = s0[i]; ks[4 + i] = s1[i]; vs[i] = v0[i]; vs[4 + i] = v1[i]; }
-    }
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      u4v qv[NC];
-#pragma unroll
-      for (int n = 0; n < NC; ++n) qv[n] = sm.qf[s][n][lane];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const u4v kc = *reinterpret_cast<const u4v*>(&w.k[(16 * b + col) * kKRow + 32 * s + 8 * g]);
-#pragma unroll
-        for (int n = 0; n < NC; ++n) sr[b][n] = mfma_q<BF>(kc, qv[n], sr[b][n]);
-      }
+    for (int s = 0; s < 8; ++s) {
+      const u4v kc = *reinterpret_cast<const u4v*>(&w.k[col * kKRow + 16 * s + 8 * h]);
+      sr = mfma_q<BF>(kc, sm.qf[s][lane], sr);
     }
     if (down) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int n = 0; n < NC; ++n) sb[b][n] *= up;
+      for (int i = 0; i < 16; ++i) sb[i] *= up;
     }
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int u = 0; u < 2; ++u) {
 #pragma unroll
-      for (int n = 0; n < NC; ++n)
+      for (int q = 0; q < 2; ++q) {
+        const f4 ks = *reinterpret_cast<const f4*>(&w.sk[16 * u + 8 * h + 4 * q]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sb[b][n][i] = __builtin_fmaf(ks[4 * b + i], sr[b][n][i], sb[b][n][i]);
+        for (int i = 0; i < 4; ++i) sb[8 * u + 4 * q + i] = __builtin_fmaf(ks[i], sr[8 * u + 4 * q + i], sb[8 * u + 4 * q + i]);
+      }
+    }
     if (edge) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int u = 0; u < 2; ++u) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = t0 + 8 * g + 4 * b + i;
-          if (t < c0 || t >= c1)
+        for (int e = 0; e < 8; ++e) {
+          const int t = t0 + 16 * u + 8 * h + e;
+          if (t < c0 || t >= c1) {
+            sb[8 * u + e] = -inf;
+            if constexpr (!C8) {         // tokens outside the chunk may hold anything
 #pragma unroll
-            for (int n = 0; n < NC; ++n) sb[b][n][i] = -inf;
-        }
-      // tokens outside the chunk may hold anything
-#pragma unroll
-      for (int k = 0; k < NB; ++k) {
-        if constexpr (!C8) {
-          h8 av = __builtin_bit_cast(h8, f.v[k]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (t0 + 8 * g + e < c0 || t0 + 8 * g + e >= c1) av[e] = (_Float16)0.f;
-          f.v[k] = __builtin_bit_cast(u4v, av);
+              for (int k = 0; k < NV; ++k) {
+                h8 av = __builtin_bit_cast(h8, f.v[k][u]);
+                av[e] = (_Float16)0.f;
+                f.v[k][u] = __builtin_bit_cast(u4v, av);
+              }
+            }
+          }
         }
       }
     }
     // ---- the reference moves for the first tile and when a score exceeds it by far
-    float mx[NC];
-    bool move = first;
+    float mx = sb[0];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      mx[n] = fmaxf(fmaxf(fmaxf(sb[0][n][0], sb[0][n][1]), fmaxf(sb[0][n][2], sb[0][n][3])),
-                    fmaxf(fmaxf(sb[1][n][0], sb[1][n][1]), fmaxf(sb[1][n][2], sb[1][n][3])));
-      move = move || mx[n] > kHead;
-    }
-    if (__ballot(move)) {
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sb[i]);
+    if (__ballot(first || mx > kHead)) {
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float by = (first ? mx > -inf : mx > kHead) ? mx - kUp : 0.f;
+      const float fall = first ? 0.f : __builtin_amdgcn_exp2f(-by);
+      m += by;
+      l *= fall;
 #pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        float c = fmaxf(mx[n], __shfl_xor(mx[n], 16));
-        c = fmaxf(c, __shfl_xor(c, 32));
-        const float by = (first ? c > -inf : c > kHead) ? c - kUp : 0.f;
-        const float fall = first ? 0.f : __builtin_amdgcn_exp2f(-by);
-        m[n] += by;
-        l[n] *= fall;
+      for (int i = 0; i < 16; ++i) sb[i] -= by;
+      if (!first) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int k = 0; k < NV; ++k) acc_a[k] *= fall;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) sb[b][n][i] -= by;
-        if (!first) {
-#pragma unroll
-          for (int k = 0; k < NB; ++k) acc_a[k][n] *= fall;
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) acc_r[k][n] *= fall;
-        }
+        for (int k = 0; k < D / 32; ++k) acc_r[k] *= fall;
       }
       first = false;
     }
     // ---- probabilities as fp16 pairs, plain and times the value scales; values:
-    // channel blocks of the basis, then of the residual.  One block of 16 rows is
-    // prepared while the products of the one before it run.
-    u4v ph[C8 ? NC : 2], pl[C8 ? NC : 2], rh[2], rl[2];
-    const auto prepare = [&](int n) {
+    // channel blocks of the basis, then of the residual
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const f4 s0 = *reinterpret_cast<const f4*>(&w.sv[16 * u + 8 * h]), s1 = *reinterpret_cast<const f4*>(&w.sv[16 * u + 8 * h + 4]);
+      u4v ph, pl, rh, rl;
       float sum[2] = {0.f, 0.f};
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        const float v0 = __builtin_amdgcn_exp2f(sb[e >> 2][n][e & 3]), v1 = __builtin_amdgcn_exp2f(sb[e >> 2][n][(e & 3) + 1]);
+        const float v0 = __builtin_amdgcn_exp2f(sb[8 * u + e]), v1 = __builtin_amdgcn_exp2f(sb[8 * u + e + 1]);
+        const float x0 = e < 4 ? s0[e & 3] : s1[e & 3], x1 = e < 4 ? s0[(e & 3) + 1] : s1[(e & 3) + 1];
         sum[0] += v0;
         sum[1] += v1;
-        uint32_t h, lo;
-        pair2(v0, v1, h, lo);
-        ph[C8 ? n : n & 1][e >> 1] = h;
-        pl[C8 ? n : n & 1][e >> 1] = lo;
-        pair2(v0 * vs[e], v1 * vs[e + 1], h, lo);
-        rh[n & 1][e >> 1] = h;
-        rl[n & 1][e >> 1] = lo;
+        uint32_t hi, lo;
+        pair2(v0, v1, hi, lo);
+        ph[e >> 1] = hi;
+        pl[e >> 1] = lo;
+        pair2(v0 * x0, v1 * x1, hi, lo);
+        rh[e >> 1] = hi;
+        rl[e >> 1] = lo;
       }
-      l[n] += sum[0] + sum[1];
-    };
-    h8 vc[D / 16];
+      l += sum[0] + sum[1];
+      const h8 p0 = __builtin_bit_cast(h8, ph), p1 = __builtin_bit_cast(h8, pl), r0 = __builtin_bit_cast(h8, rh), r1 = __builtin_bit_cast(h8, rl);
 #pragma unroll
-    for (int k = 0; k < D / 16; ++k) vc[k] = __builtin_bit_cast(h8, *reinterpret_cast<const u4v*>(&w.v[(16 * k + col) * TT + 8 * g]));
-    prepare(0);
-#pragma unroll
-    for (int n = 0; n < NC; ++n) {
-      const h8 r0 = __builtin_bit_cast(h8, rh[n & 1]), r1 = __builtin_bit_cast(h8, rl[n & 1]);
-      if constexpr (!C8) {
-        const h8 p0 = __builtin_bit_cast(h8, ph[n & 1]), p1 = __builtin_bit_cast(h8, pl[n & 1]);
-#pragma unroll
-        for (int k = 0; k < NB; ++k) acc_a[k][n] = mfma_h(__builtin_bit_cast(h8, f.v[k]), p0, acc_a[k][n]);
-#pragma unroll
-        for (int k = 0; k < NB; ++k) acc_a[k][n] = mfma_h(__builtin_bit_cast(h8, f.v[k]), p1, acc_a[k][n]);
+      for (int k = 0; k < D / 32; ++k) {
+        const h8 vc = __builtin_bit_cast(h8, *reinterpret_cast<const u4v*>(&w.v[value_place(32 * k + col, 16 * u + 8 * h)]));
+        acc_r[k] = mfma_h(vc, r0, acc_r[k]);
+        acc_r[k] = mfma_h(vc, r1, acc_r[k]);
       }
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) acc_r[k][n] = mfma_h(vc[k], r0, acc_r[k][n]);
+      for (int k = 0; k < NV; ++k) {
+        if constexpr (C8) {
+          const u4v sw = *reinterpret_cast<const u4v*>(&sm.vs[wv][min(2 * k + (col >> 4), NB - 1)][16 * u + 8 * h]);
+          float v[8];
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) acc_r[k][n] = mfma_h(vc[k], r1, acc_r[k][n]);
-      if (n + 1 < NC) {
-        prepare(n + 1);
-        interleave<(C8 ? 0 : 2) * NB + D / 8>();
-      }
-    }
-    if constexpr (C8) {                  // one block dequantized at a time
+          for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.v[k][u].x, f.v[k][u].y}, e) * half_bits_to_float((uint16_t)(sw[e >> 1] >> (16 * (e & 1))));
+          if (edge) {
 #pragma unroll
-      for (int k = 0; k < NB; ++k) {
-        const u4v sw = *reinterpret_cast<const u4v*>(&sm.vs[wv][k][8 * g]);
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.v[k].x, f.v[k].y}, e) * half_bits_to_float((uint16_t)(sw[e >> 1] >> (16 * (e & 1))));
-        if (edge) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (t0 + 8 * g + e < c0 || t0 + 8 * g + e >= c1) v[e] = 0.f;
+            for (int e = 0; e < 8; ++e)
+              if (t0 + 16 * u + 8 * h + e < c0 || t0 + 16 * u + 8 * h + e >= c1) v[e] = 0.f;
+          }
+          h8 hi, lo;
+          split8(v, hi, lo);
+          acc_a[k] = mfma_h(hi, p0, acc_a[k]);
+          acc_a[k] = mfma_h(hi, p1, acc_a[k]);
+          acc_a[k] = mfma_h(lo, p0, acc_a[k]);
+        } else {
+          acc_a[k] = mfma_h(__builtin_bit_cast(h8, f.v[k][u]), p0, acc_a[k]);
+          acc_a[k] = mfma_h(__builtin_bit_cast(h8, f.v[k][u]), p1, acc_a[k]);
         }
-        h8 hi, lo;
-        split8(v, hi, lo);
-#pragma unroll
-        for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
-#pragma unroll
-        for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(hi, __builtin_bit_cast(h8, pl[n]), acc_a[k][n]);
-#pragma unroll
-        for (int n = 0; n < NC; ++n) acc_a[k][n] = mfma_h(lo, __builtin_bit_cast(h8, ph[n]), acc_a[k][n]);
       }
     }
     load_v<NB, C8>(f, sx, lp, jn);
@@ -915,29 +828,22 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
   }
 
   // ---- join the waves: common reference per row, then sums in wave order -----------
-#pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    l[n] += __shfl_xor(l[n], 16);
-    l[n] += __shfl_xor(l[n], 32);
-    if (g == 0) {
-      sm.m[wv][16 * n + col] = first ? -inf : m[n];
-      sm.l[wv][16 * n + col] = l[n];
-    }
+  l += __shfl_xor(l, 32);
+  if (h == 0) {
+    sm.m[wv][col] = first ? -inf : m;
+    sm.l[wv][col] = l;
   }
   __syncthreads();                       // the code tiles are done with
-  float mine[NC];
+  float ms = -inf;
 #pragma unroll
-  for (int n = 0; n < NC; ++n) {
-    float ms = -inf;
+  for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][col]);
+  const float mine = first ? 0.f : __builtin_amdgcn_exp2f(m - ms);
 #pragma unroll
-    for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][16 * n + col]);
-    mine[n] = first ? 0.f : __builtin_amdgcn_exp2f(m[n] - ms);
-  }
+  for (int k = 0; k < D / 32; ++k)
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-    for (int n = 0; n < NC; ++n)
-      *reinterpret_cast<f4*>(&sm.acc[wv][16 * n + col][16 * k + 4 * g]) = acc_r[k][n] * (mine[n] * exf);
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f4*>(&sm.acc[wv][col][32 * k + 8 * q + 4 * h]) =
+          f4{acc_r[k][4 * q], acc_r[k][4 * q + 1], acc_r[k][4 * q + 2], acc_r[k][4 * q + 3]} * (mine * exf);
   __syncthreads();
   for (int i = threadIdx.x; i < R * (D / 4); i += 64 * NW) {
     const int r = i / (D / 4), c = 4 * (i % (D / 4));
@@ -951,10 +857,12 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
   }
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < NB; ++k)
+  for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int n = 0; n < NC; ++n)
-      *reinterpret_cast<f4*>(&sm.acc[wv][16 * n + col][16 * k + 4 * g]) = acc_a[k][n] * mine[n];
+    for (int q = 0; q < 4; ++q)
+      if (32 * k + 8 * q < rb)
+        *reinterpret_cast<f4*>(&sm.acc[wv][col][32 * k + 8 * q + 4 * h]) =
+            f4{acc_a[k][4 * q], acc_a[k][4 * q + 1], acc_a[k][4 * q + 2], acc_a[k][4 * q + 3]} * mine;
   __syncthreads();
   for (int i = threadIdx.x; i < R * (rb / 4); i += 64 * NW) {
     const int r = i / (rb / 4), c = 4 * (i % (rb / 4));
@@ -976,33 +884,24 @@ __global__ __launch_bounds__(64 * kWaves<NC>, kWaves<NC> / 4) void tree_split_ke
   }
 }
 
-template <int NB, int NC, bool BF>
-void launch_tree_c(const TreeArgs& a, dim3 grid, hipStream_t s) {
-  if (a.c8) hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, true>), grid, dim3(64 * kWaves<NC>), 0, s, a);
-  else hipLaunchKernelGGL((tree_split_kernel<NB, NC, BF, false>), grid, dim3(64 * kWaves<NC>), 0, s, a);
-}
-
 template <int NB, bool BF>
-void launch_tree_b(const TreeArgs& a, dim3 grid, hipStream_t s) {
-  if constexpr (NB <= 4) {
-    if (a.rows == 64) return launch_tree_c<NB, 4, BF>(a, grid, s);
-    if (a.rows == 32) return launch_tree_c<NB, 2, BF>(a, grid, s);
-  }
-  launch_tree_c<NB, 1, BF>(a, grid, s);
+void launch_tree_b(const TreeArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.n_pairs + 7) / 8 * 8 * a.max_nrb)), block(64 * kWaves<NB>);
+  if (a.c8) hipLaunchKernelGGL((tree_split_kernel<NB, BF, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((tree_split_kernel<NB, BF, false>), grid, block, 0, s, a);
 }
 
 template <bool BF>
 void launch_tree_split(const TreeArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n_pairs + 7) / 8 * 8 * a.max_nrb));
   switch (a.rb / 16) {
-    case 1: launch_tree_b<1, BF>(a, grid, s); break;
-    case 2: launch_tree_b<2, BF>(a, grid, s); break;
-    case 3: launch_tree_b<3, BF>(a, grid, s); break;
-    case 4: launch_tree_b<4, BF>(a, grid, s); break;
-    case 5: launch_tree_b<5, BF>(a, grid, s); break;
-    case 6: launch_tree_b<6, BF>(a, grid, s); break;
-    case 7: launch_tree_b<7, BF>(a, grid, s); break;
-    default: launch_tree_b<8, BF>(a, grid, s); break;
+    case 1: launch_tree_b<1, BF>(a, s); break;
+    case 2: launch_tree_b<2, BF>(a, s); break;
+    case 3: launch_tree_b<3, BF>(a, s); break;
+    case 4: launch_tree_b<4, BF>(a, s); break;
+    case 5: launch_tree_b<5, BF>(a, s); break;
+    case 6: launch_tree_b<6, BF>(a, s); break;
+    case 7: launch_tree_b<7, BF>(a, s); break;
+    default: launch_tree_b<8, BF>(a, s); break;
   }
 }
 
