@@ -17,11 +17,11 @@ struct alignas(16) MergeSmem {
   float part[kMW][kMR][2 * D];
   float m[kMW][kMR], l[kMW][kMR];
   float as[kMR][D];
-  u4v basis[128 * D / 8];
 };
 
 __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) {
   __shared__ MergeSmem sm;
+  extern __shared__ u4v basis[];         // r_b rows of B^V
   const int b = blockIdx.z, h = blockIdx.y, H = a.n_kv_heads, rb = a.rb;
   const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const u4v* bv = reinterpret_cast<const u4v*>(a.basis + (int64_t)b * a.basis_b_stride + (int64_t)(h * 2 + 1) * rb * D);
@@ -93,7 +93,7 @@ __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) 
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i)
-    if (i * 16 < rb) sm.basis[threadIdx.x + 256 * i] = bw[i];
+    if (i * 16 < rb) basis[threadIdx.x + 256 * i] = bw[i];
   __syncthreads();
   const int r = threadIdx.x >> 7, c = threadIdx.x & 127;     // a thread per output
   float ms = -inf, ls = 0.f, out = 0.f, av = 0.f;
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(64 * kMW) void tree_merge_kernel(const TreeArgs a) 
   out *= inv;
   sm.as[r][c] = c < rb ? av * inv : 0.f;
   __syncthreads();
-  const uint16_t* bas = reinterpret_cast<const uint16_t*>(sm.basis);
+  const uint16_t* bas = reinterpret_cast<const uint16_t*>(basis);
 #pragma unroll 8
   for (int i = 0; i < rb; ++i) out = __builtin_fmaf(sm.as[r][i], half_bits_to_float(bas[i * D + c]), out);
   if (r0 + r < rows)
@@ -127,7 +127,7 @@ hipError_t launch_tree(const TreeArgs& a, int max_rows, hipStream_t s) {
   else launch_tree_split<false>(a, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(tree_merge_kernel, dim3((max_rows + kMR - 1) / kMR, a.n_kv_heads, a.batch), dim3(64 * kMW), 0, s, a);
+  hipLaunchKernelGGL(tree_merge_kernel, dim3((max_rows + kMR - 1) / kMR, a.n_kv_heads, a.batch), dim3(64 * kMW), (unsigned)(a.rb * D * 2), s, a);
   return hipGetLastError();
 }
 

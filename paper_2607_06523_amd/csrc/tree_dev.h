@@ -323,17 +323,6 @@ __device__ __forceinline__ void draft_item(const TreeArgs& a, const Item& it, Dr
   }
 }
 
-// Dequantized int8 coefficients, code * scale = hi + lo exactly (18 bits).
-__device__ __forceinline__ void split8(const float (&v)[8], h8& hi, h8& lo) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    hi[j] = (_Float16)v[j];
-    lo[j] = (_Float16)(v[j] - (float)hi[j]);
-  }
-}
-
-__device__ __forceinline__ float byte_at(u2v w, int j) { return (float)(int8_t)(w[j >> 2] >> (8 * (j & 3))); }
-
 // Two values as fp16 pairs, rounded towards zero: hi and lo halves.  v - hi is
 // exact; the mixed-precision fma takes hi as it is packed.
 __device__ __forceinline__ void pair2(float v0, float v1, uint32_t& hi, uint32_t& lo) {
@@ -342,6 +331,27 @@ __device__ __forceinline__ void pair2(float v0, float v1, uint32_t& hi, uint32_t
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d0) : "v"(hi), "v"(v0));
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d1) : "v"(hi), "v"(v1));
   lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(d0, d1));
+}
+
+// Eight int8 coefficients, code * scale = hi + lo exactly (18 bits).  A code plus
+// 128 is a byte, which converts in one instruction; (code + 128) s - 128 s is
+// code s, exact in one fused multiply-add.
+template <typename Scale>
+__device__ __forceinline__ void dequant8(u4v w, Scale scale, h8& hi, h8& lo) {
+  u4v ph, pl;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const uint32_t x = w[e >> 2] ^ 0x80808080u;
+    const float s0 = scale(e), s1 = scale(e + 1);
+    const float v0 = __builtin_fmaf((float)((x >> (8 * (e & 3))) & 0xff), s0, -128.f * s0);
+    const float v1 = __builtin_fmaf((float)((x >> (8 * (e & 3) + 8)) & 0xff), s1, -128.f * s1);
+    uint32_t h, l;
+    pair2(v0, v1, h, l);
+    ph[e >> 1] = h;
+    pl[e >> 1] = l;
+  }
+  hi = __builtin_bit_cast(h8, ph);
+  lo = __builtin_bit_cast(h8, pl);
 }
 
 // Streams of a chunk and KV head; offsets count from the chunk's first 16-token block.
@@ -601,11 +611,8 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       const h8 qh = __builtin_bit_cast(h8, sm.qt[0][s][lane]), ql = __builtin_bit_cast(h8, sm.qt[1][s][lane]);
       if constexpr (C8) {
         const float sc = half_bits_to_float((uint16_t)f.ks[s]);
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.k[s].x, f.k[s].y}, e) * sc;
         h8 kh, kl;
-        split8(v, kh, kl);
+        dequant8(f.k[s], [&](int) { return sc; }, kh, kl);
         sb = mfma_h(kh, qh, sb);
         sb = mfma_h(kh, ql, sb);
         sb = mfma_h(kl, qh, sb);
@@ -794,16 +801,13 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       for (int k = 0; k < NV; ++k) {
         if constexpr (C8) {
           const u4v sw = *reinterpret_cast<const u4v*>(&sm.vs[wv][min(2 * k + (col >> 4), NB - 1)][16 * u + 8 * h]);
-          float v[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = byte_at(u2v{f.v[k][u].x, f.v[k][u].y}, e) * half_bits_to_float((uint16_t)(sw[e >> 1] >> (16 * (e & 1))));
+          h8 hi, lo;
+          dequant8(f.v[k][u], [&](int e) { return half_bits_to_float((uint16_t)(sw[e >> 1] >> (16 * (e & 1)))); }, hi, lo);
           if (edge) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              if (t0 + 16 * u + 8 * h + e < c0 || t0 + 16 * u + 8 * h + e >= c1) v[e] = 0.f;
+              if (t0 + 16 * u + 8 * h + e < c0 || t0 + 16 * u + 8 * h + e >= c1) hi[e] = lo[e] = (_Float16)0.f;
           }
-          h8 hi, lo;
-          split8(v, hi, lo);
           acc_a[k] = mfma_h(hi, p0, acc_a[k]);
           acc_a[k] = mfma_h(hi, p1, acc_a[k]);
           acc_a[k] = mfma_h(lo, p0, acc_a[k]);
