@@ -1249,14 +1249,14 @@ void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int64_t split, int b, int6
   nrb = (n * (d->n_q_heads / d->n_kv_heads) + kTreeRows - 1) / kTreeRows;
 }
 
-// Chunk size, in rounds of a workgroup's waves over their tiles.  A workgroup
-// takes about kFixed rounds before and after them, one of the drafted nodes about
-// kDraft; a compute unit holds one.  Of the chunk sizes that give every compute unit
-// 1 to 8 workgroups, or one tile per wave more, the one whose estimated end is
-// first: full rounds of the longest workgroup, or the work shared out evenly
-// plus one workgroup's length where sequences are ragged.
+// Chunk size.  Counted in rounds of a workgroup's waves over their tiles (2 to 2.6 us
+// at r_b 48), a workgroup takes about kFixed rounds before and after them and one of
+// the drafted nodes about kDraft; a compute unit holds one workgroup.  Of the sizes
+// that give every compute unit 1 to 8 workgroups, or one tile per wave more, the one
+// whose estimated end is first is taken: full rounds of the longest workgroup, or the
+// work shared out evenly plus one workgroup's length where sequences are ragged.
 int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t) {
-  constexpr int64_t q = kTreeWaves * kTreeTile, kCU = kTargetWorkgroups / 2, kFixed = 3, kDraft = 2;
+  constexpr int64_t q = kTreeWaves * kTreeTile, kCU = kTargetWorkgroups / 2, kFixed = 5, kDraft = 4;
   if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets
   int64_t total = 0, chunks, nrb;
   for (int b = 0; b < d->batch; ++b) {
@@ -1327,7 +1327,10 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
   if ((st = split_args(d, c, layer, q, q_type, sm_scale, workspace, a)) != DWKV_OK) return st;
   const TreePlan p = tree_plan(d, tree);
   if (ws_bytes < p.bytes) return DWKV_E_WORKSPACE;
-  if ((p.pairs * d->n_kv_heads + 8) * p.max_nrb > 0x7fffffff) return DWKV_E_UNSUPPORTED;
+  // the merge has one grid layer per sequence; a slab's int8 scales are one buffer of 2^30 bytes
+  if ((p.pairs * d->n_kv_heads + 8) * p.max_nrb > 0x7fffffff || d->batch > 65535 ||
+      (d->coef_format == DWKV_COEF_I8 && (int64_t)d->basis_rank / 16 * d->total_tokens * 2 > (1 << 30)))
+    return DWKV_E_UNSUPPORTED;
   if (tree->n_nodes == 0) return DWKV_OK;
   TreeArgs t;
   std::memset(&t, 0, sizeof(t));
