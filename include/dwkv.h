@@ -553,8 +553,8 @@ size_t dwkv_tree_workspace_bytes(const dwkv_dims* dims, const dwkv_tree* tree);
  * dims allow.  Scores and value sums are accurate to about float32, as the
  * decode's.  The coefficients' padding tokens must be finite.  Two launches
  * (none when N = 0).  DWKV_E_UNSUPPORTED for more than 65535 sequences, and for
- * int8 coefficients when r_b / 16 * T exceeds 2^29.  Every device pointer 16-byte aligned, parent 4-byte, the
- * residual and block scales 2-byte. */
+ * int8 coefficients when r_b / 16 * T exceeds 2^29.  Every device pointer 16-byte aligned, cu_seqlens,
+ * cu_nodes and parent 4-byte, the block scales 2-byte. */
 dwkv_status dwkv_tree_decode(const dwkv_dims* dims, const dwkv_cache* cache, int32_t layer, const dwkv_tree* tree,
                              const void* q, int32_t q_type, int64_t q_stride, const void* k_new, const void* v_new,
                              int64_t kv_stride, float sm_scale, float* out, void* workspace, size_t ws_bytes,

@@ -61,11 +61,18 @@ class _on:
 
 
 def _all_on(index, *tensors):
-    """Whether every tensor (None aside) is on GPU ``index``."""
+    """Whether every tensor (None aside) is on GPU ``index`` (-1, the CPU, is none)."""
     for x in tensors:
         if x is not None and x.get_device() != index:
             return False
-    return True
+    return index >= 0
+
+
+def _nbytes(workspace):
+    """Bytes from a workspace's start on."""
+    if not workspace.is_contiguous():
+        raise TypeError("workspace must be contiguous")
+    return workspace.nbytes
 
 
 def probe_schedule(step: int, period: int, n_heads: int, n_kv_heads: int, n_pos: int = 1):
@@ -175,7 +182,7 @@ def tree_verify(tree: DraftTree, token, target, u, u_next, draft=None, max_child
         st = load().dwkv_tree_verify(B, tree.ref, token.data_ptr(), V, kinds[target.dtype], target.data_ptr(),
                                      draft.data_ptr() if draft is not None else None, u.data_ptr(), u_next.data_ptr(),
                                      int(max_children), path.data_ptr(), n_kept.data_ptr(), nxt.data_ptr(), ws.data_ptr(),
-                                     ws.numel(), torch.cuda.current_stream(tree.index).cuda_stream)
+                                     _nbytes(ws), torch.cuda.current_stream(tree.index).cuda_stream)
     binding.check(st, "dwkv_tree_verify")
     return path, n_kept, nxt
 
@@ -637,6 +644,8 @@ class DeviceCache:
             raise ValueError("the rows of q, k_new and v_new must have no gaps inside")
         if N > 1 and ks[0] != vs[0]:
             raise ValueError("k_new and v_new must have the same row stride")
+        if N > 1 and (qs[0] < Hq * d or ks[0] < Hk * d):
+            raise ValueError("the rows of q, k_new and v_new must not overlap")
         index = self.basis.get_device()
         if tree.index != index or not _all_on(index, q, k_new, v_new, out, workspace):
             raise ValueError("every tensor must be on the cache's device")
@@ -651,7 +660,7 @@ class DeviceCache:
             st = self.lib.dwkv_tree_decode(C.byref(self.dims), C.byref(self.cstruct), int(layer), tree.ref, q.data_ptr(),
                                            F16 if q.dtype == torch.float16 else BF16, qs[0] if N > 1 else 0, k_new.data_ptr(),
                                            v_new.data_ptr(), ks[0] if N > 1 else 0, float(sm_scale or 0.0), out.data_ptr(),
-                                           ws.data_ptr(), ws.numel(), torch.cuda.current_stream(index).cuda_stream)
+                                           ws.data_ptr(), _nbytes(ws), torch.cuda.current_stream(index).cuda_stream)
         binding.check(st, "dwkv_tree_decode")
         return out
 
@@ -685,7 +694,7 @@ class DeviceCache:
         with _on(torch, index):
             st = self.lib.dwkv_repack(C.byref(self.dims), C.byref(self.cstruct), C.byref(src.dims), C.byref(src.cstruct),
                                       src_token.data_ptr() or None, src_seq.data_ptr(), None if new_code is None else new_code.data_ptr(),
-                                      n_new, ws.data_ptr(), ws.numel(), torch.cuda.current_stream(index).cuda_stream)
+                                      n_new, ws.data_ptr(), _nbytes(ws), torch.cuda.current_stream(index).cuda_stream)
         binding.check(st, "dwkv_repack")
 
     def residual_map(self, layer: int, z: int, kv_head: int, t0: int, t1: int):

@@ -1323,8 +1323,14 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
   if (q_stride == 0) q_stride = qrow;
   if (kv_stride == 0) kv_stride = kvrow;
   if (q_stride < qrow || kv_stride < kvrow || q_stride % 8 || kv_stride % 8) return DWKV_E_DIMS;
+  dwkv_cache held = *c;
+  if (d->total_tokens == 0) {            // arrays of tokens are not there without any, and not read
+    for (const void** x : {&held.coef_k, &held.coef_v, (const void**)&held.res_scale, (const void**)&held.coef_k_scale,
+                           (const void**)&held.coef_v_scale})
+      if (!*x) *x = workspace;
+  }
   SplitArgs a;                           // checks the cache, layer and query
-  if ((st = split_args(d, c, layer, q, q_type, sm_scale, workspace, a)) != DWKV_OK) return st;
+  if ((st = split_args(d, &held, layer, q, q_type, sm_scale, workspace, a)) != DWKV_OK) return st;
   const TreePlan p = tree_plan(d, tree);
   if (ws_bytes < p.bytes) return DWKV_E_WORKSPACE;
   // the merge has one grid layer per sequence; a slab's int8 scales are one buffer of 2^30 bytes
@@ -1499,7 +1505,9 @@ dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_d
   if (!aligned4(src_token) || !aligned4(src_seq) || !aligned16(workspace)) return DWKV_E_ALIGN;
   const void* const pairs[][2] = {{to->basis, from->basis}, {to->coef_k, from->coef_k}, {to->coef_v, from->coef_v},
                                   {to->rank_code, from->rank_code}, {to->res_off, from->res_off}, {to->res_idx, from->res_idx},
-                                  {to->res_val, from->res_val}, {to->res_scale, from->res_scale}};
+                                  {to->res_val, from->res_val}, {to->res_scale, from->res_scale},
+                                  {c8 ? to->coef_k_scale : nullptr, c8 ? from->coef_k_scale : nullptr},
+                                  {c8 ? to->coef_v_scale : nullptr, c8 ? from->coef_v_scale : nullptr}};
   for (const auto& p : pairs)
     if (p[0] && p[0] == p[1]) return DWKV_E_DIMS;        // not in place
   if (ws_bytes < dwkv_repack_workspace_bytes(dst)) return DWKV_E_WORKSPACE;
