@@ -551,8 +551,9 @@ size_t dwkv_tree_workspace_bytes(const dwkv_dims* dims, const dwkv_tree* tree);
  *   workspace:  >= dwkv_tree_workspace_bytes(dims, tree), no initial contents
  * Both coefficient formats, every basis rank, group and level table that
  * dims allow.  Scores and value sums are accurate to about float32, as the
- * decode's.  The coefficients' padding tokens must be finite.  Two launches
- * (none when N = 0).  DWKV_E_UNSUPPORTED for more than 65535 sequences, and for
+ * decode's.  The coefficients' padding tokens must be finite, and an int8
+ * coefficient, code times scale, within fp16's range (else the rows that see it
+ * are not finite).  Two launches (none when N = 0).  DWKV_E_UNSUPPORTED for more than 65535 sequences, and for
  * int8 coefficients when r_b / 16 * T exceeds 2^29.  Every device pointer 16-byte aligned, cu_seqlens,
  * cu_nodes and parent 4-byte, the block scales 2-byte. */
 dwkv_status dwkv_tree_decode(const dwkv_dims* dims, const dwkv_cache* cache, int32_t layer, const dwkv_tree* tree,

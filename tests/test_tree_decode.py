@@ -216,6 +216,25 @@ def test_scales_over_the_whole_range(fmt, rb):
     check(got, want, bound(host, top), f"wide scales {fmt}")
 
 
+@pytest.mark.parametrize("rb", [16, 48, 112])
+def test_block_scales_over_a_wide_range(rb):
+    """int8 block scales from 2^-5 to 2^-2 (keys) and from 2^-12 to 2^7 (values), another for every token of a value
+    block; the bound of the fp16 coefficients, whose products are as exact."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import DraftTree
+    w = Workload(name="tree", batch=2, n_layers=2, window=1, n_kv_heads=2, n_q_heads=8, head_dim=D, context=901, basis_rank=rb,
+                 levels=(0, 8), probs=(0.5, 0.5), q_dtype="f16", seed=15, coef_format="int8", coef_scale_mode="wide")
+    host = generate(_Fixed(w, [901, 70]), threads=4)
+    rng = np.random.default_rng(rb)
+    cu, parent = make_tree([10, 7], "tree", rng)
+    q, k, v = inputs(host, 17, rng)
+    announce(f"tree decode wide block scales {rb}")
+    got = device_cache(host).tree_decode(1, DraftTree(cu, torch.from_numpy(parent).cuda()), q.cuda(), k.cuda(), v.cuda()).cpu().numpy()
+    want, top = reference(host, 1, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy())
+    check(got, want, bound(host, top), f"wide block scales {rb}")
+
+
 def test_queries_beyond_fp16():
     """bf16 queries whose projections exceed fp16's range: scores in the hundred thousands, the softmax one-hot."""
     torch = torch_gpu()
