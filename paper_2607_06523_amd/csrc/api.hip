@@ -1333,8 +1333,9 @@ dwkv_status dwkv_tree_decode(const dwkv_dims* d, const dwkv_cache* c, int32_t la
   if ((st = split_args(d, &held, layer, q, q_type, sm_scale, workspace, a)) != DWKV_OK) return st;
   const TreePlan p = tree_plan(d, tree);
   if (ws_bytes < p.bytes) return DWKV_E_WORKSPACE;
-  // the merge has one grid layer per sequence; a slab's int8 scales are one buffer of 2^30 bytes
-  if ((p.pairs * d->n_kv_heads + 8) * p.max_nrb > 0x7fffffff || d->batch > 65535 ||
+  // a grid's threads are counted in 32 bits; the merge has one grid layer per
+  // sequence; a slab's int8 scales are one buffer of 2^30 bytes
+  if ((p.pairs * d->n_kv_heads + 8) * p.max_nrb > 0xffffffffll / (64 * kTreeWaves) || d->batch > 65535 ||
       (d->coef_format == DWKV_COEF_I8 && (int64_t)d->basis_rank / 16 * d->total_tokens * 2 > (1 << 30)))
     return DWKV_E_UNSUPPORTED;
   if (tree->n_nodes == 0) return DWKV_OK;

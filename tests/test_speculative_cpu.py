@@ -105,6 +105,9 @@ def test_tree_decode_sizes_past_its_addressing(lib):  # noqa: F811
     kw = dict(batch=1, cu_seqlens_host=[0, T], total_tokens=T, levels=(0, 2), res_stride=2**30)
     d, keep = dims(coef_format=binding.COEF_I8, **kw)
     assert tree_decode(lib, d, t) == UNSUPPORTED
+    d, keep = dims(split_tokens=64, **kw)                             # 2^22 chunks of 2 heads, 1 block of rows
+    need = lib.dwkv_tree_workspace_bytes(C.byref(d), C.byref(t))
+    assert tree_decode(lib, d, t, ws_bytes=need - 1) == WORKSPACE and tree_decode(lib, d, t, ws_bytes=need) == UNSUPPORTED
 
 
 def test_a_tree_without_nodes_is_no_call(lib):  # noqa: F811
