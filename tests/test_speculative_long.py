@@ -1,4 +1,4 @@
-"""The speculative step's calls where sizes leave nothing to spare: a cache
+"""The speculative step's calls where little is left to spare: at once, captured, a cache
 without a token, and one whose arrays pass 2^32 bytes and 2^31 elements, against
 plain computation on the GPU in float64 (attention) and plain indexing
 (repacking)."""
@@ -94,3 +94,63 @@ def test_arrays_past_32_bits():
         assert torch.equal(dst.res_idx[l, :, h, :2 * T - 2], src.res_idx[l, :, h, 2:2 * T])
         assert torch.equal(dst.res_val[l, :, h, :T - 1], src.res_val[l, :, h, 1:T])
     assert torch.equal(dst.res_off[0, H - 1, :T], off[0, 0, :T]) and int(dst.res_off[0, H - 1, T]) == 2 * T - 2
+
+
+def test_calls_at_once_and_a_captured_repack():
+    """Calls on two streams with workspaces of their own, nothing between them, and a captured repack whose source
+    tokens change between its replays: all as the calls one after another."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import DraftTree, tree_verify, tree_verify_workspace
+    host = make_host([2100, 900], 4, 48)
+    dc = device_cache(host)
+    rng = np.random.default_rng(21)
+    cu, parent = make_tree([30, 11], "tree", rng)
+    tree = DraftTree(cu, torch.from_numpy(parent).cuda())
+    x = [[torch.from_numpy(rng.standard_normal((41, h, D)).astype(np.float16)).cuda() for h in (8, 2, 2)] for _ in range(2)]
+    p = torch.softmax(torch.from_numpy(rng.standard_normal((2, 41, 5003)).astype(np.float32)).cuda(), -1)
+    tok = torch.from_numpy(rng.integers(0, 5003, 41).astype(np.int32)).cuda()
+    u = torch.from_numpy(rng.random(43).astype(np.float32)).cuda()
+    perm = [torch.from_numpy(rng.permutation(3000).astype(np.int32)).cuda() for _ in range(4)]
+    seq = torch.tensor([1, 0], dtype=torch.int32, device="cuda")
+    dst = [dc.empty_like([2100, 900]) for _ in range(2)]
+    arrays = lambda c: [c.coef_k, c.coef_v, c.rank_code, c.res_off, c.res_idx, c.res_val, c.res_scale, c.basis]
+
+    def calls(i, ws):
+        out = dc.tree_decode(i, tree, *x[i], workspace=ws[0])
+        kept = tree_verify(tree, tok, p[i], u[:41], u[41:], draft=p[1 - i], max_children=3, workspace=ws[1])
+        dst[i].repack_from(dc, perm[i], seq, workspace=ws[2])
+        return [out, *kept]
+
+    ws = [(dc.tree_workspace(tree), tree_verify_workspace(tree, 5003, 3), dst[i].repack_workspace()) for i in range(2)]
+    announce("one call after another")
+    want = []
+    for i in range(2):
+        want.append([t.clone() for t in calls(i, ws[i]) + arrays(dst[i])])
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    announce("calls at once")
+    for _ in range(3):
+        got = []
+        for i, s in enumerate(streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                got.append(calls(i, ws[i]))
+        torch.cuda.synchronize()
+        for i in range(2):
+            for a, b in zip(got[i] + arrays(dst[i]), want[i]):
+                assert torch.equal(a, b)
+    announce("a captured repack")
+    src_token = perm[0].clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        dst[0].repack_from(dc, src_token, seq, workspace=ws[0][2])
+    for i in (2, 3, 1):
+        src_token.copy_(perm[i])
+        graph.replay()
+        dst[1].repack_from(dc, perm[i], seq, workspace=ws[1][2])
+        torch.cuda.synchronize()
+        e = int(dst[0].res_off[..., -1].min())
+        for a, b in zip(arrays(dst[0]), arrays(dst[1])):
+            cut = {id(dst[0].res_idx): e, id(dst[0].res_val): e // 2}.get(id(a))      # entries past the last keep older ones
+            assert torch.equal(a[..., :cut], b[..., :cut])
