@@ -154,3 +154,34 @@ def test_calls_at_once_and_a_captured_repack():
         for a, b in zip(arrays(dst[0]), arrays(dst[1])):
             cut = {id(dst[0].res_idx): e, id(dst[0].res_val): e // 2}.get(id(a))      # entries past the last keep older ones
             assert torch.equal(a[..., :cut], b[..., :cut])
+
+
+@pytest.mark.parametrize("dt", ["float32", "float16", "bfloat16"])
+def test_verify_without_nodes_and_rows_off_16_bytes(dt):
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import DraftTree, tree_verify
+    dtype = getattr(torch, dt)
+    announce(f"verify without nodes {dt}")
+    u = torch.rand(60, generator=torch.Generator().manual_seed(3)).cuda()
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    p0 = torch.zeros((0, 77), dtype=dtype, device="cuda")
+    path, kept, after = tree_verify(DraftTree([0, 0, 0], none), none, p0, u[:0], u[:2], draft=p0, max_children=2)
+    assert path.numel() == 0 and kept.tolist() == [0, 0] and after.tolist() == [-1, -1]
+    announce(f"verify of rows off 16 bytes {dt}")
+    rng = np.random.default_rng(9)
+    N, V = 40, 4099
+    cu, parent = make_tree([33, 7], "tree", rng)
+    tree = DraftTree(cu, torch.from_numpy(parent).cuda())
+    tok = torch.from_numpy(rng.integers(0, V, N).astype(np.int32)).cuda()
+    p, q = (torch.softmax(torch.from_numpy(rng.standard_normal((N, V)).astype(np.float32) * 3), -1).to(dtype).cuda() for _ in range(2))
+    want = tree_verify(tree, tok, p, u[:N], u[N:N + 2], draft=q, max_children=3)
+    for a, b in ((1, 0), (0, 3), (5, 2)):
+        off = []
+        for x, o in ((p, a), (q, b)):
+            buf = torch.full((N * V + 8,), float("nan"), dtype=dtype, device="cuda")
+            buf[o:o + N * V] = x.flatten()
+            off.append(buf[o:o + N * V].view(N, V))
+        got = tree_verify(tree, tok, off[0], u[:N], u[N:N + 2], draft=off[1], max_children=3)
+        for x, y in zip(got, want):
+            assert torch.equal(x, y)
