@@ -1254,7 +1254,10 @@ void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int64_t split, int b, int6
 // the drafted nodes about kDraft; a compute unit holds one workgroup.  Of the sizes
 // that give every compute unit 1 to 8 workgroups, or one tile per wave more, the one
 // whose estimated end is first is taken: full rounds of the longest workgroup, or the
-// work shared out evenly plus one workgroup's length where sequences are ragged.
+// work shared out evenly plus one workgroup's length.  Where most workgroups are
+// shorter than the longest (ragged sequences) they fill in for each other, and half
+// a length is left: 16 int8 sequences of 8K to 16K take 198 us with the 5376-token
+// chunks that this gives and 208 with the 2816 of a whole length.
 int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t) {
   constexpr int64_t q = kTreeWaves * kTreeTile, kCU = kTargetWorkgroups / 2, kFixed = 5, kDraft = 4;
   if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets
@@ -1277,7 +1280,9 @@ int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t) {
       if (chunks > 0) most = std::max(most, kFixed + (std::min(len, c) + q - 1) / q);
     }
     const int64_t rounds = (wgs + kCU - 1) / kCU;
-    const int64_t time = std::min((rounds * most + (rounds * kCU - wgs < drafts ? kDraft : 0)) * kCU, work + most * kCU);
+    const bool ragged = 10 * (work - drafts * kDraft) < 9 * wgs * most;
+    const int64_t even = std::max(work + most * kCU / (ragged ? 2 : 1), most * kCU);
+    const int64_t time = std::min((rounds * most + (rounds * kCU - wgs < drafts ? kDraft : 0)) * kCU, even);
     if (time < best_time) {
       best_time = time;
       best = c;
