@@ -106,6 +106,10 @@ __device__ __forceinline__ uint16_t code_bits(float v) {   // v an int4 code: ex
 __device__ __forceinline__ int key_row(int t) { return 16 * (t >> 4) + 8 * ((t >> 2) & 1) + 4 * ((t >> 3) & 1) + (t & 3); }
 __device__ __forceinline__ int row_token(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
+// Binary places by which a row's q~ is scaled down, so that fp16 holds its largest
+// number `big`; a row has its own, and nothing of the rows beside it.
+__device__ __forceinline__ int row_down(float big) { return max(0, __builtin_amdgcn_frexp_expf(big) - 15); }
+
 // Place of (channel, token) in the value code tile: a channel's four 8-token
 // pieces are dealt by channel, so that 16 lanes reading the same piece of 16
 // channels touch every bank once.
@@ -137,7 +141,7 @@ struct alignas(16) TreeSmem {
   static constexpr int NW = kWaves<NB>;
   float m[NW][R], l[NW][R];
   uint32_t odd[D];                       // channels with entries of value scales that are not finite: bits +inf, -inf, NaN
-  float big;                             // largest |q~|
+  float big[R];                          // largest finite |q~| of a row
   alignas(16) uint16_t vs[C8 ? NW : 1][C8 ? NB : 1][C8 ? TT : 8];   // value block scales of a tile (int8)
   union {
     struct {
@@ -525,24 +529,21 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
   for (int i = threadIdx.x; i < 8 * 64; i += 64 * NW) {
     const int ln = i & 63, s = i >> 6, r = ln & 31;
     u4v w = {0, 0, 0, 0};
-    if (r < rows_left) {
-      const int row = it.rb * R + r, p = a.parent[it.n0 + row / a.group];
-      w = q_piece(a, it, row, 16 * s + 8 * (ln >> 5));
-      if (p < -1 || p >= row / a.group) w = u4v{0, 0, 0, 0};           // absent: its query may be anything
-    }
+    // a query meets its own column of every product alone: an absent node's may be anything
+    if (r < rows_left) w = q_piece(a, it, it.rb * R + r, 16 * s + 8 * (ln >> 5));
     sm.qf[s][ln] = w;
   }
-  if (threadIdx.x == 0) sm.big = 0.f;
+  if (threadIdx.x < R) sm.big[threadIdx.x] = 0.f;
   if (threadIdx.x < D) sm.odd[threadIdx.x] = 0;
   WaveTile& w = sm.w[wv];
   for (int i = lane; i < (int)((sizeof(w.k) + sizeof(w.v)) / 16); i += 64) reinterpret_cast<u4v*>(&w)[i] = u4v{0, 0, 0, 0};
   __syncthreads();
   {
     f4 q[PER];
-    float big = 0.f;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const int tile = wv + NW * u, n = tile % 2;
+      float big = 0.f;
       f4 c = {0.f, 0.f, 0.f, 0.f};
       if (tile < TILES) {
 #pragma unroll
@@ -562,16 +563,16 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
         if (m < __builtin_inff()) big = fmaxf(big, m);
       }
       q[u] = c;
+      big = fmaxf(big, __shfl_xor(big, 16));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      if (tile < TILES && g == 0) atomicMax(reinterpret_cast<int*>(&sm.big[16 * n + c16]), __builtin_bit_cast(int, big));
     }
-    // |q~| beyond fp16 is scaled down for the whole workgroup (scores stay float32)
-    for (int d = 32; d; d >>= 1) big = fmaxf(big, __shfl_xor(big, d));
-    if (lane == 0) atomicMax(reinterpret_cast<int*>(&sm.big), __builtin_bit_cast(int, big));
     __syncthreads();
-    const float dn = __builtin_ldexpf(1.f, -max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15));
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
       const int tile = wv + NW * u;
       if (tile >= TILES) continue;
+      const float dn = __builtin_ldexpf(1.f, -row_down(sm.big[16 * (tile % 2) + c16]));
       h4 hi, lo;                                       // basis rows 16 (tile / 2) + 4 g + i, row 16 (tile % 2) + c16
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -584,8 +585,8 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       reinterpret_cast<h4*>(&sm.qt[1][tile / 2][ln])[g & 1] = lo;
     }
   }
-  const int down = __builtin_amdgcn_readfirstlane(max(0, __builtin_amdgcn_frexp_expf(sm.big) - 15));
-  const float up = __builtin_ldexpf(1.f, down), fdn = __builtin_ldexpf(1.f, -down);
+  const float fdn = __builtin_ldexpf(1.f, -row_down(sm.big[col]));
+  const bool scaled = __ballot(fdn != 1.f) != 0;         // the same rows in every wave
   uint32_t e0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.oa);
   load_entries<NB, C8>(f, sx, lp, j0, e0, lane);
   load_vs<NB, C8>(f, sx, lp, j0, Ti);
@@ -726,7 +727,8 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       const u4v kc = *reinterpret_cast<const u4v*>(&w.k[col * kKRow + 16 * s + 8 * h]);
       sr = mfma_q<BF>(kc, sm.qf[s][lane], sr);
     }
-    if (down) {
+    if (scaled) {
+      const float up = __builtin_ldexpf(1.f, row_down(sm.big[col]));
 #pragma unroll
       for (int i = 0; i < 16; ++i) sb[i] *= up;
     }

@@ -1,0 +1,65 @@
+"""What a row of dwkv_tree_decode keeps beside rows, tokens and scales of quite
+another size, against plain float64 attention.  Tolerances are those of
+test_tree_decode (its `bound`), from the scores of the rows compared, unless a
+test derives its own."""
+import numpy as np
+import pytest
+
+from gpu_util import announce, device_cache, lib_ready, torch_gpu
+from test_tree_decode import D, bound, check, inputs, make_host, make_tree, reference
+
+pytestmark = pytest.mark.gpu
+
+
+def run(host, cu, parent, q, k, v, layer=0, split=0, sm_scale=None):
+    torch = torch_gpu()
+    from paper_2607_06523_amd import DraftTree
+    tree = DraftTree(cu, torch.from_numpy(np.asarray(parent, dtype=np.int32)).cuda())
+    return device_cache(host, split_tokens=split).tree_decode(layer, tree, q.cuda(), k.cuda(), v.cuda(), sm_scale=sm_scale).cpu().numpy()
+
+
+@pytest.mark.parametrize("fmt,rb", [("f16", 48), ("int8", 32), ("f16", 96)])
+@pytest.mark.parametrize("power", [20, 30, 40, 100])
+def test_rows_beside_large_queries(power, fmt, rb):
+    """Ordinary nodes and heads share blocks of 32 rows with bf16 queries 2^power times as large.  The ordinary rows keep
+    the bound of their own scores.  The large rows' softmax is one-hot: what is left is a value's own error, 2^-21."""
+    torch_gpu()
+    lib_ready()
+    host = make_host([600], 4, rb, fmt=fmt)
+    rng = np.random.default_rng(21)
+    cu, parent = make_tree([9], "tree", rng)
+    q, k, v = inputs(host, 9, rng)
+    big = np.zeros((9, 8), bool)
+    big[3:5] = True                                     # whole nodes
+    big[6:, 1::4] = True                                # one head of a group
+    q[big] *= 2.0 ** power
+    announce(f"tree decode rows beside queries of 2^{power} {fmt} {rb}")
+    got = run(host, cu, parent, q, k, v)
+    want, _ = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy())
+    small = q.clone()
+    small[big] = 0.0
+    _, top = reference(host, 0, cu, parent, small.double().numpy(), k.double().numpy(), v.double().numpy())
+    check(got[~big], want[~big], bound(host, top), f"ordinary rows, 2^{power}")
+    check(got[big], want[big], 2.0 ** -21 * 4, f"large rows, 2^{power}")
+
+
+def test_large_queries_of_other_nodes_change_nothing():
+    """Large finite numbers in a sibling's query, in an absent node's and in its child's: the other rows are equal bit by
+    bit."""
+    torch = torch_gpu()
+    lib_ready()
+    host = make_host([333, 70], 4, 48, seed=9)
+    rng = np.random.default_rng(4)
+    cu = np.array([0, 8, 13], dtype=np.int32)
+    parent = np.array([-1, 0, 0, 1, -2, 4, 4, 2] + [-1, 0, 9, 2, 0], dtype=np.int32)
+    q, k, v = inputs(host, 13, rng)
+    want = run(host, cu, parent, q, k, v)
+    other = [3, 4, 5, 6, 10, 11]                        # a leaf, absent nodes and nodes below them
+    rest = [i for i in range(13) if i not in other]
+    for fill in (1e30, -3e38, 1e12, float("inf"), float("nan")):
+        q2 = q.clone()
+        q2[other] = fill
+        announce(f"tree decode, other nodes' queries {fill}")
+        got = run(host, cu, parent, q2, k, v)
+        assert np.array_equal(got[rest], want[rest]), fill
+        assert np.all(got[[4, 5, 6, 10, 11]] == 0), fill
