@@ -24,9 +24,9 @@
 //    drafted nodes, whose masks it derives from the parents.
 //  * tree_merge_kernel joins the partials and applies B^V.
 //
-// Precision: q~ and the probabilities are fp16 pairs (hi + lo, 22 bits), the
-// codes, fp16 coefficients and queries are exact, sums and softmax statistics
-// are float32.  One half alone would cost 2^-11 of a score or probability, fifty
+// Precision: q~ and the probabilities are fp16 pairs (hi + lo, 22 bits), a row's q~
+// scaled to fill them (row_down), the codes, fp16 coefficients and queries are
+// exact, sums and softmax statistics are float32.  One half alone would cost 2^-11 of a score or probability, fifty
 // times what the decode keeps.
 //
 // Measured at 65536 tokens, r_b 48, G 4, 8 KV heads, mean rank 1.9 (110 MB): 64 nodes
@@ -106,9 +106,12 @@ __device__ __forceinline__ uint16_t code_bits(float v) {   // v an int4 code: ex
 __device__ __forceinline__ int key_row(int t) { return 16 * (t >> 4) + 8 * ((t >> 2) & 1) + 4 * ((t >> 3) & 1) + (t & 3); }
 __device__ __forceinline__ int row_token(int r) { return 16 * (r >> 4) + 8 * ((r >> 2) & 1) + 4 * ((r >> 3) & 1) + (r & 3); }
 
-// Binary places by which a row's q~ is scaled down, so that fp16 holds its largest
-// number `big`; a row has its own, and nothing of the rows beside it.
-__device__ __forceinline__ int row_down(float big) { return max(0, __builtin_amdgcn_frexp_expf(big) - 15); }
+// Binary places by which a row's q~ is scaled down, or up where negative, so that
+// its largest number `big` is between 2^14 and 2^15: pairs hold it to 22 bits, and
+// numbers 2^17 times smaller as well.  A row has its own scale, and nothing of
+// the rows beside it.  2^48 is enough: what pairs lose then is below 2^-50 of a
+// score with the largest coefficients.
+__device__ __forceinline__ int row_down(float big) { return max(big > 0.f ? __builtin_amdgcn_frexp_expf(big) - 15 : 0, -48); }
 
 // Place of (channel, token) in the value code tile: a channel's four 8-token
 // pieces are dealt by channel, so that 16 lanes reading the same piece of 16
@@ -585,8 +588,7 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       reinterpret_cast<h4*>(&sm.qt[1][tile / 2][ln])[g & 1] = lo;
     }
   }
-  const float fdn = __builtin_ldexpf(1.f, -row_down(sm.big[col]));
-  const bool scaled = __ballot(fdn != 1.f) != 0;         // the same rows in every wave
+  const bool scaled = __ballot(row_down(sm.big[col]) != 0) != 0;
   uint32_t e0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)f.oa);
   load_entries<NB, C8>(f, sx, lp, j0, e0, lane);
   load_vs<NB, C8>(f, sx, lp, j0, Ti);
@@ -612,12 +614,7 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
     // tile's key coefficients, entries and value coefficients are requested
     // in that order, each once its predecessor's registers are free.
     // ---- basis part of the scores: register 8 u + e is token 16 u + 8 h + e, row col
-    f16v sb, sr = {};
-    {
-      const float c = -m * fdn;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sb[i] = c;
-    }
+    f16v sb = {}, sr = {};
 #pragma unroll
     for (int s = 0; s < NB; ++s) {
       const h8 qh = __builtin_bit_cast(h8, sm.qt[0][s][lane]), ql = __builtin_bit_cast(h8, sm.qt[1][s][lane]);
@@ -727,10 +724,13 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       const u4v kc = *reinterpret_cast<const u4v*>(&w.k[col * kKRow + 16 * s + 8 * h]);
       sr = mfma_q<BF>(kc, sm.qf[s][lane], sr);
     }
-    if (scaled) {
+    if (scaled) {                        // but for zero queries; as a branch it keeps what follows from crowding the products' registers
       const float up = __builtin_ldexpf(1.f, row_down(sm.big[col]));
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sb[i] *= up;
+      for (int i = 0; i < 16; ++i) sb[i] = __builtin_fmaf(sb[i], up, -m);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sb[i] -= m;
     }
 #pragma unroll
     for (int u = 0; u < 2; ++u) {

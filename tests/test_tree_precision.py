@@ -63,3 +63,37 @@ def test_large_queries_of_other_nodes_change_nothing():
         got = run(host, cu, parent, q2, k, v)
         assert np.array_equal(got[rest], want[rest]), fill
         assert np.all(got[[4, 5, 6, 10, 11]] == 0), fill
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int8"])
+@pytest.mark.parametrize("small", ["queries", "sm_scale", "basis rows"])
+@pytest.mark.parametrize("shift", [8, 13])
+def test_small_projections_of_large_coefficients(shift, small, fmt):
+    """Coefficients 2^shift times as large and queries, sm_scale or some rows of the bases so much smaller: the scores stay
+    and so does their bound."""
+    torch_gpu()
+    lib_ready()
+    host = make_host([800, 90], 4, 48, fmt=fmt)
+    rng = np.random.default_rng(33)
+    cu, parent = make_tree([9, 5], "tree", rng)
+    q, k, v = inputs(host, 14, rng)
+    f = 2.0 ** shift
+    rows = slice(16, 32) if small == "basis rows" else slice(0, 48)
+    if fmt == "int8":
+        host.coef_scale_k[:, :, rows.start // 16:rows.stop // 16] *= np.float16(f)
+    else:
+        host.coef_k[..., rows] *= np.float16(f)
+    scale = D ** -0.5
+    if small == "basis rows":
+        host.basis[:, :, :, 0, rows] /= np.float16(f)
+    else:
+        host.res_scale[:, 0] *= np.float16(f)
+        if small == "queries":
+            q /= f
+        else:
+            scale /= f
+    announce(f"tree decode small {small} 2^-{shift} {fmt}")
+    got = run(host, cu, parent, q, k, v, layer=1, sm_scale=scale)
+    want, top = reference(host, 1, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy(), scale=scale)
+    assert 0.5 < top < 20.0
+    check(got, want, bound(host, top), f"small {small} 2^-{shift} {fmt}")
