@@ -601,10 +601,10 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
   for (int k = 0; k < NV; ++k) acc_a[k] = f16v{};
 #pragma unroll
   for (int k = 0; k < D / 32; ++k) acc_r[k] = f16v{};
-  bool first = true;
+  const float inf = __builtin_inff();
+  float lim = -inf;                      // a score past it moves the row's reference; -inf: the row has none yet
   int ex = -24;                          // |s^V| <= 2^ex of the tiles so far
   float exf = __builtin_ldexpf(1.f, -24), exi = __builtin_ldexpf(1.f, 24);
-  const float inf = __builtin_inff();
 
 #pragma unroll 1
   for (int j = wvu; j < ntile; j += NW) {
@@ -761,25 +761,23 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
         }
       }
     }
-    // ---- the reference moves for the first tile and when a score exceeds it by far
+    // ---- a row's reference moves for its first score above -inf, and when one exceeds it by far
     float mx = sb[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sb[i]);
-    if (__ballot(first || mx > kHead)) {
+    if (__ballot(mx > lim)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float by = (first ? mx > -inf : mx > kHead) ? mx - kUp : 0.f;
-      const float fall = first ? 0.f : __builtin_amdgcn_exp2f(-by);
+      const float by = mx > lim ? mx - kUp : 0.f;
+      const float fall = lim > -inf ? __builtin_amdgcn_exp2f(-by) : 1.f;
       m += by;
       l *= fall;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sb[i] -= by;
-      if (!first) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k) acc_a[k] *= fall;
+      for (int k = 0; k < NV; ++k) acc_a[k] *= fall;
 #pragma unroll
-        for (int k = 0; k < D / 32; ++k) acc_r[k] *= fall;
-      }
-      first = false;
+      for (int k = 0; k < D / 32; ++k) acc_r[k] *= fall;
+      if (mx > lim) lim = kHead;
     }
     // ---- probabilities as fp16 pairs, plain and times the value scales; values:
     // channel blocks of the basis, then of the residual
@@ -847,14 +845,14 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
   // ---- join the waves: common reference per row, then sums in wave order -----------
   l += __shfl_xor(l, 32);
   if (h == 0) {
-    sm.m[wv][col] = first ? -inf : m;
+    sm.m[wv][col] = lim > -inf ? m : -inf;
     sm.l[wv][col] = l;
   }
   __syncthreads();                       // the code tiles are done with
   float ms = -inf;
 #pragma unroll
   for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][col]);
-  const float mine = first ? 0.f : __builtin_amdgcn_exp2f(m - ms);
+  const float mine = lim > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.f;
 #pragma unroll
   for (int k = 0; k < D / 32; ++k)
 #pragma unroll

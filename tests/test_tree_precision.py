@@ -6,6 +6,8 @@ import numpy as np
 import pytest
 
 from gpu_util import announce, device_cache, lib_ready, torch_gpu
+import test_tree_decode
+from oracle.factorized import reconstruct
 from test_tree_decode import D, bound, check, inputs, make_host, make_tree, reference
 
 pytestmark = pytest.mark.gpu
@@ -97,3 +99,42 @@ def test_small_projections_of_large_coefficients(shift, small, fmt):
     want, top = reference(host, 1, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy(), scale=scale)
     assert 0.5 < top < 20.0
     check(got, want, bound(host, top), f"small {small} 2^-{shift} {fmt}")
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_scores_of_minus_infinity_leave_the_rest(monkeypatch, dtype, fmt):
+    """The first 400 tokens of a sequence have infinite key scales, which stay with their entries and make their every
+    score -inf; the other tokens' scores and the drafted keys' lie far below zero.  The rows are the attention of what is
+    not -inf, in a sequence of such tokens alone that of the nodes."""
+    torch_gpu()
+    lib_ready()
+    host = make_host([1000, 90], 4, 32, (2,), fmt=fmt, dtype=dtype)
+    rng = np.random.default_rng(17)
+    host.res_val[:, 0] = 0xFF                           # every key code -1
+    host.res_scale[:, 0] = np.float16(4000.0)
+    off = np.zeros(1090, bool)
+    off[:400] = off[1000:] = True
+    cu, parent = make_tree([10, 4], "tree", rng)
+    q, k, v = inputs(host, 14, rng)
+    q = q.abs() + 0.25
+    k[:10] = -60.0
+    finite = reconstruct
+
+    def with_infinite_scales(h, layer, z, head, b):
+        X = finite(h, layer, z, head, b)
+        if z == 0:                                      # from the finite scales' keys
+            t0, t1 = int(host.cu_seqlens[b]), int(host.cu_seqlens[b + 1])
+            for t in np.nonzero(off[t0:t1])[0]:
+                e = int(host.res_off[layer // host.window, head, t0 + t])
+                X[t, host.res_idx[layer, 0, head, e:e + 2]] = -np.inf
+        return X
+    monkeypatch.setattr(test_tree_decode, "reconstruct", with_infinite_scales)
+    want, _ = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy())
+    K = finite(host, 0, 0, 0, 0)[400:]
+    top = max(float(np.abs(K @ q[i, h].double().numpy()).max()) for i in range(10) for h in range(4)) * D ** -0.5 * 1.4427
+    assert np.all(np.isfinite(want)) and 300.0 < top < 6000.0
+    host.res_scale[:, 0, :, off] = np.inf
+    announce(f"tree decode, scores of -inf {fmt} {dtype}")
+    got = run(host, cu, parent, q, k, v, split=1024)
+    check(got, want, bound(host, top), f"scores of -inf {fmt} {dtype}")
