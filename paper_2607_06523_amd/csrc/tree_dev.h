@@ -61,6 +61,8 @@ constexpr int kKRow = D + 8;             // halves per token row of the key code
 constexpr int kWaitVmcnt0 = 0x0F70;      // s_waitcnt immediate: vmcnt(0) only
 constexpr float kUp = 6.0f;              // a moved reference leaves the largest probability at 2^6,
 constexpr float kHead = 14.0f;           // and moves again when one exceeds 2^14: fp16 pairs hold both ends
+constexpr float kFull = 15.5f;           // largest exponent of a scaled residual weight
+constexpr int kMost = 90;                // largest exponent of their scale: 2^90 2^16 2^kFull and its sums stay finite
 
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -123,7 +125,7 @@ __device__ __forceinline__ uint32_t value_place(uint32_t c, uint32_t t) { return
 struct alignas(16) WaveTile {
   uint16_t k[TT * kKRow + 8];            // key codes [token place][channel], zero between tiles
   uint16_t v[D * TT + 8];                // value codes (value_place)
-  float sk[TT], sv[TT];                  // residual scales of the tile's tokens (sv in units of 2^ex)
+  float sk[TT], sv[TT];                  // residual scales of the tile's tokens
   uint8_t mark[128];
 };
 constexpr uint32_t kNoKey = TT * kKRow, kNoValue = D * TT;
@@ -142,7 +144,7 @@ constexpr int kWaves = NB > 4 ? 4 : 8;
 template <int NB, bool C8>
 struct alignas(16) TreeSmem {
   static constexpr int NW = kWaves<NB>;
-  float m[NW][R], l[NW][R];
+  float m[NW][R], l[NW][R];              // statistics; during the tiles m holds a row's largest residual weight
   uint32_t odd[D];                       // channels with entries of value scales that are not finite: bits +inf, -inf, NaN
   float big[R];                          // largest finite |q~| of a row
   alignas(16) uint16_t vs[C8 ? NW : 1][C8 ? NB : 1][C8 ? TT : 8];   // value block scales of a tile (int8)
@@ -603,8 +605,11 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
   for (int k = 0; k < D / 32; ++k) acc_r[k] = f16v{};
   const float inf = __builtin_inff();
   float lim = -inf;                      // a score past it moves the row's reference; -inf: the row has none yet
-  int ex = -24;                          // |s^V| <= 2^ex of the tiles so far
-  float exf = __builtin_ldexpf(1.f, -24), exi = __builtin_ldexpf(1.f, 24);
+  // acc_r is the residual sum times rs, a power of two of the row's own: 2^-ex, or more
+  // where none of the row's weights p |s^V| so far would otherwise reach 4
+  int ex = -24;                          // |s^V| < 2^ex of the tiles so far
+  float exf = __builtin_ldexpf(1.f, -24), rs = __builtin_ldexpf(1.f, kMost);
+  sm.m[wv][col] = 0.f;
 
 #pragma unroll 1
   for (int j = wvu; j < ntile; j += NW) {
@@ -654,12 +659,9 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
     if (__ballot(!odd_v && fabsf(fv) > exf)) {           // rare: larger value scales
       int e = !odd_v && fv != 0.f ? __builtin_amdgcn_frexp_expf(fv) : -24;
       for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
-      const float fall = __builtin_ldexpf(1.f, ex - e);
       ex = e;
       exf = __builtin_ldexpf(1.f, e);
-      exi = __builtin_ldexpf(1.f, -e);
-#pragma unroll
-      for (int k = 0; k < D / 32; ++k) acc_r[k] *= fall;
+      lim = fminf(lim, kFull - (ex + __builtin_amdgcn_frexp_expf(rs) - 1));
     }
     const bool odd = __ballot(odd_k || odd_v) != 0;
     // A key scale that is not finite goes with its entries into the code tile.  A
@@ -667,7 +669,7 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
     // channels end as infinities of their sign or NaN whatever the rest is; they
     // are noted, and left out here.
     w.sk[lane & 31] = odd_k ? a.qscale : fk * a.qscale;
-    w.sv[lane & 31] = odd_v ? 0.f : fv * exi;
+    w.sv[lane & 31] = odd_v ? 0.f : fv;
     // ---- entries into the code tiles, 64 pairs at a time (ranks are even, so a pair belongs to one token)
     const uint32_t e1 = (uint32_t)__builtin_amdgcn_readlane((int)ob, 31);
     const uint32_t np = e1 > en ? min(e1 - en, (uint32_t)(TT * D)) / 2 : 0u;
@@ -761,13 +763,16 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
         }
       }
     }
-    // ---- a row's reference moves for its first score above -inf, and when one exceeds it by far
+    // ---- a row's reference moves for its first score above -inf, and when one exceeds it
+    // by far; the scale of its residual weights follows, also where a score allows a
+    // weight that would exceed fp16's range
     float mx = sb[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, sb[i]);
     if (__ballot(mx > lim)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float by = mx > lim ? mx - kUp : 0.f;
+      const bool past = mx > lim;
+      const float by = past && (lim == -inf || mx > kHead) ? mx - kUp : 0.f;
       const float fall = lim > -inf ? __builtin_amdgcn_exp2f(-by) : 1.f;
       m += by;
       l *= fall;
@@ -775,9 +780,30 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       for (int i = 0; i < 16; ++i) sb[i] -= by;
 #pragma unroll
       for (int k = 0; k < NV; ++k) acc_a[k] *= fall;
+      float top = 0.f;
+      int at = 8 * h;
+      asm("" : "+v"(at));                // what follows is computed here and again below: kept, it has no registers
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) acc_r[k] *= fall;
-      if (mx > lim) lim = kHead;
+      for (int q = 0; q < 4; ++q) {
+        const f4 s = *reinterpret_cast<const f4*>(&w.sv[at + 16 * (q >> 1) + 4 * (q & 1)]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = sb[4 * q + i];
+          asm("" : "+v"(x));
+          top = fmaxf(top, __builtin_amdgcn_exp2f(x) * fabsf(s[i]));
+        }
+      }
+      top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), sm.m[wv][col] * fall);
+      const int was = __builtin_amdgcn_frexp_expf(rs) - 1;
+      const int er = !past ? was : top > 0.f ? min(max(-ex, 3 - __builtin_amdgcn_frexp_expf(top)), kMost) : kMost;
+      const float g = __builtin_ldexpf(fall, er - was);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) acc_r[k] *= g;
+      if (past) {
+        rs = __builtin_ldexpf(1.f, er);
+        lim = fminf(kHead, kFull - (ex + er));
+        sm.m[wv][col] = top;
+      }
     }
     // ---- probabilities as fp16 pairs, plain and times the value scales; values:
     // channel blocks of the basis, then of the residual
@@ -789,7 +815,7 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const float v0 = __builtin_amdgcn_exp2f(sb[8 * u + e]), v1 = __builtin_amdgcn_exp2f(sb[8 * u + e + 1]);
-        const float x0 = e < 4 ? s0[e & 3] : s1[e & 3], x1 = e < 4 ? s0[(e & 3) + 1] : s1[(e & 3) + 1];
+        const float x0 = (e < 4 ? s0[e & 3] : s1[e & 3]) * rs, x1 = (e < 4 ? s0[(e & 3) + 1] : s1[(e & 3) + 1]) * rs;
         sum[0] += v0;
         sum[1] += v1;
         uint32_t hi, lo;
@@ -852,13 +878,13 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
   float ms = -inf;
 #pragma unroll
   for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][col]);
-  const float mine = lim > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.f;
+  const float mine = lim > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.f, unit = __builtin_ldexpf(1.f, 1 - __builtin_amdgcn_frexp_expf(rs));
 #pragma unroll
   for (int k = 0; k < D / 32; ++k)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       *reinterpret_cast<f4*>(&sm.acc[wv][col][32 * k + 8 * q + 4 * h]) =
-          f4{acc_r[k][4 * q], acc_r[k][4 * q + 1], acc_r[k][4 * q + 2], acc_r[k][4 * q + 3]} * (mine * exf);
+          f4{acc_r[k][4 * q], acc_r[k][4 * q + 1], acc_r[k][4 * q + 2], acc_r[k][4 * q + 3]} * (mine * unit);
   __syncthreads();
   for (int i = threadIdx.x; i < R * (D / 4); i += 64 * NW) {
     const int r = i / (D / 4), c = 4 * (i % (D / 4));

@@ -138,3 +138,31 @@ def test_scores_of_minus_infinity_leave_the_rest(monkeypatch, dtype, fmt):
     announce(f"tree decode, scores of -inf {fmt} {dtype}")
     got = run(host, cu, parent, q, k, v, split=1024)
     check(got, want, bound(host, top), f"scores of -inf {fmt} {dtype}")
+
+
+@pytest.mark.parametrize("fmt,rb", [("f16", 48), ("int8", 32), ("f16", 112)])
+@pytest.mark.parametrize("place", [3, 500, 890])
+def test_large_value_scale_of_a_token_not_attended_to(place, fmt, rb):
+    """One token's value scale is 2^25 times the others', which are all that most rows attend to (its probability is below
+    2^-50 there); the values are residuals alone.  Two nodes attend to that token instead."""
+    torch = torch_gpu()
+    lib_ready()
+    host = make_host([900, 70], 4, rb, (4, 16), fmt=fmt)
+    rng = np.random.default_rng(place)
+    host.coef_v[...] = 0
+    host.res_scale[:, 1] = (rng.uniform(0.5, 1.0, host.res_scale[:, 1].shape) * 2.0 ** -10).astype(np.float16)
+    cu, parent = make_tree([10, 4], "tree", rng)
+    q, k, v = inputs(host, 14, rng, amp=0.1)
+    v *= 2.0 ** -10
+    for h in range(2):
+        K = reconstruct(host, 0, 0, h, 0)[place]
+        host.res_scale[0, 1, h, place] = 2.0 ** 15
+        away = torch.from_numpy(K * (50.0 / (D ** -0.5 * 1.4427 * (K @ K)))).float()
+        q[:10, 4 * h:4 * h + 4] -= away.to(q.dtype)
+        q[[2, 7], 4 * h:4 * h + 4] += (2 * away).to(q.dtype)
+        k[:10, h] = torch.from_numpy(K).half()          # the drafted keys are not looked at either
+    announce(f"tree decode, a large value scale at {place} {fmt} {rb}")
+    got = run(host, cu, parent, q, k, v)
+    want, top = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy())
+    assert top < 100.0 and np.abs(want[[0, 1, 3, 4]]).max() < 1.0 < np.abs(want[[2, 7]]).max()
+    check(got, want, bound(host, top), f"value scale at {place} {fmt} {rb}")
