@@ -24,9 +24,9 @@
 //    drafted nodes, whose masks it derives from the parents.
 //  * tree_merge_kernel joins the partials and applies B^V.
 //
-// Precision: q~ and the probabilities are fp16 pairs (hi + lo, 22 bits), a row's q~
-// scaled to fill them (row_down), the codes, fp16 coefficients and queries are
-// exact, sums and softmax statistics are float32.  One half alone would cost 2^-11 of a score or probability, fifty
+// Precision: q~, the probabilities and their products with the value scales are fp16
+// pairs (hi + lo, 22 bits) in units of the row's own (row_down, kUp, rs); the codes,
+// fp16 coefficients and queries are exact, sums and softmax statistics are float32.  One half alone would cost 2^-11 of a score or probability, fifty
 // times what the decode keeps.
 //
 // Measured at 65536 tokens, r_b 48, G 4, 8 KV heads, mean rank 1.9 (110 MB): 64 nodes
@@ -59,8 +59,12 @@ constexpr int TT = kTreeTile;            // tokens per tile
 constexpr int R = kTreeRows;             // rows of a workgroup
 constexpr int kKRow = D + 8;             // halves per token row of the key code tile (16-byte pad: no bank conflicts)
 constexpr int kWaitVmcnt0 = 0x0F70;      // s_waitcnt immediate: vmcnt(0) only
-constexpr float kUp = 6.0f;              // a moved reference leaves the largest probability at 2^6,
-constexpr float kHead = 14.0f;           // and moves again when one exceeds 2^14: fp16 pairs hold both ends
+// A moved reference leaves the largest probability at 2^kUp and moves again when one
+// exceeds 2^kHead, the most that fp16 holds: 22 bits down to 2^-12 of the largest,
+// below it a grid of 2^-33 of the largest.  With 12 for kUp references move often
+// enough to cost 3 to 6% (16 int8 sequences 219 us, 208 at 9 and at 6).
+constexpr float kUp = 9.0f;
+constexpr float kHead = 15.5f;
 constexpr float kFull = 15.5f;           // largest exponent of a scaled residual weight
 constexpr int kMost = 90;                // largest exponent of their scale: 2^90 2^16 2^kFull and its sums stay finite
 
@@ -345,14 +349,16 @@ __device__ __forceinline__ void draft_item(const TreeArgs& a, const Item& it, Dr
   }
 }
 
-// Two values as fp16 pairs, rounded towards zero: hi and lo halves.  v - hi is
-// exact; the mixed-precision fma takes hi as it is packed.
+// Two values as fp16 pairs, hi and lo halves, rounded to nearest: on fp16's grid of
+// 2^-24 the error then has no direction, and sums of many do not drift.  v - hi is
+// exact; the mixed-precision fma takes hi as it is packed (its forms that round to
+// fp16 would save one instruction in four and took 3% longer).
 __device__ __forceinline__ void pair2(float v0, float v1, uint32_t& hi, uint32_t& lo) {
-  hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(v0, v1));
+  hi = __builtin_bit_cast(uint32_t, h2{(_Float16)v0, (_Float16)v1});
   float d0, d1;
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d0) : "v"(hi), "v"(v0));
   asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d1) : "v"(hi), "v"(v1));
-  lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(d0, d1));
+  lo = __builtin_bit_cast(uint32_t, h2{(_Float16)d0, (_Float16)d1});
 }
 
 // Eight int8 coefficients with their scales in pairs, code * scale = hi + lo exactly:
@@ -772,7 +778,8 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
     if (__ballot(mx > lim)) {
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       const bool past = mx > lim;
-      const float by = past && (lim == -inf || mx > kHead) ? mx - kUp : 0.f;
+      float by = past && (lim == -inf || mx > kHead) ? mx - kUp : 0.f;
+      by = mx - by > kHead ? mx : by;    // scores of 2^27 and more come in steps beyond kUp
       const float fall = lim > -inf ? __builtin_amdgcn_exp2f(-by) : 1.f;
       m += by;
       l *= fall;

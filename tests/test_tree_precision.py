@@ -166,3 +166,36 @@ def test_large_value_scale_of_a_token_not_attended_to(place, fmt, rb):
     want, top = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy())
     assert top < 100.0 and np.abs(want[[0, 1, 3, 4]]).max() < 1.0 < np.abs(want[[2, 7]]).max()
     check(got, want, bound(host, top), f"value scale at {place} {fmt} {rb}")
+
+
+@pytest.mark.parametrize("rb", [16, 96])
+@pytest.mark.parametrize("gap", [10, 18])
+def test_probabilities_far_below_the_largest(gap, rb):
+    """Tokens with empty values take most of the attention, in the first tile of every wave of one chunk; the other 16384
+    tokens' probabilities are 2^-gap of theirs, and the row is theirs.  Scores are one product each, so the bound is
+    tighter than random scores': S is kept to 2^-22 of 18 (3e-6 of a probability), float32 sums of 16384 terms of either
+    sign to sqrt(16384) 2^-24 (7.6e-6), the 128 additions of a lane's sum of probabilities to 2^-17 (7.6e-6), and a
+    probability of 2^-9, 18 binades below the largest, to 2^-25 / sqrt(3) of either sign (8.8e-6 of it): together 2.7e-5,
+    below 2^-15."""
+    torch = torch_gpu()
+    lib_ready()
+    T = 16384
+    host = make_host([T], 4, rb, (0,))
+    rng = np.random.default_rng(gap)
+    host.basis[:, :, :, 0] = 0
+    host.basis[:, :, :, 0, 0, 0] = 1
+    host.coef_k[...] = 0
+    host.coef_k[..., 0] = rng.uniform(0.0, 0.5, host.coef_k.shape[:-1])
+    sinks = np.arange(0, 256, 32)
+    host.coef_k[:, :, sinks, 0] = 32
+    host.coef_v[:, :, sinks // 16, :, sinks % 16] = 0
+    cu, parent = make_tree([3], "tree", rng)
+    q, k, v = inputs(host, 3, rng)
+    q[...] = 0
+    q[..., 0] = 1
+    k[...] = 0
+    scale = gap * np.log(2.0) / 32
+    announce(f"tree decode, probabilities 2^-{gap} of the largest, r_b {rb}")
+    got = run(host, cu, parent, q, k, v, split=T, sm_scale=scale)
+    want, _ = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy(), scale=scale)
+    check(got, want, 2.0 ** -15, f"probabilities 2^-{gap} of the largest, r_b {rb}")
