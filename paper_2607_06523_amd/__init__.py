@@ -239,9 +239,13 @@ class DeviceCache:
                     n_q_heads: int, levels, coef_scale_k=None, coef_scale_v=None, coef_format: str = "f16",
                     q_dtype: str = "bf16", split_tokens: int = 0):
         """A cache over device tensors that are in the C ABI's layouts already
-        (include/dwkv.h, dwkv_cache); they are used in place.  res_off is int32
-        bits; cu_seqlens [B+1] is a host array.  Such a cache holds no queries."""
+        (include/dwkv.h, dwkv_cache); they are used in place.  coef_format is "f16"
+        or "int8".  Tensors have the layouts' types or are integers of their
+        bits (res_off: int32); cu_seqlens [B+1] is a host array.  Such a cache holds
+        no queries."""
         import torch
+        if coef_format not in ("f16", "int8"):
+            raise ValueError(f'coef_format must be "f16" or "int8", not {coef_format!r}')
         self = cls.__new__(cls)
         self.torch, self.lib, self.device = torch, binding.load(), basis.device
         self.coef_format, self.q_dtype, self.q = coef_format, q_dtype, None
@@ -253,17 +257,20 @@ class DeviceCache:
         self.basis_rank, self.res_stride = int(basis.shape[-2]), int(res_idx.shape[-1])
         L, H, T, rb, M = self.n_layers, self.n_kv_heads, self.total_tokens, self.basis_rank, self.n_layers // self.window
         T16, i8 = -(-T // 16) * 16, coef_format == "int8"
-        want = {"basis": (basis, self.batch * M * H * 2 * rb * self.head_dim, 2), "coef_k": (coef_k, L * H * T16 * rb, 1 if i8 else 2),
-                "coef_v": (coef_v, L * H * T16 * rb, 1 if i8 else 2), "rank_code": (rank_code, M * H * T, 1),
-                "res_off": (res_off, M * H * (T + 1), 4), "res_idx": (res_idx, L * 2 * H * self.res_stride, 1),
-                "res_val": (res_val, L * 2 * H * (self.res_stride // 2), 1), "res_scale": (res_scale, L * 2 * H * T, 2)}
+        byte, half = (torch.uint8, torch.int8), (torch.float16, torch.int16, torch.uint16)
+        word, coef = (torch.int32, torch.uint32), byte if i8 else half
+        want = {"basis": (basis, self.batch * M * H * 2 * rb * self.head_dim, half), "coef_k": (coef_k, L * H * T16 * rb, coef),
+                "coef_v": (coef_v, L * H * T16 * rb, coef), "rank_code": (rank_code, M * H * T, byte),
+                "res_off": (res_off, M * H * (T + 1), word), "res_idx": (res_idx, L * 2 * H * self.res_stride, byte),
+                "res_val": (res_val, L * 2 * H * (self.res_stride // 2), byte), "res_scale": (res_scale, L * 2 * H * T, half)}
         if i8:
-            want.update(coef_scale_k=(coef_scale_k, L * H * (rb // 16) * T, 2), coef_scale_v=(coef_scale_v, L * H * (rb // 16) * T, 2))
+            want.update(coef_scale_k=(coef_scale_k, L * H * (rb // 16) * T, half),
+                        coef_scale_v=(coef_scale_v, L * H * (rb // 16) * T, half))
         else:
             coef_scale_k = coef_scale_v = None
-        for name, (x, n, size) in want.items():
-            if x is None or x.numel() != n or x.element_size() != size or not x.is_contiguous() or x.device != self.device:
-                raise ValueError(f"{name} must be a contiguous tensor of {n} elements of {size} bytes on {self.device}")
+        for name, (x, n, types) in want.items():
+            if x is None or x.numel() != n or x.dtype not in types or not x.is_contiguous() or x.device != self.device:
+                raise ValueError(f"{name} must be a contiguous {types[0]} tensor of {n} elements on {self.device}")
         self.basis, self.coef_k, self.coef_v = basis, coef_k, coef_v
         self.coef_scale_k, self.coef_scale_v = coef_scale_k, coef_scale_v
         self.rank_code, self.res_off, self.res_idx, self.res_val, self.res_scale = rank_code, res_off, res_idx, res_val, res_scale
