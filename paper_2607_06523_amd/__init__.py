@@ -132,7 +132,7 @@ class DraftTree:
         import torch
         if parent.dtype != torch.int32 or parent.dim() != 1 or not parent.is_contiguous():
             raise TypeError("parent must be a contiguous int32 vector")
-        self.cu_host = np.ascontiguousarray(cu_nodes, dtype=np.int32)
+        self.cu_host = np.array(cu_nodes, dtype=np.int32, order="C")    # a copy: the caller's array may change, the device's does not
         if self.cu_host.ndim != 1 or len(self.cu_host) < 2 or int(self.cu_host[-1]) != parent.numel():
             raise ValueError("cu_nodes must be [B+1] and end at the number of nodes")
         self.parent = parent
@@ -220,7 +220,7 @@ class DeviceCache:
         self.q_dtype = host.q_dtype
         qdt = torch.float16 if host.q_dtype == "f16" else torch.bfloat16
         self.q = up(host.q_bits.view(np.int16), torch.int16).view(qdt)
-        self.cu_host = np.ascontiguousarray(host.cu_seqlens, dtype=np.int32)
+        self.cu_host = np.array(host.cu_seqlens, dtype=np.int32, order="C")   # a copy, as the device's
         self.cu = torch.from_numpy(self.cu_host).to(dev)
         self.batch = len(self.cu_host) - 1
         self.n_layers = host.n_layers
@@ -249,7 +249,7 @@ class DeviceCache:
         self = cls.__new__(cls)
         self.torch, self.lib, self.device = torch, binding.load(), basis.device
         self.coef_format, self.q_dtype, self.q = coef_format, q_dtype, None
-        self.cu_host = np.ascontiguousarray(cu_seqlens, dtype=np.int32)
+        self.cu_host = np.array(cu_seqlens, dtype=np.int32, order="C")  # a copy, as the device's
         self.cu = torch.from_numpy(self.cu_host).to(self.device)
         self.batch, self.total_tokens = len(self.cu_host) - 1, int(self.cu_host[-1])
         self.window, self.levels, self.n_q_heads = int(window), tuple(int(x) for x in levels), int(n_q_heads)

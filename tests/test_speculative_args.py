@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2607_06523_amd import DeviceCache
+from paper_2607_06523_amd import DeviceCache, DraftTree
 from test_speculative_cpu import a_cache
 
 
@@ -48,3 +48,27 @@ def test_caches_of_the_types_or_their_bits_are_taken():
             assert dc.coef_k.data_ptr() == b["coef_k"].data_ptr()
             new = dc.empty_like([4, 9])
             assert new.coef_format == dc.coef_format and np.array_equal(new.cu_host, [0, 4, 13])
+
+
+def test_trees_and_caches_keep_their_own_starts():
+    """A program refills its arrays for the next step: the handles' host sides stay with their device sides."""
+    cu, parent = np.array([0, 3, 7], np.int32), torch.tensor([-1, 0, 1, -1, 0, 0, 2], dtype=torch.int32)
+    tree = DraftTree(cu, parent)
+    lens = np.array([0, 5, 8], np.int32)
+    dc = DeviceCache.from_device(**{**a_cache((5, 3)), "cu_seqlens": lens})
+    cu[1], lens[1] = 1, 2
+    for x, want in ((tree, [0, 3, 7]), (dc, [0, 5, 8])):
+        assert x.cu.tolist() == want and x.cu_host.tolist() == want
+    assert tree.cstruct.cu_nodes_host[:3] == [0, 3, 7] and dc.dims.cu_seqlens_host[:3] == [0, 5, 8]
+    dc.set_split(64)
+    assert dc.dims.cu_seqlens_host[:3] == [0, 5, 8]
+
+
+def test_host_caches_keep_their_own_starts():
+    from synth import TINY, generate
+    host = generate(TINY, threads=2)
+    want = host.cu_seqlens = np.array(host.cu_seqlens, dtype=np.int32)
+    dc = DeviceCache(host, device="cpu")
+    want = want.copy()
+    host.cu_seqlens[1:] -= 1
+    assert np.array_equal(dc.cu_host, want) and dc.cu.tolist() == want.tolist()
