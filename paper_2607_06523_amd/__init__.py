@@ -377,13 +377,19 @@ class DeviceCache:
         return ws
 
     # -- calls -----------------------------------------------------------------------
+    def _query(self, layer: int, q):
+        if q is not None:
+            return q
+        if self.q is None:
+            raise ValueError("this cache holds no queries: q must be given")
+        return self.q[layer]
+
     def decode(self, layer: int, q=None, sm_scale: float | None = None, probe: ProbeRef | None = None,
                out=None, workspace=None, with_ref: bool = True, err=None):
         """Per-layer decode attention; returns out [B,Hq,d] fp32, or
         (out, err [B, n*G], out_ref [B, n*G, d]) with a probe (err may be given)."""
         torch = self.torch
-        if q is None:
-            q = self.q[layer]
+        q = self._query(layer, q)
         qt = F16 if q.dtype == torch.float16 else BF16
         if q.dtype not in (torch.float16, torch.bfloat16):
             raise TypeError("q must be float16 or bfloat16")
@@ -413,8 +419,7 @@ class DeviceCache:
         workspace); out [B,Hq,d] fp32 (and err [B, n*G] with a probe) must be
         given or are allocated here by torch.  Returns out, or (out, err)."""
         torch = self.torch
-        if q is None:
-            q = self.q[layer]
+        q = self._query(layer, q)
         if q.dtype not in (torch.float16, torch.bfloat16):
             raise TypeError("q must be float16 or bfloat16")
         qt = F16 if q.dtype == torch.float16 else BF16
@@ -435,8 +440,7 @@ class DeviceCache:
         """First half of decode: the split-K pass(es); dwkv_decode_merge finishes it
         (with the same probe and err)."""
         torch = self.torch
-        if q is None:
-            q = self.q[layer]
+        q = self._query(layer, q)
         qt = F16 if q.dtype == torch.float16 else BF16
         p, keep = self._probe_struct(probe, err, None)
         ws = workspace if workspace is not None else self.workspace(probe)
@@ -540,8 +544,7 @@ class DeviceCache:
                 raise TypeError("x_k / x_v must be contiguous float16")
         if gate is not None and (gate.dtype != torch.float32 or not gate.is_contiguous()):
             raise TypeError("gate must be contiguous float32")
-        if q is None:
-            q = self.q[layer]
+        q = self._query(layer, q)
         if q.dtype not in (torch.float16, torch.bfloat16):
             raise TypeError("q must be float16 or bfloat16")
         qt = F16 if q.dtype == torch.float16 else BF16
@@ -566,8 +569,7 @@ class DeviceCache:
         """dwkv_decode plus the router's attention features: phi fp32 [M, Hkv, T, 4]
         (columns 0 mass, 1 spike) is updated in place; returns out [B, Hq, d]."""
         torch = self.torch
-        if q is None:
-            q = self.q[layer]
+        q = self._query(layer, q)
         qt = F16 if q.dtype == torch.float16 else BF16
         if out is None:
             out = torch.empty((self.batch, self.n_q_heads, self.head_dim), dtype=torch.float32, device=self.device)

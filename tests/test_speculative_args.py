@@ -72,3 +72,13 @@ def test_host_caches_keep_their_own_starts():
     want = want.copy()
     host.cu_seqlens[1:] -= 1
     assert np.array_equal(dc.cu_host, want) and dc.cu.tolist() == want.tolist()
+
+
+def test_caches_without_queries_say_so():
+    x = torch.zeros((1, 2, 128), dtype=torch.float16)
+    dc = DeviceCache.from_device(**a_cache())
+    for cache in (dc, dc.empty_like([7])):
+        for call in (lambda: cache.decode(0), lambda: cache.decode_noalloc(0), lambda: cache.decode_partials(0),
+                     lambda: cache.decode_append(0, x, x), lambda: cache.decode_features(0, None)):
+            with pytest.raises(ValueError, match="holds no queries"):
+                call()
