@@ -649,7 +649,8 @@ class DeviceCache:
         if q.shape != (N, Hq, d) or k_new.shape != (N, Hk, d) or v_new.shape != (N, Hk, d):
             raise ValueError("q must be [N, Hq, d], k_new and v_new [N, Hkv, d]")
         qs, ks, vs = q.stride(), k_new.stride(), v_new.stride()
-        if N > 0 and not qs[1:] == ks[1:] == vs[1:] == (d, 1):
+        if N > 0 and not qs[1:] == ks[1:] == vs[1:] == (d, 1) and any(
+                x.stride(2) != 1 or x.shape[1] > 1 and x.stride(1) != d for x in (q, k_new, v_new)):   # one head has no stride
             raise ValueError("the rows of q, k_new and v_new must have no gaps inside")
         if N > 1 and ks[0] != vs[0]:
             raise ValueError("k_new and v_new must have the same row stride")

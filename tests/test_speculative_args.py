@@ -82,3 +82,21 @@ def test_caches_without_queries_say_so():
                      lambda: cache.decode_append(0, x, x), lambda: cache.decode_features(0, None)):
             with pytest.raises(ValueError, match="holds no queries"):
                 call()
+
+
+def test_one_head_has_no_stride():
+    """[1, N, d] turned to [N, 1, d] is contiguous, whatever stride its one head carries."""
+    u8 = lambda *s: torch.zeros(s, dtype=torch.uint8)
+    f16 = lambda *s: torch.zeros(s, dtype=torch.float16)
+    dc = DeviceCache.from_device(basis=f16(1, 1, 1, 2, 16, 128), coef_k=f16(2, 1, 16, 16), coef_v=f16(2, 1, 16, 16), rank_code=u8(1, 1, 5),
+                                 res_off=torch.zeros((1, 1, 6), dtype=torch.int32), res_idx=u8(2, 2, 1, 1024), res_val=u8(2, 2, 1, 512),
+                                 res_scale=f16(2, 2, 1, 5), cu_seqlens=[0, 5], window=2, n_q_heads=1, levels=(0, 2))
+    tree = DraftTree([0, 3], torch.tensor([-1, 0, 1], dtype=torch.int32))
+    one = f16(1, 3, 128).transpose(0, 1)
+    assert one.is_contiguous() and one.stride(1) != 128
+    with pytest.raises(ValueError, match="device"):     # past the strides: nothing of it is on a GPU
+        dc.tree_decode(0, tree, one, one, one)
+    gaps = f16(3, 1, 256)[:, :, ::2]
+    for args in ((gaps, one, one), (one, gaps, one), (one, one, gaps)):
+        with pytest.raises(ValueError, match="gaps"):
+            dc.tree_decode(0, tree, *args)
