@@ -407,7 +407,7 @@ struct VerifyArgs {
   int32_t* path;
   int32_t* n_kept;
   int32_t* next;
-  double* z;                   // [N][max_children][zblk] partial sums of Z_k (k >= 1)
+  double* z;                   // [N][max_children - 1][zblk] partial sums of Z_k, k = 1 .. max_children - 1
   double* sum;                 // [B][nblk] sums of r over chunks of the last row
   struct VerifyEnd* end;       // [B] the node the walk ends at
   int32_t batch, n_nodes, vocab, p_type, max_children, zblk, nblk;

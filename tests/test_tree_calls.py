@@ -26,3 +26,43 @@ def test_one_kv_head_from_a_turned_tensor(G):
     got = device_cache(host).tree_decode(1, DraftTree(cu, torch.from_numpy(parent).cuda()), q, k, v).cpu().numpy()
     want, top = reference(host, 1, cu, parent, *(x.cpu().double().numpy() for x in (q, k, v)))
     check(got, want, bound(host, top), f"one KV head, G {G}")
+
+
+def test_a_graph_and_other_verifications_share_a_workspace():
+    """Between the replays of a captured call with a draft its workspace serves a call without one and one of another
+    tree, whose parts lie elsewhere in it: each gives the definition's outputs, each time."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import DraftTree, tree_verify, tree_verify_workspace
+    rng = np.random.default_rng(41)
+    sets = [make_drafts([20, 9], 3001, rng, 3, True), make_drafts([33, 1, 6], 3001, rng, 5, True)]
+    trees = [DraftTree(a[0], torch.from_numpy(a[1]).cuda()) for a in sets]
+    ws = max((tree_verify_workspace(t, 3001, n) for t, n in zip(trees, (3, 5))), key=lambda w: w.numel())
+    ws.fill_(0xFF)
+    gpu = [[x.cuda() if hasattr(x, "cuda") else torch.from_numpy(x).cuda() for x in a[2:]] for a in sets]
+
+    def call(i, children, draft):
+        token, target, q, u, un = gpu[i]
+        return tree_verify(trees[i], token, target, u, un, draft=q if draft else None, max_children=children, workspace=ws)
+
+    def want(i, children, draft):
+        cu, parent, token, target, q, _, _ = sets[i]
+        u, un = (x.cpu().numpy() for x in gpu[i][3:])
+        out = verify_reference(cu, parent, token, target.double().numpy(), q.double().numpy() if draft else None, u, un, children)
+        assert out[3] > 1e-12
+        return out[:3]
+    announce("tree verify, a graph and other calls in one workspace")
+    call(0, 3, True)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = call(0, 3, True)
+    for step in range(4):
+        for i in range(2):
+            for x in gpu[i][3:]:
+                x.copy_(torch.from_numpy(np.minimum(rng.random(x.numel()).astype(np.float32), 0.9999999)))
+        graph.replay()
+        got = [(captured, (0, 3, True)), (call(0, 2, False), (0, 2, False)), (call(1, 5, True), (1, 5, True))]
+        torch.cuda.synchronize()
+        for out, args in got:
+            for a, b in zip(out, want(*args)):
+                assert np.array_equal(a.cpu().numpy(), b), (step, args)
