@@ -877,15 +877,16 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
 
   // ---- join the waves: common reference per row, then sums in wave order -----------
   l += __shfl_xor(l, 32);
+  const bool none = lim == -inf && l == 0.f;   // no score above -inf, nor one that is no number
   if (h == 0) {
-    sm.m[wv][col] = lim > -inf ? m : -inf;
+    sm.m[wv][col] = none ? -inf : m;
     sm.l[wv][col] = l;
   }
   __syncthreads();                       // the code tiles are done with
   float ms = -inf;
 #pragma unroll
   for (int u = 0; u < NW; ++u) ms = fmaxf(ms, sm.m[u][col]);
-  const float mine = lim > -inf ? __builtin_amdgcn_exp2f(m - ms) : 0.f, unit = __builtin_ldexpf(1.f, 1 - __builtin_amdgcn_frexp_expf(rs));
+  const float mine = none ? 0.f : __builtin_amdgcn_exp2f(m - ms), unit = __builtin_ldexpf(1.f, 1 - __builtin_amdgcn_frexp_expf(rs));
 #pragma unroll
   for (int k = 0; k < D / 32; ++k)
 #pragma unroll

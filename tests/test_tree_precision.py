@@ -199,3 +199,22 @@ def test_probabilities_far_below_the_largest(gap, rb):
     got = run(host, cu, parent, q, k, v, split=T, sm_scale=scale)
     want, _ = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy(), scale=scale)
     check(got, want, 2.0 ** -15, f"probabilities 2^-{gap} of the largest, r_b {rb}")
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int8"])
+def test_scores_that_are_no_numbers_reach_their_rows(fmt):
+    """A key that is no number, as a sequence's one token and among others: every row of its sequence is no number, and no
+    other row."""
+    torch_gpu()
+    lib_ready()
+    host = make_host([1, 40, 700, 33], 4, 32, (0, 8), fmt=fmt)
+    for t in (0, 1 + 40 + 300):
+        (host.coef_scale_k[:, :, 0] if fmt == "int8" else host.coef_k[..., 0])[..., t] = np.nan
+    rng = np.random.default_rng(3)
+    cu, parent = make_tree([3, 5, 9, 4], "tree", rng)
+    q, k, v = inputs(host, 21, rng)
+    announce(f"tree decode, keys that are no numbers {fmt}")
+    got = run(host, cu, parent, q, k, v)
+    bad = np.zeros(21, bool)
+    bad[:3] = bad[8:17] = True
+    assert np.all(np.isnan(got[bad])) and np.all(np.isfinite(got[~bad]))
