@@ -66,7 +66,8 @@ constexpr int kWaitVmcnt0 = 0x0F70;      // s_waitcnt immediate: vmcnt(0) only
 constexpr float kUp = 9.0f;
 constexpr float kHead = 15.5f;
 constexpr float kFull = 15.5f;           // largest exponent of a scaled residual weight
-constexpr int kMost = 90;                // largest exponent of their scale: 2^90 2^16 2^kFull and its sums stay finite
+constexpr int kMost = 40;                // largest exponent of their scale: also that of rows without one
+constexpr int kNoScale = -64;            // ex before the first value scale: lim is kHead then, whatever rs is
 
 __device__ __forceinline__ void wave_lds_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -612,10 +613,11 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
   const float inf = __builtin_inff();
   float lim = -inf;                      // a score past it moves the row's reference; -inf: the row has none yet
   // acc_r is the residual sum times rs, a power of two of the row's own: 2^-ex, or more
-  // where none of the row's weights p |s^V| so far would otherwise reach 4
-  int ex = -24;                          // |s^V| < 2^ex of the tiles so far
-  float exf = __builtin_ldexpf(1.f, -24), rs = __builtin_ldexpf(1.f, kMost);
+  // where the row's largest weight p |s^V| so far (in sm.m) would not reach 1/4 with it
+  int ex = kNoScale;                     // |s^V| < 2^ex of the tiles so far
+  float exf = __builtin_ldexpf(1.f, kNoScale), rs = __builtin_ldexpf(1.f, kMost);
   sm.m[wv][col] = 0.f;
+  const auto unit_of = [&](float top) { return top > 0.f ? min(max(-ex, -1 - __builtin_amdgcn_frexp_expf(top)), kMost) : kMost; };
 
 #pragma unroll 1
   for (int j = wvu; j < ntile; j += NW) {
@@ -663,11 +665,16 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
     const float fk = own ? half_bits_to_float((uint16_t)sk) : 0.f, fv = own ? half_bits_to_float((uint16_t)sv) : 0.f;
     const bool odd_k = !(fabsf(fk) < inf), odd_v = !(fabsf(fv) < inf);
     if (__ballot(!odd_v && fabsf(fv) > exf)) {           // rare: larger value scales
-      int e = !odd_v && fv != 0.f ? __builtin_amdgcn_frexp_expf(fv) : -24;
+      int e = !odd_v && fv != 0.f ? __builtin_amdgcn_frexp_expf(fv) : kNoScale;
       for (int d = 32; d; d >>= 1) e = max(e, __shfl_xor(e, d));
       ex = e;
       exf = __builtin_ldexpf(1.f, e);
-      lim = fminf(lim, kFull - (ex + __builtin_amdgcn_frexp_expf(rs) - 1));
+      const int er = unit_of(sm.m[wv][col]);
+      const float g = __builtin_ldexpf(1.f, er + 1 - __builtin_amdgcn_frexp_expf(rs));
+      rs *= g;
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) acc_r[k] *= g;
+      if (lim > -inf) lim = fminf(kHead, kFull - (ex + er));
     }
     const bool odd = __ballot(odd_k || odd_v) != 0;
     // A key scale that is not finite goes with its entries into the code tile.  A
@@ -785,8 +792,6 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       l *= fall;
 #pragma unroll
       for (int i = 0; i < 16; ++i) sb[i] -= by;
-#pragma unroll
-      for (int k = 0; k < NV; ++k) acc_a[k] *= fall;
       float top = 0.f;
       int at = 8 * h;
       asm("" : "+v"(at));                // what follows is computed here and again below: kept, it has no registers
@@ -801,11 +806,16 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
         }
       }
       top = fmaxf(fmaxf(top, __shfl_xor(top, 32)), sm.m[wv][col] * fall);
-      const int was = __builtin_amdgcn_frexp_expf(rs) - 1;
-      const int er = !past ? was : top > 0.f ? min(max(-ex, 3 - __builtin_amdgcn_frexp_expf(top)), kMost) : kMost;
+      const int was = __builtin_amdgcn_frexp_expf(rs) - 1, er = past ? unit_of(top) : was;
       const float g = __builtin_ldexpf(fall, er - was);
+      if (__ballot(fall != 1.f)) {
 #pragma unroll
-      for (int k = 0; k < D / 32; ++k) acc_r[k] *= g;
+        for (int k = 0; k < NV; ++k) acc_a[k] *= fall;
+      }
+      if (__ballot(g != 1.f) && j > wvu) {     // nothing is summed up yet at the wave's first tile
+#pragma unroll
+        for (int k = 0; k < D / 32; ++k) acc_r[k] *= g;
+      }
       if (past) {
         rs = __builtin_ldexpf(1.f, er);
         lim = fminf(kHead, kFull - (ex + er));

@@ -218,3 +218,28 @@ def test_scores_that_are_no_numbers_reach_their_rows(fmt):
     bad = np.zeros(21, bool)
     bad[:3] = bad[8:17] = True
     assert np.all(np.isnan(got[bad])) and np.all(np.isfinite(got[~bad]))
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int8"])
+@pytest.mark.parametrize("amp", [0.3, 5.0])
+def test_few_tokens_hold_all_the_values(amp, fmt):
+    """A dozen of 3000 tokens have a value at all, a residual's, at scales from 2^-12 to 2^10 and probabilities far apart:
+    each row is their sum, to the bound of its scores."""
+    torch_gpu()
+    lib_ready()
+    host = make_host([3000, 50], 4, 32, (0, 4, 16), fmt=fmt)
+    rng = np.random.default_rng(int(amp))
+    host.coef_v[...] = 0
+    rho = np.diff(host.res_off[0, 0].astype(np.int64))
+    some = np.sort(rng.choice(np.nonzero(rho[:3000])[0], 12, replace=False))
+    scale = np.zeros(host.res_scale[:, 1].shape, np.float16)
+    scale[..., some] = 2.0 ** rng.uniform(-12, 10, scale[..., some].shape)
+    host.res_scale[:, 1] = scale
+    cu, parent = make_tree([9, 2], "tree", rng)
+    q, k, v = inputs(host, 11, rng, amp=amp)
+    v[...] = 0
+    announce(f"tree decode, few values, amp {amp} {fmt}")
+    got = run(host, cu, parent, q, k, v, split=1024)
+    want, top = reference(host, 0, cu, parent, q.double().numpy(), k.double().numpy(), v.double().numpy())
+    assert np.all(got[9:] == 0) and np.all(want[9:] == 0)
+    check(got, want, bound(host, top), f"few values, amp {amp} {fmt}")
