@@ -66,3 +66,47 @@ def test_a_graph_and_other_verifications_share_a_workspace():
         for out, args in got:
             for a, b in zip(out, want(*args)):
                 assert np.array_equal(a.cpu().numpy(), b), (step, args)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int8"])
+def test_growth_into_spare_room(fmt):
+    """A cache laid out with fresh slots as a sequence of its own behind each live one takes the kept tokens without being
+    copied: a handle over the same tensors with the starts moved, then compress.  Its live sequences are those of a cache
+    grown by a repack."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import DeviceCache, DraftTree
+    host = make_host([200, 90], 4, 32, (0, 4, 8), fmt=fmt)
+    dc = device_cache(host)
+    rng = np.random.default_rng(6)
+    dev = lambda x: torch.from_numpy(np.asarray(x, dtype=np.int32)).cuda()
+    codes = torch.from_numpy(rng.integers(0, 3, (2, 2, 32)).astype(np.uint8)).cuda()
+    room = dc.empty_like([200, 16, 90, 16])
+    slots = -1 - np.arange(32)
+    announce(f"a cache with spare room {fmt}")
+    room.repack_from(dc, dev(np.concatenate([np.arange(200), slots[:16], np.arange(200, 290), slots[16:]])), dev([0, 0, 1, 1]),
+                     new_code=codes)
+    kept = (3, 5)
+    grown = DeviceCache.from_device(
+        basis=room.basis, coef_k=room.coef_k, coef_v=room.coef_v, rank_code=room.rank_code, res_off=room.res_off, res_idx=room.res_idx,
+        res_val=room.res_val, res_scale=room.res_scale, coef_scale_k=room.coef_scale_k, coef_scale_v=room.coef_scale_v,
+        cu_seqlens=np.cumsum([0, 203, 13, 95, 11]), window=room.window, n_q_heads=room.n_q_heads, levels=room.levels, coef_format=fmt)
+    plain = dc.empty_like([203, 95])
+    plain.repack_from(dc, dev(np.concatenate([np.arange(200), slots[:3], np.arange(200, 290), slots[16:21]])), dev([0, 1]), new_code=codes)
+    x = [[torch.from_numpy(rng.standard_normal((n, 2, D)).astype(np.float16)).cuda() for n in kept] for _ in range(2)]
+    for layer in range(2):
+        for c, ends in ((grown, (203, 311)), (plain, (203, 298))):
+            for b, t1 in enumerate(ends):
+                c.compress(layer, x[0][b], x[1][b], t1 - kept[b], t1)
+    assert grown.validate() == (True, -1) and plain.validate() == (True, -1)
+    cu, parent = make_tree([6, 4], "tree", rng)
+    q, k, v = (torch.from_numpy(rng.standard_normal((10, h, D)).astype(np.float16)).cuda() for h in (8, 2, 2))
+    parent = torch.from_numpy(parent).cuda()
+    for layer in range(2):
+        a = grown.tree_decode(layer, DraftTree([0, 6, 6, 10, 10], parent), q, k, v)
+        b = plain.tree_decode(layer, DraftTree(cu, parent), q, k, v)
+        # the same attention over chunks that start elsewhere: twice what a sum of 298 float32 terms may be off by
+        check(a.cpu().numpy(), b.cpu().numpy(), 2 * bound(host, 20.0), f"spare room, layer {layer}")
+        qd = q[:4].contiguous()
+        c, d = grown.decode(layer, q=qd)[[0, 2]], plain.decode(layer, q=qd[[0, 2]].contiguous())
+        check(c.cpu().numpy(), d.cpu().numpy(), 2 * bound(host, 20.0), f"spare room, decode of layer {layer}")
