@@ -30,12 +30,14 @@
 // times what the decode keeps.
 //
 // Measured at 65536 tokens, r_b 48, G 4, 8 KV heads, mean rank 1.9 (110 MB): 64 nodes
-// 171 us with the merge.  The pairs and the dense code tiles make it 38 products per
-// tile and 32 rows, 163 GFLOP in all, 0.95 PFLOP/s; the matrix cores are busy 48%
+// 175 us with the merge.  The pairs and the dense code tiles make it 38 products per
+// tile and 32 rows, 163 GFLOP in all, 0.93 PFLOP/s; the matrix cores are busy 45%
 // of the compute units' cycles and the clock falls to 1.9 GHz, so that a kernel with
-// 11% fewer cycles took the same time.  8 nodes: 40 us, 2.7 TB/s: 4 us until a
-// workgroup's q~ is there, 24 for its 9 tiles per wave, 4 to join its waves, 5
-// for the merge, 3 to start.  Blocks of 64 rows (each tile's codes scattered half
+// 11% fewer cycles took the same time.  8 nodes: 41 us, 2.65 TB/s.  Traced, where
+// launches do not overlap: 37 for this pass, of them 4 until a workgroup's q~ is
+// there and 4 to join its waves, most of the rest its 9 tiles per wave, and 7
+// for the merge.  A scale of its own for every row, in place of one per workgroup or
+// wave, is 2 to 4% of these times.  Blocks of 64 rows (each tile's codes scattered half
 // as often) do not fit the registers: the loop's spills wait for its loads.
 #pragma once
 #include "entry.h"
