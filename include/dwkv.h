@@ -553,12 +553,13 @@ size_t dwkv_tree_workspace_bytes(const dwkv_dims* dims, const dwkv_tree* tree);
  * dims allow.  Scores and value sums are accurate to about float32, as the
  * decode's: a probability has 22 bits down to 2^-12 of a row's largest and is
  * kept to 2^-34 of it below that, and so is its product with a residual value
- * scale, to 2^-23 of the row's largest such.  The coefficients' padding tokens must be finite, and an int8
- * coefficient, code times scale, within fp16's range (else the rows that see it
- * are not finite).  Two launches (none when N = 0).  DWKV_E_UNSUPPORTED for more than 65535 sequences, for
- * more than 2^23 workgroups (chunks of split_tokens times KV heads times blocks of
- * 32 rows), and for int8 coefficients when r_b / 16 * T exceeds 2^29.  Every device pointer 16-byte aligned, cu_seqlens,
- * cu_nodes and parent 4-byte, the block scales 2-byte. */
+ * scale, to 2^-23 of the row's largest such.  The coefficients' padding tokens
+ * must be finite, and an int8 coefficient, code times scale, within fp16's range
+ * (else the rows that see it are not finite).  Two launches (none when N = 0).
+ * DWKV_E_UNSUPPORTED for more than 65535 sequences, for more than 2^23 workgroups
+ * (chunks of split_tokens times KV heads times blocks of 32 rows), and for int8
+ * coefficients when r_b / 16 * T exceeds 2^29.  Every device pointer 16-byte
+ * aligned, cu_seqlens, cu_nodes and parent 4-byte, the block scales 2-byte. */
 dwkv_status dwkv_tree_decode(const dwkv_dims* dims, const dwkv_cache* cache, int32_t layer, const dwkv_tree* tree,
                              const void* q, int32_t q_type, int64_t q_stride, const void* k_new, const void* v_new,
                              int64_t kv_stride, float sm_scale, float* out, void* workspace, size_t ws_bytes,

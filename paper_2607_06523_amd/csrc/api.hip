@@ -1252,17 +1252,17 @@ void tree_seq(const dwkv_dims* d, const dwkv_tree* t, int64_t split, int b, int6
 // Chunk size.  Counted in rounds of eight waves over their tiles (2 to 2.6 us at r_b 48;
 // the four waves of r_b above 64 take each such round in two), a workgroup takes about
 // kFixed rounds before and after them and one of the drafted nodes about kDraft; a
-// compute unit holds one workgroup.  Of the sizes
-// that give every compute unit 1 to 8 workgroups, or one tile per wave more, the one
-// whose estimated end is first is taken: full rounds of the longest workgroup, or the
-// work shared out evenly plus one workgroup's length.  Where most workgroups are
-// shorter than the longest (ragged sequences) they fill in for each other, and half
-// a length is left: 16 int8 sequences of 8K to 16K take 201 us with the 5376-token
-// chunks that this gives and 211 with the 2816 of a whole length, 24 up to 12K 238
-// and 250, 20 fp16 ones up to 9K 162 and 177, but 12 up to 20K 214 and 202.  For these and
-// for one sequence of 64K at r_b 48 to 128 the plan is within 10% of the best of 23 sizes
-// from 512 to 32768 tokens.  Many short sequences it splits too little: 40 up to 6K take
-// 270 us unsplit and 212 with 3328.
+// compute unit holds one workgroup.  Of the sizes that give every compute unit 1 to 8
+// workgroups, or one tile per wave more, the one whose estimated end is first is
+// taken: full rounds of the longest workgroup, or the work shared out evenly plus one
+// workgroup's length.  Where most workgroups are shorter than the longest (ragged
+// sequences) they fill in for each other, and half a length is left: 16 int8
+// sequences of 8K to 16K take 201 us with the 5376-token chunks that this gives and
+// 211 with the 2816 of a whole length, 24 up to 12K 238 and 250, 20 fp16 ones up to 9K
+// 162 and 177, but 12 up to 20K 214 and 202.  For these and for one sequence of 64K at
+// r_b 48 to 128 the plan is within 10% of the best of 23 sizes from 512 to 32768
+// tokens.  Many short sequences it splits too little: 40 up to 6K take 270 us unsplit
+// and 212 with 3328.
 int64_t tree_split(const dwkv_dims* d, const dwkv_tree* t) {
   constexpr int64_t q = kTreeWaves * kTreeTile, kCU = kTargetWorkgroups / 2, kFixed = 5, kDraft = 4;
   if (d->split_tokens > 0) return std::min(d->split_tokens, 1 << 20);   // a chunk's streams have 32-bit offsets

@@ -12,8 +12,9 @@ namespace {
 // fourth chunk with a running maximum and sum of their own, a lane four columns
 // (residual channels, then a~): no load waits for another's value.  Sums in a
 // fixed order.  Bound by latency: 5 us for 20 rows of 5 partials, 7.5 for 32 rows
-// of 30 and for 256 of 5, 15 for 25 blocks of 32 rows in 16 sequences (traced); pairs of rows keep B^V's read (12 KB at r_b 48) below the
-// partials' own.  grid (row pairs of the longest sequence, Hkv, B)
+// of 30 and for 256 of 5, 15 for 25 blocks of 32 rows in 16 sequences (traced); pairs
+// of rows keep B^V's read (12 KB at r_b 48) below the partials' own.
+// grid (row pairs of the longest sequence, Hkv, B)
 constexpr int kMR = 2, kMW = 4;
 struct alignas(16) MergeSmem {
   float part[kMW][kMR][2 * D];

@@ -26,8 +26,9 @@
 //
 // Precision: q~, the probabilities and their products with the value scales are fp16
 // pairs (hi + lo, 22 bits) in units of the row's own (row_down, kUp, rs); the codes,
-// fp16 coefficients and queries are exact, sums and softmax statistics are float32.  One half alone would cost 2^-11 of a score or probability, fifty
-// times what the decode keeps.
+// fp16 coefficients and queries are exact, sums and softmax statistics are float32.
+// One half alone would cost 2^-11 of a score or probability, fifty times what the
+// decode keeps.
 //
 // Measured at 65536 tokens, r_b 48, G 4, 8 KV heads, mean rank 1.9 (110 MB): 64 nodes
 // 175 us with the merge.  The pairs and the dense code tiles make it 38 products per
@@ -37,8 +38,8 @@
 // launches do not overlap: 37 for this pass, of them 4 until a workgroup's q~ is
 // there and 4 to join its waves, most of the rest its 9 tiles per wave, and 7
 // for the merge.  A scale of its own for every row, in place of one per workgroup or
-// wave, is 2 to 4% of these times.  Blocks of 64 rows (each tile's codes scattered half
-// as often) do not fit the registers: the loop's spills wait for its loads.
+// wave, is 2 to 4% of these times.  Blocks of 64 rows (each tile's codes scattered
+// half as often) do not fit the registers: the loop's spills wait for its loads.
 #pragma once
 #include "entry.h"
 #include "internal.h"
@@ -741,7 +742,7 @@ __global__ __launch_bounds__(64 * kWaves<NB>, kWaves<NB> / 4) void tree_split_ke
       const u4v kc = *reinterpret_cast<const u4v*>(&w.k[col * kKRow + 16 * s + 8 * h]);
       sr = mfma_q<BF>(kc, sm.qf[s][lane], sr);
     }
-    if (scaled) {                        // but for zero queries; as a branch it keeps what follows from crowding the products' registers
+    if (scaled) {                        // all but zero queries; the branch keeps what follows out of the products' registers
       const float up = __builtin_ldexpf(1.f, row_down(sm.big[col]));
 #pragma unroll
       for (int i = 0; i < 16; ++i) sb[i] = __builtin_fmaf(sb[i], up, -m);
