@@ -62,7 +62,7 @@ typedef enum dwkv_status {
                              dwkv_static_scratch_bytes()                           */
 } dwkv_status;
 
-typedef enum dwkv_qtype { DWKV_F16 = 0, DWKV_BF16 = 1, DWKV_F32 = 2 /* dwkv_tree_verify only */ } dwkv_qtype;
+typedef enum dwkv_qtype { DWKV_F16 = 0, DWKV_BF16 = 1, DWKV_F32 = 2 /* not in a cache or a decode's queries */ } dwkv_qtype;
 
 /* Shape of one factorized cache (all sequences packed along the token axis). */
 typedef struct dwkv_dims {
@@ -636,6 +636,169 @@ size_t dwkv_repack_workspace_bytes(const dwkv_dims* dst);
 dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_dims* src, const dwkv_cache* from,
                         const int32_t* src_token, const int32_t* src_seq, const uint8_t* new_code, int64_t n_new,
                         void* workspace, size_t ws_bytes, void* stream);
+
+/* ---- Rotary positions, a paged dense cache, logits into probabilities ---------
+ * What a program has between its model's projections and the calls above: keys
+ * are cached after their rotation and drafts are verified against probabilities.
+ * The paged cache is the dense one of dwkv_dense_decode in a form that grows:
+ * its lengths and page tables are device arrays, so a captured graph follows them. */
+
+typedef struct dwkv_rope_table {
+  const double* freq;     /* DEVICE [n_pairs] radians per position of each pair (dwkv_rope_freqs);
+                             8-byte aligned                                          */
+  int32_t n_pairs;        /* the first 2 n_pairs channels of a head turn, the others stay  */
+  int32_t interleaved;    /* 0: pair i is channels (i, n_pairs + i);  1: (2i, 2i + 1)  */
+  float scale;            /* factor on the turned channels (1: none)                  */
+} dwkv_rope_table;
+
+typedef enum dwkv_rope_scaling {
+  DWKV_ROPE_PLAIN = 0,    /* f_i = base^(-i / n_pairs)                              */
+  DWKV_ROPE_LINEAR = 1,   /* f_i / factor                                           */
+  DWKV_ROPE_BASE = 2,     /* base raised by factor^(n_pairs / (n_pairs - 1)): the lowest
+                             frequency is divided by factor, the highest stays      */
+  DWKV_ROPE_RAMP = 3      /* by the turns r_i = context f_i / (2 pi) that a pair makes over the
+                             context that the model was trained on: f_i / factor up to
+                             `low` turns, f_i from `high` on, and between them
+                             s f_i + (1 - s) f_i / factor, s = (r_i - low) / (high - low) */
+} dwkv_rope_scaling;
+
+/* The frequencies of a table, on the HOST: freq_host [n_pairs], written.  factor
+ * > 0 and, for DWKV_ROPE_RAMP, context > 0 and low < high (else unused).
+ * DWKV_E_DIMS for bad arguments (n_pairs < 1; base not positive and finite). */
+dwkv_status dwkv_rope_freqs(int32_t n_pairs, double base, int32_t scaling, double factor, double context,
+                            double low, double high, double* freq_host);
+
+/* Rotary positions.  For row r, head h and pair i with channels (a, b),
+ * t = pos[r] freq[i] (float64) and m = scale:
+ *   a' = m (a cos t - b sin t),   b' = m (b cos t + a sin t)
+ * Channels past 2 n_pairs are copied.  inverse != 0 turns by -t: with the same
+ * scale that is the gradient with respect to x, and with 1 / scale it takes a rotation
+ * back.  float32 arithmetic, one rounding to out_type.
+ *   x:        n_rows rows of [n_heads][head_dim] in x_type (DWKV_F16, DWKV_BF16 or
+ *             DWKV_F32), x_stride elements apart (a fused projection's queries and keys
+ *             are turned in one call)
+ *   out:      the same shape in out_type, out_stride elements apart.  In place
+ *             (out == x) when types and strides agree; no other overlap
+ *   strides:  multiples of 8, at least n_heads head_dim; 0 = rows without a gap
+ *   pos:      DEVICE int32 [n_rows]
+ * head_dim: a multiple of 8, at most 512; 2 n_pairs <= head_dim, n_pairs >= 1.  x and
+ * out 16-byte aligned, pos 4-byte.  n_rows up to 2^27.  One launch (none for no rows). */
+dwkv_status dwkv_rope(int64_t n_rows, int32_t n_heads, int32_t head_dim, const dwkv_rope_table* table, int32_t inverse,
+                      const void* x, int32_t x_type, int64_t x_stride, const int32_t* pos, void* out,
+                      int32_t out_type, int64_t out_stride, void* stream);
+
+/* A dense cache in pages.  Token t of sequence b lies in page
+ * page_table[b][t / page_size] at slot t % page_size.  A page id outside
+ * [0, n_pages) is no page: nothing is stored there, and its tokens are not
+ * attended to (pages before a window can be given back). */
+typedef struct dwkv_pages {
+  int32_t type;           /* DWKV_F16 or DWKV_BF16                                  */
+  int32_t batch;          /* B sequences, at most 4096                              */
+  int32_t n_layers;
+  int32_t n_kv_heads;     /* Hkv                                                   */
+  int32_t head_dim;       /* d: a multiple of 32, 32..256                          */
+  int32_t page_size;      /* tokens of a page: a power of two, 16 or more          */
+  int32_t n_pages;        /* pages of a layer                                      */
+  int32_t max_pages;      /* columns of page_table                                 */
+  void* k;                /* [n_layers][n_pages][Hkv][page_size/16][d/8][16][8]: keys in tiles of
+                             16 tokens x 8 channels, as dwkv_cache.coef_k           */
+  void* v;                /* [n_layers][n_pages][Hkv][page_size/8][d][8]: values in blocks of 8
+                             tokens, as dwkv_cache.coef_v                           */
+  const int32_t* page_table; /* DEVICE [B][max_pages]                              */
+  const int32_t* seq_len; /* DEVICE [B] tokens of each sequence, the new ones included (held
+                             to [0, max_pages page_size])                          */
+} dwkv_pages;
+
+/* Stores new tokens: row r of sequence b, the j-th of its n_b new ones
+ * (cu_new[b] + j = r), becomes token seq_len[b] - n_b + j of layer `layer`: its key
+ * turned at its position, its value as it is, both rounded once to the cache's
+ * type.  Its queries are turned too, into q_out.
+ *   n_rows:  N rows of q, k and v
+ *   cu_new:  DEVICE [B+1] packed starts of the new rows, or NULL: N = B, one row for
+ *            each sequence.  Rows from cu_new[B] on are left out, q_out's too
+ *   k, v:    rows of [Hkv][d] in x_type (DWKV_F16, DWKV_BF16 or DWKV_F32), kv_stride
+ *            elements apart;  q: NULL, or rows of [n_q_heads][d], q_stride apart
+ *   table:   NULL: nothing turns;  pos: DEVICE int32 [N] positions, NULL: the
+ *            tokens' places in their sequences
+ *   q_out:   [N][n_q_heads][d] in the cache's type, no overlap with the inputs
+ * A row whose place lies before the sequence's start (a sequence of length 0 in a
+ * padded batch), past its table or in no page is not stored.  A place in one page
+ * that two sequences share must not be written by both.  Strides are multiples of
+ * 8, 0 = rows without a gap; k, v, q, q_out and the pages are 16-byte aligned, the
+ * integer arrays 4-byte.  N up to 2^27.  One launch (none for no rows). */
+dwkv_status dwkv_page_append(const dwkv_pages* pages, int32_t layer, int32_t n_rows, const int32_t* cu_new, const void* k,
+                             const void* v, int32_t x_type, int64_t kv_stride, const void* q, int64_t q_stride,
+                             int32_t n_q_heads, const dwkv_rope_table* table, const int32_t* pos, void* q_out, void* stream);
+
+/* Bytes of device workspace dwkv_page_decode needs (0 when arguments are invalid). */
+size_t dwkv_page_workspace_bytes(const dwkv_pages* pages, int32_t n_q_heads);
+
+/* Attention of one new token per sequence over the paged cache:
+ *   out[b][hq] = softmax_t(sm_scale q[b][hq] . k_t) v_t
+ * over the tokens t of sequence b that lie in a page, with window > 0 the last
+ * `window` tokens of it only; KV head hq / (n_q_heads / Hkv).  A sequence
+ * with none of them gets zeros, and so does a row whose scores are all -inf.
+ * What a token does not see changes nothing, infinities and NaN included.
+ *   q:        [B] rows of [n_q_heads][d] in the cache's type, q_stride elements
+ *             apart (a multiple of 8; 0 = rows without a gap)
+ *   sm_scale: <= 0 selects 1/sqrt(d)
+ *   out:      fp32 [B][n_q_heads][d], written
+ *   workspace:>= dwkv_page_workspace_bytes bytes, no initial contents
+ * Scores and sums are float32; probabilities have 22 bits (24 in bfloat16 caches)
+ * down to 2^-12 of a row's largest.  n_q_heads is a multiple of Hkv, any group.
+ * q, out, pages and workspace are 16-byte aligned.  Two launches.
+ * DWKV_E_UNSUPPORTED for lists of 2^31 or more tiles of 32 tokens. */
+dwkv_status dwkv_page_decode(const dwkv_pages* pages, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,
+                             float sm_scale, int32_t window, float* out, void* workspace, size_t ws_bytes, void* stream);
+
+/* What is done to rows of logits.  S sequences; every array may be NULL (its rule is
+ * left out).  All on the DEVICE. */
+typedef struct dwkv_logits_rules {
+  const float* params;        /* [S][4]: repetition, presence, frequency, temperature   */
+  const int32_t* history;     /* [S] rows of token ids, history_stride apart: the prompt,
+                                 then what was said; ids outside [0, vocab) are no tokens */
+  int64_t history_stride;
+  const int32_t* history_len; /* [S] ids of each row (held to [0, history_stride])      */
+  const int32_t* prompt_len;  /* [S] how many of them are the prompt's; NULL: none      */
+  const int32_t* cu_bias;     /* [S+1] packed starts of the biases                      */
+  const int32_t* bias_id;     /* [n_bias] token ids (those outside [0, vocab) are left out) */
+  const float* bias;          /* [n_bias]                                              */
+  int32_t n_bias;
+  const uint32_t* mask;       /* [N] rows of words, mask_stride apart: bit t % 32 of word
+                                 t / 32 is 1 where token t is allowed                   */
+  int64_t mask_stride;        /* at least (vocab + 31) / 32                            */
+} dwkv_logits_rules;
+
+/* Bytes of device workspace dwkv_logits needs (0 when arguments are invalid). */
+size_t dwkv_logits_workspace_bytes(int32_t n_rows, int32_t vocab);
+
+/* Rows of logits made ready to draw from, or to verify drafts against
+ * (dwkv_tree_verify's target or draft).  For entry t of a row, in this order, each
+ * step in float32:
+ *   z = l;   t in the history: z = z > 0 ? z / repetition : z repetition
+ *   t said c > 0 times:        z = z - frequency c - presence
+ *   z = z + bias (one listed twice adds twice);   not allowed: z = -inf
+ * and out = z, or with probs != 0
+ *   out = softmax(z / temperature);  temperature <= 0 or NaN: 1 at the first largest
+ *         z that is not -inf or NaN, else 0
+ * A row of nothing but -inf has probabilities 0, one with a NaN or +inf NaN. "Said"
+ * are the history's ids from prompt_len on and, with a tree, the tokens on the
+ * path from node 0 to the row's node, node 0's not (it is the history's last).
+ *   batch:   S sequences
+ *   tree:    NULL: N = S rows, one for each sequence; else N = n_nodes rows, row i
+ *            the logits after node i.  A path ends at a parent that is not a lower
+ *            node of its sequence
+ *   token:   int32 [N] the nodes' tokens (with a tree)
+ *   logits:  N rows of vocab in l_type, l_stride elements apart (0 = no gap)
+ *   out:     [N][vocab] in out_type, rounded once.  It may be logits when types agree
+ *            and rows have no gap; no other overlap
+ *   workspace: with probs, >= dwkv_logits_workspace_bytes(N, vocab), no initial
+ *            contents, 16-byte aligned; else unused
+ * Pointers are aligned to their type.  N up to 65535, vocab up to 2^30.  One launch,
+ * with probs two (none for no rows). */
+dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, const void* logits,
+                        int32_t l_type, int64_t l_stride, const dwkv_logits_rules* rules, int32_t probs, void* out,
+                        int32_t out_type, void* workspace, size_t ws_bytes, void* stream);
 
 /* Number of sink words dwkv_hbm_read writes (its block count). */
 int32_t dwkv_hbm_read_blocks(void);

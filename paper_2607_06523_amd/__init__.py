@@ -18,6 +18,15 @@ Several drafted tokens per sequence:
     path, n_kept, nxt = tree_verify(tree, token, target, u, u_next, draft=draft)
     new = cache.empty_like(seqlens, res_stride)   # then the tokens that stay, with room for the kept ones
     new.repack_from(cache, src_token, src_seq, new_code=codes)
+
+Between a model's projections and those calls, and the dense cache in pages:
+
+    table = RopeTable(rope_freqs(128, base=5e5), interleaved=False)   # .to the GPU by itself
+    qk = rope(rows[:, :Hq + Hkv], pos, table)     # [N, heads, d], or in place with out=
+    pages = PagedCache.empty(page_table, seq_len, n_pages=4096, page_size=64, n_kv_heads=8, n_q_heads=32)
+    q = pages.append(layer, k, v, q=q, rope=table)                    # new tokens, turned on the way
+    out = pages.decode(layer, q)                  # fp32 [B, Hq, d]
+    target = adjust_logits(logits, LogitsRules(params=params, history=ids, history_len=n), tree=tree, token=token)
 """
 from __future__ import annotations
 
@@ -30,7 +39,8 @@ from . import binding, layout
 from .binding import DwkvError, F16, BF16, F32
 
 __all__ = ["DeviceCache", "ProbeRef", "DraftTree", "DwkvError", "load", "F16", "BF16", "F32", "hbm_read",
-           "hbm_read_blocks", "probe_schedule", "tree_verify", "tree_verify_workspace"]
+           "hbm_read_blocks", "probe_schedule", "tree_verify", "tree_verify_workspace", "rope_freqs", "RopeTable", "rope",
+           "PagedCache", "LogitsRules", "adjust_logits", "adjust_logits_workspace"]
 
 
 def load():
@@ -741,3 +751,328 @@ class DeviceCache:
             return False, int(bad.value)
         binding.check(st, "dwkv_validate")
         return True, -1
+
+
+def _kinds(torch):
+    return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _heads(x, name):
+    """The row stride of x [N, H, d], whose rows have no gaps inside."""
+    if x.dim() != 3:
+        raise ValueError(f"{name} must be [rows, heads, d]")
+    n, h, d = x.shape
+    s = x.stride()
+    if n > 0 and (s[2] != 1 or h > 1 and s[1] != d):
+        raise ValueError(f"the rows of {name} must have no gaps inside")
+    if n > 1 and s[0] < h * d:
+        raise ValueError(f"the rows of {name} must not overlap")
+    return s[0] if n > 1 else 0
+
+
+def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, context: float = 0.0,
+               low: float = 1.0, high: float = 4.0):
+    """dwkv_rope_freqs: radians per position of the rot_dim / 2 pairs, a float64
+    tensor on the host.  scaling "plain", "linear", "base" or "ramp" (by the turns,
+    from low to high, that a pair makes over the context trained on)."""
+    import torch
+    if scaling not in binding.ROPE_SCALING:
+        raise ValueError(f"scaling must be one of {sorted(binding.ROPE_SCALING)}, not {scaling!r}")
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError("rot_dim must be even and positive")
+    f = torch.empty(int(rot_dim) // 2, dtype=torch.float64)
+    binding.check(load().dwkv_rope_freqs(f.numel(), float(base), binding.ROPE_SCALING[scaling], float(factor), float(context),
+                                         float(low), float(high), C.cast(f.data_ptr(), C.POINTER(C.c_double))), "dwkv_rope_freqs")
+    return f
+
+
+class RopeTable:
+    """Rotary positions of the first 2 len(freq) channels of a head: freq float64,
+    radians per position of each pair (moved to the GPU); pair i is channels
+    (i, n + i), or (2i, 2i + 1) when interleaved; scale: factor on those channels."""
+
+    def __init__(self, freq, interleaved: bool = False, scale: float = 1.0, device: str = "cuda"):
+        import torch
+        if freq.dtype != torch.float64 or freq.dim() != 1 or freq.numel() < 1 or not freq.is_contiguous():
+            raise TypeError("freq must be a contiguous float64 vector")
+        self.freq = freq if freq.is_cuda else freq.to(device)
+        t = binding.RopeTable()
+        t.freq, t.n_pairs, t.interleaved, t.scale = self.freq.data_ptr(), self.freq.numel(), int(bool(interleaved)), float(scale)
+        self.cstruct, self.ref, self.index, self.rot_dim = t, C.byref(t), self.freq.get_device(), 2 * self.freq.numel()
+
+
+def rope(x, pos, table: RopeTable, inverse: bool = False, out=None):
+    """dwkv_rope: the heads of x [N, H, d] (float16, bfloat16 or float32; rows may be
+    slices of wider ones) turned at pos int32 [N].  inverse turns back: with the
+    same table that is the gradient with respect to x.  out: like x, of any of those
+    types (x itself: in place); returns it."""
+    import torch
+    kinds = _kinds(torch)
+    if x.dtype not in kinds:
+        raise TypeError("x must be float16, bfloat16 or float32")
+    xs = _heads(x, "x")
+    N, H, d = x.shape
+    if pos.dtype != torch.int32 or pos.numel() != N or not pos.is_contiguous():
+        raise TypeError("pos must be contiguous int32 [N]")
+    if out is None:
+        out = torch.empty((N, H, d), dtype=x.dtype, device=x.device)
+    elif out.dtype not in kinds or out.shape != x.shape:
+        raise TypeError("out must be float16, bfloat16 or float32 of x's shape")
+    os = _heads(out, "out")
+    if not _all_on(table.index, x, pos, out):
+        raise ValueError("every tensor must be on the table's device")
+    with _on(torch, table.index):
+        st = load().dwkv_rope(N, H, d, table.ref, int(bool(inverse)), x.data_ptr(), kinds[x.dtype], xs, pos.data_ptr(),
+                              out.data_ptr(), kinds[out.dtype], os, torch.cuda.current_stream(table.index).cuda_stream)
+    binding.check(st, "dwkv_rope")
+    return out
+
+
+class PagedCache:
+    """A dense cache in pages, used in place: k [L, n_pages, Hkv, page/16, d/8, 16, 8]
+    and v [L, n_pages, Hkv, page/8, d, 8] float16 or bfloat16; page_table int32
+    [B, columns], an id outside the pool being no page; seq_len int32 [B], the new
+    tokens included.  The program changes page_table and seq_len on the device."""
+
+    def __init__(self, k, v, page_table, seq_len, n_q_heads: int):
+        import torch
+        self.torch, self.lib = torch, binding.load()
+        if k.dtype not in (torch.float16, torch.bfloat16) or v.dtype != k.dtype:
+            raise TypeError("k and v must be float16 or bfloat16, of one type")
+        if k.dim() != 7 or v.dim() != 6 or tuple(k.shape[5:]) != (16, 8) or v.shape[5] != 8:
+            raise ValueError("k must be [L, n_pages, Hkv, page/16, d/8, 16, 8] and v [L, n_pages, Hkv, page/8, d, 8]")
+        L, n, H, p16, d8 = k.shape[:5]
+        if tuple(v.shape) != (L, n, H, 2 * p16, 8 * d8, 8):
+            raise ValueError("k and v must be pages of one shape")
+        if not k.is_contiguous() or not v.is_contiguous():
+            raise ValueError("k and v must be contiguous")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or not page_table.is_contiguous():
+            raise TypeError("page_table must be contiguous int32 [B, columns]")
+        B = page_table.shape[0]
+        if seq_len.dtype != torch.int32 or seq_len.numel() != B or not seq_len.is_contiguous():
+            raise TypeError("seq_len must be contiguous int32 [B]")
+        self.index = k.get_device()
+        if not _all_on(self.index, k, v, page_table, seq_len):
+            raise ValueError("every tensor must be on one GPU")
+        self.k, self.v, self.page_table, self.seq_len, self.device = k, v, page_table, seq_len, k.device
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, n, H, 16 * p16, 8 * d8
+        self.batch, self.n_q_heads = B, int(n_q_heads)
+        c = binding.Pages()
+        c.type, c.batch, c.n_layers, c.n_kv_heads = F16 if k.dtype == torch.float16 else BF16, B, L, H
+        c.head_dim, c.page_size, c.n_pages, c.max_pages = self.head_dim, self.page_size, n, page_table.shape[1]
+        c.k, c.v, c.page_table, c.seq_len = k.data_ptr(), v.data_ptr(), page_table.data_ptr(), seq_len.data_ptr()
+        self.cstruct, self.ref = c, C.byref(c)
+        self._bytes = int(self.lib.dwkv_page_workspace_bytes(self.ref, self.n_q_heads))
+        if self._bytes == 0:
+            raise DwkvError(3, "dwkv_page_workspace_bytes")
+        self._ws = None
+
+    @classmethod
+    def empty(cls, page_table, seq_len, *, n_pages: int, page_size: int, n_kv_heads: int, n_q_heads: int, head_dim: int = 128,
+              n_layers: int = 1, dtype=None):
+        """A zero-filled pool for that table."""
+        import torch
+        dt = torch.float16 if dtype is None else dtype
+        if page_size < 16 or page_size % 16 or head_dim % 8:
+            raise ValueError("page_size must be a multiple of 16 and head_dim of 8")
+        z = lambda *s: torch.zeros((n_layers, n_pages, n_kv_heads) + s, dtype=dt, device=page_table.device)
+        return cls(z(page_size // 16, head_dim // 8, 16, 8), z(page_size // 8, head_dim, 8), page_table, seq_len, n_q_heads)
+
+    def append(self, layer: int, k, v, cu_new=None, q=None, rope: RopeTable | None = None, pos=None, q_out=None):
+        """dwkv_page_append: rows k, v [N, Hkv, d] (float16, bfloat16 or float32; rows
+        may be slices of wider ones, with one stride) become the last tokens of their
+        sequences, which seq_len counts already: one row for each sequence, or rows
+        cu_new[b] to cu_new[b + 1] (int32 [B+1], device).  rope turns the keys, and the
+        queries q [N, H, d], at pos int32 [N] or at the tokens' places.  Returns q_out
+        [N, H, d] of the cache's type, or None without q."""
+        torch = self.torch
+        kinds = _kinds(torch)
+        if k.dtype not in kinds or v.dtype != k.dtype or q is not None and q.dtype != k.dtype:
+            raise TypeError("k, v and q must be float16, bfloat16 or float32, of one type")
+        ks, vs = _heads(k, "k"), _heads(v, "v")
+        N = k.shape[0]
+        if k.shape != v.shape or k.shape[1] != self.n_kv_heads or k.shape[2] != self.head_dim:
+            raise ValueError("k and v must be [N, Hkv, d]")
+        if ks != vs:
+            raise ValueError("k and v must have the same row stride")
+        qs = nq = 0
+        if q is not None:
+            qs, nq = _heads(q, "q"), q.shape[1]
+            if q.shape[0] != N or q.shape[2] != self.head_dim:
+                raise ValueError("q must be [N, H, d]")
+            if q_out is None:
+                q_out = torch.empty((N, nq, self.head_dim), dtype=self.k.dtype, device=self.device)
+            elif q_out.dtype != self.k.dtype or q_out.shape != q.shape or not q_out.is_contiguous():
+                raise TypeError("q_out must be contiguous [N, H, d] of the cache's type")
+        elif q_out is not None:
+            raise ValueError("q_out without q")
+        if cu_new is None:
+            if N != self.batch:
+                raise ValueError("without cu_new there is one row for each sequence")
+        elif cu_new.dtype != torch.int32 or cu_new.numel() != self.batch + 1 or not cu_new.is_contiguous():
+            raise TypeError("cu_new must be contiguous int32 [B+1]")
+        if pos is not None and (pos.dtype != torch.int32 or pos.numel() != N or not pos.is_contiguous()):
+            raise TypeError("pos must be contiguous int32 [N]")
+        if not _all_on(self.index, k, v, q, q_out, cu_new, pos, rope.freq if rope is not None else None):
+            raise ValueError("every tensor must be on the cache's device")
+        with _on(torch, self.index):
+            st = self.lib.dwkv_page_append(self.ref, int(layer), N, None if cu_new is None else cu_new.data_ptr(), k.data_ptr(),
+                                           v.data_ptr(), kinds[k.dtype], ks, None if q is None else q.data_ptr(), qs, nq,
+                                           None if rope is None else rope.ref, None if pos is None else pos.data_ptr(),
+                                           None if q is None else q_out.data_ptr(),
+                                           torch.cuda.current_stream(self.index).cuda_stream)
+        binding.check(st, "dwkv_page_append")
+        return q_out
+
+    def workspace(self):
+        """A workspace for ``decode``."""
+        return self.torch.empty(self._bytes, dtype=self.torch.uint8, device=self.device)
+
+    def decode(self, layer: int, q, sm_scale: float | None = None, window: int = 0, out=None, workspace=None):
+        """dwkv_page_decode: attention of one new token per sequence, q [B, Hq, d] of
+        the cache's type (rows may be slices of wider ones), over the tokens that
+        seq_len counts (window > 0: the last of them only).  Returns out fp32
+        [B, Hq, d].  Without a workspace the cache's own is used: give one to calls
+        that may overlap."""
+        torch = self.torch
+        B, Hq, d = self.batch, self.n_q_heads, self.head_dim
+        if q.dtype != self.k.dtype:
+            raise TypeError("q must have the cache's type")
+        if q.shape != (B, Hq, d):
+            raise ValueError("q must be [B, Hq, d]")
+        qs = _heads(q, "q")
+        if out is None:
+            out = torch.empty((B, Hq, d), dtype=torch.float32, device=self.device)
+        elif out.dtype != torch.float32 or out.shape != (B, Hq, d) or not out.is_contiguous():
+            raise TypeError("out must be contiguous float32 [B, Hq, d]")
+        if workspace is None:
+            if self._ws is None:
+                self._ws = self.workspace()
+            workspace = self._ws
+        if not _all_on(self.index, q, out, workspace):
+            raise ValueError("every tensor must be on the cache's device")
+        with _on(torch, self.index):
+            st = self.lib.dwkv_page_decode(self.ref, int(layer), q.data_ptr(), qs, Hq, float(sm_scale or 0.0), int(window),
+                                           out.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
+                                           torch.cuda.current_stream(self.index).cuda_stream)
+        binding.check(st, "dwkv_page_decode")
+        return out
+
+
+class LogitsRules:
+    """What ``adjust_logits`` does to rows (dwkv_logits_rules), every part optional,
+    all on one GPU: params float32 [S, 4] (repetition, presence, frequency,
+    temperature); history int32 [S, L] token ids with history_len int32 [S] and
+    prompt_len int32 [S]; bias (starts int32 [S+1], ids int32, values float32); mask int32
+    [N, words], bit t % 32 of word t / 32 set where token t is allowed."""
+
+    def __init__(self, params=None, history=None, history_len=None, prompt_len=None, bias=None, mask=None):
+        import torch
+        i32 = torch.int32
+        S = set()
+        if params is not None:
+            if params.dtype != torch.float32 or params.dim() != 2 or params.shape[1] != 4 or not params.is_contiguous():
+                raise TypeError("params must be contiguous float32 [S, 4]")
+            S.add(params.shape[0])
+        if history is not None:
+            if history.dtype != i32 or history.dim() != 2 or history.numel() and history.stride(1) != 1:
+                raise TypeError("history must be int32 [S, L]")
+            if history.shape[0] > 1 and history.stride(0) < history.shape[1]:
+                raise ValueError("the rows of history must not overlap")
+            if history_len is None:
+                raise ValueError("history_len must be given with history")
+            S.add(history.shape[0])
+        elif history_len is not None or prompt_len is not None:
+            raise ValueError("history_len and prompt_len belong to a history")
+        for name, x in (("history_len", history_len), ("prompt_len", prompt_len)):
+            if x is not None:
+                if x.dtype != i32 or x.dim() != 1 or not x.is_contiguous():
+                    raise TypeError(f"{name} must be contiguous int32 [S]")
+                S.add(x.numel())
+        if bias is not None:
+            cu, ids, val = bias
+            if cu.dtype != i32 or ids.dtype != i32 or val.dtype != torch.float32 or not all(
+                    x.dim() == 1 and x.is_contiguous() for x in bias) or ids.numel() != val.numel():
+                raise TypeError("bias must be contiguous vectors: int32 [S+1] starts, int32 ids, as many float32 values")
+            S.add(cu.numel() - 1)
+        if mask is not None and (mask.dtype != i32 or mask.dim() != 2 or mask.numel() and mask.stride(1) != 1):
+            raise TypeError("mask must be int32 [N, words]")
+        if mask is not None and mask.shape[0] > 1 and mask.stride(0) < mask.shape[1]:
+            raise ValueError("the rows of mask must not overlap")
+        if len(S) > 1:
+            raise ValueError("the rules are of different numbers of sequences")
+        self.n_seq = S.pop() if S else None
+        self.keep = [x for x in (params, history, history_len, prompt_len, mask) + tuple(bias or ()) if x is not None]
+        self.mask = mask
+        self.index = self.keep[0].get_device() if self.keep else None
+        if self.keep and not _all_on(self.index, *self.keep):
+            raise ValueError("every tensor must be on one GPU")
+        ptr = lambda x: None if x is None else x.data_ptr()
+        r = binding.LogitsRules()
+        r.params, r.mask = ptr(params), ptr(mask)
+        if history is not None and history.shape[1] > 0:
+            # the room that a length is held to is the row's own, not the gap behind it
+            if history.shape[0] > 1 and history.stride(0) != history.shape[1]:
+                raise ValueError("the rows of history must have no gap")
+            r.history, r.history_stride = ptr(history), history.shape[1]
+            r.history_len, r.prompt_len = ptr(history_len), ptr(prompt_len)
+        if bias is not None and bias[1].numel() > 0:
+            r.cu_bias, r.bias_id, r.bias, r.n_bias = ptr(bias[0]), ptr(bias[1]), ptr(bias[2]), bias[1].numel()
+        if mask is not None:
+            r.mask_stride = mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
+        self.cstruct, self.ref = r, C.byref(r)
+
+
+def adjust_logits_workspace(logits):
+    """A workspace for ``adjust_logits`` of such rows, with probabilities."""
+    import torch
+    n = int(load().dwkv_logits_workspace_bytes(*logits.shape))
+    if n == 0:
+        raise DwkvError(3, "dwkv_logits_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=logits.device)
+
+
+def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, token=None, probs: bool = True, out=None,
+                  workspace=None):
+    """dwkv_logits: penalties, biases, masks and temperature on logits [N, vocab]
+    (float32, float16 or bfloat16; rows may be slices of wider ones), and with probs the
+    probabilities they leave.  Row i is sequence i, or with a tree node i, its path's
+    tokens (token int32 [N]) behind its sequence's history.  out [N, vocab], by default
+    float32 with probs, else the logits' type; logits itself: in place."""
+    import torch
+    kinds = _kinds(torch)
+    if logits.dtype not in kinds or logits.dim() != 2 or logits.numel() and logits.stride(1) != 1:
+        raise TypeError("logits must be [N, vocab] of float32, float16 or bfloat16")
+    N, V = logits.shape
+    if N > 1 and logits.stride(0) < V:
+        raise ValueError("the rows of logits must not overlap")
+    S = N
+    if tree is not None:
+        S = tree.batch
+        if tree.n_nodes != N:
+            raise ValueError("logits must have a row for each node")
+        if token is None or token.dtype != torch.int32 or token.numel() != N or not token.is_contiguous():
+            raise TypeError("token must be contiguous int32 [N]")
+    elif token is not None:
+        raise ValueError("token without a tree")
+    if rules.n_seq is not None and rules.n_seq != S:
+        raise ValueError("the rules are of another number of sequences")
+    if rules.mask is not None and (rules.mask.shape[0] != N or rules.mask.shape[1] < (V + 31) // 32):
+        raise ValueError("mask must have a row of (vocab + 31) / 32 words for each row")
+    if out is None:
+        out = torch.empty((N, V), dtype=torch.float32 if probs else logits.dtype, device=logits.device)
+    elif out.dtype not in kinds or out.shape != logits.shape or not out.is_contiguous():
+        raise TypeError("out must be contiguous [N, vocab] of float32, float16 or bfloat16")
+    index = logits.get_device()
+    if rules.index not in (None, index) or tree is not None and tree.index != index or not _all_on(index, logits, token, out, workspace):
+        raise ValueError("every tensor must be on the logits' device")
+    if N == 0:
+        return out
+    ws = workspace if workspace is not None or not probs else adjust_logits_workspace(logits)
+    with _on(torch, index):
+        st = load().dwkv_logits(S, tree.ref if tree is not None else None, None if token is None else token.data_ptr(), V,
+                                logits.data_ptr(), kinds[logits.dtype], logits.stride(0) if N > 1 else 0, rules.ref, int(bool(probs)),
+                                out.data_ptr(), kinds[out.dtype], None if ws is None else ws.data_ptr(),
+                                0 if ws is None else _nbytes(ws), torch.cuda.current_stream(index).cuda_stream)
+    binding.check(st, "dwkv_logits")
+    return out

@@ -19,6 +19,7 @@ MAX_PROBE_HEADS = 64
 F16, BF16, F32 = 0, 1, 2
 MAX_TREE_NODES = 64
 COEF_F16, COEF_I8 = 0, 1
+ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "ramp": 3}
 
 STATUS = {0: "ok", 1: "null pointer", 2: "inconsistent dimensions", 3: "unsupported shape",
           4: "workspace too small", 5: "malformed cache layout", 6: "HIP runtime error",
@@ -64,6 +65,22 @@ class Tree(C.Structure):
                 ("parent", C.c_void_p)]
 
 
+class RopeTable(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("n_pairs", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float)]
+
+
+class Pages(C.Structure):
+    _fields_ = [("type", C.c_int32), ("batch", C.c_int32), ("n_layers", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("page_table", C.c_void_p), ("seq_len", C.c_void_p)]
+
+
+class LogitsRules(C.Structure):
+    _fields_ = [("params", C.c_void_p), ("history", C.c_void_p), ("history_stride", C.c_int64), ("history_len", C.c_void_p),
+                ("prompt_len", C.c_void_p), ("cu_bias", C.c_void_p), ("bias_id", C.c_void_p), ("bias", C.c_void_p),
+                ("n_bias", C.c_int32), ("mask", C.c_void_p), ("mask_stride", C.c_int64)]
+
+
 EXPORTS = ["dwkv_abi_version", "dwkv_status_str", "dwkv_split_tokens", "dwkv_decode_kernel", "dwkv_workspace_bytes",
            "dwkv_decode_launches", "dwkv_decode", "dwkv_decode_partials", "dwkv_decode_merge",
            "dwkv_static_scratch_bytes", "dwkv_decode_noalloc", "dwkv_route_workspace_bytes", "dwkv_route",
@@ -73,7 +90,8 @@ EXPORTS = ["dwkv_abi_version", "dwkv_status_str", "dwkv_split_tokens", "dwkv_dec
            "dwkv_dense_decode", "dwkv_residual_map",
            "dwkv_validate_workspace_bytes", "dwkv_validate", "dwkv_hbm_read_blocks", "dwkv_hbm_read",
            "dwkv_tree_workspace_bytes", "dwkv_tree_decode", "dwkv_tree_verify_workspace_bytes", "dwkv_tree_verify",
-           "dwkv_repack_workspace_bytes", "dwkv_repack"]
+           "dwkv_repack_workspace_bytes", "dwkv_repack", "dwkv_rope_freqs", "dwkv_rope", "dwkv_page_append",
+           "dwkv_page_workspace_bytes", "dwkv_page_decode", "dwkv_logits_workspace_bytes", "dwkv_logits"]
 
 _lib = None
 
@@ -193,6 +211,25 @@ def load(path: str = LIB_PATH):
     lib.dwkv_repack.restype = C.c_int
     lib.dwkv_repack.argtypes = [P(Dims), P(Cache), P(Dims), P(Cache), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                 C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.dwkv_rope_freqs.restype = C.c_int
+    lib.dwkv_rope_freqs.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
+                                    P(C.c_double)]
+    lib.dwkv_rope.restype = C.c_int
+    lib.dwkv_rope.argtypes = [C.c_int64, C.c_int32, C.c_int32, P(RopeTable), C.c_int32, C.c_void_p, C.c_int32, C.c_int64,
+                              C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]
+    lib.dwkv_page_append.restype = C.c_int
+    lib.dwkv_page_append.argtypes = [P(Pages), C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64,
+                                     C.c_void_p, C.c_int64, C.c_int32, P(RopeTable), C.c_void_p, C.c_void_p, C.c_void_p]
+    lib.dwkv_page_workspace_bytes.restype = C.c_size_t
+    lib.dwkv_page_workspace_bytes.argtypes = [P(Pages), C.c_int32]
+    lib.dwkv_page_decode.restype = C.c_int
+    lib.dwkv_page_decode.argtypes = [P(Pages), C.c_int32, C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_int32, C.c_void_p,
+                                     C.c_void_p, C.c_size_t, C.c_void_p]
+    lib.dwkv_logits_workspace_bytes.restype = C.c_size_t
+    lib.dwkv_logits_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+    lib.dwkv_logits.restype = C.c_int
+    lib.dwkv_logits.argtypes = [C.c_int32, P(Tree), C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_int64, P(LogitsRules),
+                                C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
     _lib = lib
     return lib
 

@@ -21,7 +21,7 @@ LIB = os.path.join(LIB_DIR, "libdwkv.so")
 ARCH = "gfx950"
 
 SOURCES = ["decode.hip", "decode_tl.hip", "aux.hip", "compress.hip", "dense.hip", "features.hip", "sketch.hip", "stream.hip", "tree.hip", "tree_bf16.hip",
-           "verify.hip", "repack.hip", "api.hip"]
+           "verify.hip", "repack.hip", "rope.hip", "pages.hip", "logits.hip", "api.hip"]
 # -packed-fp32-ops: never emit packed fp32 VALU ops (v_pk_{add,mul,fma}_f32)
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-I", INCLUDE, "-I", CSRC,
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-result"]

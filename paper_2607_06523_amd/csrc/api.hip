@@ -1551,3 +1551,285 @@ dwkv_status dwkv_repack(const dwkv_dims* dst, const dwkv_cache* to, const dwkv_d
 }
 
 }  // extern "C"
+
+namespace {
+
+bool number_type(int32_t t) { return t == DWKV_F16 || t == DWKV_BF16 || t == DWKV_F32; }
+
+dwkv_status check_rope(const dwkv_rope_table* t, int32_t head_dim) {
+  if (t->n_pairs < 1 || t->n_pairs > head_dim / 2) return DWKV_E_DIMS;
+  if (!t->freq) return DWKV_E_NULL;
+  if (reinterpret_cast<uintptr_t>(t->freq) & 7u) return DWKV_E_ALIGN;
+  return DWKV_OK;
+}
+
+RopeSpec rope_spec(const dwkv_rope_table* t, bool inverse) {
+  RopeSpec s;
+  std::memset(&s, 0, sizeof(s));
+  if (!t) return s;
+  s.freq = t->freq;
+  s.n_pairs = t->n_pairs;
+  s.interleaved = t->interleaved != 0;
+  s.inverse = inverse;
+  s.scale = t->scale;
+  return s;
+}
+
+// Rows of `width` elements, `stride` apart (0: no gap).
+bool row_stride(int64_t& stride, int64_t width) {
+  if (stride == 0) stride = width;
+  return stride >= width && stride % 8 == 0;
+}
+
+constexpr int64_t kMostRows = (int64_t)1 << 27;
+
+dwkv_status check_pages(const dwkv_pages* p) {
+  if (!p) return DWKV_E_NULL;
+  if (p->batch < 1 || p->n_layers < 1 || p->n_kv_heads < 1 || p->n_pages < 1 || p->max_pages < 1 || p->page_size < 1 || p->head_dim < 1)
+    return DWKV_E_DIMS;
+  if (p->type != DWKV_F16 && p->type != DWKV_BF16) return DWKV_E_UNSUPPORTED;
+  if (p->head_dim % 32 != 0 || p->head_dim > 256) return DWKV_E_UNSUPPORTED;
+  if (p->page_size < 16 || (p->page_size & (p->page_size - 1)) != 0) return DWKV_E_UNSUPPORTED;
+  if (p->batch > kPageMaxBatch || p->n_kv_heads > 65535) return DWKV_E_UNSUPPORTED;
+  // a token's place and a page's elements are 32-bit numbers
+  if ((int64_t)p->max_pages * p->page_size > 0x7fffffff - 64) return DWKV_E_UNSUPPORTED;
+  if ((int64_t)p->page_size * p->head_dim > 0x3fffffff) return DWKV_E_UNSUPPORTED;
+  if (!p->k || !p->v || !p->page_table || !p->seq_len) return DWKV_E_NULL;
+  if (!aligned16(p->k) || !aligned16(p->v) || !aligned4(p->page_table) || !aligned4(p->seq_len)) return DWKV_E_ALIGN;
+  return DWKV_OK;
+}
+
+int page_shift(const dwkv_pages* p) {
+  int s = 0;
+  while ((16 << s) < p->page_size) ++s;
+  return s;
+}
+
+// Elements of one layer's keys (or values).
+int64_t page_layer(const dwkv_pages* p) { return (int64_t)p->n_pages * p->n_kv_heads * p->page_size * p->head_dim; }
+
+dwkv_status check_page_heads(const dwkv_pages* p, int32_t n_q_heads) {
+  if (n_q_heads < 1 || n_q_heads % p->n_kv_heads != 0) return DWKV_E_DIMS;
+  if (n_q_heads > 65535) return DWKV_E_UNSUPPORTED;
+  // the list of tiles of every sequence, KV head and block of 16 heads
+  const int64_t group = n_q_heads / p->n_kv_heads, tiles = ((int64_t)p->max_pages * p->page_size + kPageTile - 1) / kPageTile + 1;
+  const double list = (double)p->batch * tiles * p->n_kv_heads * (double)((group + 15) / 16);
+  if (list >= 2147483647.0 - 4.0 * kPageWG * kPageWaves) return DWKV_E_UNSUPPORTED;
+  return DWKV_OK;
+}
+
+struct PageWs {
+  size_t plan, total;
+};
+PageWs page_ws(const dwkv_pages* p, int32_t n_q_heads) {
+  PageWs w;
+  const size_t rows = std::min(n_q_heads / p->n_kv_heads, 16);
+  w.plan = align_up((size_t)2 * kPageWG * kPageWaves * rows * (p->head_dim + 4) * sizeof(float), 256);
+  w.total = w.plan + align_up(((size_t)p->batch + 1) * sizeof(int32_t), 256);
+  return w;
+}
+
+}  // namespace
+
+extern "C" {
+
+dwkv_status dwkv_rope_freqs(int32_t n_pairs, double base, int32_t scaling, double factor, double context, double low,
+                            double high, double* freq_host) {
+  if (!freq_host) return DWKV_E_NULL;
+  if (n_pairs < 1 || !(base > 0.0) || !std::isfinite(base) || scaling < DWKV_ROPE_PLAIN || scaling > DWKV_ROPE_RAMP) return DWKV_E_DIMS;
+  if (scaling != DWKV_ROPE_PLAIN && (!(factor > 0.0) || !std::isfinite(factor))) return DWKV_E_DIMS;
+  if (scaling == DWKV_ROPE_RAMP && (!(context > 0.0) || !std::isfinite(context) || !(low < high) || !std::isfinite(high - low)))
+    return DWKV_E_DIMS;
+  if (scaling == DWKV_ROPE_BASE && n_pairs > 1) base *= std::pow(factor, (double)n_pairs / (n_pairs - 1));
+  for (int32_t i = 0; i < n_pairs; ++i) {
+    double f = std::pow(base, -(double)i / n_pairs);
+    if (scaling == DWKV_ROPE_LINEAR) f /= factor;
+    if (scaling == DWKV_ROPE_RAMP) {
+      const double turns = context * f / 6.283185307179586476925;
+      const double s = std::min(1.0, std::max(0.0, (turns - low) / (high - low)));
+      f = s * f + (1.0 - s) * f / factor;
+    }
+    freq_host[i] = f;
+  }
+  return DWKV_OK;
+}
+
+dwkv_status dwkv_rope(int64_t n_rows, int32_t n_heads, int32_t head_dim, const dwkv_rope_table* table, int32_t inverse,
+                      const void* x, int32_t x_type, int64_t x_stride, const int32_t* pos, void* out, int32_t out_type,
+                      int64_t out_stride, void* stream) {
+  if (!table) return DWKV_E_NULL;
+  if (n_rows < 0 || n_heads < 1 || head_dim < 1) return DWKV_E_DIMS;
+  if (!number_type(x_type) || !number_type(out_type)) return DWKV_E_DIMS;
+  if (head_dim % 8 != 0 || head_dim > 512 || n_heads > 65535 || n_rows > kMostRows) return DWKV_E_UNSUPPORTED;
+  const dwkv_status st = check_rope(table, head_dim);
+  if (st != DWKV_OK) return st;
+  const int64_t width = (int64_t)n_heads * head_dim;
+  if (!row_stride(x_stride, width) || !row_stride(out_stride, width)) return DWKV_E_DIMS;
+  if (n_rows == 0) return DWKV_OK;
+  if (!x || !pos || !out) return DWKV_E_NULL;
+  if (!aligned16(x) || !aligned16(out) || !aligned4(pos)) return DWKV_E_ALIGN;
+  if (x == out && (x_type != out_type || x_stride != out_stride)) return DWKV_E_DIMS;   // in place: element by element
+  RopeArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.t = rope_spec(table, inverse != 0);
+  a.x = x;
+  a.out = out;
+  a.pos = pos;
+  a.n_rows = n_rows;
+  a.x_stride = x_stride;
+  a.out_stride = out_stride;
+  a.n_heads = n_heads;
+  a.d = head_dim;
+  return hip_status(launch_rope(a, x_type, out_type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+dwkv_status dwkv_page_append(const dwkv_pages* p, int32_t layer, int32_t n_rows, const int32_t* cu_new, const void* k,
+                             const void* v, int32_t x_type, int64_t kv_stride, const void* q, int64_t q_stride,
+                             int32_t n_q_heads, const dwkv_rope_table* table, const int32_t* pos, void* q_out, void* stream) {
+  dwkv_status st = check_pages(p);
+  if (st != DWKV_OK) return st;
+  if (layer < 0 || layer >= p->n_layers || n_rows < 0 || !number_type(x_type)) return DWKV_E_DIMS;
+  if (!cu_new && n_rows != p->batch) return DWKV_E_DIMS;
+  if (n_rows > kMostRows) return DWKV_E_UNSUPPORTED;
+  if (table && (st = check_rope(table, p->head_dim)) != DWKV_OK) return st;
+  if (!row_stride(kv_stride, (int64_t)p->n_kv_heads * p->head_dim)) return DWKV_E_DIMS;
+  if (q) {
+    if (n_q_heads < 1) return DWKV_E_DIMS;
+    if (n_q_heads > 65535) return DWKV_E_UNSUPPORTED;
+    if (!row_stride(q_stride, (int64_t)n_q_heads * p->head_dim)) return DWKV_E_DIMS;
+  }
+  if (n_rows == 0) return DWKV_OK;
+  if (!k || !v || (q && !q_out)) return DWKV_E_NULL;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || !aligned4(cu_new) || !aligned4(pos)) return DWKV_E_ALIGN;
+  AppendArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.t = rope_spec(table, false);
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_pages = static_cast<uint16_t*>(p->k) + layer * page_layer(p);
+  a.v_pages = static_cast<uint16_t*>(p->v) + layer * page_layer(p);
+  a.cu_new = cu_new;
+  a.pos = pos;
+  a.table = p->page_table;
+  a.len = p->seq_len;
+  a.q_stride = q_stride;
+  a.kv_stride = kv_stride;
+  a.n_rows = n_rows;
+  a.batch = p->batch;
+  a.n_q_heads = q ? n_q_heads : 0;
+  a.n_kv_heads = p->n_kv_heads;
+  a.d = p->head_dim;
+  a.n_pages = p->n_pages;
+  a.max_pages = p->max_pages;
+  a.page_shift = page_shift(p);
+  return hip_status(launch_append(a, x_type, p->type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+size_t dwkv_page_workspace_bytes(const dwkv_pages* pages, int32_t n_q_heads) {
+  if (check_pages(pages) != DWKV_OK || check_page_heads(pages, n_q_heads) != DWKV_OK) return 0;
+  return page_ws(pages, n_q_heads).total;
+}
+
+dwkv_status dwkv_page_decode(const dwkv_pages* p, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,
+                             float sm_scale, int32_t window, float* out, void* workspace, size_t ws_bytes, void* stream) {
+  dwkv_status st = check_pages(p);
+  if (st != DWKV_OK) return st;
+  if ((st = check_page_heads(p, n_q_heads)) != DWKV_OK) return st;
+  if (layer < 0 || layer >= p->n_layers || window < 0) return DWKV_E_DIMS;
+  if (!row_stride(q_stride, (int64_t)n_q_heads * p->head_dim)) return DWKV_E_DIMS;
+  if (!q || !out || !workspace) return DWKV_E_NULL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(workspace)) return DWKV_E_ALIGN;
+  const PageWs w = page_ws(p, n_q_heads);
+  if (ws_bytes < w.total) return DWKV_E_WORKSPACE;
+  PageArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.k = static_cast<const uint16_t*>(p->k) + layer * page_layer(p);
+  a.v = static_cast<const uint16_t*>(p->v) + layer * page_layer(p);
+  a.table = p->page_table;
+  a.len = p->seq_len;
+  a.q = static_cast<const uint16_t*>(q);
+  a.out = out;
+  a.part = static_cast<float*>(workspace);
+  a.plan = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + w.plan);
+  a.q_stride = q_stride;
+  a.batch = p->batch;
+  a.n_kv_heads = p->n_kv_heads;
+  a.group = n_q_heads / p->n_kv_heads;
+  a.n_rb = (a.group + 15) / 16;
+  a.rows = std::min(a.group, 16);
+  a.n_pages = p->n_pages;
+  a.max_pages = p->max_pages;
+  a.page_shift = page_shift(p);
+  a.window = window;
+  a.qscale = (float)((sm_scale > 0.f ? (double)sm_scale : 1.0 / std::sqrt((double)p->head_dim)) * 1.44269504088896340736);
+  return hip_status(launch_page_decode(a, p->head_dim, p->type, reinterpret_cast<hipStream_t>(stream)));
+}
+
+size_t dwkv_logits_workspace_bytes(int32_t n_rows, int32_t vocab) {
+  if (n_rows < 0 || n_rows > 65535 || vocab < 1 || vocab > (1 << 30)) return 0;
+  return align_up(std::max<size_t>(1, (size_t)n_rows * logits_most_runs(vocab)) * sizeof(LogitsPart), 256);
+}
+
+dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, const void* logits,
+                        int32_t l_type, int64_t l_stride, const dwkv_logits_rules* r, int32_t probs, void* out,
+                        int32_t out_type, void* workspace, size_t ws_bytes, void* stream) {
+  if (!r) return DWKV_E_NULL;
+  if (batch < 1 || vocab < 1) return DWKV_E_DIMS;
+  if (tree) {
+    const dwkv_status st = check_tree(tree, batch);
+    if (st != DWKV_OK) return st;
+  }
+  const int32_t n = tree ? tree->n_nodes : batch;
+  if (!number_type(l_type) || !number_type(out_type)) return DWKV_E_DIMS;
+  if (n > 65535 || vocab > (1 << 30)) return DWKV_E_UNSUPPORTED;
+  if (l_stride == 0) l_stride = vocab;
+  if (l_stride < vocab) return DWKV_E_DIMS;
+  if (r->history && (r->history_stride < 0 || r->history_stride > 0x7fffffff - 4096)) return DWKV_E_DIMS;
+  if (r->bias && r->n_bias < 0) return DWKV_E_DIMS;
+  if (r->bias && r->n_bias > 0x7fffffff - 4096) return DWKV_E_UNSUPPORTED;
+  if (r->mask && r->mask_stride < (vocab + 31) / 32) return DWKV_E_DIMS;
+  if ((r->history && !r->history_len) || (r->bias && (!r->cu_bias || !r->bias_id))) return DWKV_E_NULL;
+  if (n == 0) return DWKV_OK;
+  if (!logits || !out || (tree && !token) || (probs && !workspace)) return DWKV_E_NULL;
+  const auto misaligned = [](const void* p, int32_t type) { return reinterpret_cast<uintptr_t>(p) & (type == DWKV_F32 ? 3u : 1u); };
+  if (misaligned(logits, l_type) || misaligned(out, out_type) || !aligned4(token) || !aligned4(r->params) || !aligned4(r->history) ||
+      !aligned4(r->history_len) || !aligned4(r->prompt_len) || !aligned4(r->cu_bias) || !aligned4(r->bias_id) || !aligned4(r->bias) ||
+      !aligned4(r->mask) || (probs && !aligned16(workspace)))
+    return DWKV_E_ALIGN;
+  if (logits == out && (l_type != out_type || l_stride != vocab)) return DWKV_E_DIMS;   // in place: element by element
+  if (probs && ws_bytes < dwkv_logits_workspace_bytes(n, vocab)) return DWKV_E_WORKSPACE;
+  LogitsArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.logits = logits;
+  a.out = out;
+  a.part = static_cast<LogitsPart*>(workspace);
+  if (tree) {
+    a.cu_nodes = tree->cu_nodes;
+    a.parent = tree->parent;
+    a.token = token;
+  }
+  a.params = r->params;
+  if (r->history && r->history_stride > 0) {
+    a.history = r->history;
+    a.history_len = r->history_len;
+    a.prompt_len = r->prompt_len;
+    a.history_stride = r->history_stride;
+  }
+  if (r->bias && r->n_bias > 0) {
+    a.cu_bias = r->cu_bias;
+    a.bias_id = r->bias_id;
+    a.bias = r->bias;
+    a.n_bias = r->n_bias;
+  }
+  a.mask = r->mask;
+  a.mask_stride = r->mask_stride;
+  a.stride = l_stride;
+  a.batch = batch;
+  a.n_rows = n;
+  a.vocab = vocab;
+  return hip_status(launch_logits(a, l_type, out_type, probs != 0, reinterpret_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"

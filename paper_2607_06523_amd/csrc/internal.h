@@ -439,6 +439,80 @@ struct RepackArgs {
 constexpr int kRepackBlock = 1024;   // tokens per workgroup of the offset scan
 hipError_t launch_repack(const RepackArgs& a, hipStream_t s);
 
+// Rotary positions and the append to a paged cache (rope.hip).
+struct RopeSpec {
+  const double* freq;          // [n_pairs] radians per position
+  int32_t n_pairs, interleaved, inverse;
+  float scale;
+};
+struct RopeArgs {
+  RopeSpec t;
+  const void* x;
+  void* out;
+  const int32_t* pos;
+  int64_t n_rows, x_stride, out_stride;
+  int32_t n_heads, d;
+  int32_t chunk;               // heads of a workgroup (launch_rope)
+};
+constexpr int kRopeRows = 16;  // rows of a workgroup
+hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s);
+
+struct AppendArgs {
+  RopeSpec t;                  // n_pairs 0: no rotation
+  const void *q, *k, *v;       // q null: n_q_heads 0
+  void *q_out, *k_pages, *v_pages;   // pages of the layer
+  const int32_t *cu_new;       // [B+1] or null: one row for each sequence
+  const int32_t *pos;          // [N] or null: the slots
+  const int32_t *table, *len;
+  int64_t q_stride, kv_stride;
+  int32_t n_rows, batch, n_q_heads, n_kv_heads, d, n_pages, max_pages;
+  int32_t page_shift;          // a page is 16 << page_shift tokens
+  int32_t chunk;               // heads of a workgroup (launch_append)
+};
+hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s);
+
+// Attention over a paged cache (pages.hip).
+constexpr int kPageWG = 256;       // workgroups of the split pass
+constexpr int kPageWaves = 8;      // waves of each
+constexpr int kPageTile = 32;      // tokens of a wave's step
+constexpr int kPageMaxBatch = 4096;
+struct PageArgs {
+  const uint16_t *k, *v;       // pages of the layer
+  const int32_t *table, *len;
+  const uint16_t* q;
+  float* out;
+  float* part;                 // [2 * waves][rows][d + 2]
+  int32_t* plan;               // [B+1] tiles before each sequence
+  int64_t q_stride;
+  int32_t batch, n_kv_heads, group, n_rb;    // n_rb: blocks of 16 heads of a group
+  int32_t rows;                // min(group, 16)
+  int32_t n_pages, max_pages, page_shift, window;
+  float qscale;                // sm_scale * log2(e)
+};
+hipError_t launch_page_decode(const PageArgs& a, int d, int type, hipStream_t s);
+
+// Rows of logits (logits.hip).
+struct LogitsPart {            // of a run of a row's entries
+  float top, sum;
+  int32_t first;
+};
+struct LogitsArgs {
+  const void* logits;          // n_rows rows, stride apart
+  void* out;                   // [n_rows][vocab]
+  LogitsPart* part;            // [n_rows][n_run]
+  const int32_t *cu_nodes, *parent, *token;   // null: row i is sequence i
+  const float* params;         // [S][4]
+  const int32_t *history, *history_len, *prompt_len;
+  const int32_t *cu_bias, *bias_id;
+  const float* bias;
+  const uint32_t* mask;
+  int64_t stride, history_stride, mask_stride;
+  int32_t batch, n_rows, vocab, n_bias;
+  int32_t run, n_run;          // entries of a workgroup (launch_logits)
+};
+int64_t logits_most_runs(int64_t vocab);
+hipError_t launch_logits(LogitsArgs a, int from, int to, bool probs, hipStream_t s);
+
 // Materialization of one layer's rebuilt keys and values (Eq. 1) as fp16.
 struct MatArgs {
   const uint16_t* basis;       // window m, sequence 0; sequence b adds b*basis_b_stride, (h, z) add (h*2+z)*rb*d

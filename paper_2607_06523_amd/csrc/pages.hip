@@ -1,0 +1,461 @@
+// Attention of one new token per sequence over a paged dense cache, gfx950.
+//
+//   out[b][hq] = sum_t p_t v_t,  p = softmax_t(sm_scale q . k_t)
+// over the tokens t of the last `window` (or all) that sequence b holds in pages.
+// Bound by HBM: 4 d bytes per token and KV head against 4 G d flop, so the products
+// run on 16x16x32 matrix instructions whatever the group is and everything else is
+// about keeping loads in flight.
+//  * Lengths and page tables are device data (a captured graph follows them), so
+//    the work is shared out on the device: tiles of 32 tokens of every (sequence,
+//    KV head, block of 16 heads) in one list, an equal run of it for each wave.
+//  * Keys lie in tiles of 16 tokens x 8 channels and values in blocks of 8 tokens, as
+//    the factorized cache's coefficients do: each wave load covers whole 128-byte lines
+//    and is an operand as it stands.  Scores come out with a lane's head down its
+//    column (tokens 4g + i of either 16); two lane-group swaps turn the probabilities
+//    into the second product's operand (tokens 8g + j).
+//  * Probabilities: the reference leaves a row's largest at 2^9 and moves when one
+//    passes 2^15.5, as 2^9 leaves small ones room in fp16's range.  They enter the
+//    product as two fp16 or three bf16 terms (22 and 24 bits): the values' type has 11
+//    or 8, which would be the output's error.
+//  * A wave writes what it has of a pair that it shares with others as a partial, and
+//    a pair of its own as output; the waves of a workgroup that all work on one
+//    pair join in LDS first.  page_merge_kernel joins the partials.
+#include <algorithm>
+
+#include "internal.h"
+
+namespace dwkv {
+namespace {
+
+constexpr int kPT = 64 * kPageWaves;
+constexpr float kNoRef = -1.7e38f;       // reference of a row without scores
+constexpr float kRefTop = 9.f, kRefMove = 15.5f;
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef __bf16 brain8 __attribute__((ext_vector_type(8)));
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+
+template <int TY>
+__device__ __forceinline__ float4_t product(uint4_t a, uint4_t b, float4_t c) {
+  if constexpr (TY == DWKV_F16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a), __builtin_bit_cast(half8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(brain8, a), __builtin_bit_cast(brain8, b), c, 0, 0, 0);
+}
+
+// Two floats rounded to the type and packed; what is left of them.
+template <int TY>
+__device__ __forceinline__ uint32_t take(float& a, float& b) {
+  if constexpr (TY == DWKV_F16) {
+    typedef _Float16 pair __attribute__((ext_vector_type(2)));
+    const pair p = {(_Float16)a, (_Float16)b};
+    a -= (float)p[0];
+    b -= (float)p[1];
+    return __builtin_bit_cast(uint32_t, p);
+  } else {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    const pair p = {(__bf16)a, (__bf16)b};
+    a -= (float)p[0];
+    b -= (float)p[1];
+    return __builtin_bit_cast(uint32_t, p);
+  }
+}
+
+struct Span {               // tokens of a sequence that its new one attends to
+  int start, len;
+};
+__device__ __forceinline__ Span span_of(const PageArgs& a, int b) {
+  const int64_t room = (int64_t)a.max_pages << (a.page_shift + 4);
+  Span s;
+  s.len = (int)min((int64_t)max(a.len[b], 0), room);
+  s.start = a.window > 0 ? max(0, s.len - a.window) : 0;
+  return s;
+}
+__device__ __forceinline__ int tiles_of(Span s) { return (s.len + kPageTile - 1) / kPageTile - s.start / kPageTile; }
+
+// Slot of the partial that run [x, ...) of wave w writes for the pair that begins at p0.
+__device__ __forceinline__ int slot_of(int w, int x, int p0) { return 2 * w + (x > p0 ? 0 : 1); }
+
+template <int D, int TY>
+__global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
+  constexpr int KS = D / 32, VB = D / 16, PS = D + 4;
+  extern __shared__ __align__(16) float smem[];
+  __shared__ int sums[kPageWaves];
+  float* joined = smem;                                        // [waves][rows][PS]
+  int* pre = reinterpret_cast<int*>(smem + kPageWaves * a.rows * PS);   // [B+1]
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int m = lane & 15, g = lane >> 4;
+
+  // tiles before each sequence
+  int base = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kPT) {
+    const int b = b0 + (int)threadIdx.x;
+    const int n = b < a.batch ? tiles_of(span_of(a, b)) : 0;
+    int inc = n;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(inc, d);
+      if (lane >= d) inc += o;
+    }
+    if (lane == 63) sums[wv] = inc;
+    __syncthreads();
+    int before = base;
+    for (int i = 0; i < kPageWaves; ++i) {
+      if (i < wv) before += sums[i];
+      base += sums[i];
+    }
+    if (b < a.batch) {
+      pre[b + 1] = before + inc;
+      if (blockIdx.x == 0) a.plan[b + 1] = before + inc;
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    pre[0] = 0;
+    if (blockIdx.x == 0) a.plan[0] = 0;
+  }
+  __syncthreads();
+
+  const int pairs = a.n_kv_heads * a.n_rb, total = base * pairs;
+  const int per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
+  const int w = blockIdx.x * kPageWaves + wv;
+  const int wg0 = min(total, (int)blockIdx.x * kPageWaves * per), wg1 = min(total, wg0 + kPageWaves * per);
+  if (wg0 >= wg1) return;
+  int x = min(total, w * per);
+  const int end = min(total, x + per);
+
+  // the sequence that holds list position i: the first with pre[b + 1] * pairs > i
+  const auto seq_at = [&](int i) {
+    int lo = 0, hi = a.batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid + 1] * pairs > i) hi = mid; else lo = mid + 1;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+  };
+  int b = seq_at(wg0);
+  const int wgT = pre[b + 1] - pre[b], wgp = (wg0 - pre[b] * pairs) / wgT;
+  const int wgp0 = __builtin_amdgcn_readfirstlane(pre[b] * pairs + wgp * wgT);
+  const bool join = wg1 <= wgp0 + __builtin_amdgcn_readfirstlane(wgT);    // one pair for the whole workgroup
+
+  float ref = kNoRef, l = 0.f;
+  float4_t o[VB];
+#pragma unroll
+  for (int i = 0; i < VB; ++i) o[i] = 0.f;
+
+  if (x < end) b = seq_at(x);
+  while (x < end) {
+    const int pb = __builtin_amdgcn_readfirstlane(pre[b]), T = __builtin_amdgcn_readfirstlane(pre[b + 1]) - pb;
+    if (T == 0) {
+      ++b;
+      continue;
+    }
+    const int pair = (x - pb * pairs) / T, p0 = pb * pairs + pair * T;
+    if (pair >= pairs) {
+      ++b;
+      continue;
+    }
+    const int n = min(end, p0 + T) - x;
+    const int h = pair / a.n_rb, r0 = (pair - h * a.n_rb) * 16;
+    const Span sp = span_of(a, b);
+    const int sh = a.page_shift + 4;
+    int t0 = (sp.start / kPageTile + (x - p0)) * kPageTile;
+
+    // ids of 64 pages, one a lane
+    const int32_t* row = a.table + (int64_t)b * a.max_pages;
+    int first = t0 >> sh;
+    int ids = first + lane < a.max_pages ? row[first + lane] : -1;
+    const uint16_t* q = a.q + b * a.q_stride + (int64_t)(h * a.group + r0 + m) * D + 8 * g;
+    uint4_t qf[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) qf[i] = r0 + m < a.group ? *reinterpret_cast<const uint4_t*>(q + 32 * i) : 0;
+
+    ref = kNoRef;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < VB; ++i) o[i] = 0.f;
+
+    // where the 16 tokens from t on lie, in elements; -1: nowhere
+    const auto place = [&](int t) -> int64_t {
+      if (t >= sp.len) return -1;
+      const int id = __builtin_amdgcn_readlane(ids, (t >> sh) - first);
+      if ((unsigned)id >= (unsigned)a.n_pages) return -1;
+      return (((int64_t)id * a.n_kv_heads + h) * (1 << sh) + (t & ((1 << sh) - 1))) * D;
+    };
+    uint4_t kf[2][KS], vf[VB];
+    int64_t at0, at1;
+    const auto find = [&](int t) {
+      if (((t + 16) >> sh) - first >= 64) {
+        first = t >> sh;
+        ids = first + lane < a.max_pages ? row[first + lane] : -1;
+      }
+      at0 = place(t);
+      at1 = place(t + 16);
+    };
+    const auto load_k = [&]() {
+      const uint16_t* k0 = a.k + max(at0, (int64_t)0);
+      const uint16_t* k1 = a.k + max(at1, (int64_t)0);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) kf[0][i] = *reinterpret_cast<const uint4_t*>(k0 + (4 * i + g) * 128 + m * 8);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) kf[1][i] = *reinterpret_cast<const uint4_t*>(k1 + (4 * i + g) * 128 + m * 8);
+    };
+    const auto load_v = [&]() {
+      const uint16_t* v0 = a.v + max(g < 2 ? at0 : at1, (int64_t)0) + (g & 1) * 8 * D + m * 8;
+#pragma unroll
+      for (int i = 0; i < VB; ++i) vf[i] = *reinterpret_cast<const uint4_t*>(v0 + i * 128);
+    };
+    find(t0);
+    load_k();
+    load_v();
+
+    for (int i = 0; i < n; ++i, t0 += kPageTile) {
+      const bool here0 = at0 >= 0, here1 = at1 >= 0;
+      const bool whole = here0 && here1 && t0 >= sp.start && t0 + kPageTile <= sp.len;
+      float4_t s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        s0 = product<TY>(kf[0][k], qf[k], s0);
+        s1 = product<TY>(kf[1][k], qf[k], s1);
+      }
+      const bool more = i + 1 < n;
+      if (more) {
+        find(t0 + kPageTile);
+        load_k();
+      }
+      float s[8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[j] = s0[j] * a.qscale;
+        s[4 + j] = s1[j] * a.qscale;
+      }
+      if (!whole) {
+        const int t = t0 + 4 * g;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (!(here0 && t + j >= sp.start && t + j < sp.len)) s[j] = -__builtin_inff();
+          if (!(here1 && t + 16 + j >= sp.start && t + 16 + j < sp.len)) s[4 + j] = -__builtin_inff();
+        }
+      }
+      float top = s[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+      if (__ballot(top > ref + kRefMove)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        if (top > ref + kRefMove) {
+          const float to = top - kRefTop, f = __builtin_amdgcn_exp2f(ref - to);
+          ref = to;
+          l *= f;
+#pragma unroll
+          for (int k = 0; k < VB; ++k) o[k] *= f;
+        }
+      }
+      float p[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        p[j] = __builtin_amdgcn_exp2f(s[j] - ref);
+        l += p[j];
+      }
+      if (!whole) {                    // nothing of a masked token's values counts
+        const int t = t0 + 8 * g;
+        const bool here = g < 2 ? here0 : here1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bool lo = here && t + 2 * j >= sp.start && t + 2 * j < sp.len;
+          const bool hi = here && t + 2 * j + 1 >= sp.start && t + 2 * j + 1 < sp.len;
+          const uint32_t keep = (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
+#pragma unroll
+          for (int k = 0; k < VB; ++k) vf[k][j] &= keep;
+        }
+      }
+#pragma unroll
+      for (int term = 0; term < (TY == DWKV_F16 ? 2 : 3); ++term) {
+        uint4_t pf;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t u = take<TY>(p[2 * j], p[2 * j + 1]), v = take<TY>(p[4 + 2 * j], p[5 + 2 * j]);
+          const auto half = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+          const auto quad = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
+          pf[j] = quad[0];
+          pf[2 + j] = quad[1];
+        }
+#pragma unroll
+        for (int k = 0; k < VB; ++k) o[k] = product<TY>(vf[k], pf, o[k]);
+      }
+      if (more) load_v();
+    }
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (!join && r0 + m < a.group) {
+      if (x == p0 && n == T) {           // a pair of this wave's own
+        float* out = a.out + ((int64_t)b * a.n_kv_heads * a.group + h * a.group + r0 + m) * D + 4 * g;
+        const float f = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+        for (int k = 0; k < VB; ++k) *reinterpret_cast<float4_t*>(out + 16 * k) = o[k] * f;
+      } else {
+        float* part = a.part + ((int64_t)slot_of(w, x, p0) * a.rows + m) * PS;
+#pragma unroll
+        for (int k = 0; k < VB; ++k) *reinterpret_cast<float4_t*>(part + 16 * k + 4 * g) = o[k];
+        if (g == 0) {
+          part[D] = ref;
+          part[D + 1] = l;
+        }
+      }
+    }
+    x += n;
+  }
+  if (!join) return;
+
+  if (m < a.rows) {
+    float* mine = joined + (wv * a.rows + m) * PS;
+#pragma unroll
+    for (int k = 0; k < VB; ++k) *reinterpret_cast<float4_t*>(mine + 16 * k + 4 * g) = o[k];
+    if (g == 0) {
+      mine[D] = ref;
+      mine[D + 1] = l;
+    }
+  }
+  __syncthreads();
+  const int h = wgp / a.n_rb, r0 = (wgp - h * a.n_rb) * 16;
+  const bool own = wg0 == wgp0 && wg1 == wgp0 + wgT;
+  for (int u = threadIdx.x; u < a.rows * (D / 4); u += kPT) {
+    const int r = u / (D / 4), c = (u - r * (D / 4)) * 4;
+    if (r0 + r >= a.group) break;
+    float top = kNoRef;
+    for (int i = 0; i < kPageWaves; ++i) top = fmaxf(top, joined[(i * a.rows + r) * PS + D]);
+    float4_t sum = 0.f;
+    float all = 0.f;
+    for (int i = 0; i < kPageWaves; ++i) {
+      const float* from = joined + (i * a.rows + r) * PS;
+      const float f = __builtin_amdgcn_exp2f(from[D] - top);
+      sum += *reinterpret_cast<const float4_t*>(from + c) * f;
+      all += from[D + 1] * f;
+    }
+    if (own) {
+      const float f = all > 0.f || all != all ? 1.f / all : 0.f;
+      *reinterpret_cast<float4_t*>(a.out + ((int64_t)b * a.n_kv_heads * a.group + h * a.group + r0 + r) * D + c) = sum * f;
+    } else {
+      float* part = a.part + ((int64_t)slot_of(blockIdx.x * kPageWaves, wg0, wgp0) * a.rows + r) * PS;
+      *reinterpret_cast<float4_t*>(part + c) = sum;
+      if (c == 0) {
+        part[D] = top;
+        part[D + 1] = all;
+      }
+    }
+  }
+}
+
+// grid (query heads, B): joins the partials of a pair that several waves shared.
+template <int D>
+__global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
+  constexpr int PS = D + 4, LN = D / 4, NG = 256 / LN;
+  constexpr int kMost = kPageWG + 4 * kPageWaves;            // partials of a pair
+  __shared__ float factor[kMost];
+  __shared__ float red[2][4];
+  __shared__ __align__(16) float sums[NG][D];
+  const int b = blockIdx.y, hq = blockIdx.x, h = hq / a.group, r = hq - h * a.group;
+  const int pairs = a.n_kv_heads * a.n_rb, total = a.plan[a.batch] * pairs;
+  const int pb = a.plan[b], T = a.plan[b + 1] - pb;
+  float* out = a.out + ((int64_t)b * gridDim.x + hq) * D;
+  if (T == 0) {
+    if (threadIdx.x < D) out[threadIdx.x] = 0.f;
+    return;
+  }
+  const int per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
+  const int p0 = pb * pairs + (h * a.n_rb + r / 16) * T, p1 = p0 + T;
+  const int w0 = p0 / per, w1 = (p1 - 1) / per;
+  if (w0 == w1) return;                                      // written by its wave
+  const int g0 = w0 / kPageWaves, g1 = w1 / kPageWaves;
+  const auto joined = [&](int g) {
+    const int x = g * kPageWaves * per;
+    return x >= p0 && min(total, x + kPageWaves * per) <= p1;
+  };
+  const bool j0 = joined(g0), j1 = joined(g1);
+  if (g0 == g1 && j0) return;                                // written by its workgroup
+  const int n0 = j0 ? 1 : min(w1, g0 * kPageWaves + kPageWaves - 1) - w0 + 1, mid = max(0, g1 - g0 - 1);
+  const int n = n0 + mid + (g1 == g0 ? 0 : j1 ? 1 : w1 - g1 * kPageWaves + 1);
+  const auto partial = [&](int i) -> const float* {
+    int slot;
+    if (i < n0) slot = j0 ? 2 * g0 * kPageWaves + 1 : 2 * (w0 + i) + (i == 0);
+    else if (i < n0 + mid) slot = 2 * (g0 + 1 + i - n0) * kPageWaves;
+    else slot = 2 * (g1 * kPageWaves + (i - n0 - mid));
+    return a.part + ((int64_t)slot * a.rows + (r & 15)) * PS;
+  };
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  float ref[2], l[2], top = kNoRef;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    ref[k] = kNoRef;
+    l[k] = 0.f;
+    if (i < n) {
+      const float2 v = *reinterpret_cast<const float2*>(partial(i) + D);
+      ref[k] = v.x;
+      l[k] = v.y;
+    }
+    top = fmaxf(top, ref[k]);
+  }
+  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) red[0][wv] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+  float all = 0.f;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    if (i < n) {
+      const float f = __builtin_amdgcn_exp2f(ref[k] - top);
+      factor[i] = f;
+      all += l[k] * f;
+    }
+  }
+  for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
+  if (lane == 0) red[1][wv] = all;
+  __syncthreads();
+  all = red[1][0] + red[1][1] + red[1][2] + red[1][3];
+  const int c = threadIdx.x % LN, k = threadIdx.x / LN;
+  float4_t sum = 0.f;
+  if (k < NG) {
+#pragma unroll 4
+    for (int i = k; i < n; i += NG) sum += *reinterpret_cast<const float4_t*>(partial(i) + 4 * c) * factor[i];
+    *reinterpret_cast<float4_t*>(&sums[k][4 * c]) = sum;
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float v = 0.f;
+    for (int i = 0; i < NG; ++i) v += sums[i][threadIdx.x];
+    out[threadIdx.x] = all > 0.f || all != all ? v / all : 0.f;
+  }
+}
+
+template <int D>
+hipError_t launch_d(const PageArgs& a, int type, hipStream_t s) {
+  const size_t lds = ((size_t)kPageWaves * a.rows * (D + 4) + a.batch + 1) * sizeof(float);
+  const void* k = type == DWKV_F16 ? (const void*)page_split_kernel<D, DWKV_F16> : (const void*)page_split_kernel<D, DWKV_BF16>;
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  if (type == DWKV_F16) hipLaunchKernelGGL((page_split_kernel<D, DWKV_F16>), dim3(kPageWG), dim3(kPT), lds, s, a);
+  else hipLaunchKernelGGL((page_split_kernel<D, DWKV_BF16>), dim3(kPageWG), dim3(kPT), lds, s, a);
+  hipLaunchKernelGGL((page_merge_kernel<D>), dim3(a.n_kv_heads * a.group, a.batch), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_page_decode(const PageArgs& a, int d, int type, hipStream_t s) {
+  switch (d) {
+    case 32: return launch_d<32>(a, type, s);
+    case 64: return launch_d<64>(a, type, s);
+    case 96: return launch_d<96>(a, type, s);
+    case 128: return launch_d<128>(a, type, s);
+    case 160: return launch_d<160>(a, type, s);
+    case 192: return launch_d<192>(a, type, s);
+    case 224: return launch_d<224>(a, type, s);
+    default: return launch_d<256>(a, type, s);
+  }
+}
+
+}  // namespace dwkv

@@ -1,0 +1,359 @@
+// Rotary positions, and new tokens into the pages of a dense cache, gfx950.
+//
+// Pair i of a head at position p turns by the angle p f_i:
+//   a' = m (a cos - b sin),  b' = m (b cos + a sin).
+// Angles are float64: at position 2^20 a float32 angle is off by 2^-4.  Each
+// workgroup takes 16 rows and works their sines and cosines out once, into LDS (16
+// rows x 64 pairs, against 16 x 64 x 40 rotations that read them), with the Taylor
+// polynomials on [-pi/4, pi/4]; then its threads stream pieces of 16 bytes.
+#include <algorithm>
+
+#include "internal.h"
+#include "rows_dev.h"
+
+namespace dwkv {
+namespace {
+
+constexpr int kRT = 256;                 // threads of a workgroup
+constexpr int kRows = kRopeRows;         // rows of a workgroup
+
+enum Pairs { HALF = 0, HALF_ODD = 1, NEXT = 2 };   // (i, n + i), n a multiple of 8 or not; (2i, 2i + 1)
+
+// sin and cos of x.  x - n pi/2 in two steps (n pi/2's upper part is exact in the
+// fused product), then Taylor to x^13 and x^14: below 2^-45 on [-pi/4, pi/4].
+__device__ __forceinline__ void sin_cos(double x, double& s, double& c) {
+  const double n = __builtin_rint(x * 0.63661977236758134308);
+  double r = __builtin_fma(n, -1.57079632679489655800, x);
+  r = __builtin_fma(n, -6.12323399573676603587e-17, r);
+  const double z = r * r;
+  double p = 1.0 / 6227020800.0;
+  p = __builtin_fma(p, z, -1.0 / 39916800.0);
+  p = __builtin_fma(p, z, 1.0 / 362880.0);
+  p = __builtin_fma(p, z, -1.0 / 5040.0);
+  p = __builtin_fma(p, z, 1.0 / 120.0);
+  p = __builtin_fma(p, z, -1.0 / 6.0);
+  p = __builtin_fma(p * z, r, r);
+  double q = -1.0 / 87178291200.0;
+  q = __builtin_fma(q, z, 1.0 / 479001600.0);
+  q = __builtin_fma(q, z, -1.0 / 3628800.0);
+  q = __builtin_fma(q, z, 1.0 / 40320.0);
+  q = __builtin_fma(q, z, -1.0 / 720.0);
+  q = __builtin_fma(q, z, 1.0 / 24.0);
+  q = __builtin_fma(q, z, -0.5);
+  q = __builtin_fma(q, z, 1.0);
+  const int k = (int)(long long)n & 3;
+  const double u = k & 1 ? q : p, v = k & 1 ? p : q;
+  s = k & 2 ? -u : u;
+  c = (k + 1) & 2 ? -v : v;
+}
+
+// (cos, sin) of row r's pair i at cs[r * n_pairs + i], already scaled.
+__device__ __forceinline__ void fill_table(float2* cs, const RopeSpec& t, const int* pos, int rows) {
+  for (int u = threadIdx.x; u < rows * t.n_pairs; u += kRT) {
+    const int r = u / t.n_pairs, i = u - r * t.n_pairs;
+    double s, c;
+    sin_cos((double)pos[r] * t.freq[i], s, c);
+    cs[u] = make_float2((float)(c * t.scale), (float)(s * (t.inverse ? -(double)t.scale : (double)t.scale)));
+  }
+}
+
+__device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
+  const float x = a, y = b;
+  a = __builtin_fmaf(x, cs.x, -(y * cs.y));
+  b = __builtin_fmaf(y, cs.x, x * cs.y);
+}
+
+// A head falls into pieces of eight pairs, or of eight channels that are copied.
+// Neighbouring pairs: eight channels a piece.  Halves: eight pairs a piece (16
+// channels), then the rest eight channels a piece.
+template <int P>
+__device__ __forceinline__ int pieces(int d, int np) {
+  return P == NEXT ? d / 8 : (np + 7) / 8 + (d - 2 * np + 7) / 8;
+}
+
+// Piece a of a head: its channels from x, turned, to put(channel, eight numbers)
+// (16-byte pieces) or put1(channel, number).
+template <int P, int TI, class Put, class Put1>
+__device__ __forceinline__ void turn_piece(const row_t<TI>* x, int a, int d, int np, const float2* cs, Put put, Put1 put1) {
+  if constexpr (P == NEXT) {
+    float8_t v = load8<TI>(x + 8 * a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * a + i < np) {
+        float lo = v[2 * i], hi = v[2 * i + 1];
+        turn(lo, hi, cs[4 * a + i]);
+        v[2 * i] = lo;
+        v[2 * i + 1] = hi;
+      }
+    put(8 * a, v);
+  } else if constexpr (P == HALF) {
+    if (8 * a < np) {
+      float8_t lo = load8<TI>(x + 8 * a), hi = load8<TI>(x + np + 8 * a);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float u = lo[i], v = hi[i];
+        turn(u, v, cs[8 * a + i]);
+        lo[i] = u;
+        hi[i] = v;
+      }
+      put(8 * a, lo);
+      put(np + 8 * a, hi);
+    } else {
+      const int c = 8 * a + np;
+      put(c, load8<TI>(x + c));
+    }
+  } else {                               // channels one at a time
+    const int turned = (np + 7) / 8;
+    if (a < turned) {
+      for (int i = 8 * a; i < np && i < 8 * a + 8; ++i) {
+        float u = (float)x[i], v = (float)x[np + i];
+        turn(u, v, cs[i]);
+        put1(i, u);
+        put1(np + i, v);
+      }
+    } else {
+      for (int c = 2 * np + 8 * (a - turned); c < d && c < 2 * np + 8 * (a - turned) + 8; ++c) put1(c, (float)x[c]);
+    }
+  }
+}
+
+// grid (rows / 16, head chunks)
+template <int P, int TI, int TO>
+__global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
+  extern __shared__ __align__(16) float2 cs[];
+  __shared__ int pos[kRows];
+  const int64_t r0 = (int64_t)blockIdx.x * kRows;
+  const int rows = (int)min((int64_t)kRows, a.n_rows - r0);
+  const int h0 = blockIdx.y * a.chunk, nh = min(a.chunk, a.n_heads - h0);
+  if (threadIdx.x < rows) pos[threadIdx.x] = a.pos[r0 + threadIdx.x];
+  __syncthreads();
+  fill_table(cs, a.t, pos, rows);
+  __syncthreads();
+  const int np = a.t.n_pairs, A = pieces<P>(a.d, np), per = A * nh;
+  const row_t<TI>* x = static_cast<const row_t<TI>*>(a.x);
+  row_t<TO>* out = static_cast<row_t<TO>*>(a.out);
+  for (int u = threadIdx.x; u < rows * per; u += kRT) {
+    const int r = u / per, w = u - r * per, h = w / A, p = w - h * A;
+    row_t<TO>* y = out + (r0 + r) * a.out_stride + (int64_t)(h0 + h) * a.d;
+    turn_piece<P, TI>(
+        x + (r0 + r) * a.x_stride + (int64_t)(h0 + h) * a.d, p, a.d, np, cs + r * np,
+        [&](int c, float8_t v) { store8<TO>(y + c, v); }, [&](int c, float v) { y[c] = (row_t<TO>)v; });
+  }
+}
+
+template <int P, int TI>
+void rope_out(const RopeArgs& a, int to, dim3 g, size_t lds, hipStream_t s) {
+  switch (to) {
+    case DWKV_F32: hipLaunchKernelGGL((rope_kernel<P, TI, DWKV_F32>), g, dim3(kRT), lds, s, a); break;
+    case DWKV_F16: hipLaunchKernelGGL((rope_kernel<P, TI, DWKV_F16>), g, dim3(kRT), lds, s, a); break;
+    default: hipLaunchKernelGGL((rope_kernel<P, TI, DWKV_BF16>), g, dim3(kRT), lds, s, a); break;
+  }
+}
+
+template <int P>
+void rope_in(const RopeArgs& a, int from, int to, dim3 g, size_t lds, hipStream_t s) {
+  switch (from) {
+    case DWKV_F32: rope_out<P, DWKV_F32>(a, to, g, lds, s); break;
+    case DWKV_F16: rope_out<P, DWKV_F16>(a, to, g, lds, s); break;
+    default: rope_out<P, DWKV_BF16>(a, to, g, lds, s); break;
+  }
+}
+
+// ---- append ------------------------------------------------------------------------
+// A workgroup takes the new rows that fall into 16 consecutive slots of one
+// sequence (aligned to 16: a tile of keys, two blocks of values) and a chunk of the
+// row's heads: queries, then keys, then values.
+
+// The sequence and the first of its 16-slot groups that workgroup w takes; false
+// past the last.  A group is counted for every 16 slots that hold a new row.
+struct Group {
+  int seq, first;          // first: slot / 16
+};
+__device__ __forceinline__ bool find_group(const AppendArgs& a, int w, Group& g) {
+  __shared__ int found[2];
+  __shared__ int sums[kRT / 64];
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  if (threadIdx.x == 0) found[0] = -1;
+  int base = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kRT) {
+    const int b = b0 + threadIdx.x;
+    int n = 0, first = 0;
+    if (b < a.batch) {
+      const int rows = a.cu_new[b + 1] - a.cu_new[b], end = a.len[b];
+      if (rows > 0) {
+        first = (int)(((int64_t)end - rows) >> 4);
+        n = ((end - 1) >> 4) - first + 1;
+      }
+    }
+    int inc = n;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(inc, d);
+      if (lane >= d) inc += o;
+    }
+    if (lane == 63) sums[wv] = inc;
+    __syncthreads();
+    int before = base, total = 0;
+    for (int i = 0; i < kRT / 64; ++i) {
+      if (i < wv) before += sums[i];
+      total += sums[i];
+    }
+    const int at = before + inc - n;
+    if (w >= at && w < at + n) {
+      found[0] = b;
+      found[1] = first + (w - at);
+    }
+    __syncthreads();
+    base += total;
+    if (base > w) break;
+  }
+  g.seq = found[0];
+  g.first = found[1];
+  return g.seq >= 0;
+}
+
+template <int P, int TI, int TC>
+__global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
+  extern __shared__ __align__(16) float2 cs[];
+  __shared__ int pos[kRows];
+  Group g;
+  int r0, end, slot0;                    // rows [r0, end) of the packed rows, r0 at slot slot0
+  if (a.cu_new) {
+    if (!find_group(a, blockIdx.x, g)) return;
+    const int c0 = a.cu_new[g.seq], c1 = a.cu_new[g.seq + 1];
+    const int64_t start = (int64_t)a.len[g.seq] - (c1 - c0), s0 = (int64_t)g.first * 16;
+    slot0 = (int)max(start, s0);
+    r0 = c0 + (int)(slot0 - start);
+    end = c0 + (int)(min(start + (c1 - c0), s0 + 16) - start);
+    if (r0 < 0 || end <= r0 || end > a.n_rows) return;          // starts that do not fit the rows
+  } else {                               // one row for each sequence
+    g.seq = blockIdx.x;
+    slot0 = a.len[g.seq] - 1;
+    r0 = blockIdx.x;
+    end = r0 + 1;
+  }
+  const int rows = end - r0, off = slot0 & 15;
+  const int np = a.t.n_pairs, d = a.d;
+  if (np > 0) {
+    if (threadIdx.x < rows) pos[threadIdx.x] = a.pos ? a.pos[r0 + threadIdx.x] : slot0 + (int)threadIdx.x;
+    __syncthreads();
+    fill_table(cs, a.t, pos, rows);
+  }
+  __syncthreads();
+  const int hq = a.n_q_heads, hk = a.n_kv_heads;
+  const int c0 = blockIdx.y * a.chunk, c1 = min(c0 + a.chunk, hq + 2 * hk);
+  const int A = pieces<P>(d, np);
+  if (c0 < hq) {                         // queries: rows of the output
+    const int nh = min(c1, hq) - c0, per = A * nh;
+    const row_t<TI>* x = static_cast<const row_t<TI>*>(a.q) + (int64_t)c0 * d;
+    row_t<TC>* out = static_cast<row_t<TC>*>(a.q_out) + (int64_t)c0 * d;
+    for (int u = threadIdx.x; u < rows * per; u += kRT) {
+      const int r = u / per, w = u - r * per, h = w / A, p = w - h * A;
+      row_t<TC>* y = out + ((int64_t)(r0 + r) * hq + h) * d;
+      turn_piece<P, TI>(
+          x + (r0 + r) * a.q_stride + (int64_t)h * d, p, d, np, cs + r * np, [&](int c, float8_t v) { store8<TC>(y + c, v); },
+          [&](int c, float v) { y[c] = (row_t<TC>)v; });
+    }
+  }
+  // the page of these slots: rows without one are not stored
+  const int page = 16 << a.page_shift;
+  const int64_t room = (int64_t)a.max_pages * page;
+  int id = -1;
+  if (slot0 >= 0 && slot0 < room) id = a.table[(int64_t)g.seq * a.max_pages + (slot0 >> (a.page_shift + 4))];
+  if (id < 0 || id >= a.n_pages) return;
+  const int t0 = slot0 & (page - 1) & ~15;                 // the group's place in its page
+  const int64_t at = ((int64_t)id * hk * page + t0) * d;     // of KV head 0
+  if (c1 > hq && c0 < hq + hk) {         // keys: [d/8][16][8] of the tile
+    const int k0 = max(c0, hq) - hq, nh = min(c1, hq + hk) - hq - k0, per = rows * A;
+    const row_t<TI>* x = static_cast<const row_t<TI>*>(a.k);
+    row_t<TC>* tile = static_cast<row_t<TC>*>(a.k_pages) + at;
+    for (int u = threadIdx.x; u < nh * per; u += kRT) {
+      const int h = u / per + k0, w = u % per, p = w / rows, r = w - p * rows;
+      row_t<TC>* y = tile + (int64_t)h * page * d + (off + r) * 8;
+      turn_piece<P, TI>(
+          x + (int64_t)(r0 + r) * a.kv_stride + (int64_t)h * d, p, d, np, cs + r * np,
+          [&](int c, float8_t v) { store8<TC>(y + c * 16, v); },
+          [&](int c, float v) { y[(c >> 3) * 128 + (c & 7)] = (row_t<TC>)v; });
+    }
+  }
+  if (c1 > hq + hk) {                    // values: two blocks of [d][8], eight channels of eight tokens a piece
+    const int v0 = max(c0, hq + hk) - hq - hk, nh = c1 - hq - hk - v0, D8 = d / 8;
+    const row_t<TI>* x = static_cast<const row_t<TI>*>(a.v);
+    row_t<TC>* blocks = static_cast<row_t<TC>*>(a.v_pages) + at;
+    for (int u = threadIdx.x; u < 2 * nh * D8; u += kRT) {
+      const int p = u % D8, w = u / D8, h = (w >> 1) + v0, blk = w & 1;
+      const int r_lo = max(0, blk * 8 - off), r_hi = min(rows, blk * 8 + 8 - off);   // rows of this block
+      if (r_lo >= r_hi) continue;
+      const row_t<TI>* src = x + (int64_t)(r0 + r_lo) * a.kv_stride + (int64_t)h * d + p * 8;
+      row_t<TC>* y = blocks + (int64_t)h * page * d + (blk * d + p * 8) * 8;
+      if (r_hi - r_lo == 8) {
+        row8_t<TC> v[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) v[t] = __builtin_convertvector(load8<TI>(src + t * a.kv_stride), row8_t<TC>);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          row8_t<TC> o;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) o[t] = v[t][c];
+          *reinterpret_cast<row8_t<TC>*>(y + c * 8) = o;
+        }
+      } else {
+        for (int r = r_lo; r < r_hi; ++r) {
+          const row8_t<TC> v = __builtin_convertvector(load8<TI>(src + (r - r_lo) * a.kv_stride), row8_t<TC>);
+#pragma unroll
+          for (int c = 0; c < 8; ++c) y[c * 8 + ((off + r) & 7)] = v[c];
+        }
+      }
+    }
+  }
+}
+
+template <int P, int TI>
+void append_out(const AppendArgs& a, int to, dim3 g, size_t lds, hipStream_t s) {
+  if (to == DWKV_F16) hipLaunchKernelGGL((append_kernel<P, TI, DWKV_F16>), g, dim3(kRT), lds, s, a);
+  else hipLaunchKernelGGL((append_kernel<P, TI, DWKV_BF16>), g, dim3(kRT), lds, s, a);
+}
+
+template <int P>
+void append_in(const AppendArgs& a, int from, int to, dim3 g, size_t lds, hipStream_t s) {
+  switch (from) {
+    case DWKV_F32: append_out<P, DWKV_F32>(a, to, g, lds, s); break;
+    case DWKV_F16: append_out<P, DWKV_F16>(a, to, g, lds, s); break;
+    default: append_out<P, DWKV_BF16>(a, to, g, lds, s); break;
+  }
+}
+
+// Heads of a workgroup: all of them where rows alone give the chip eight workgroups
+// per compute unit, fewer otherwise, but a piece for each thread.
+int head_chunk(int64_t groups, int rows, int heads, int d) {
+  const int64_t want = (2048 + groups - 1) / groups;
+  const int least = std::max(1, kRT / (rows * (d / 8)));
+  return std::min(heads, std::max(least, (int)((heads + want - 1) / want)));
+}
+
+}  // namespace
+
+hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s) {
+  const int64_t groups = (a.n_rows + kRows - 1) / kRows;
+  a.chunk = head_chunk(groups, (int)std::min<int64_t>(kRows, a.n_rows), a.n_heads, a.d);
+  const dim3 g((unsigned)groups, (a.n_heads + a.chunk - 1) / a.chunk);
+  const size_t lds = (size_t)std::min<int64_t>(kRows, a.n_rows) * a.t.n_pairs * sizeof(float2);
+  if (a.t.interleaved) rope_in<NEXT>(a, from, to, g, lds, s);
+  else if (a.t.n_pairs % 8 == 0) rope_in<HALF>(a, from, to, g, lds, s);
+  else rope_in<HALF_ODD>(a, from, to, g, lds, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s) {
+  // a sequence's n rows touch at most n groups, and at most n / 16 + 2
+  const int64_t groups = a.cu_new ? std::min<int64_t>(a.n_rows, a.n_rows / 16 + 2 * (int64_t)a.batch) : a.n_rows;
+  const int heads = a.n_q_heads + 2 * a.n_kv_heads;
+  a.chunk = head_chunk(groups, a.cu_new ? std::min(kRows, a.n_rows) : 1, heads, a.d);
+  const dim3 g((unsigned)groups, (heads + a.chunk - 1) / a.chunk);
+  const size_t lds = (size_t)(a.cu_new ? std::min(kRows, a.n_rows) : 1) * a.t.n_pairs * sizeof(float2);
+  if (a.t.interleaved) append_in<NEXT>(a, from, to, g, lds, s);
+  else if (a.t.n_pairs % 8 == 0) append_in<HALF>(a, from, to, g, lds, s);
+  else append_in<HALF_ODD>(a, from, to, g, lds, s);
+  return hipGetLastError();
+}
+
+}  // namespace dwkv

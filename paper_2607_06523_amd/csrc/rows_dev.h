@@ -1,0 +1,32 @@
+// Rows of 16- and 32-bit numbers as float32, eight at a time (library private).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "dwkv.h"
+
+namespace dwkv {
+
+typedef float float8_t __attribute__((ext_vector_type(8), aligned(16)));
+typedef _Float16 half8_t __attribute__((ext_vector_type(8), aligned(16)));
+typedef __bf16 brain8_t __attribute__((ext_vector_type(8), aligned(16)));
+
+template <int T> struct RowType;
+template <> struct RowType<DWKV_F16> { using one = _Float16; using eight = half8_t; };
+template <> struct RowType<DWKV_BF16> { using one = __bf16; using eight = brain8_t; };
+template <> struct RowType<DWKV_F32> { using one = float; using eight = float8_t; };
+template <int T> using row_t = typename RowType<T>::one;
+template <int T> using row8_t = typename RowType<T>::eight;
+
+// Eight numbers at a 16-byte aligned place.
+template <int T>
+__device__ __forceinline__ float8_t load8(const row_t<T>* p) {
+  return __builtin_convertvector(*reinterpret_cast<const row8_t<T>*>(p), float8_t);
+}
+// Rounded to nearest even.
+template <int T>
+__device__ __forceinline__ void store8(row_t<T>* p, float8_t x) {
+  *reinterpret_cast<row8_t<T>*>(p) = __builtin_convertvector(x, row8_t<T>);
+}
+
+}  // namespace dwkv
