@@ -1618,6 +1618,10 @@ dwkv_status check_page_heads(const dwkv_pages* p, int32_t n_q_heads) {
   return DWKV_OK;
 }
 
+size_t logits_parts(int32_t n_rows, int32_t vocab) {
+  return align_up(std::max<size_t>(1, (size_t)n_rows * logits_most_runs(vocab)) * sizeof(LogitsPart), 256);
+}
+
 struct PageWs {
   size_t plan, total;
 };
@@ -1769,7 +1773,7 @@ dwkv_status dwkv_page_decode(const dwkv_pages* p, int32_t layer, const void* q, 
 
 size_t dwkv_logits_workspace_bytes(int32_t n_rows, int32_t vocab) {
   if (n_rows < 0 || n_rows > 65535 || vocab < 1 || vocab > (1 << 30)) return 0;
-  return align_up(std::max<size_t>(1, (size_t)n_rows * logits_most_runs(vocab)) * sizeof(LogitsPart), 256);
+  return logits_parts(n_rows, vocab) + align_up((size_t)n_rows * ((vocab + 7) / 8) * sizeof(uint2), 256);
 }
 
 dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, const void* logits,
@@ -1804,7 +1808,11 @@ dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* tok
   std::memset(&a, 0, sizeof(a));
   a.logits = logits;
   a.out = out;
-  a.part = static_cast<LogitsPart*>(workspace);
+  if (probs) {
+    a.part = static_cast<LogitsPart*>(workspace);
+    a.code = reinterpret_cast<uint2*>(static_cast<char*>(workspace) + logits_parts(n, vocab));
+    a.code_stride = (vocab + 7) / 8;
+  }
   if (tree) {
     a.cu_nodes = tree->cu_nodes;
     a.parent = tree->parent;

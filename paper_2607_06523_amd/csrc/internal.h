@@ -500,6 +500,8 @@ struct LogitsArgs {
   const void* logits;          // n_rows rows, stride apart
   void* out;                   // [n_rows][vocab]
   LogitsPart* part;            // [n_rows][n_run]
+  uint2* code;                 // [n_rows] rows of a byte for each entry
+  int64_t code_stride;
   const int32_t *cu_nodes, *parent, *token;   // null: row i is sequence i
   const float* params;         // [S][4]
   const int32_t *history, *history_len, *prompt_len;

@@ -29,4 +29,18 @@ __device__ __forceinline__ void store8(row_t<T>* p, float8_t x) {
   *reinterpret_cast<row8_t<T>*>(p) = __builtin_convertvector(x, row8_t<T>);
 }
 
+// The same at any place that the type's own alignment allows.
+template <int T> struct AnyPlace;
+template <> struct AnyPlace<DWKV_F16> { typedef _Float16 eight __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct AnyPlace<DWKV_BF16> { typedef __bf16 eight __attribute__((ext_vector_type(8), aligned(2))); };
+template <> struct AnyPlace<DWKV_F32> { typedef float eight __attribute__((ext_vector_type(8), aligned(4))); };
+template <int T>
+__device__ __forceinline__ float8_t load8_any(const row_t<T>* p) {
+  return __builtin_convertvector(*reinterpret_cast<const typename AnyPlace<T>::eight*>(p), float8_t);
+}
+template <int T>
+__device__ __forceinline__ void store8_any(row_t<T>* p, float8_t x) {
+  *reinterpret_cast<typename AnyPlace<T>::eight*>(p) = __builtin_convertvector(x, typename AnyPlace<T>::eight);
+}
+
 }  // namespace dwkv
