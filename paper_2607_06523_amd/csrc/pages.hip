@@ -196,14 +196,14 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
       const uint16_t* k0 = a.k + max(at0, (int64_t)0);
       const uint16_t* k1 = a.k + max(at1, (int64_t)0);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) kf[0][i] = *reinterpret_cast<const uint4_t*>(k0 + (4 * i + g) * 128 + m * 8);
+      for (int i = 0; i < KS; ++i) kf[0][i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(k0 + (4 * i + g) * 128 + m * 8));
 #pragma unroll
-      for (int i = 0; i < KS; ++i) kf[1][i] = *reinterpret_cast<const uint4_t*>(k1 + (4 * i + g) * 128 + m * 8);
+      for (int i = 0; i < KS; ++i) kf[1][i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(k1 + (4 * i + g) * 128 + m * 8));
     };
     const auto load_v = [&]() {
       const uint16_t* v0 = a.v + max(g < 2 ? at0 : at1, (int64_t)0) + (g & 1) * 8 * D + m * 8;
 #pragma unroll
-      for (int i = 0; i < VB; ++i) vf[i] = *reinterpret_cast<const uint4_t*>(v0 + i * 128);
+      for (int i = 0; i < VB; ++i) vf[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(v0 + i * 128));
     };
     find(t0);
     load_k();
