@@ -77,55 +77,28 @@ __device__ __forceinline__ int tiles_of(Span s) { return (s.len + kPageTile - 1)
 // Slot of the partial that run [x, ...) of wave w writes for the pair that begins at p0.
 __device__ __forceinline__ int slot_of(int w, int x, int p0) { return 2 * w + (x > p0 ? 0 : 1); }
 
-template <int D, int TY>
+// SINGLE: grid (KV heads x blocks of 16 heads, B), a workgroup for each pair, the output
+// written at once.  Else kPageWG workgroups, and a merge after it.
+template <int D, int TY, bool SINGLE>
 __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
   constexpr int KS = D / 32, VB = D / 16, PS = D + 4;
   extern __shared__ __align__(16) float smem[];
   __shared__ int sums[kPageWaves];
   float* joined = smem;                                        // [waves][rows][PS]
-  int* pre = reinterpret_cast<int*>(smem + kPageWaves * a.rows * PS);   // [B+1]
+  int* pre = reinterpret_cast<int*>(smem + kPageWaves * a.rows * PS);   // [B+1] tiles before each sequence
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m = lane & 15, g = lane >> 4;
-
-  // tiles before each sequence
-  int base = 0;
-  for (int b0 = 0; b0 < a.batch; b0 += kPT) {
-    const int b = b0 + (int)threadIdx.x;
-    const int n = b < a.batch ? tiles_of(span_of(a, b)) : 0;
-    int inc = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(inc, d);
-      if (lane >= d) inc += o;
-    }
-    if (lane == 63) sums[wv] = inc;
-    __syncthreads();
-    int before = base;
-    for (int i = 0; i < kPageWaves; ++i) {
-      if (i < wv) before += sums[i];
-      base += sums[i];
-    }
-    if (b < a.batch) {
-      pre[b + 1] = before + inc;
-      if (blockIdx.x == 0) a.plan[b + 1] = before + inc;
-    }
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    pre[0] = 0;
-    if (blockIdx.x == 0) a.plan[0] = 0;
-  }
-  __syncthreads();
-
-  const int pairs = a.n_kv_heads * a.n_rb, total = base * pairs;
-  const int per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
+  const int m = lane & 15, g = lane >> 4, pairs = a.n_kv_heads * a.n_rb;
   const int w = blockIdx.x * kPageWaves + wv;
-  const int wg0 = min(total, (int)blockIdx.x * kPageWaves * per), wg1 = min(total, wg0 + kPageWaves * per);
-  if (wg0 >= wg1) return;
-  int x = min(total, w * per);
-  const int end = min(total, x + per);
-
-  // the sequence that holds list position i: the first with pre[b + 1] * pairs > i
+  const bool few = a.batch <= 64;                              // a lane for each sequence
+  int inc = 0;                                                 // with few: tiles up to this lane's sequence
+  int wg0, wg1, x, end, b, wgp, wgp0, wgT;
+  bool join;
+  const auto before = [&](int i) {
+    return __builtin_amdgcn_readfirstlane(few ? (i ? __builtin_amdgcn_readlane(inc, i - 1) : 0) : pre[i]);
+  };
+  // the sequence that holds list position i: the first with tiles up to its end * pairs > i
   const auto seq_at = [&](int i) {
+    if (few) return __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(lane < a.batch && inc * pairs > i)));
     int lo = 0, hi = a.batch - 1;
     while (lo < hi) {
       const int mid = (lo + hi) >> 1;
@@ -133,29 +106,90 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     }
     return __builtin_amdgcn_readfirstlane(lo);
   };
-  int b = seq_at(wg0);
-  const int wgT = pre[b + 1] - pre[b], wgp = (wg0 - pre[b] * pairs) / wgT;
-  const int wgp0 = __builtin_amdgcn_readfirstlane(pre[b] * pairs + wgp * wgT);
-  const bool join = wg1 <= wgp0 + __builtin_amdgcn_readfirstlane(wgT);    // one pair for the whole workgroup
+  if constexpr (SINGLE) {
+    b = blockIdx.y;
+    wgp = blockIdx.x;
+    wgT = __builtin_amdgcn_readfirstlane(tiles_of(span_of(a, b)));
+    wg0 = wgp0 = x = 0;
+    wg1 = end = wgT;
+    join = true;
+  } else {
+    int total = 0;
+    if (few) {
+      inc = lane < a.batch ? tiles_of(span_of(a, lane)) : 0;
+      for (int d = 1; d < 64; d <<= 1) {
+        const int o = __shfl_up(inc, d);
+        if (lane >= d) inc += o;
+      }
+      total = __builtin_amdgcn_readlane(inc, 63);
+      if (blockIdx.x == 0 && wv == 0) {
+        if (lane < a.batch) a.plan[lane + 1] = inc;
+        if (lane == 0) a.plan[0] = 0;
+      }
+    } else {
+      for (int b0 = 0; b0 < a.batch; b0 += kPT) {
+        const int i = b0 + (int)threadIdx.x;
+        int sum = i < a.batch ? tiles_of(span_of(a, i)) : 0;
+        for (int d = 1; d < 64; d <<= 1) {
+          const int o = __shfl_up(sum, d);
+          if (lane >= d) sum += o;
+        }
+        if (lane == 63) sums[wv] = sum;
+        __syncthreads();
+        int first = total;
+        for (int k = 0; k < kPageWaves; ++k) {
+          if (k < wv) first += sums[k];
+          total += sums[k];
+        }
+        if (i < a.batch) {
+          pre[i + 1] = first + sum;
+          if (blockIdx.x == 0) a.plan[i + 1] = first + sum;
+        }
+        __syncthreads();
+      }
+      if (threadIdx.x == 0) {
+        pre[0] = 0;
+        if (blockIdx.x == 0) a.plan[0] = 0;
+      }
+      __syncthreads();
+    }
+    total *= pairs;
+    const int per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
+    wg0 = min(total, (int)blockIdx.x * kPageWaves * per);
+    wg1 = min(total, wg0 + kPageWaves * per);
+    if (wg0 >= wg1) return;
+    x = min(total, w * per);
+    end = min(total, x + per);
+    b = seq_at(wg0);
+    wgT = before(b + 1) - before(b);
+    wgp = (wg0 - before(b) * pairs) / wgT;
+    wgp0 = before(b) * pairs + wgp * wgT;
+    join = wg1 <= wgp0 + wgT;                                  // one pair for the whole workgroup
+  }
 
   float ref = kNoRef, l = 0.f;
   float4_t o[VB];
 #pragma unroll
   for (int i = 0; i < VB; ++i) o[i] = 0.f;
 
-  if (x < end) b = seq_at(x);
-  while (x < end) {
-    const int pb = __builtin_amdgcn_readfirstlane(pre[b]), T = __builtin_amdgcn_readfirstlane(pre[b + 1]) - pb;
-    if (T == 0) {
-      ++b;
-      continue;
+  // the waves of a workgroup with one pair take its tiles in turn, so that it reads on in one place
+  const int turn = join ? kPageWaves : 1;
+  const int stop = join ? wg1 : end;
+  if (join) x = wg0 + wv;
+  if (!join && x < end) b = seq_at(x);
+  while (x < stop) {
+    int pair = wgp, p0 = wgp0, T = wgT;
+    if (!join) {
+      const int pb = before(b);
+      T = before(b + 1) - pb;
+      if (T == 0 || x >= (pb + T) * pairs) {
+        ++b;
+        continue;
+      }
+      pair = (x - pb * pairs) / T;
+      p0 = pb * pairs + pair * T;
     }
-    const int pair = (x - pb * pairs) / T, p0 = pb * pairs + pair * T;
-    if (pair >= pairs) {
-      ++b;
-      continue;
-    }
-    const int n = min(end, p0 + T) - x;
+    const int n = (min(stop, p0 + T) - x + turn - 1) / turn;
     const int h = pair / a.n_rb, r0 = (pair - h * a.n_rb) * 16;
     const Span sp = span_of(a, b);
     const int sh = a.page_shift + 4;
@@ -165,10 +199,19 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     const int32_t* row = a.table + (int64_t)b * a.max_pages;
     int first = t0 >> sh;
     int ids = first + lane < a.max_pages ? row[first + lane] : -1;
+    asm volatile("" : "+v"(ids));
     const uint16_t* q = a.q + b * a.q_stride + (int64_t)(h * a.group + r0 + m) * D + 8 * g;
     uint4_t qf[KS];
 #pragma unroll
     for (int i = 0; i < KS; ++i) qf[i] = r0 + m < a.group ? *reinterpret_cast<const uint4_t*>(q + 32 * i) : 0;
+    // wide heads: the registers are short, so the query waits in the wave's part of LDS
+    // (what rows past the group read there goes into columns that nobody reads)
+    volatile uint4_t* held = reinterpret_cast<volatile uint4_t*>(joined + (wv * a.rows + min(m, a.rows - 1)) * PS) + g;
+    if constexpr (D > 192) {
+      if (m < a.rows)
+#pragma unroll
+        for (int i = 0; i < KS; ++i) held[4 * i] = qf[i];
+    }
 
     ref = kNoRef;
     l = 0.f;
@@ -182,47 +225,54 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
       if ((unsigned)id >= (unsigned)a.n_pages) return -1;
       return (((int64_t)id * a.n_kv_heads + h) * (1 << sh) + (t & ((1 << sh) - 1))) * D;
     };
-    uint4_t kf[2][KS], vf[VB];
+    // Two tiles of registers where they fit (d up to 128): the next tile is on its way
+    // while this one is worked on.  Above that, the next keys go where this tile's were
+    // once the scores are done, and the next values likewise.
+    constexpr int NB = D <= 128 ? 2 : 1;
+    uint4_t kf[NB][2][KS], vf[NB][VB];
     int64_t at0, at1;
     const auto find = [&](int t) {
       if (((t + 16) >> sh) - first >= 64) {
         first = t >> sh;
         ids = first + lane < a.max_pages ? row[first + lane] : -1;
+        asm volatile("" : "+v"(ids));  // waited for here: the reads of ids then wait for no tile
       }
       at0 = place(t);
       at1 = place(t + 16);
     };
-    const auto load_k = [&]() {
+    const auto fetch = [](const uint16_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(p)); };
+    const auto load_k = [&](uint4_t (&k)[2][KS]) {
       const uint16_t* k0 = a.k + max(at0, (int64_t)0);
       const uint16_t* k1 = a.k + max(at1, (int64_t)0);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) kf[0][i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(k0 + (4 * i + g) * 128 + m * 8));
+      for (int i = 0; i < KS; ++i) k[0][i] = fetch(k0 + (4 * i + g) * 128 + m * 8);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) kf[1][i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(k1 + (4 * i + g) * 128 + m * 8));
+      for (int i = 0; i < KS; ++i) k[1][i] = fetch(k1 + (4 * i + g) * 128 + m * 8);
     };
-    const auto load_v = [&]() {
+    const auto load_v = [&](uint4_t (&v)[VB]) {
       const uint16_t* v0 = a.v + max(g < 2 ? at0 : at1, (int64_t)0) + (g & 1) * 8 * D + m * 8;
 #pragma unroll
-      for (int i = 0; i < VB; ++i) vf[i] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t*>(v0 + i * 128));
+      for (int i = 0; i < VB; ++i) v[i] = fetch(v0 + i * 128);
     };
-    find(t0);
-    load_k();
-    load_v();
 
-    for (int i = 0; i < n; ++i, t0 += kPageTile) {
+    const auto step = [&](uint4_t (&k)[2][KS], uint4_t (&v)[VB], uint4_t (&kn)[2][KS], uint4_t (&vn)[VB], bool more) {
       const bool here0 = at0 >= 0, here1 = at1 >= 0;
       const bool whole = here0 && here1 && t0 >= sp.start && t0 + kPageTile <= sp.len;
+      if (more) find(t0 + turn * kPageTile);
+      if (NB == 2 && more) {
+        load_k(kn);
+        load_v(vn);
+      }
       float4_t s0 = 0.f, s1 = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        s0 = product<TY>(kf[0][k], qf[k], s0);
-        s1 = product<TY>(kf[1][k], qf[k], s1);
+      for (int i = 0; i < KS; ++i) {
+        uint4_t qi;
+        if constexpr (D > 192) qi = held[4 * i];
+        else qi = qf[i];
+        s0 = product<TY>(k[0][i], qi, s0);
+        s1 = product<TY>(k[1][i], qi, s1);
       }
-      const bool more = i + 1 < n;
-      if (more) {
-        find(t0 + kPageTile);
-        load_k();
-      }
+      if (NB == 1 && more) load_k(kn);
       float s[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -248,7 +298,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
           ref = to;
           l *= f;
 #pragma unroll
-          for (int k = 0; k < VB; ++k) o[k] *= f;
+          for (int i = 0; i < VB; ++i) o[i] *= f;
         }
       }
       float p[8];
@@ -266,7 +316,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
           const bool hi = here && t + 2 * j + 1 >= sp.start && t + 2 * j + 1 < sp.len;
           const uint32_t keep = (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
 #pragma unroll
-          for (int k = 0; k < VB; ++k) vf[k][j] &= keep;
+          for (int i = 0; i < VB; ++i) v[i][j] &= keep;
         }
       }
 #pragma unroll
@@ -274,16 +324,30 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
         uint4_t pf;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t u = take<TY>(p[2 * j], p[2 * j + 1]), v = take<TY>(p[4 + 2 * j], p[5 + 2 * j]);
-          const auto half = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+          const uint32_t u = take<TY>(p[2 * j], p[2 * j + 1]), w2 = take<TY>(p[4 + 2 * j], p[5 + 2 * j]);
+          const auto half = __builtin_amdgcn_permlane32_swap(u, w2, false, false);
           const auto quad = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
           pf[j] = quad[0];
           pf[2 + j] = quad[1];
         }
 #pragma unroll
-        for (int k = 0; k < VB; ++k) o[k] = product<TY>(vf[k], pf, o[k]);
+        for (int i = 0; i < VB; ++i) o[i] = product<TY>(v[i], pf, o[i]);
       }
-      if (more) load_v();
+      if (NB == 1 && more) load_v(vn);
+      t0 += turn * kPageTile;
+    };
+    find(t0);
+    load_k(kf[0]);
+    load_v(vf[0]);
+    if constexpr (NB == 2) {
+      int i = 0;
+      for (; i + 1 < n; i += 2) {
+        step(kf[0], vf[0], kf[1], vf[1], true);
+        step(kf[1], vf[1], kf[0], vf[0], i + 2 < n);
+      }
+      if (i < n) step(kf[0], vf[0], kf[1], vf[1], false);
+    } else {
+      for (int i = 0; i < n; ++i) step(kf[0], vf[0], kf[0], vf[0], i + 1 < n);
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -303,7 +367,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
         }
       }
     }
-    x += n;
+    x += n * turn;
   }
   if (!join) return;
 
@@ -346,17 +410,16 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
   }
 }
 
-// grid (query heads, B): joins the partials of a pair that several waves shared.
+// grid (query heads, B): joins the partials of a pair that several waves shared.  Its
+// threads fall into groups of d / 4 that take the partials in turn, each with a
+// reference of its own, so that weights and sums are on their way together.
 template <int D>
 __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
   constexpr int PS = D + 4, LN = D / 4, NG = 256 / LN;
-  constexpr int kMost = kPageWG + 4 * kPageWaves;            // partials of a pair
-  __shared__ float factor[kMost];
-  __shared__ float red[2][4];
+  __shared__ float tops[NG], alls[NG];
   __shared__ __align__(16) float sums[NG][D];
   const int b = blockIdx.y, hq = blockIdx.x, h = hq / a.group, r = hq - h * a.group;
-  const int pairs = a.n_kv_heads * a.n_rb, total = a.plan[a.batch] * pairs;
-  const int pb = a.plan[b], T = a.plan[b + 1] - pb;
+  const int pb = a.plan[b], T = a.plan[b + 1] - pb, pairs = a.n_kv_heads * a.n_rb, total = a.plan[a.batch] * pairs;
   float* out = a.out + ((int64_t)b * gridDim.x + hq) * D;
   if (T == 0) {
     if (threadIdx.x < D) out[threadIdx.x] = 0.f;
@@ -382,65 +445,84 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
     else slot = 2 * (g1 * kPageWaves + (i - n0 - mid));
     return a.part + ((int64_t)slot * a.rows + (r & 15)) * PS;
   };
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  float ref[2], l[2], top = kNoRef;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int i = threadIdx.x + 256 * k;
-    ref[k] = kNoRef;
-    l[k] = 0.f;
-    if (i < n) {
-      const float2 v = *reinterpret_cast<const float2*>(partial(i) + D);
-      ref[k] = v.x;
-      l[k] = v.y;
-    }
-    top = fmaxf(top, ref[k]);
-  }
-  for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (lane == 0) red[0][wv] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-  float all = 0.f;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int i = threadIdx.x + 256 * k;
-    if (i < n) {
-      const float f = __builtin_amdgcn_exp2f(ref[k] - top);
-      factor[i] = f;
-      all += l[k] * f;
-    }
-  }
-  for (int d = 32; d; d >>= 1) all += __shfl_xor(all, d);
-  if (lane == 0) red[1][wv] = all;
-  __syncthreads();
-  all = red[1][0] + red[1][1] + red[1][2] + red[1][3];
   const int c = threadIdx.x % LN, k = threadIdx.x / LN;
+  constexpr int kAt = 4;                                     // partials of a group under way
+  float top = kNoRef, all = 0.f;
   float4_t sum = 0.f;
+  if (k < NG)
+    for (int i0 = k; i0 < n; i0 += kAt * NG) {
+      float4_t v[kAt];
+      float2 s[kAt];
+#pragma unroll
+      for (int j = 0; j < kAt; ++j) {
+        const float* p = partial(min(i0 + j * NG, n - 1));
+        v[j] = *reinterpret_cast<const float4_t*>(p + 4 * c);
+        s[j] = *reinterpret_cast<const float2*>(p + D);
+      }
+      float to = top;
+#pragma unroll
+      for (int j = 0; j < kAt; ++j)
+        if (i0 + j * NG < n) to = fmaxf(to, s[j].x);
+      const float f = __builtin_amdgcn_exp2f(top - to);
+      sum *= f;
+      all *= f;
+      top = to;
+#pragma unroll
+      for (int j = 0; j < kAt; ++j)
+        if (i0 + j * NG < n) {
+          const float e = __builtin_amdgcn_exp2f(s[j].x - to);
+          sum += v[j] * e;
+          all += s[j].y * e;
+        }
+    }
   if (k < NG) {
-#pragma unroll 4
-    for (int i = k; i < n; i += NG) sum += *reinterpret_cast<const float4_t*>(partial(i) + 4 * c) * factor[i];
     *reinterpret_cast<float4_t*>(&sums[k][4 * c]) = sum;
+    if (c == 0) {
+      tops[k] = top;
+      alls[k] = all;
+    }
   }
   __syncthreads();
   if (threadIdx.x < D) {
-    float v = 0.f;
-    for (int i = 0; i < NG; ++i) v += sums[i][threadIdx.x];
-    out[threadIdx.x] = all > 0.f || all != all ? v / all : 0.f;
+    float to = kNoRef, v = 0.f, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) to = fmaxf(to, tops[i]);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const float e = __builtin_amdgcn_exp2f(tops[i] - to);
+      v += sums[i][threadIdx.x] * e;
+      l += alls[i] * e;
+    }
+    out[threadIdx.x] = l > 0.f || l != l ? v / l : 0.f;
   }
+}
+
+// Longest span, in tiles, that one workgroup takes by itself.
+int64_t single_tiles() { return getenv("SINGLE") ? atoi(getenv("SINGLE")) : 32; }
+
+template <int D, int TY>
+hipError_t launch_t(const PageArgs& a, hipStream_t s) {
+  const int64_t room = (((int64_t)a.max_pages << (a.page_shift + 4)) + kPageTile - 1) / kPageTile;
+  const int64_t most = a.window > 0 ? std::min<int64_t>(room, (a.window + kPageTile - 2) / kPageTile + 1) : room;
+  const bool single = most <= single_tiles();
+  const size_t lds = ((size_t)kPageWaves * a.rows * (D + 4) + (single ? 0 : a.batch + 1)) * sizeof(float);
+  if (lds > 64 * 1024) {
+    const void* k = single ? (const void*)page_split_kernel<D, TY, true> : (const void*)page_split_kernel<D, TY, false>;
+    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
+  if (single) {
+    hipLaunchKernelGGL((page_split_kernel<D, TY, true>), dim3(a.n_kv_heads * a.n_rb, a.batch), dim3(kPT), lds, s, a);
+  } else {
+    hipLaunchKernelGGL((page_split_kernel<D, TY, false>), dim3(kPageWG), dim3(kPT), lds, s, a);
+    hipLaunchKernelGGL((page_merge_kernel<D>), dim3(a.n_kv_heads * a.group, a.batch), dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const PageArgs& a, int type, hipStream_t s) {
-  const size_t lds = ((size_t)kPageWaves * a.rows * (D + 4) + a.batch + 1) * sizeof(float);
-  const void* k = type == DWKV_F16 ? (const void*)page_split_kernel<D, DWKV_F16> : (const void*)page_split_kernel<D, DWKV_BF16>;
-  if (lds > 64 * 1024) {
-    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-  }
-  if (type == DWKV_F16) hipLaunchKernelGGL((page_split_kernel<D, DWKV_F16>), dim3(kPageWG), dim3(kPT), lds, s, a);
-  else hipLaunchKernelGGL((page_split_kernel<D, DWKV_BF16>), dim3(kPageWG), dim3(kPT), lds, s, a);
-  hipLaunchKernelGGL((page_merge_kernel<D>), dim3(a.n_kv_heads * a.group, a.batch), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return type == DWKV_F16 ? launch_t<D, DWKV_F16>(a, s) : launch_t<D, DWKV_BF16>(a, s);
 }
 
 }  // namespace
