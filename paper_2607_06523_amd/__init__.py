@@ -753,21 +753,52 @@ class DeviceCache:
         return True, -1
 
 
-def _kinds(torch):
-    return {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+class _Runtime:
+    """What every call below needs of torch, looked up once."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        self.kinds = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+        self.device = torch.cuda.current_device
+        # the stream's handle without the object around it
+        self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+    def call(self, index, where, f, *args):
+        """f(*args, stream) on GPU index, its status checked."""
+        if self.device() == index:
+            st = f(*args, self.stream(index))
+        else:
+            with _on(self.torch, index):
+                st = f(*args, self.stream(index))
+        if st != 0:
+            raise DwkvError(st, where)
+
+
+_runtime_ = None
+
+
+def _runtime():
+    global _runtime_
+    if _runtime_ is None:
+        _runtime_ = _Runtime()
+    return _runtime_
 
 
 def _heads(x, name):
-    """The row stride of x [N, H, d], whose rows have no gaps inside."""
-    if x.dim() != 3:
+    """Shape and row stride of x [N, H, d], whose rows have no gaps inside."""
+    shape, s = x.shape, x.stride()
+    if len(shape) != 3:
         raise ValueError(f"{name} must be [rows, heads, d]")
-    n, h, d = x.shape
-    s = x.stride()
+    n, h, d = shape
     if n > 0 and (s[2] != 1 or h > 1 and s[1] != d):
         raise ValueError(f"the rows of {name} must have no gaps inside")
-    if n > 1 and s[0] < h * d:
+    if n <= 1:
+        return n, h, d, 0
+    if s[0] < h * d:
         raise ValueError(f"the rows of {name} must not overlap")
-    return s[0] if n > 1 else 0
+    return n, h, d, s[0]
 
 
 def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, context: float = 0.0,
@@ -806,25 +837,22 @@ def rope(x, pos, table: RopeTable, inverse: bool = False, out=None):
     slices of wider ones) turned at pos int32 [N].  inverse turns back: with the
     same table that is the gradient with respect to x.  out: like x, of any of those
     types (x itself: in place); returns it."""
-    import torch
-    kinds = _kinds(torch)
+    rt = _runtime_ or _runtime()
+    kinds, i32 = rt.kinds, rt.torch.int32
     if x.dtype not in kinds:
         raise TypeError("x must be float16, bfloat16 or float32")
-    xs = _heads(x, "x")
-    N, H, d = x.shape
-    if pos.dtype != torch.int32 or pos.numel() != N or not pos.is_contiguous():
+    N, H, d, xs = _heads(x, "x")
+    if pos.dtype != i32 or pos.numel() != N or not pos.is_contiguous():
         raise TypeError("pos must be contiguous int32 [N]")
     if out is None:
-        out = torch.empty((N, H, d), dtype=x.dtype, device=x.device)
+        out = rt.torch.empty((N, H, d), dtype=x.dtype, device=x.device)
     elif out.dtype not in kinds or out.shape != x.shape:
         raise TypeError("out must be float16, bfloat16 or float32 of x's shape")
-    os = _heads(out, "out")
+    os = _heads(out, "out")[3]
     if not _all_on(table.index, x, pos, out):
         raise ValueError("every tensor must be on the table's device")
-    with _on(torch, table.index):
-        st = load().dwkv_rope(N, H, d, table.ref, int(bool(inverse)), x.data_ptr(), kinds[x.dtype], xs, pos.data_ptr(),
-                              out.data_ptr(), kinds[out.dtype], os, torch.cuda.current_stream(table.index).cuda_stream)
-    binding.check(st, "dwkv_rope")
+    rt.call(table.index, "dwkv_rope", load().dwkv_rope, N, H, d, table.ref, 1 if inverse else 0, x.data_ptr(), kinds[x.dtype], xs,
+            pos.data_ptr(), out.data_ptr(), kinds[out.dtype], os)
     return out
 
 
@@ -856,7 +884,7 @@ class PagedCache:
             raise ValueError("every tensor must be on one GPU")
         self.k, self.v, self.page_table, self.seq_len, self.device = k, v, page_table, seq_len, k.device
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, n, H, 16 * p16, 8 * d8
-        self.batch, self.n_q_heads = B, int(n_q_heads)
+        self.batch, self.n_q_heads, self.shape = B, int(n_q_heads), (B, int(n_q_heads), 8 * d8)
         c = binding.Pages()
         c.type, c.batch, c.n_layers, c.n_kv_heads = F16 if k.dtype == torch.float16 else BF16, B, L, H
         c.head_dim, c.page_size, c.n_pages, c.max_pages = self.head_dim, self.page_size, n, page_table.shape[1]
@@ -885,23 +913,22 @@ class PagedCache:
         cu_new[b] to cu_new[b + 1] (int32 [B+1], device).  rope turns the keys, and the
         queries q [N, H, d], at pos int32 [N] or at the tokens' places.  Returns q_out
         [N, H, d] of the cache's type, or None without q."""
-        torch = self.torch
-        kinds = _kinds(torch)
-        if k.dtype not in kinds or v.dtype != k.dtype or q is not None and q.dtype != k.dtype:
+        rt = _runtime_ or _runtime()
+        kinds, i32, kind = rt.kinds, rt.torch.int32, k.dtype
+        if kind not in kinds or v.dtype != kind or q is not None and q.dtype != kind:
             raise TypeError("k, v and q must be float16, bfloat16 or float32, of one type")
-        ks, vs = _heads(k, "k"), _heads(v, "v")
-        N = k.shape[0]
-        if k.shape != v.shape or k.shape[1] != self.n_kv_heads or k.shape[2] != self.head_dim:
+        N, H, d, ks = _heads(k, "k")
+        if _heads(v, "v") != (N, H, d, ks):
+            raise ValueError("k and v must have the same shape and row stride")
+        if H != self.n_kv_heads or d != self.head_dim:
             raise ValueError("k and v must be [N, Hkv, d]")
-        if ks != vs:
-            raise ValueError("k and v must have the same row stride")
         qs = nq = 0
         if q is not None:
-            qs, nq = _heads(q, "q"), q.shape[1]
-            if q.shape[0] != N or q.shape[2] != self.head_dim:
+            n, nq, dq, qs = _heads(q, "q")
+            if n != N or dq != d:
                 raise ValueError("q must be [N, H, d]")
             if q_out is None:
-                q_out = torch.empty((N, nq, self.head_dim), dtype=self.k.dtype, device=self.device)
+                q_out = rt.torch.empty((N, nq, d), dtype=self.k.dtype, device=self.device)
             elif q_out.dtype != self.k.dtype or q_out.shape != q.shape or not q_out.is_contiguous():
                 raise TypeError("q_out must be contiguous [N, H, d] of the cache's type")
         elif q_out is not None:
@@ -909,19 +936,16 @@ class PagedCache:
         if cu_new is None:
             if N != self.batch:
                 raise ValueError("without cu_new there is one row for each sequence")
-        elif cu_new.dtype != torch.int32 or cu_new.numel() != self.batch + 1 or not cu_new.is_contiguous():
+        elif cu_new.dtype != i32 or cu_new.numel() != self.batch + 1 or not cu_new.is_contiguous():
             raise TypeError("cu_new must be contiguous int32 [B+1]")
-        if pos is not None and (pos.dtype != torch.int32 or pos.numel() != N or not pos.is_contiguous()):
+        if pos is not None and (pos.dtype != i32 or pos.numel() != N or not pos.is_contiguous()):
             raise TypeError("pos must be contiguous int32 [N]")
-        if not _all_on(self.index, k, v, q, q_out, cu_new, pos, rope.freq if rope is not None else None):
+        if not _all_on(self.index, k, v, q, q_out, cu_new, pos) or rope is not None and rope.index != self.index:
             raise ValueError("every tensor must be on the cache's device")
-        with _on(torch, self.index):
-            st = self.lib.dwkv_page_append(self.ref, int(layer), N, None if cu_new is None else cu_new.data_ptr(), k.data_ptr(),
-                                           v.data_ptr(), kinds[k.dtype], ks, None if q is None else q.data_ptr(), qs, nq,
-                                           None if rope is None else rope.ref, None if pos is None else pos.data_ptr(),
-                                           None if q is None else q_out.data_ptr(),
-                                           torch.cuda.current_stream(self.index).cuda_stream)
-        binding.check(st, "dwkv_page_append")
+        rt.call(self.index, "dwkv_page_append", self.lib.dwkv_page_append, self.ref, int(layer), N,
+                None if cu_new is None else cu_new.data_ptr(), k.data_ptr(), v.data_ptr(), kinds[kind], ks,
+                None if q is None else q.data_ptr(), qs, nq, None if rope is None else rope.ref,
+                None if pos is None else pos.data_ptr(), None if q is None else q_out.data_ptr())
         return q_out
 
     def workspace(self):
@@ -934,16 +958,15 @@ class PagedCache:
         seq_len counts (window > 0: the last of them only).  Returns out fp32
         [B, Hq, d].  Without a workspace the cache's own is used: give one to calls
         that may overlap."""
-        torch = self.torch
-        B, Hq, d = self.batch, self.n_q_heads, self.head_dim
+        rt = _runtime_ or _runtime()
         if q.dtype != self.k.dtype:
             raise TypeError("q must have the cache's type")
-        if q.shape != (B, Hq, d):
+        B, Hq, d, qs = _heads(q, "q")
+        if (B, Hq, d) != self.shape:
             raise ValueError("q must be [B, Hq, d]")
-        qs = _heads(q, "q")
         if out is None:
-            out = torch.empty((B, Hq, d), dtype=torch.float32, device=self.device)
-        elif out.dtype != torch.float32 or out.shape != (B, Hq, d) or not out.is_contiguous():
+            out = rt.torch.empty(self.shape, dtype=rt.torch.float32, device=self.device)
+        elif out.dtype != rt.torch.float32 or out.shape != self.shape or not out.is_contiguous():
             raise TypeError("out must be contiguous float32 [B, Hq, d]")
         if workspace is None:
             if self._ws is None:
@@ -951,11 +974,8 @@ class PagedCache:
             workspace = self._ws
         if not _all_on(self.index, q, out, workspace):
             raise ValueError("every tensor must be on the cache's device")
-        with _on(torch, self.index):
-            st = self.lib.dwkv_page_decode(self.ref, int(layer), q.data_ptr(), qs, Hq, float(sm_scale or 0.0), int(window),
-                                           out.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
-                                           torch.cuda.current_stream(self.index).cuda_stream)
-        binding.check(st, "dwkv_page_decode")
+        rt.call(self.index, "dwkv_page_decode", self.lib.dwkv_page_decode, self.ref, int(layer), q.data_ptr(), qs, Hq,
+                float(sm_scale or 0.0), int(window), out.data_ptr(), workspace.data_ptr(), _nbytes(workspace))
         return out
 
 
@@ -1039,19 +1059,20 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     probabilities they leave.  Row i is sequence i, or with a tree node i, its path's
     tokens (token int32 [N]) behind its sequence's history.  out [N, vocab], by default
     float32 with probs, else the logits' type; logits itself: in place."""
-    import torch
-    kinds = _kinds(torch)
+    rt = _runtime_ or _runtime()
+    kinds, i32 = rt.kinds, rt.torch.int32
     if logits.dtype not in kinds or logits.dim() != 2 or logits.numel() and logits.stride(1) != 1:
         raise TypeError("logits must be [N, vocab] of float32, float16 or bfloat16")
     N, V = logits.shape
-    if N > 1 and logits.stride(0) < V:
+    ls = logits.stride(0) if N > 1 else 0
+    if N > 1 and ls < V:
         raise ValueError("the rows of logits must not overlap")
     S = N
     if tree is not None:
         S = tree.batch
         if tree.n_nodes != N:
             raise ValueError("logits must have a row for each node")
-        if token is None or token.dtype != torch.int32 or token.numel() != N or not token.is_contiguous():
+        if token is None or token.dtype != i32 or token.numel() != N or not token.is_contiguous():
             raise TypeError("token must be contiguous int32 [N]")
     elif token is not None:
         raise ValueError("token without a tree")
@@ -1060,7 +1081,7 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     if rules.mask is not None and (rules.mask.shape[0] != N or rules.mask.shape[1] < (V + 31) // 32):
         raise ValueError("mask must have a row of (vocab + 31) / 32 words for each row")
     if out is None:
-        out = torch.empty((N, V), dtype=torch.float32 if probs else logits.dtype, device=logits.device)
+        out = rt.torch.empty((N, V), dtype=rt.torch.float32 if probs else logits.dtype, device=logits.device)
     elif out.dtype not in kinds or out.shape != logits.shape or not out.is_contiguous():
         raise TypeError("out must be contiguous [N, vocab] of float32, float16 or bfloat16")
     index = logits.get_device()
@@ -1069,10 +1090,7 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     if N == 0:
         return out
     ws = workspace if workspace is not None or not probs else adjust_logits_workspace(logits)
-    with _on(torch, index):
-        st = load().dwkv_logits(S, tree.ref if tree is not None else None, None if token is None else token.data_ptr(), V,
-                                logits.data_ptr(), kinds[logits.dtype], logits.stride(0) if N > 1 else 0, rules.ref, int(bool(probs)),
-                                out.data_ptr(), kinds[out.dtype], None if ws is None else ws.data_ptr(),
-                                0 if ws is None else _nbytes(ws), torch.cuda.current_stream(index).cuda_stream)
-    binding.check(st, "dwkv_logits")
+    rt.call(index, "dwkv_logits", load().dwkv_logits, S, None if tree is None else tree.ref, None if token is None else token.data_ptr(),
+            V, logits.data_ptr(), kinds[logits.dtype], ls, rules.ref, 1 if probs else 0, out.data_ptr(), kinds[out.dtype],
+            None if ws is None else ws.data_ptr(), 0 if ws is None else _nbytes(ws))
     return out

@@ -497,14 +497,21 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
   }
 }
 
-// Longest span, in tiles, that one workgroup takes by itself.
-int64_t single_tiles() { return getenv("SINGLE") ? atoi(getenv("SINGLE")) : 32; }
+// Whether every pair gets one workgroup: by the longest span that the table or the
+// window allows (lengths are the device's).  A launch and the merge are saved: with 8
+// heads and up to 1000 tokens, 1, 8, 32 and 64 sequences take 7.3, 9.9, 18 and 34 us
+// against 8.7, 9.8, 23 and 40; at 2000 tokens 1 and 8 sequences take 11 and 18 against
+// 8.5 and 14.  With two workgroups per compute unit and more, up to 4096 tokens,
+// the even end of the list is not missed: 64 x 4096 tokens 160 us against 170, 64
+// ragged sequences 91 against 91, 256 of up to 1500 135 against 163 (33 of 2000 to
+// 4096, one workgroup per compute unit and a few: 84 against 76).
+bool one_workgroup_each(int64_t tiles, int64_t pairs) { return tiles <= 32 || (tiles <= 128 && pairs >= 2 * kPageWG); }
 
 template <int D, int TY>
 hipError_t launch_t(const PageArgs& a, hipStream_t s) {
   const int64_t room = (((int64_t)a.max_pages << (a.page_shift + 4)) + kPageTile - 1) / kPageTile;
   const int64_t most = a.window > 0 ? std::min<int64_t>(room, (a.window + kPageTile - 2) / kPageTile + 1) : room;
-  const bool single = most <= single_tiles();
+  const bool single = one_workgroup_each(most, (int64_t)a.n_kv_heads * a.n_rb * a.batch);
   const size_t lds = ((size_t)kPageWaves * a.rows * (D + 4) + (single ? 0 : a.batch + 1)) * sizeof(float);
   if (lds > 64 * 1024) {
     const void* k = single ? (const void*)page_split_kernel<D, TY, true> : (const void*)page_split_kernel<D, TY, false>;
