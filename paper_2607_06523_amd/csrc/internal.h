@@ -510,7 +510,7 @@ struct LogitsArgs {
   const uint32_t* mask;
   int64_t stride, history_stride, mask_stride;
   int32_t batch, n_rows, vocab, n_bias;
-  int32_t run, n_run;          // entries of a workgroup (launch_logits)
+  int32_t run, n_run, whole;   // entries of a workgroup; whether that is a row (launch_logits)
 };
 int64_t logits_most_runs(int64_t vocab);
 hipError_t launch_logits(LogitsArgs a, int from, int to, bool probs, hipStream_t s);

@@ -22,9 +22,10 @@
 namespace dwkv {
 namespace {
 
-constexpr int kLT = 512;                 // threads of a workgroup
-constexpr int kLWaves = kLT / 64;
-constexpr int kStep = 8 * kLT;           // entries of one round
+constexpr int kRunThreads = 512;         // of a workgroup with a run of a row
+constexpr int kRowThreads = 1024;        // with a whole row
+constexpr int kStep = 8 * kRunThreads;   // entries of a run's round
+constexpr int kMostWhole = 32 * kRowThreads;     // entries of a row that one workgroup takes (128 KB of LDS)
 constexpr uint32_t kInPrompt = 1u << 31;
 constexpr int kIds = 16;                 // ids of the history that a thread has under way
 
@@ -55,11 +56,12 @@ __device__ __forceinline__ Rules rules_of(const LogitsArgs& a, int b) {
 // lengths and then for the first ids of each list.
 struct Lists {
   int hist[kIds], n, m;                  // history: ids, their number, the prompt's
-  int id, e0, e1;                        // biases: this thread's id of the first kLT, their places
+  int id, e0, e1;                        // biases: this thread's id of the first NT, their places
   float val;
   int parent, token;                     // of the tree's node of this lane
 };
-// Every kLT-th id from i0 on, -1 past the list's end; without branches, so that nothing waits between the loads.
+// Every NT-th id from i0 on, -1 past the list's end; without branches, so that nothing waits between the loads.
+template <int NT>
 __device__ __forceinline__ void fetch_ids(const int32_t* h, int i0, int n, int (&id)[kIds]) {
   if (n <= 0) {
 #pragma unroll
@@ -67,10 +69,11 @@ __device__ __forceinline__ void fetch_ids(const int32_t* h, int i0, int n, int (
     return;
   }
 #pragma unroll
-  for (int j = 0; j < kIds; ++j) id[j] = h[min(i0 + j * kLT, n - 1)];
+  for (int j = 0; j < kIds; ++j) id[j] = h[min(i0 + j * NT, n - 1)];
 #pragma unroll
-  for (int j = 0; j < kIds; ++j) id[j] = i0 + j * kLT < n ? id[j] : -1;
+  for (int j = 0; j < kIds; ++j) id[j] = i0 + j * NT < n ? id[j] : -1;
 }
+template <int NT>
 __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
   const int b = at.seq, tid = threadIdx.x, lane = tid & 63;
   Lists x;
@@ -87,7 +90,7 @@ __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
   x.e0 = max(x.e0, 0);
   x.e1 = min(x.e1, a.n_bias);
   const int32_t* h = a.history + b * a.history_stride;
-  fetch_ids(h, tid, x.n, x.hist);
+  fetch_ids<NT>(h, tid, x.n, x.hist);
   x.id = x.e0 + tid < x.e1 ? a.bias_id[x.e0 + tid] : -1;
   x.val = x.e0 + tid < x.e1 ? a.bias[x.e0 + tid] : 0.f;
   return x;
@@ -95,9 +98,10 @@ __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
 
 // How often the row's history holds each entry of [v0, v0 + a.run), and the bias of
 // each: LDS words, kInPrompt set for a token of the prompt.
+template <int NT>
 __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int v0, Lists& x, uint32_t* seen, float* bias) {
   const int run = min(a.run, a.vocab - v0), b = at.seq, tid = threadIdx.x;
-  for (int i = tid; i < a.run / 4; i += kLT) {
+  for (int i = tid; i < a.run / 4; i += NT) {
     reinterpret_cast<uint4*>(seen)[i] = make_uint4(0, 0, 0, 0);
     if (a.bias) reinterpret_cast<float4*>(bias)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
@@ -114,24 +118,24 @@ __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int 
         seen[i] = 0;
       }
     }
-    e += kLT;
+    e += NT;
     x.id = e + tid < x.e1 ? a.bias_id[e + tid] : -1;
     x.val = e + tid < x.e1 ? a.bias[e + tid] : 0.f;
   }
   const int32_t* h = a.history + b * a.history_stride;
   for (int i0 = tid; i0 < x.n;) {
-    const int mine = (int)min((int64_t)x.m - i0, (int64_t)kIds * kLT);     // the prompt's are the j with j * kLT < mine
+    const int mine = (int)min((int64_t)x.m - i0, (int64_t)kIds * NT);     // the prompt's are the j with j * NT < mine
 #pragma unroll
     for (int j = 0; j < kIds; ++j) {
       const uint32_t i = (uint32_t)x.hist[j] - (uint32_t)v0;   // ids below 0 lie past every run
       if (i < (uint32_t)run) {
-        if (j * kLT < mine) atomicOr(&seen[i], kInPrompt);
+        if (j * NT < mine) atomicOr(&seen[i], kInPrompt);
         else atomicAdd(&seen[i], 1u);
       }
     }
-    i0 += kIds * kLT;
+    i0 += kIds * NT;
     if (i0 - tid >= x.n) break;
-    fetch_ids(h, i0, x.n, x.hist);
+    fetch_ids<NT>(h, i0, x.n, x.hist);
   }
   if (a.cu_nodes && tid < 64) {          // the path from node 0, itself not counted, to the row's node
     int node = __builtin_amdgcn_readfirstlane(row - at.first);
@@ -169,33 +173,35 @@ struct Mine {
   float8_t z[R];
   uint32_t ok[R];
 };
-template <int T, int R>
+template <int T, int NT, int R>
 __device__ __forceinline__ void load(const LogitsArgs& a, int row, int v0, Mine<R>& x) {
   const row_t<T>* l = static_cast<const row_t<T>*>(a.logits) + row * a.stride;
   const uint8_t* mask = reinterpret_cast<const uint8_t*>(a.mask + row * a.mask_stride);
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    const int v = v0 + 8 * (int)threadIdx.x + j * kStep;
+    const int v = v0 + 8 * ((int)threadIdx.x + j * NT);
     x.z[j] = load8_near<T>(l, v, a.vocab);
     x.ok[j] = a.mask && v < a.vocab ? mask[v >> 3] : 0xff;
   }
 }
 
-__device__ __forceinline__ float changed(float l, bool seen, uint32_t said, const Rules& r) {
-  const float z = seen ? l * (l > 0.f ? r.less : r.rep) : l;
-  return said ? z - r.freq * (float)said - r.pres : z;
+// l of an entry that the history holds, said so often (0: in the prompt only).
+__device__ __forceinline__ float changed(float l, bool seen, float said, const Rules& r) {
+  const float m = seen ? (l > 0.f ? r.less : r.rep) : 1.f;
+  const float off = said > 0.f ? __builtin_fmaf(r.freq, said, r.pres) : 0.f;
+  return __builtin_fmaf(l, m, -off);
 }
 
 // l into z.  What the lists made of eight entries goes to the second launch as a byte
 // of each: 0 untouched, 1 .. 126 how often it was said, kSeen in the prompt only;
 // all ones: a bias or a larger count among them, their z are in the output.
 constexpr uint32_t kSeen = 0x80;
-template <bool TELL, int R>
+template <bool TELL, int NT, int R>
 __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const uint32_t* seen, const float* bias, Mine<R>& x,
                                       uint2 (&code)[R]) {
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    const int at = 8 * (int)threadIdx.x + j * kStep;
+    const int at = 8 * ((int)threadIdx.x + j * NT);
     bool tell = false;
     code[j] = make_uint2(0, 0);
     if (seen) {
@@ -205,7 +211,7 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t said = c[i] & ~kInPrompt;
-        x.z[j][i] = changed(x.z[j][i], c[i] != 0, said, r);
+        x.z[j][i] = changed(x.z[j][i], c[i] != 0, (float)said, r);
         if constexpr (TELL) {
           (i < 4 ? code[j].x : code[j].y) |= (said ? said & 127 : c[i] ? kSeen : 0) << (8 * (i & 3));
           tell |= said > 126;
@@ -223,7 +229,8 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
 }
 
 template <int R>
-__device__ __forceinline__ void hide(Mine<R>& x) {         // what the mask does not allow
+__device__ __forceinline__ void hide(const LogitsArgs& a, Mine<R>& x) {     // what the mask does not allow
+  if (!a.mask) return;
 #pragma unroll
   for (int j = 0; j < R; ++j)
 #pragma unroll
@@ -264,28 +271,48 @@ __device__ __forceinline__ int wave_min(int v) {
 template <int TO>
 constexpr bool kept = TO == DWKV_F32;
 
-// grid (runs, rows): the logits out, or a run's part of the softmax: its largest entry,
-// where that is first, and the sum of exp2((z - largest) scale)
-template <int T, int TO, bool PROBS, int R>
-__global__ __launch_bounds__(kLT) void logits_kernel(const LogitsArgs a) {
+// What the first launch makes of a run: its logits; its part of the softmax (the largest
+// entry, the sum of exp2 of the distances to it, and for a greedy row where it is
+// first); or, where a run is a whole row, its probabilities.
+enum Makes { LOGITS, PART, WHOLE };
+
+// exp2((z - top) scale) of this thread's entries, and their sum.
+template <int R>
+__device__ __forceinline__ float weights(const Mine<R>& x, float top, float scale, float8_t (&e)[R]) {
+  const float ref = top == -__builtin_inff() ? 0.f : top;
+  float sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < R; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      e[j][i] = __builtin_amdgcn_exp2f((x.z[j][i] - ref) * scale);
+      sum += e[j][i];
+    }
+  return sum;
+}
+
+// grid (runs, rows)
+template <int T, int TO, Makes M, int R>
+__global__ __launch_bounds__(M == WHOLE ? kRowThreads : kRunThreads) void logits_kernel(const LogitsArgs a) {
+  constexpr int NT = M == WHOLE ? kRowThreads : kRunThreads, NW = NT / 64;
   extern __shared__ __align__(16) uint32_t lds[];
-  __shared__ LogitsPart parts[kLWaves];
+  __shared__ LogitsPart parts[NW];
   const int row = blockIdx.y, v0 = blockIdx.x * a.run, tid = threadIdx.x;
   const Row at = row_of(a, row);
   const Rules r = rules_of(a, at.seq);
-  const bool counts = a.history || a.cu_nodes, lists = counts || a.bias;
+  const bool counts = a.history || a.cu_nodes;
   float* bias = reinterpret_cast<float*>(lds + a.run);
   Mine<R> x;
-  if (lists) {
-    Lists w = fetch(a, at);
-    load<T>(a, row, v0, x);
-    count(a, row, at, v0, w, lds, bias);
+  if (counts || a.bias) {
+    Lists w = fetch<NT>(a, at);
+    load<T, NT>(a, row, v0, x);
+    count<NT>(a, row, at, v0, w, lds, bias);
     uint2 code[R];
-    shape<PROBS && kept<TO>>(a, r, counts ? lds : nullptr, bias, x, code);
-    if constexpr (PROBS && kept<TO>) {
+    shape<M == PART && kept<TO>, NT>(a, r, counts ? lds : nullptr, bias, x, code);
+    if constexpr (M == PART && kept<TO>) {
 #pragma unroll
       for (int j = 0; j < R; ++j) {
-        const int v = v0 + 8 * tid + j * kStep;
+        const int v = v0 + 8 * (tid + j * NT);
         if (v < a.vocab) {
           a.code[row * a.code_stride + (v >> 3)] = code[j];
           if (code[j].x == 0xffffffffu) put8<TO>(a, row, v, x.z[j]);
@@ -293,154 +320,178 @@ __global__ __launch_bounds__(kLT) void logits_kernel(const LogitsArgs a) {
       }
     }
   } else {
-    load<T>(a, row, v0, x);
+    load<T, NT>(a, row, v0, x);
   }
-  hide(x);
-  if constexpr (PROBS) {
-    const float scale = scale_of(r);
-    float top = -__builtin_inff(), sum = 0.f;
-    int first = a.vocab;
+  hide(a, x);
+  if constexpr (M == LOGITS) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) put8<TO>(a, row, v0 + 8 * (tid + j * NT), x.z[j]);
+    return;
+  }
+  const float scale = scale_of(r);
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int j = 0; j < R; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, x.z[j][i]);
+  top = wave_max(top);
+  if ((tid & 63) == 0) parts[tid >> 6].top = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NW; ++i) top = fmaxf(top, parts[i].top);
+  float8_t e[R];
+  float sum = 0.f;
+  int first = a.vocab;
+  if (r.temp > 0.f) {
+    sum = wave_sum(weights(x, top, scale, e));
+  } else {
 #pragma unroll
     for (int j = 0; j < R; ++j)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (x.z[j][i] > top) {
-          top = x.z[j][i];
-          first = v0 + 8 * tid + j * kStep + i;
-        }
-    const float mine = top;
-    top = wave_max(top);
-    if ((tid & 63) == 0) parts[tid >> 6].top = top;
-    __syncthreads();
+        if (x.z[j][i] == top) first = min(first, v0 + 8 * (tid + j * NT) + i);
+    first = wave_min(first);
+  }
+  if ((tid & 63) == 0) {
+    parts[tid >> 6].sum = sum;
+    parts[tid >> 6].first = first;
+  }
+  __syncthreads();
+  sum = 0.f;
+  first = a.vocab;
 #pragma unroll
-    for (int i = 0; i < kLWaves; ++i) top = fmaxf(top, parts[i].top);
-    const float ref = top == -__builtin_inff() ? 0.f : top;
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum += __builtin_amdgcn_exp2f((x.z[j][i] - ref) * scale);
-    sum = wave_sum(sum);
-    first = wave_min(mine == top ? first : a.vocab);
-    if ((tid & 63) == 0) {
-      parts[tid >> 6].sum = sum;
-      parts[tid >> 6].first = first;
-    }
-    __syncthreads();
-    if (tid == 0) {
-      LogitsPart p = {top, 0.f, a.vocab};
-#pragma unroll
-      for (int i = 0; i < kLWaves; ++i) {
-        p.sum += parts[i].sum;
-        p.first = min(p.first, parts[i].first);
-      }
-      a.part[(int64_t)row * a.n_run + blockIdx.x] = p;
-    }
+  for (int i = 0; i < NW; ++i) {
+    sum += parts[i].sum;
+    first = min(first, parts[i].first);
+  }
+  if constexpr (M == PART) {
+    if (tid == 0) a.part[(int64_t)row * a.n_run + blockIdx.x] = {top, sum, first};
   } else {
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const int one = top > -__builtin_inff() ? first - 8 * tid : -1;
 #pragma unroll
-    for (int j = 0; j < R; ++j) put8<TO>(a, row, v0 + 8 * tid + j * kStep, x.z[j]);
+    for (int j = 0; j < R; ++j) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[j][i] = r.temp > 0.f ? e[j][i] * f : one == 8 * j * NT + i ? 1.f : 0.f;
+      put8<TO>(a, row, 8 * (tid + j * NT), e[j]);
+    }
   }
 }
 
 // grid (runs, rows): the probabilities out
 template <int T, int TO, int R>
-__global__ __launch_bounds__(kLT) void probs_kernel(const LogitsArgs a) {
+__global__ __launch_bounds__(kRunThreads) void probs_kernel(const LogitsArgs a) {
+  constexpr int NT = kRunThreads;
   extern __shared__ __align__(16) uint32_t lds[];
   const int row = blockIdx.y, v0 = blockIdx.x * a.run, tid = threadIdx.x, lane = tid & 63;
   const Row at = row_of(a, row);
   const Rules r = rules_of(a, at.seq);
   const bool counts = a.history || a.cu_nodes, lists = counts || a.bias;
   const float scale = scale_of(r);
-  Mine<R> x;
-  Lists w;
-  if (lists && !kept<TO>) w = fetch(a, at);
-  uint2 code[R];
-  if (lists && kept<TO>) {
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const int v = v0 + 8 * tid + j * kStep;
-      code[j] = v < a.vocab ? a.code[row * a.code_stride + (v >> 3)] : make_uint2(0, 0);
-    }
-  }
-  load<T>(a, row, v0, x);
   // every wave joins the row's parts, in one order
   const LogitsPart* part = a.part + (int64_t)row * a.n_run;
+  if (!(r.temp > 0.f)) {
+    float top = -__builtin_inff();
+    int first = a.vocab;
+    for (int i = lane; i < a.n_run; i += 64) top = fmaxf(top, part[i].top);
+    top = wave_max(top);
+    for (int i = lane; i < a.n_run; i += 64)
+      if (part[i].top == top) first = min(first, part[i].first);
+    first = wave_min(first);
+    const int one = top > -__builtin_inff() ? first - v0 - 8 * tid : -1;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      float8_t e;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) e[i] = one == 8 * j * NT + i ? 1.f : 0.f;
+      put8<TO>(a, row, v0 + 8 * (tid + j * NT), e);
+    }
+    return;
+  }
+  Mine<R> x;
+  Lists w;
+  uint2 code[R];
+  if (lists) {
+    if constexpr (kept<TO>) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        const int v = v0 + 8 * (tid + j * NT);
+        code[j] = v < a.vocab ? a.code[row * a.code_stride + (v >> 3)] : make_uint2(0, 0);
+      }
+    } else {
+      w = fetch<NT>(a, at);
+    }
+  }
+  load<T, NT>(a, row, v0, x);
   float top = -__builtin_inff(), sum = 0.f;
   for (int i = lane; i < a.n_run; i += 64) top = fmaxf(top, part[i].top);
   top = wave_max(top);
   const float ref = top == -__builtin_inff() ? 0.f : top;
-  int first = a.vocab;
-  for (int i = lane; i < a.n_run; i += 64) {
-    const LogitsPart p = part[i];
-    sum += p.sum * __builtin_amdgcn_exp2f((p.top - ref) * scale);
-    if (p.top == top) first = min(first, p.first);
-  }
-  if (r.temp > 0.f) {
-    sum = wave_sum(sum);
-    if (lists) {
-      if constexpr (kept<TO>) {
+  for (int i = lane; i < a.n_run; i += 64) sum += part[i].sum * __builtin_amdgcn_exp2f((part[i].top - ref) * scale);
+  sum = wave_sum(sum);
+  if (lists) {
+    if constexpr (kept<TO>) {
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-          const int v = v0 + 8 * tid + j * kStep;
-          if (code[j].x == 0xffffffffu) {
-            x.z[j] = load8_near<DWKV_F32>(static_cast<const float*>(a.out) + (int64_t)row * a.vocab, v, a.vocab);
-          } else {
+      for (int j = 0; j < R; ++j) {
+        if (code[j].x == 0xffffffffu) {
+          x.z[j] = load8_near<DWKV_F32>(static_cast<const float*>(a.out) + (int64_t)row * a.vocab, v0 + 8 * (tid + j * NT), a.vocab);
+        } else {
+          const uint2 said = make_uint2(code[j].x & 0x7f7f7f7fu, code[j].y & 0x7f7f7f7fu);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t c = ((i < 4 ? code[j].x : code[j].y) >> (8 * (i & 3))) & 255;
-              x.z[j][i] = changed(x.z[j][i], c != 0, c & kSeen ? 0 : c, r);
-            }
+          for (int i = 0; i < 8; ++i) {
+            const int at8 = 8 * (i & 3);
+            x.z[j][i] = changed(x.z[j][i], (((i < 4 ? code[j].x : code[j].y) >> at8) & 255) != 0,
+                                (float)(((i < 4 ? said.x : said.y) >> at8) & 255), r);
           }
         }
-      } else {
-        float* bias = reinterpret_cast<float*>(lds + a.run);
-        count(a, row, at, v0, w, lds, bias);
-        shape<false>(a, r, counts ? lds : nullptr, bias, x, code);
       }
+    } else {
+      float* bias = reinterpret_cast<float*>(lds + a.run);
+      count<NT>(a, row, at, v0, w, lds, bias);
+      shape<false, NT>(a, r, counts ? lds : nullptr, bias, x, code);
     }
-    hide(x);
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x.z[j][i] = __builtin_amdgcn_exp2f((x.z[j][i] - ref) * scale) * f;
-  } else {
-    first = wave_min(first);
-    const int one = top > -__builtin_inff() ? first - v0 - 8 * tid : -1;
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x.z[j][i] = one == j * kStep + i ? 1.f : 0.f;
   }
+  hide(a, x);
+  float8_t e[R];
+  weights(x, top, scale, e);
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-  for (int j = 0; j < R; ++j) put8<TO>(a, row, v0 + 8 * tid + j * kStep, x.z[j]);
+  for (int j = 0; j < R; ++j) put8<TO>(a, row, v0 + 8 * (tid + j * NT), e[j] * f);
 }
 
-template <int T, int TO, int R>
-void launch_r(const LogitsArgs& a, bool probs, size_t lds, hipStream_t s) {
+template <int T, int TO, Makes M, int R>
+hipError_t launch_one(const LogitsArgs& a, size_t lds, hipStream_t s) {
+  if (lds > 64 * 1024) {
+    const hipError_t e = hipFuncSetAttribute((const void*)logits_kernel<T, TO, M, R>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+  }
   const dim3 g(a.n_run, a.n_rows);
-  if (probs) {
-    hipLaunchKernelGGL((logits_kernel<T, TO, true, R>), g, dim3(kLT), lds, s, a);
-    hipLaunchKernelGGL((probs_kernel<T, TO, R>), g, dim3(kLT), kept<TO> ? 0 : lds, s, a);
-  } else {
-    hipLaunchKernelGGL((logits_kernel<T, TO, false, R>), g, dim3(kLT), lds, s, a);
+  hipLaunchKernelGGL((logits_kernel<T, TO, M, R>), g, dim3(M == WHOLE ? kRowThreads : kRunThreads), lds, s, a);
+  if constexpr (M == PART) hipLaunchKernelGGL((probs_kernel<T, TO, R>), g, dim3(kRunThreads), kept<TO> ? 0 : lds, s, a);
+  return hipGetLastError();
+}
+
+template <int T, int TO, Makes M>
+hipError_t launch_r(const LogitsArgs& a, size_t lds, hipStream_t s) {
+  switch (a.run / (8 * (M == WHOLE ? kRowThreads : kRunThreads))) {
+    case 1: return launch_one<T, TO, M, 1>(a, lds, s);
+    case 2: return launch_one<T, TO, M, 2>(a, lds, s);
+    default: return launch_one<T, TO, M, 4>(a, lds, s);
   }
 }
 
 template <int T, int TO>
-void launch_t(const LogitsArgs& a, bool probs, size_t lds, hipStream_t s) {
-  switch (a.run / kStep) {
-    case 1: launch_r<T, TO, 1>(a, probs, lds, s); break;
-    case 2: launch_r<T, TO, 2>(a, probs, lds, s); break;
-    default: launch_r<T, TO, 4>(a, probs, lds, s); break;
-  }
+hipError_t launch_t(const LogitsArgs& a, bool probs, size_t lds, hipStream_t s) {
+  if (!probs) return launch_r<T, TO, LOGITS>(a, lds, s);
+  return a.whole ? launch_r<T, TO, WHOLE>(a, lds, s) : launch_r<T, TO, PART>(a, lds, s);
 }
 
 template <int T>
-void launch_from(const LogitsArgs& a, int to, bool probs, size_t lds, hipStream_t s) {
+hipError_t launch_from(const LogitsArgs& a, int to, bool probs, size_t lds, hipStream_t s) {
   switch (to) {
-    case DWKV_F32: launch_t<T, DWKV_F32>(a, probs, lds, s); break;
-    case DWKV_F16: launch_t<T, DWKV_F16>(a, probs, lds, s); break;
-    default: launch_t<T, DWKV_BF16>(a, probs, lds, s); break;
+    case DWKV_F32: return launch_t<T, DWKV_F32>(a, probs, lds, s);
+    case DWKV_F16: return launch_t<T, DWKV_F16>(a, probs, lds, s);
+    default: return launch_t<T, DWKV_BF16>(a, probs, lds, s);
   }
 }
 
@@ -450,17 +501,25 @@ void launch_from(const LogitsArgs& a, int to, bool probs, size_t lds, hipStream_
 int64_t logits_most_runs(int64_t vocab) { return (vocab + kStep - 1) / kStep; }
 
 hipError_t launch_logits(LogitsArgs a, int from, int to, bool probs, hipStream_t s) {
-  // 64 KB of LDS at most, so that a compute unit holds two workgroups
+  const int words = a.bias ? 2 : a.history || a.cu_nodes ? 1 : 0;
   a.run = kStep;
-  while (a.run < (a.bias ? 2 : 4) * kStep && (int64_t)a.n_rows * ((a.vocab + 2 * a.run - 1) / (2 * a.run)) >= 512) a.run *= 2;
-  a.n_run = (a.vocab + a.run - 1) / a.run;
-  const size_t lds = a.bias ? 8 * (size_t)a.run : a.history || a.cu_nodes ? 4 * (size_t)a.run : 0;
-  switch (from) {
-    case DWKV_F32: launch_from<DWKV_F32>(a, to, probs, lds, s); break;
-    case DWKV_F16: launch_from<DWKV_F16>(a, to, probs, lds, s); break;
-    default: launch_from<DWKV_BF16>(a, to, probs, lds, s); break;
+  // One launch instead of two: 1, 64 and 256 rows of 16000 entries behind 2000 tokens take
+  // 7.9, 8.7 and 12 us in it and 8.1, 9.7 and 17 in two; of 32000, where one workgroup is
+  // slow, 10.9, 12.6 and 18 against 8.3, 12.1 and 26.
+  a.whole = probs && a.vocab <= (a.n_rows >= 128 ? kMostWhole : kMostWhole / 2) / (a.bias ? 2 : 1);
+  if (a.whole) {
+    for (a.run = 8 * kRowThreads; a.run < a.vocab;) a.run *= 2;
+  } else {
+    // 64 KB of LDS at most, so that a compute unit holds two workgroups
+    while (a.run < (a.bias ? 2 : 4) * kStep && (int64_t)a.n_rows * ((a.vocab + 2 * a.run - 1) / (2 * a.run)) >= 512) a.run *= 2;
   }
-  return hipGetLastError();
+  a.n_run = (a.vocab + a.run - 1) / a.run;
+  const size_t lds = (size_t)4 * words * a.run;
+  switch (from) {
+    case DWKV_F32: return launch_from<DWKV_F32>(a, to, probs, lds, s);
+    case DWKV_F16: return launch_from<DWKV_F16>(a, to, probs, lds, s);
+    default: return launch_from<DWKV_BF16>(a, to, probs, lds, s);
+  }
 }
 
 }  // namespace dwkv

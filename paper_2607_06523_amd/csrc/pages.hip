@@ -93,6 +93,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
   int inc = 0;                                                 // with few: tiles up to this lane's sequence
   int wg0, wg1, x, end, b, wgp, wgp0, wgT;
   bool join;
+  int early = -1;                                              // SINGLE: ids of the wave's first pages, before the length is known
   const auto before = [&](int i) {
     return __builtin_amdgcn_readfirstlane(few ? (i ? __builtin_amdgcn_readlane(inc, i - 1) : 0) : pre[i]);
   };
@@ -109,6 +110,8 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
   if constexpr (SINGLE) {
     b = blockIdx.y;
     wgp = blockIdx.x;
+    const int p = ((wv * kPageTile) >> (a.page_shift + 4)) + lane;
+    if (p < a.max_pages) early = a.table[(int64_t)b * a.max_pages + p];
     wgT = __builtin_amdgcn_readfirstlane(tiles_of(span_of(a, b)));
     wg0 = wgp0 = x = 0;
     wg1 = end = wgT;
@@ -198,7 +201,8 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     // ids of 64 pages, one a lane
     const int32_t* row = a.table + (int64_t)b * a.max_pages;
     int first = t0 >> sh;
-    int ids = first + lane < a.max_pages ? row[first + lane] : -1;
+    int ids = early;
+    if (!SINGLE || a.window > 0) ids = first + lane < a.max_pages ? row[first + lane] : -1;
     asm volatile("" : "+v"(ids));
     const uint16_t* q = a.q + b * a.q_stride + (int64_t)(h * a.group + r0 + m) * D + 8 * g;
     uint4_t qf[KS];
