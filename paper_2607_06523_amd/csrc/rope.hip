@@ -4,8 +4,12 @@
 //   a' = m (a cos - b sin),  b' = m (b cos + a sin).
 // Angles are float64: at position 2^20 a float32 angle is off by 2^-4.  Each
 // workgroup takes 16 rows and works their sines and cosines out once, into LDS (16
-// rows x 64 pairs, against 16 x 64 x 40 rotations that read them), with the Taylor
-// polynomials on [-pi/4, pi/4]; then its threads stream pieces of 16 bytes.
+// rows x 64 pairs, against 16 x 64 x 40 rotations that read them): the angle is brought
+// into [-pi/4, pi/4] in float64 and the Taylor polynomials there are float64 for
+// float32 outputs, float32 for outputs of 16 bits (off by 2^-23 where those have 2^-11).
+// Then its threads stream pieces of 16 bytes.  Bound by HBM: what a call of many rows
+// writes goes past the caches (8000 rows of 40 heads turned in 28 us, 5.9 TB/s, against
+// 38 with plain stores; appended with 8 heads of values 35 against 48).
 #include <algorithm>
 
 #include "internal.h"
@@ -20,27 +24,44 @@ constexpr int kRows = kRopeRows;         // rows of a workgroup
 enum Pairs { HALF = 0, HALF_ODD = 1, NEXT = 2 };   // (i, n + i), n a multiple of 8 or not; (2i, 2i + 1)
 
 // sin and cos of x.  x - n pi/2 in two steps (n pi/2's upper part is exact in the
-// fused product), then Taylor to x^13 and x^14: below 2^-45 on [-pi/4, pi/4].
+// fused product), then Taylor: to x^13 and x^14 in float64 (below 2^-45 on
+// [-pi/4, pi/4]), to x^9 and x^8 in float32 (2^-28 and 2^-25).
+template <bool FULL>
 __device__ __forceinline__ void sin_cos(double x, double& s, double& c) {
   const double n = __builtin_rint(x * 0.63661977236758134308);
   double r = __builtin_fma(n, -1.57079632679489655800, x);
   r = __builtin_fma(n, -6.12323399573676603587e-17, r);
-  const double z = r * r;
-  double p = 1.0 / 6227020800.0;
-  p = __builtin_fma(p, z, -1.0 / 39916800.0);
-  p = __builtin_fma(p, z, 1.0 / 362880.0);
-  p = __builtin_fma(p, z, -1.0 / 5040.0);
-  p = __builtin_fma(p, z, 1.0 / 120.0);
-  p = __builtin_fma(p, z, -1.0 / 6.0);
-  p = __builtin_fma(p * z, r, r);
-  double q = -1.0 / 87178291200.0;
-  q = __builtin_fma(q, z, 1.0 / 479001600.0);
-  q = __builtin_fma(q, z, -1.0 / 3628800.0);
-  q = __builtin_fma(q, z, 1.0 / 40320.0);
-  q = __builtin_fma(q, z, -1.0 / 720.0);
-  q = __builtin_fma(q, z, 1.0 / 24.0);
-  q = __builtin_fma(q, z, -0.5);
-  q = __builtin_fma(q, z, 1.0);
+  double p, q;
+  if constexpr (FULL) {
+    const double z = r * r;
+    p = 1.0 / 6227020800.0;
+    p = __builtin_fma(p, z, -1.0 / 39916800.0);
+    p = __builtin_fma(p, z, 1.0 / 362880.0);
+    p = __builtin_fma(p, z, -1.0 / 5040.0);
+    p = __builtin_fma(p, z, 1.0 / 120.0);
+    p = __builtin_fma(p, z, -1.0 / 6.0);
+    p = __builtin_fma(p * z, r, r);
+    q = -1.0 / 87178291200.0;
+    q = __builtin_fma(q, z, 1.0 / 479001600.0);
+    q = __builtin_fma(q, z, -1.0 / 3628800.0);
+    q = __builtin_fma(q, z, 1.0 / 40320.0);
+    q = __builtin_fma(q, z, -1.0 / 720.0);
+    q = __builtin_fma(q, z, 1.0 / 24.0);
+    q = __builtin_fma(q, z, -0.5);
+    q = __builtin_fma(q, z, 1.0);
+  } else {
+    const float f = (float)r, z = f * f;
+    float u = 1.f / 362880.f;
+    u = __builtin_fmaf(u, z, -1.f / 5040.f);
+    u = __builtin_fmaf(u, z, 1.f / 120.f);
+    u = __builtin_fmaf(u, z, -1.f / 6.f);
+    p = __builtin_fmaf(u * z, f, f);
+    float v = 1.f / 40320.f;
+    v = __builtin_fmaf(v, z, -1.f / 720.f);
+    v = __builtin_fmaf(v, z, 1.f / 24.f);
+    v = __builtin_fmaf(v, z, -0.5f);
+    q = __builtin_fmaf(v, z, 1.f);
+  }
   const int k = (int)(long long)n & 3;
   const double u = k & 1 ? q : p, v = k & 1 ? p : q;
   s = k & 2 ? -u : u;
@@ -48,11 +69,12 @@ __device__ __forceinline__ void sin_cos(double x, double& s, double& c) {
 }
 
 // (cos, sin) of row r's pair i at cs[r * n_pairs + i], already scaled.
+template <int TO>
 __device__ __forceinline__ void fill_table(float2* cs, const RopeSpec& t, const int* pos, int rows) {
   for (int u = threadIdx.x; u < rows * t.n_pairs; u += kRT) {
     const int r = u / t.n_pairs, i = u - r * t.n_pairs;
     double s, c;
-    sin_cos((double)pos[r] * t.freq[i], s, c);
+    sin_cos<TO == DWKV_F32>((double)pos[r] * t.freq[i], s, c);
     cs[u] = make_float2((float)(c * t.scale), (float)(s * (t.inverse ? -(double)t.scale : (double)t.scale)));
   }
 }
@@ -118,7 +140,7 @@ __device__ __forceinline__ void turn_piece(const row_t<TI>* x, int a, int d, int
 }
 
 // grid (rows / 16, head chunks)
-template <int P, int TI, int TO>
+template <int P, int TI, int TO, bool PAST>
 __global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
   extern __shared__ __align__(16) float2 cs[];
   __shared__ int pos[kRows];
@@ -127,7 +149,7 @@ __global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
   const int h0 = blockIdx.y * a.chunk, nh = min(a.chunk, a.n_heads - h0);
   if (threadIdx.x < rows) pos[threadIdx.x] = a.pos[r0 + threadIdx.x];
   __syncthreads();
-  fill_table(cs, a.t, pos, rows);
+  fill_table<TO>(cs, a.t, pos, rows);
   __syncthreads();
   const int np = a.t.n_pairs, A = pieces<P>(a.d, np), per = A * nh;
   const row_t<TI>* x = static_cast<const row_t<TI>*>(a.x);
@@ -137,25 +159,31 @@ __global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
     row_t<TO>* y = out + (r0 + r) * a.out_stride + (int64_t)(h0 + h) * a.d;
     turn_piece<P, TI>(
         x + (r0 + r) * a.x_stride + (int64_t)(h0 + h) * a.d, p, a.d, np, cs + r * np,
-        [&](int c, float8_t v) { store8<TO>(y + c, v); }, [&](int c, float v) { y[c] = (row_t<TO>)v; });
+        [&](int c, float8_t v) { store8<TO, PAST>(y + c, v); }, [&](int c, float v) { y[c] = (row_t<TO>)v; });
   }
 }
 
+template <int P, int TI, int TO>
+void rope_past(const RopeArgs& a, bool past, dim3 g, size_t lds, hipStream_t s) {
+  if (past) hipLaunchKernelGGL((rope_kernel<P, TI, TO, true>), g, dim3(kRT), lds, s, a);
+  else hipLaunchKernelGGL((rope_kernel<P, TI, TO, false>), g, dim3(kRT), lds, s, a);
+}
+
 template <int P, int TI>
-void rope_out(const RopeArgs& a, int to, dim3 g, size_t lds, hipStream_t s) {
+void rope_out(const RopeArgs& a, int to, bool past, dim3 g, size_t lds, hipStream_t s) {
   switch (to) {
-    case DWKV_F32: hipLaunchKernelGGL((rope_kernel<P, TI, DWKV_F32>), g, dim3(kRT), lds, s, a); break;
-    case DWKV_F16: hipLaunchKernelGGL((rope_kernel<P, TI, DWKV_F16>), g, dim3(kRT), lds, s, a); break;
-    default: hipLaunchKernelGGL((rope_kernel<P, TI, DWKV_BF16>), g, dim3(kRT), lds, s, a); break;
+    case DWKV_F32: rope_past<P, TI, DWKV_F32>(a, past, g, lds, s); break;
+    case DWKV_F16: rope_past<P, TI, DWKV_F16>(a, past, g, lds, s); break;
+    default: rope_past<P, TI, DWKV_BF16>(a, past, g, lds, s); break;
   }
 }
 
 template <int P>
-void rope_in(const RopeArgs& a, int from, int to, dim3 g, size_t lds, hipStream_t s) {
+void rope_in(const RopeArgs& a, int from, int to, bool past, dim3 g, size_t lds, hipStream_t s) {
   switch (from) {
-    case DWKV_F32: rope_out<P, DWKV_F32>(a, to, g, lds, s); break;
-    case DWKV_F16: rope_out<P, DWKV_F16>(a, to, g, lds, s); break;
-    default: rope_out<P, DWKV_BF16>(a, to, g, lds, s); break;
+    case DWKV_F32: rope_out<P, DWKV_F32>(a, to, past, g, lds, s); break;
+    case DWKV_F16: rope_out<P, DWKV_F16>(a, to, past, g, lds, s); break;
+    default: rope_out<P, DWKV_BF16>(a, to, past, g, lds, s); break;
   }
 }
 
@@ -164,32 +192,55 @@ void rope_in(const RopeArgs& a, int from, int to, dim3 g, size_t lds, hipStream_
 // sequence (aligned to 16: a tile of keys, two blocks of values) and a chunk of the
 // row's heads: queries, then keys, then values.
 
-// The sequence and the first of its 16-slot groups that workgroup w takes; false
-// past the last.  A group is counted for every 16 slots that hold a new row.
+// The group of 16 slots that workgroup w takes: sequence, slot / 16, and the sequence's
+// rows and length.  A sequence has a group for every 16 slots that hold a new row of it.
 struct Group {
-  int seq, first;          // first: slot / 16
+  int seq, first, c0, c1, len;
 };
+__device__ __forceinline__ int groups_of(int rows, int len, int& first) {
+  if (rows <= 0) return 0;
+  first = (int)(((int64_t)len - rows) >> 4);
+  return ((len - 1) >> 4) - first + 1;
+}
+// False past the last group.  Up to 64 sequences every wave finds it by itself.
 __device__ __forceinline__ bool find_group(const AppendArgs& a, int w, Group& g) {
-  __shared__ int found[2];
+  __shared__ int found[5];
   __shared__ int sums[kRT / 64];
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const auto upto = [&](int n) {
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(n, d);
+      if (lane >= d) n += o;
+    }
+    return n;
+  };
+  if (a.batch <= 64) {
+    const int b = min(lane, a.batch - 1), c0 = a.cu_new[b], c1 = a.cu_new[b + 1], len = a.len[b];
+    int first = 0;
+    const int n = lane < a.batch ? groups_of(c1 - c0, len, first) : 0;
+    const int inc = upto(n);
+    const unsigned long long here = __ballot(w < inc && w >= inc - n);
+    if (!here) return false;
+    const int k = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(here));
+    g.seq = k;
+    g.c0 = __builtin_amdgcn_readlane(c0, k);
+    g.c1 = __builtin_amdgcn_readlane(c1, k);
+    g.len = __builtin_amdgcn_readlane(len, k);
+    g.first = __builtin_amdgcn_readlane(first, k) + w - (__builtin_amdgcn_readlane(inc, k) - __builtin_amdgcn_readlane(n, k));
+    return true;
+  }
   if (threadIdx.x == 0) found[0] = -1;
   int base = 0;
   for (int b0 = 0; b0 < a.batch; b0 += kRT) {
     const int b = b0 + threadIdx.x;
-    int n = 0, first = 0;
+    int n = 0, first = 0, c0 = 0, c1 = 0, len = 0;
     if (b < a.batch) {
-      const int rows = a.cu_new[b + 1] - a.cu_new[b], end = a.len[b];
-      if (rows > 0) {
-        first = (int)(((int64_t)end - rows) >> 4);
-        n = ((end - 1) >> 4) - first + 1;
-      }
+      c0 = a.cu_new[b];
+      c1 = a.cu_new[b + 1];
+      len = a.len[b];
+      n = groups_of(c1 - c0, len, first);
     }
-    int inc = n;
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(inc, d);
-      if (lane >= d) inc += o;
-    }
+    const int inc = upto(n);
     if (lane == 63) sums[wv] = inc;
     __syncthreads();
     int before = base, total = 0;
@@ -201,17 +252,19 @@ __device__ __forceinline__ bool find_group(const AppendArgs& a, int w, Group& g)
     if (w >= at && w < at + n) {
       found[0] = b;
       found[1] = first + (w - at);
+      found[2] = c0;
+      found[3] = c1;
+      found[4] = len;
     }
     __syncthreads();
     base += total;
     if (base > w) break;
   }
-  g.seq = found[0];
-  g.first = found[1];
+  g = {found[0], found[1], found[2], found[3], found[4]};
   return g.seq >= 0;
 }
 
-template <int P, int TI, int TC>
+template <int P, int TI, int TC, bool PAST>
 __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
   extern __shared__ __align__(16) float2 cs[];
   __shared__ int pos[kRows];
@@ -219,11 +272,10 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
   int r0, end, slot0;                    // rows [r0, end) of the packed rows, r0 at slot slot0
   if (a.cu_new) {
     if (!find_group(a, blockIdx.x, g)) return;
-    const int c0 = a.cu_new[g.seq], c1 = a.cu_new[g.seq + 1];
-    const int64_t start = (int64_t)a.len[g.seq] - (c1 - c0), s0 = (int64_t)g.first * 16;
+    const int64_t start = (int64_t)g.len - (g.c1 - g.c0), s0 = (int64_t)g.first * 16;
     slot0 = (int)max(start, s0);
-    r0 = c0 + (int)(slot0 - start);
-    end = c0 + (int)(min(start + (c1 - c0), s0 + 16) - start);
+    r0 = g.c0 + (int)(slot0 - start);
+    end = g.c0 + (int)(min(start + (g.c1 - g.c0), s0 + 16) - start);
     if (r0 < 0 || end <= r0 || end > a.n_rows) return;          // starts that do not fit the rows
   } else {                               // one row for each sequence
     g.seq = blockIdx.x;
@@ -231,12 +283,16 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
     r0 = blockIdx.x;
     end = r0 + 1;
   }
+  // the page of these slots: rows without one are not stored
+  const int page = 16 << a.page_shift;
+  int id = -1;
+  if (slot0 >= 0 && slot0 < (int64_t)a.max_pages * page) id = a.table[(int64_t)g.seq * a.max_pages + (slot0 >> (a.page_shift + 4))];
   const int rows = end - r0, off = slot0 & 15;
   const int np = a.t.n_pairs, d = a.d;
   if (np > 0) {
     if (threadIdx.x < rows) pos[threadIdx.x] = a.pos ? a.pos[r0 + threadIdx.x] : slot0 + (int)threadIdx.x;
     __syncthreads();
-    fill_table(cs, a.t, pos, rows);
+    fill_table<TC>(cs, a.t, pos, rows);
   }
   __syncthreads();
   const int hq = a.n_q_heads, hk = a.n_kv_heads;
@@ -250,15 +306,10 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
       const int r = u / per, w = u - r * per, h = w / A, p = w - h * A;
       row_t<TC>* y = out + ((int64_t)(r0 + r) * hq + h) * d;
       turn_piece<P, TI>(
-          x + (r0 + r) * a.q_stride + (int64_t)h * d, p, d, np, cs + r * np, [&](int c, float8_t v) { store8<TC>(y + c, v); },
+          x + (r0 + r) * a.q_stride + (int64_t)h * d, p, d, np, cs + r * np, [&](int c, float8_t v) { store8<TC, PAST>(y + c, v); },
           [&](int c, float v) { y[c] = (row_t<TC>)v; });
     }
   }
-  // the page of these slots: rows without one are not stored
-  const int page = 16 << a.page_shift;
-  const int64_t room = (int64_t)a.max_pages * page;
-  int id = -1;
-  if (slot0 >= 0 && slot0 < room) id = a.table[(int64_t)g.seq * a.max_pages + (slot0 >> (a.page_shift + 4))];
   if (id < 0 || id >= a.n_pages) return;
   const int t0 = slot0 & (page - 1) & ~15;                 // the group's place in its page
   const int64_t at = ((int64_t)id * hk * page + t0) * d;     // of KV head 0
@@ -271,7 +322,7 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
       row_t<TC>* y = tile + (int64_t)h * page * d + (off + r) * 8;
       turn_piece<P, TI>(
           x + (int64_t)(r0 + r) * a.kv_stride + (int64_t)h * d, p, d, np, cs + r * np,
-          [&](int c, float8_t v) { store8<TC>(y + c * 16, v); },
+          [&](int c, float8_t v) { store8<TC, PAST>(y + c * 16, v); },
           [&](int c, float v) { y[(c >> 3) * 128 + (c & 7)] = (row_t<TC>)v; });
     }
   }
@@ -297,49 +348,64 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
           *reinterpret_cast<row8_t<TC>*>(y + c * 8) = o;
         }
       } else {
-        for (int r = r_lo; r < r_hi; ++r) {
-          const row8_t<TC> v = __builtin_convertvector(load8<TI>(src + (r - r_lo) * a.kv_stride), row8_t<TC>);
+        row8_t<TC> v[8];
+        const int t0 = (off + r_lo) & 7, n = r_hi - r_lo;            // tokens t0 .. t0 + n - 1 of the block
 #pragma unroll
-          for (int c = 0; c < 8; ++c) y[c * 8 + ((off + r) & 7)] = v[c];
-        }
+        for (int t = 0; t < 8; ++t) v[t] = __builtin_convertvector(load8<TI>(src + min(t, n - 1) * a.kv_stride), row8_t<TC>);
+#pragma unroll
+        for (int t = 0; t < 8; ++t)
+          if (t < n)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) y[c * 8 + t0 + t] = v[t][c];
       }
     }
   }
 }
 
+template <int P, int TI, int TC>
+void append_past(const AppendArgs& a, bool past, dim3 g, size_t lds, hipStream_t s) {
+  if (past) hipLaunchKernelGGL((append_kernel<P, TI, TC, true>), g, dim3(kRT), lds, s, a);
+  else hipLaunchKernelGGL((append_kernel<P, TI, TC, false>), g, dim3(kRT), lds, s, a);
+}
+
 template <int P, int TI>
-void append_out(const AppendArgs& a, int to, dim3 g, size_t lds, hipStream_t s) {
-  if (to == DWKV_F16) hipLaunchKernelGGL((append_kernel<P, TI, DWKV_F16>), g, dim3(kRT), lds, s, a);
-  else hipLaunchKernelGGL((append_kernel<P, TI, DWKV_BF16>), g, dim3(kRT), lds, s, a);
+void append_out(const AppendArgs& a, int to, bool past, dim3 g, size_t lds, hipStream_t s) {
+  if (to == DWKV_F16) append_past<P, TI, DWKV_F16>(a, past, g, lds, s);
+  else append_past<P, TI, DWKV_BF16>(a, past, g, lds, s);
 }
 
 template <int P>
-void append_in(const AppendArgs& a, int from, int to, dim3 g, size_t lds, hipStream_t s) {
+void append_in(const AppendArgs& a, int from, int to, bool past, dim3 g, size_t lds, hipStream_t s) {
   switch (from) {
-    case DWKV_F32: append_out<P, DWKV_F32>(a, to, g, lds, s); break;
-    case DWKV_F16: append_out<P, DWKV_F16>(a, to, g, lds, s); break;
-    default: append_out<P, DWKV_BF16>(a, to, g, lds, s); break;
+    case DWKV_F32: append_out<P, DWKV_F32>(a, to, past, g, lds, s); break;
+    case DWKV_F16: append_out<P, DWKV_F16>(a, to, past, g, lds, s); break;
+    default: append_out<P, DWKV_BF16>(a, to, past, g, lds, s); break;
   }
 }
 
-// Heads of a workgroup: all of them where rows alone give the chip eight workgroups
-// per compute unit, fewer otherwise, but a piece for each thread.
+// Heads of a workgroup: all of them where rows alone give the chip four workgroups
+// per compute unit, fewer otherwise, but a piece for each thread.  (Eight and 16 a
+// unit work the same sines out more often: 16384 rows appended 88, 91 and 95 us.)
 int head_chunk(int64_t groups, int rows, int heads, int d) {
-  const int64_t want = (2048 + groups - 1) / groups;
+  const int64_t want = (1024 + groups - 1) / groups;
   const int least = std::max(1, kRT / (rows * (d / 8)));
   return std::min(heads, std::max(least, (int)((heads + want - 1) / want)));
 }
+
+// Whether what is written goes past the caches: more than the eight L2s hold.
+bool past_caches(int64_t rows, int heads, int d, int type) { return rows * heads * d * (type == DWKV_F32 ? 4 : 2) > (32 << 20); }
 
 }  // namespace
 
 hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s) {
   const int64_t groups = (a.n_rows + kRows - 1) / kRows;
   a.chunk = head_chunk(groups, (int)std::min<int64_t>(kRows, a.n_rows), a.n_heads, a.d);
+  const bool past = past_caches(a.n_rows, a.n_heads, a.d, to);
   const dim3 g((unsigned)groups, (a.n_heads + a.chunk - 1) / a.chunk);
   const size_t lds = (size_t)std::min<int64_t>(kRows, a.n_rows) * a.t.n_pairs * sizeof(float2);
-  if (a.t.interleaved) rope_in<NEXT>(a, from, to, g, lds, s);
-  else if (a.t.n_pairs % 8 == 0) rope_in<HALF>(a, from, to, g, lds, s);
-  else rope_in<HALF_ODD>(a, from, to, g, lds, s);
+  if (a.t.interleaved) rope_in<NEXT>(a, from, to, past, g, lds, s);
+  else if (a.t.n_pairs % 8 == 0) rope_in<HALF>(a, from, to, past, g, lds, s);
+  else rope_in<HALF_ODD>(a, from, to, past, g, lds, s);
   return hipGetLastError();
 }
 
@@ -348,11 +414,12 @@ hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s) {
   const int64_t groups = a.cu_new ? std::min<int64_t>(a.n_rows, a.n_rows / 16 + 2 * (int64_t)a.batch) : a.n_rows;
   const int heads = a.n_q_heads + 2 * a.n_kv_heads;
   a.chunk = head_chunk(groups, a.cu_new ? std::min(kRows, a.n_rows) : 1, heads, a.d);
+  const bool past = past_caches(a.n_rows, heads, a.d, to);
   const dim3 g((unsigned)groups, (heads + a.chunk - 1) / a.chunk);
   const size_t lds = (size_t)(a.cu_new ? std::min(kRows, a.n_rows) : 1) * a.t.n_pairs * sizeof(float2);
-  if (a.t.interleaved) append_in<NEXT>(a, from, to, g, lds, s);
-  else if (a.t.n_pairs % 8 == 0) append_in<HALF>(a, from, to, g, lds, s);
-  else append_in<HALF_ODD>(a, from, to, g, lds, s);
+  if (a.t.interleaved) append_in<NEXT>(a, from, to, past, g, lds, s);
+  else if (a.t.n_pairs % 8 == 0) append_in<HALF>(a, from, to, past, g, lds, s);
+  else append_in<HALF_ODD>(a, from, to, past, g, lds, s);
   return hipGetLastError();
 }
 

@@ -28,6 +28,13 @@ template <int T>
 __device__ __forceinline__ void store8(row_t<T>* p, float8_t x) {
   *reinterpret_cast<row8_t<T>*>(p) = __builtin_convertvector(x, row8_t<T>);
 }
+// The same, PAST: past the caches.
+template <int T, bool PAST>
+__device__ __forceinline__ void store8(row_t<T>* p, float8_t x) {
+  const row8_t<T> v = __builtin_convertvector(x, row8_t<T>);
+  if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<row8_t<T>*>(p));
+  else *reinterpret_cast<row8_t<T>*>(p) = v;
+}
 
 // The same at any place that the type's own alignment allows.
 template <int T> struct AnyPlace;
