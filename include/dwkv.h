@@ -682,7 +682,7 @@ dwkv_status dwkv_rope_freqs(int32_t n_pairs, double base, int32_t scaling, doubl
  *   strides:  multiples of 8, at least n_heads head_dim; 0 = rows without a gap
  *   pos:      DEVICE int32 [n_rows]
  * head_dim: a multiple of 8, at most 512; 2 n_pairs <= head_dim, n_pairs >= 1.  x and
- * out 16-byte aligned, pos 4-byte.  n_rows up to 2^27.  One launch (none for no rows). */
+ * out 16-byte aligned, pos 4-byte.  n_rows up to 2^24.  One launch (none for no rows). */
 dwkv_status dwkv_rope(int64_t n_rows, int32_t n_heads, int32_t head_dim, const dwkv_rope_table* table, int32_t inverse,
                       const void* x, int32_t x_type, int64_t x_stride, const int32_t* pos, void* out,
                       int32_t out_type, int64_t out_stride, void* stream);
@@ -725,7 +725,7 @@ typedef struct dwkv_pages {
  * padded batch), past its table or in no page is not stored.  A place in one page
  * that two sequences share must not be written by both.  Strides are multiples of
  * 8, 0 = rows without a gap; k, v, q, q_out and the pages are 16-byte aligned, the
- * integer arrays 4-byte.  N up to 2^27.  One launch (none for no rows). */
+ * integer arrays 4-byte.  N up to 2^24.  One launch (none for no rows). */
 dwkv_status dwkv_page_append(const dwkv_pages* pages, int32_t layer, int32_t n_rows, const int32_t* cu_new, const void* k,
                              const void* v, int32_t x_type, int64_t kv_stride, const void* q, int64_t q_stride,
                              int32_t n_q_heads, const dwkv_rope_table* table, const int32_t* pos, void* q_out, void* stream);

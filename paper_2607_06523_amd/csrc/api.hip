@@ -1581,7 +1581,7 @@ bool row_stride(int64_t& stride, int64_t width) {
   return stride >= width && stride % 8 == 0;
 }
 
-constexpr int64_t kMostRows = (int64_t)1 << 27;
+constexpr int64_t kMostRows = (int64_t)1 << 24;   // grids stay under 2^32 threads
 
 dwkv_status check_pages(const dwkv_pages* p) {
   if (!p) return DWKV_E_NULL;

@@ -452,9 +452,8 @@ struct RopeArgs {
   const int32_t* pos;
   int64_t n_rows, x_stride, out_stride;
   int32_t n_heads, d;
-  int32_t chunk;               // heads of a workgroup (launch_rope)
+  int32_t rows, chunk;         // rows and heads of a workgroup (launch_rope)
 };
-constexpr int kRopeRows = 16;  // rows of a workgroup
 hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s);
 
 struct AppendArgs {
@@ -467,7 +466,8 @@ struct AppendArgs {
   int64_t q_stride, kv_stride;
   int32_t n_rows, batch, n_q_heads, n_kv_heads, d, n_pages, max_pages;
   int32_t page_shift;          // a page is 16 << page_shift tokens
-  int32_t chunk;               // heads of a workgroup (launch_append)
+  // launch_append: workgroups that fill pages, their heads and chunks of heads; of the others rows, heads, chunks
+  int32_t n_fill, kv_chunk, kv_chunks, rows, q_chunk, q_chunks;
 };
 hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s);
 

@@ -3,8 +3,8 @@
 // Pair i of a head at position p turns by the angle p f_i:
 //   a' = m (a cos - b sin),  b' = m (b cos + a sin).
 // Angles are float64: at position 2^20 a float32 angle is off by 2^-4.  Each
-// workgroup takes 16 rows and works their sines and cosines out once, into LDS (16
-// rows x 64 pairs, against 16 x 64 x 40 rotations that read them): the angle is brought
+// workgroup works the sines and cosines of its rows out once, into LDS (64 pairs of a row,
+// against 64 x 40 rotations that read them): the angle is brought
 // into [-pi/4, pi/4] in float64 and the Taylor polynomials there are float64 for
 // float32 outputs, float32 for outputs of 16 bits (off by 2^-23 where those have 2^-11).
 // Then its threads stream pieces of 16 bytes.  Bound by HBM: what a call of many rows
@@ -19,7 +19,8 @@ namespace dwkv {
 namespace {
 
 constexpr int kRT = 256;                 // threads of a workgroup
-constexpr int kRows = kRopeRows;         // rows of a workgroup
+constexpr int kRows = 2;                 // rows of a workgroup, at most
+constexpr int kSlots = 16;               // slots of a workgroup that fills pages
 
 enum Pairs { HALF = 0, HALF_ODD = 1, NEXT = 2 };   // (i, n + i), n a multiple of 8 or not; (2i, 2i + 1)
 
@@ -139,13 +140,13 @@ __device__ __forceinline__ void turn_piece(const row_t<TI>* x, int a, int d, int
   }
 }
 
-// grid (rows / 16, head chunks)
+// grid (rows / a.rows, head chunks)
 template <int P, int TI, int TO, bool PAST>
 __global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
   extern __shared__ __align__(16) float2 cs[];
   __shared__ int pos[kRows];
-  const int64_t r0 = (int64_t)blockIdx.x * kRows;
-  const int rows = (int)min((int64_t)kRows, a.n_rows - r0);
+  const int64_t r0 = (int64_t)blockIdx.x * a.rows;
+  const int rows = (int)min((int64_t)a.rows, a.n_rows - r0);
   const int h0 = blockIdx.y * a.chunk, nh = min(a.chunk, a.n_heads - h0);
   if (threadIdx.x < rows) pos[threadIdx.x] = a.pos[r0 + threadIdx.x];
   __syncthreads();
@@ -188,9 +189,10 @@ void rope_in(const RopeArgs& a, int from, int to, bool past, dim3 g, size_t lds,
 }
 
 // ---- append ------------------------------------------------------------------------
-// A workgroup takes the new rows that fall into 16 consecutive slots of one
-// sequence (aligned to 16: a tile of keys, two blocks of values) and a chunk of the
-// row's heads: queries, then keys, then values.
+// Two kinds of workgroups in one launch.  The first fill pages: each takes the new rows
+// that fall into 16 consecutive slots of one sequence (aligned to 16: a tile of keys,
+// two blocks of values) and some of the heads of keys and values.  The others turn
+// queries, a row or two each, as rope_kernel does.
 
 // The group of 16 slots that workgroup w takes: sequence, slot / 16, and the sequence's
 // rows and length.  A sequence has a group for every 16 slots that hold a new row of it.
@@ -264,29 +266,100 @@ __device__ __forceinline__ bool find_group(const AppendArgs& a, int w, Group& g)
   return g.seq >= 0;
 }
 
+// Where rows r0 .. r0 + rows - 1 lie in their sequences; false in `in`: behind the last start.
+__device__ __forceinline__ void find_rows(const AppendArgs& a, int r0, int rows, int* place, bool* in) {
+  __shared__ int before[kRows];
+  const int lane = threadIdx.x & 63;
+  if (!a.cu_new) {
+    if (threadIdx.x < rows) {
+      place[threadIdx.x] = a.len[r0 + threadIdx.x] - 1;
+      in[threadIdx.x] = true;
+    }
+  } else if (a.batch <= 64) {
+    const int b = min(lane, a.batch - 1), c1 = a.cu_new[b + 1], len = a.len[b];
+    for (int j = 0; j < rows; ++j) {
+      const unsigned long long after = __ballot(lane < a.batch && c1 > r0 + j);
+      const int k = after ? __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(after)) : 0;
+      if (threadIdx.x == 0) {
+        in[j] = after != 0;
+        place[j] = __builtin_amdgcn_readlane(len, k) - (__builtin_amdgcn_readlane(c1, k) - (r0 + j));
+      }
+    }
+  } else {                               // sequences that end before the row
+    if (threadIdx.x < kRows) before[threadIdx.x] = 0;
+    __syncthreads();
+    int n[kRows] = {};
+    for (int b = threadIdx.x; b < a.batch; b += kRT) {
+      const int c1 = a.cu_new[b + 1];
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) n[j] += c1 <= r0 + j;
+    }
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) atomicAdd(&before[j], n[j]);
+    __syncthreads();
+    if (threadIdx.x < rows) {
+      const int b = before[threadIdx.x];
+      in[threadIdx.x] = b < a.batch;
+      if (b < a.batch) place[threadIdx.x] = a.len[b] - (a.cu_new[b + 1] - (r0 + (int)threadIdx.x));
+    }
+  }
+}
+
+template <int P, int TI, int TC, bool PAST>
+__device__ __forceinline__ void append_queries(const AppendArgs& a, int w, float2* cs) {
+  __shared__ int pos[kRows];
+  __shared__ bool in[kRows];
+  const int group = w / a.q_chunks, c0 = (w - group * a.q_chunks) * a.q_chunk, nh = min(a.q_chunk, a.n_q_heads - c0);
+  const int r0 = group * a.rows, rows = min(a.rows, a.n_rows - r0), np = a.t.n_pairs, d = a.d;
+  find_rows(a, r0, rows, pos, in);
+  __syncthreads();
+  if (a.pos && threadIdx.x < rows) pos[threadIdx.x] = a.pos[r0 + threadIdx.x];
+  __syncthreads();
+  if (np > 0) {
+    fill_table<TC>(cs, a.t, pos, rows);
+    __syncthreads();
+  }
+  const int A = pieces<P>(d, np), per = A * nh;
+  const row_t<TI>* x = static_cast<const row_t<TI>*>(a.q) + r0 * a.q_stride + (int64_t)c0 * d;
+  row_t<TC>* out = static_cast<row_t<TC>*>(a.q_out) + ((int64_t)r0 * a.n_q_heads + c0) * d;
+  for (int u = threadIdx.x; u < rows * per; u += kRT) {
+    const int r = u / per, v = u - r * per, h = v / A, p = v - h * A;
+    if (!in[r]) continue;
+    row_t<TC>* y = out + ((int64_t)r * a.n_q_heads + h) * d;
+    turn_piece<P, TI>(
+        x + r * a.q_stride + (int64_t)h * d, p, d, np, cs + r * np, [&](int c, float8_t z) { store8<TC, PAST>(y + c, z); },
+        [&](int c, float z) { y[c] = (row_t<TC>)z; });
+  }
+}
+
 template <int P, int TI, int TC, bool PAST>
 __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
   extern __shared__ __align__(16) float2 cs[];
-  __shared__ int pos[kRows];
+  __shared__ int pos[kSlots];
+  if ((int)blockIdx.x >= a.n_fill) {
+    append_queries<P, TI, TC, PAST>(a, blockIdx.x - a.n_fill, cs);
+    return;
+  }
+  const int w = blockIdx.x / a.kv_chunks;
   Group g;
   int r0, end, slot0;                    // rows [r0, end) of the packed rows, r0 at slot slot0
   if (a.cu_new) {
-    if (!find_group(a, blockIdx.x, g)) return;
+    if (!find_group(a, w, g)) return;
     const int64_t start = (int64_t)g.len - (g.c1 - g.c0), s0 = (int64_t)g.first * 16;
     slot0 = (int)max(start, s0);
     r0 = g.c0 + (int)(slot0 - start);
     end = g.c0 + (int)(min(start + (g.c1 - g.c0), s0 + 16) - start);
     if (r0 < 0 || end <= r0 || end > a.n_rows) return;          // starts that do not fit the rows
   } else {                               // one row for each sequence
-    g.seq = blockIdx.x;
+    g.seq = w;
     slot0 = a.len[g.seq] - 1;
-    r0 = blockIdx.x;
+    r0 = w;
     end = r0 + 1;
   }
   // the page of these slots: rows without one are not stored
   const int page = 16 << a.page_shift;
-  int id = -1;
-  if (slot0 >= 0 && slot0 < (int64_t)a.max_pages * page) id = a.table[(int64_t)g.seq * a.max_pages + (slot0 >> (a.page_shift + 4))];
+  if (slot0 < 0 || slot0 >= (int64_t)a.max_pages * page) return;
+  const int id = a.table[(int64_t)g.seq * a.max_pages + (slot0 >> (a.page_shift + 4))];
   const int rows = end - r0, off = slot0 & 15;
   const int np = a.t.n_pairs, d = a.d;
   if (np > 0) {
@@ -295,26 +368,13 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
     fill_table<TC>(cs, a.t, pos, rows);
   }
   __syncthreads();
-  const int hq = a.n_q_heads, hk = a.n_kv_heads;
-  const int c0 = blockIdx.y * a.chunk, c1 = min(c0 + a.chunk, hq + 2 * hk);
+  const int hk = a.n_kv_heads, c0 = ((int)blockIdx.x - w * a.kv_chunks) * a.kv_chunk, c1 = min(c0 + a.kv_chunk, 2 * hk);
   const int A = pieces<P>(d, np);
-  if (c0 < hq) {                         // queries: rows of the output
-    const int nh = min(c1, hq) - c0, per = A * nh;
-    const row_t<TI>* x = static_cast<const row_t<TI>*>(a.q) + (int64_t)c0 * d;
-    row_t<TC>* out = static_cast<row_t<TC>*>(a.q_out) + (int64_t)c0 * d;
-    for (int u = threadIdx.x; u < rows * per; u += kRT) {
-      const int r = u / per, w = u - r * per, h = w / A, p = w - h * A;
-      row_t<TC>* y = out + ((int64_t)(r0 + r) * hq + h) * d;
-      turn_piece<P, TI>(
-          x + (r0 + r) * a.q_stride + (int64_t)h * d, p, d, np, cs + r * np, [&](int c, float8_t v) { store8<TC, PAST>(y + c, v); },
-          [&](int c, float v) { y[c] = (row_t<TC>)v; });
-    }
-  }
   if (id < 0 || id >= a.n_pages) return;
   const int t0 = slot0 & (page - 1) & ~15;                 // the group's place in its page
   const int64_t at = ((int64_t)id * hk * page + t0) * d;     // of KV head 0
-  if (c1 > hq && c0 < hq + hk) {         // keys: [d/8][16][8] of the tile
-    const int k0 = max(c0, hq) - hq, nh = min(c1, hq + hk) - hq - k0, per = rows * A;
+  if (c0 < hk) {                         // keys: [d/8][16][8] of the tile
+    const int k0 = c0, nh = min(c1, hk) - k0, per = rows * A;
     const row_t<TI>* x = static_cast<const row_t<TI>*>(a.k);
     row_t<TC>* tile = static_cast<row_t<TC>*>(a.k_pages) + at;
     for (int u = threadIdx.x; u < nh * per; u += kRT) {
@@ -326,8 +386,8 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
           [&](int c, float v) { y[(c >> 3) * 128 + (c & 7)] = (row_t<TC>)v; });
     }
   }
-  if (c1 > hq + hk) {                    // values: two blocks of [d][8], eight channels of eight tokens a piece
-    const int v0 = max(c0, hq + hk) - hq - hk, nh = c1 - hq - hk - v0, D8 = d / 8;
+  if (c1 > hk) {                         // values: two blocks of [d][8], eight channels of eight tokens a piece
+    const int v0 = max(c0, hk) - hk, nh = c1 - hk - v0, D8 = d / 8;
     const row_t<TI>* x = static_cast<const row_t<TI>*>(a.v);
     row_t<TC>* blocks = static_cast<row_t<TC>*>(a.v_pages) + at;
     for (int u = threadIdx.x; u < 2 * nh * D8; u += kRT) {
@@ -384,13 +444,16 @@ void append_in(const AppendArgs& a, int from, int to, bool past, dim3 g, size_t 
 }
 
 // Heads of a workgroup: all of them where rows alone give the chip four workgroups
-// per compute unit, fewer otherwise, but a piece for each thread.  (Eight and 16 a
-// unit work the same sines out more often: 16384 rows appended 88, 91 and 95 us.)
+// per compute unit, fewer otherwise, but a piece for each thread.
 int head_chunk(int64_t groups, int rows, int heads, int d) {
   const int64_t want = (1024 + groups - 1) / groups;
   const int least = std::max(1, kRT / (rows * (d / 8)));
   return std::min(heads, std::max(least, (int)((heads + want - 1) / want)));
 }
+
+// Rows of a workgroup.  Few, so that the workgroups at work read and write in one place
+// that moves on: 16384 rows of 40 heads take 64 us with 2, 69, 72 and 74 with 4, 8 and 16.
+int rows_of(int64_t n_rows) { return n_rows >= 2048 ? kRows : 1; }
 
 // Whether what is written goes past the caches: more than the eight L2s hold.
 bool past_caches(int64_t rows, int heads, int d, int type) { return rows * heads * d * (type == DWKV_F32 ? 4 : 2) > (32 << 20); }
@@ -398,11 +461,12 @@ bool past_caches(int64_t rows, int heads, int d, int type) { return rows * heads
 }  // namespace
 
 hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s) {
-  const int64_t groups = (a.n_rows + kRows - 1) / kRows;
-  a.chunk = head_chunk(groups, (int)std::min<int64_t>(kRows, a.n_rows), a.n_heads, a.d);
+  a.rows = rows_of(a.n_rows);
+  const int64_t groups = (a.n_rows + a.rows - 1) / a.rows;
+  a.chunk = head_chunk(groups, a.rows, a.n_heads, a.d);
   const bool past = past_caches(a.n_rows, a.n_heads, a.d, to);
   const dim3 g((unsigned)groups, (a.n_heads + a.chunk - 1) / a.chunk);
-  const size_t lds = (size_t)std::min<int64_t>(kRows, a.n_rows) * a.t.n_pairs * sizeof(float2);
+  const size_t lds = (size_t)a.rows * a.t.n_pairs * sizeof(float2);
   if (a.t.interleaved) rope_in<NEXT>(a, from, to, past, g, lds, s);
   else if (a.t.n_pairs % 8 == 0) rope_in<HALF>(a, from, to, past, g, lds, s);
   else rope_in<HALF_ODD>(a, from, to, past, g, lds, s);
@@ -412,11 +476,20 @@ hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s) {
 hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s) {
   // a sequence's n rows touch at most n groups, and at most n / 16 + 2
   const int64_t groups = a.cu_new ? std::min<int64_t>(a.n_rows, a.n_rows / 16 + 2 * (int64_t)a.batch) : a.n_rows;
-  const int heads = a.n_q_heads + 2 * a.n_kv_heads;
-  a.chunk = head_chunk(groups, a.cu_new ? std::min(kRows, a.n_rows) : 1, heads, a.d);
-  const bool past = past_caches(a.n_rows, heads, a.d, to);
-  const dim3 g((unsigned)groups, (heads + a.chunk - 1) / a.chunk);
-  const size_t lds = (size_t)(a.cu_new ? std::min(kRows, a.n_rows) : 1) * a.t.n_pairs * sizeof(float2);
+  const int slots = a.cu_new ? std::min(kSlots, a.n_rows) : 1;
+  a.kv_chunk = head_chunk(groups, slots, 2 * a.n_kv_heads, a.d);
+  a.kv_chunks = (2 * a.n_kv_heads + a.kv_chunk - 1) / a.kv_chunk;
+  a.rows = rows_of(a.n_rows);
+  const int64_t q_groups = a.n_q_heads > 0 ? (a.n_rows + a.rows - 1) / a.rows : 0;
+  a.q_chunk = a.q_chunks = 1;
+  if (q_groups > 0) {
+    a.q_chunk = head_chunk(q_groups, a.rows, a.n_q_heads, a.d);
+    a.q_chunks = (a.n_q_heads + a.q_chunk - 1) / a.q_chunk;
+  }
+  a.n_fill = (int)(groups * a.kv_chunks);
+  const bool past = past_caches(a.n_rows, a.n_q_heads + 2 * a.n_kv_heads, a.d, to);
+  const dim3 g((unsigned)(a.n_fill + q_groups * a.q_chunks));
+  const size_t lds = (size_t)std::max(slots, a.rows) * a.t.n_pairs * sizeof(float2);
   if (a.t.interleaved) append_in<NEXT>(a, from, to, past, g, lds, s);
   else if (a.t.n_pairs % 8 == 0) append_in<HALF>(a, from, to, past, g, lds, s);
   else append_in<HALF_ODD>(a, from, to, past, g, lds, s);

@@ -83,7 +83,7 @@ def test_rope_refused(lib):
                      (dict(rows=-1), 2), (dict(heads=0), 2), (dict(d=0), 2), (dict(xt=3), 2), (dict(ot=-1), 2), (dict(pairs=0), 2),
                      (dict(pairs=33), 2), (dict(xs=64), 2), (dict(xs=132), 2), (dict(os=120), 2),
                      (dict(out=FAKE, ot=2), 2), (dict(out=FAKE, xs=136), 2),
-                     (dict(d=60, pairs=4), 3), (dict(d=520), 3), (dict(rows=(1 << 27) + 1), 3), (dict(heads=65536), 3),
+                     (dict(d=60, pairs=4), 3), (dict(d=520), 3), (dict(rows=(1 << 24) + 1), 3), (dict(heads=65536), 3),
                      (dict(x=FAKE + 8), 7), (dict(out=FAKE + 2), 7), (dict(pos=FAKE + 2), 7), (dict(freq=FAKE + 4), 7)]:
         assert rope_status(lib, **kw) == want, kw
 
@@ -155,7 +155,7 @@ def test_append_refused(lib):
     for kw, want in [(dict(layer=2), 2), (dict(layer=-1), 2), (dict(n=-1, cu=FAKE), 2), (dict(n=3), 2), (dict(xt=3), 2),
                      (dict(ks=64), 2), (dict(ks=130), 2), (dict(nq=0), 2), (dict(qs=128), 2), (dict(qs=260), 2),
                      (dict(table=T(pairs=0)), 2), (dict(table=T(pairs=33)), 2), (dict(table=T(freq=None)), 1), (dict(table=T(freq=FAKE + 4)), 7),
-                     (dict(k=None), 1), (dict(v=None), 1), (dict(q_out=None), 1), (dict(n=(1 << 27) + 1, cu=FAKE), 3),
+                     (dict(k=None), 1), (dict(v=None), 1), (dict(q_out=None), 1), (dict(n=(1 << 24) + 1, cu=FAKE), 3),
                      (dict(k=FAKE + 8), 7), (dict(v=FAKE + 8), 7), (dict(q=FAKE + 8), 7), (dict(q_out=FAKE + 8), 7),
                      (dict(cu=FAKE + 2), 7), (dict(pos=FAKE + 2), 7)]:
         assert append_status(lib, **kw) == want, kw
