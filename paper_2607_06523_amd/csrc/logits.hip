@@ -106,17 +106,25 @@ __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int 
     if (a.bias) reinterpret_cast<float4*>(bias)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
   }
   __syncthreads();
+  __shared__ int again;
   for (int e = x.e0; e < x.e1;) {        // an entry listed twice adds twice, in the list's order
     const uint32_t i = (uint32_t)x.id - (uint32_t)v0;
     bool left = i < (uint32_t)run;
-    while (__syncthreads_or(left)) {
+    for (;;) {
+      if (tid == 0) again = 0;
       if (left) atomicMax(&seen[i], ~(uint32_t)tid);       // the first in the list goes first
       __syncthreads();
-      if (left && seen[i] == ~(uint32_t)tid) {
+      const bool mine = left && seen[i] == ~(uint32_t)tid;
+      left = left && !mine;
+      if (left) again = 1;
+      __syncthreads();
+      if (mine) {
         bias[i] += x.val;
-        left = false;
         seen[i] = 0;
       }
+      const bool more = again;
+      __syncthreads();
+      if (!more) break;
     }
     e += NT;
     x.id = e + tid < x.e1 ? a.bias_id[e + tid] : -1;
@@ -209,19 +217,22 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
       *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(seen + at);
       *reinterpret_cast<uint4*>(c + 4) = *reinterpret_cast<const uint4*>(seen + at + 4);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t said = c[i] & ~kInPrompt;
-        x.z[j][i] = changed(x.z[j][i], c[i] != 0, (float)said, r);
-        if constexpr (TELL) {
-          (i < 4 ? code[j].x : code[j].y) |= (said ? said & 127 : c[i] ? kSeen : 0) << (8 * (i & 3));
-          tell |= said > 126;
+      for (int i = 0; i < 8; ++i)
+        if (__any(c[i] != 0)) {          // few entries are in a list: mostly a wave has none of its 64
+          const uint32_t said = c[i] & ~kInPrompt;
+          x.z[j][i] = changed(x.z[j][i], c[i] != 0, (float)said, r);
+          if constexpr (TELL) {
+            (i < 4 ? code[j].x : code[j].y) |= (said ? said & 127 : c[i] ? kSeen : 0) << (8 * (i & 3));
+            tell |= said > 126;
+          }
         }
-      }
     }
     if (a.bias) {
       const float8_t d = *reinterpret_cast<const float8_t*>(bias + at);
+      uint32_t any = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) tell |= !(d[i] == 0.f);
+      for (int i = 0; i < 8; ++i) any |= __builtin_bit_cast(uint32_t, (float)d[i]);
+      tell |= any != 0;
       x.z[j] += d;
     }
     if (tell) code[j] = make_uint2(0xffffffffu, 0xffffffffu);
@@ -436,12 +447,10 @@ __global__ __launch_bounds__(kRunThreads) void probs_kernel(const LogitsArgs a) 
         if (code[j].x == 0xffffffffu) {
           x.z[j] = load8_near<DWKV_F32>(static_cast<const float*>(a.out) + (int64_t)row * a.vocab, v0 + 8 * (tid + j * NT), a.vocab);
         } else {
-          const uint2 said = make_uint2(code[j].x & 0x7f7f7f7fu, code[j].y & 0x7f7f7f7fu);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const int at8 = 8 * (i & 3);
-            x.z[j][i] = changed(x.z[j][i], (((i < 4 ? code[j].x : code[j].y) >> at8) & 255) != 0,
-                                (float)(((i < 4 ? said.x : said.y) >> at8) & 255), r);
+            const uint32_t c = ((i < 4 ? code[j].x : code[j].y) >> (8 * (i & 3))) & 255;
+            if (__any(c != 0)) x.z[j][i] = changed(x.z[j][i], c != 0, (float)(c & 127), r);
           }
         }
       }

@@ -44,6 +44,10 @@ APPEND = [
     ([1000], [77], 16, 4, 128, 128, False, "bf16", "bf16", 256),
     ([33, 7], [1, 250], 0, 2, 256, 30, False, "f16", "f16", 128),     # keys alone
     ([20, 5], [3, 0], 4, 1, 160, 0, False, "f32", "f16", 16),         # nothing turns
+    ([1001, 0, 1, 700, 700, 333], [5, 8, 0, 64, 3, 0], 3, 1, 64, 64, False, "bf16", "bf16", 32),   # two rows a workgroup, across sequences
+    ([n % 4 for n in range(150)], [n % 23 for n in range(150)], 2, 1, 32, 32, True, "f16", "f16", 16),   # more than a wave's lanes
+    ([1] * 70, list(range(70)), 2, 2, 64, 20, False, "bf16", "f16", 16),
+    ([0] * 300 + [40] + [0] * 300 + [9, 1], [0] * 601 + [3, 7], 1, 1, 32, 32, False, "f32", "bf16", 16),
 ]
 
 
@@ -168,12 +172,15 @@ DECODE = [
     ([1024, 1000], 1, 7, 64, 16, "f16", 513, []),
     ([100, 40, 16], 2, 4, 64, 16, "bf16", 0, [(0, 0), (0, 3), (0, 6), (1, 1), (2, 0)]),
     ([600], 1, 4, 128, 16, "f16", 300, [(0, c) for c in range(20)] + [(0, 30)]),
+    ([5000, 2000, 31], 2, 18, 64, 32, "bf16", 3001, [(0, c) for c in range(70)] + [(1, 9)]),
+    ([1700] * 5 + [0, 1], 3, 4, 128, 16, "f16", 0, [(1, 50)]),
 ]
 
 
-def decode_case(torch, case, seed=0, sharp=2.0, junk=float("nan")):
+def decode_case(torch, case, seed=0, sharp=2.0, junk=float("nan"), spare=1):
+    """spare: columns of the table past the longest sequence (many: a workgroup does not take a pair alone)."""
     lens, H, G, d, page, kind, window, gone = case
-    table, n_pages = deal(lens, page, columns=-(-max(max(lens), 1) // page) + 1, seed=seed)
+    table, n_pages = deal(lens, page, columns=-(-max(max(lens), 1) // page) + spare, seed=seed)
     rng = np.random.default_rng(seed)
     k, v = pool(torch, kind, n_pages, H, page, d, seed=seed)
     for b, c in gone:
@@ -197,13 +204,14 @@ def reference(case, table, k, v, q, sm_scale=None):
     return attend(q.double().cpu().numpy(), K, V, table, case[0], case[6], sm_scale)
 
 
+@pytest.mark.parametrize("spare", [1, 700])
 @pytest.mark.parametrize("case", DECODE, ids=lambda c: f"{len(c[0])}x{max(c[0])}-h{c[1]}-g{c[2]}-d{c[3]}-p{c[4]}-{c[5]}-w{c[6]}-{len(c[7])}")
-def test_decode(case):
+def test_decode(case, spare):
     torch = torch_gpu()
     lib_ready()
     from paper_2607_06523_amd import PagedCache
-    announce(f"page decode {case}")
-    table, k, v, q = decode_case(torch, case)
+    announce(f"page decode {case} {spare}")
+    table, k, v, q = decode_case(torch, case, spare=spare)
     cache = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=q.shape[1])
     out = cache.decode(0, q, window=case[6])
     want, tol = reference(case, table, k, v, q)
@@ -264,17 +272,18 @@ def test_decode_rows_without_scores():
     assert torch.equal(out, want)
 
 
-@pytest.mark.parametrize("B,top", [(300, 40), (4096, 3), (70, 600)])
-def test_decode_of_many_sequences(B, top):
+@pytest.mark.parametrize("B,top,H,G,d,spare", [(300, 40, 2, 2, 32, 1), (300, 40, 2, 2, 32, 300), (4096, 3, 2, 2, 32, 70), (70, 600, 2, 2, 32, 1),
+                                               (70, 600, 2, 2, 32, 200), (4096, 2, 1, 16, 256, 70), (64, 1500, 8, 1, 32, 1), (65, 300, 1, 20, 64, 100)])
+def test_decode_of_many_sequences(B, top, H, G, d, spare):
     torch = torch_gpu()
     lib_ready()
     from paper_2607_06523_amd import PagedCache
     announce(f"page decode of {B} sequences")
     lens = np.random.default_rng(B).integers(0, top + 1, B).tolist()
     lens[-1] = top
-    case = (lens, 2, 2, 32, 16, "f16", 0, [])
-    table, k, v, q = decode_case(torch, case)
-    out = PagedCache(k, v, i32(torch, table), i32(torch, lens), n_q_heads=4).decode(0, q)
+    case = (lens, H, G, d, 16, "f16", 0, [])
+    table, k, v, q = decode_case(torch, case, spare=spare)
+    out = PagedCache(k, v, i32(torch, table), i32(torch, lens), n_q_heads=H * G).decode(0, q)
     want, tol = reference(case, table, k, v, q)
     check(out.cpu().numpy(), want, tol, "many")
 
@@ -346,16 +355,18 @@ def test_decode_on_two_streams():
         assert all(torch.equal(o, wants[i]) for o in outs[i])
 
 
-def test_step_captured():
+@pytest.mark.parametrize("G,d,columns", [(4, 64, 8), (4, 64, 100), (16, 256, 100)])
+def test_step_captured(G, d, columns):
     """Append and decode in one graph that follows the lengths and the page table: replayed with the
     program's own work between, in a workspace that another graph shares."""
     torch = torch_gpu()
     lib_ready()
     from paper_2607_06523_amd import PagedCache, RopeTable, rope_freqs
-    announce("paged step captured")
-    B, H, G, d, page = 3, 2, 4, 64, 16
+    announce(f"paged step captured {G} {d} {columns}")
+    B, H, page = 3, 2, 16
     k, v = pool(torch, "f16", 24, H, page, d)
-    table = torch.arange(24, dtype=torch.int32, device="cuda").view(3, 8)[:, torch.randperm(8)].contiguous()
+    table = torch.full((3, columns), -1, dtype=torch.int32, device="cuda")
+    table[:, :8] = torch.arange(24, dtype=torch.int32, device="cuda").view(3, 8)[:, torch.randperm(8)]
     lens = i32(torch, [30, 0, 100])
     t = RopeTable(rope_freqs(64))
     cache = PagedCache(k, v, table, lens, n_q_heads=H * G)
