@@ -1790,7 +1790,8 @@ dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* tok
   if (n > 65535 || vocab > (1 << 30)) return DWKV_E_UNSUPPORTED;
   if (l_stride == 0) l_stride = vocab;
   if (l_stride < vocab) return DWKV_E_DIMS;
-  if (r->history && (r->history_stride < 0 || r->history_stride > 0x7fffffff - 4096)) return DWKV_E_DIMS;
+  if (r->history && r->history_stride < 0) return DWKV_E_DIMS;
+  if (r->history && r->history_stride >= 1 << 29) return DWKV_E_UNSUPPORTED;   // a list's bytes are 32-bit offsets
   if (r->bias && r->n_bias < 0) return DWKV_E_DIMS;
   if (r->bias && r->n_bias > 0x7fffffff - 4096) return DWKV_E_UNSUPPORTED;
   if (r->mask && r->mask_stride < (vocab + 31) / 32) return DWKV_E_DIMS;

@@ -54,24 +54,21 @@ __device__ __forceinline__ Rules rules_of(const LogitsArgs& a, int b) {
 
 // What counting reads first, all of it on its way at once: two waits in all, for the
 // lengths and then for the first ids of each list.
+typedef int int4_t __attribute__((ext_vector_type(4)));
 struct Lists {
-  int hist[kIds], n, m;                  // history: ids, their number, the prompt's
+  int4_t hist[kIds / 4];                 // history: ids 4 tid + 4 NT j + k, 0 past the end
+  int n, m;                              // their number, the prompt's
   int id, e0, e1;                        // biases: this thread's id of the first NT, their places
   float val;
   int parent, token;                     // of the tree's node of this lane
 };
-// Every NT-th id from i0 on, -1 past the list's end; without branches, so that nothing waits between the loads.
+// Four ids of each kIds / 4 stretches of 4 NT from `base` on, 0 past the list's end.
 template <int NT>
-__device__ __forceinline__ void fetch_ids(const int32_t* h, int i0, int n, int (&id)[kIds]) {
-  if (n <= 0) {
+__device__ __forceinline__ void fetch_ids(const int32_t* h, int base, int n, int4_t (&id)[kIds / 4]) {
+  const __amdgpu_buffer_rsrc_t list = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(h), 0, 4 * n, 0x00020000);
 #pragma unroll
-    for (int j = 0; j < kIds; ++j) id[j] = -1;
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kIds; ++j) id[j] = h[min(i0 + j * NT, n - 1)];
-#pragma unroll
-  for (int j = 0; j < kIds; ++j) id[j] = i0 + j * NT < n ? id[j] : -1;
+  for (int j = 0; j < kIds / 4; ++j)
+    id[j] = __builtin_bit_cast(int4_t, __builtin_amdgcn_raw_buffer_load_b128(list, 16 * ((int)threadIdx.x + j * NT), 4 * base, 0));
 }
 template <int NT>
 __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
@@ -90,7 +87,7 @@ __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
   x.e0 = max(x.e0, 0);
   x.e1 = min(x.e1, a.n_bias);
   const int32_t* h = a.history + b * a.history_stride;
-  fetch_ids<NT>(h, tid, x.n, x.hist);
+  fetch_ids<NT>(h, 0, x.n, x.hist);
   x.id = x.e0 + tid < x.e1 ? a.bias_id[x.e0 + tid] : -1;
   x.val = x.e0 + tid < x.e1 ? a.bias[x.e0 + tid] : 0.f;
   return x;
@@ -131,19 +128,22 @@ __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int 
     x.val = e + tid < x.e1 ? a.bias[e + tid] : 0.f;
   }
   const int32_t* h = a.history + b * a.history_stride;
-  for (int i0 = tid; i0 < x.n;) {
-    const int mine = (int)min((int64_t)x.m - i0, (int64_t)kIds * NT);     // the prompt's are the j with j * NT < mine
+  for (int base = 0; base < x.n;) {
 #pragma unroll
-    for (int j = 0; j < kIds; ++j) {
-      const uint32_t i = (uint32_t)x.hist[j] - (uint32_t)v0;   // ids below 0 lie past every run
-      if (i < (uint32_t)run) {
-        if (j * NT < mine) atomicOr(&seen[i], kInPrompt);
-        else atomicAdd(&seen[i], 1u);
+    for (int j = 0; j < kIds / 4; ++j) {
+      const int lo = base + 4 * NT * j, hi = lo + 4 * NT, at = lo + 4 * tid;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t i = (uint32_t)x.hist[j][k] - (uint32_t)v0;      // ids below 0 lie past every run
+        if (hi > x.n) i = at + k < x.n ? i : ~0u;
+        if (i < (uint32_t)run) {
+          if (hi <= x.m || (lo < x.m && at + k < x.m)) atomicOr(&seen[i], kInPrompt);
+          else atomicAdd(&seen[i], 1u);
+        }
       }
     }
-    i0 += kIds * NT;
-    if (i0 - tid >= x.n) break;
-    fetch_ids<NT>(h, i0, x.n, x.hist);
+    base += kIds * NT;
+    if (base < x.n) fetch_ids<NT>(h, base, x.n, x.hist);
   }
   if (a.cu_nodes && tid < 64) {          // the path from node 0, itself not counted, to the row's node
     int node = __builtin_amdgcn_readfirstlane(row - at.first);
@@ -185,9 +185,19 @@ template <int T, int NT, int R>
 __device__ __forceinline__ void load(const LogitsArgs& a, int row, int v0, Mine<R>& x) {
   const row_t<T>* l = static_cast<const row_t<T>*>(a.logits) + row * a.stride;
   const uint8_t* mask = reinterpret_cast<const uint8_t*>(a.mask + row * a.mask_stride);
+  const int first = v0 + 8 * (int)threadIdx.x;
+  if (v0 + 8 * NT * R <= a.vocab) {      // a run inside the row
+#pragma unroll
+    for (int j = 0; j < R; ++j) x.z[j] = load8_any<T>(l + first + 8 * j * NT);
+    if (a.mask) {
+#pragma unroll
+      for (int j = 0; j < R; ++j) x.ok[j] = mask[(first >> 3) + j * NT];
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    const int v = v0 + 8 * ((int)threadIdx.x + j * NT);
+    const int v = first + 8 * j * NT;
     x.z[j] = load8_near<T>(l, v, a.vocab);
     x.ok[j] = a.mask && v < a.vocab ? mask[v >> 3] : 0xff;
   }
@@ -201,8 +211,8 @@ __device__ __forceinline__ float changed(float l, bool seen, float said, const R
 }
 
 // l into z.  What the lists made of eight entries goes to the second launch as a byte
-// of each: 0 untouched, 1 .. 126 how often it was said, kSeen in the prompt only;
-// all ones: a bias or a larger count among them, their z are in the output.
+// of each: how often it was said, up to 126, and kSeen if it is in the prompt; all
+// ones: a bias or a larger count among them, their z are in the output.
 constexpr uint32_t kSeen = 0x80;
 template <bool TELL, int NT, int R>
 __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const uint32_t* seen, const float* bias, Mine<R>& x,
@@ -211,6 +221,7 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
   for (int j = 0; j < R; ++j) {
     const int at = 8 * ((int)threadIdx.x + j * NT);
     bool tell = false;
+    uint32_t most = 0;
     code[j] = make_uint2(0, 0);
     if (seen) {
       uint32_t c[8];
@@ -222,8 +233,8 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
           const uint32_t said = c[i] & ~kInPrompt;
           x.z[j][i] = changed(x.z[j][i], c[i] != 0, (float)said, r);
           if constexpr (TELL) {
-            (i < 4 ? code[j].x : code[j].y) |= (said ? said & 127 : c[i] ? kSeen : 0) << (8 * (i & 3));
-            tell |= said > 126;
+            (i < 4 ? code[j].x : code[j].y) |= ((c[i] & 127) | (c[i] >> 24 & kSeen)) << (8 * (i & 3));
+            most = max(most, said);
           }
         }
     }
@@ -235,7 +246,7 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
       tell |= any != 0;
       x.z[j] += d;
     }
-    if (tell) code[j] = make_uint2(0xffffffffu, 0xffffffffu);
+    if (tell || most > 126) code[j] = make_uint2(0xffffffffu, 0xffffffffu);
   }
 }
 
