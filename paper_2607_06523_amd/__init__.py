@@ -760,8 +760,9 @@ class _Runtime:
         import torch
         self.torch = torch
         self.kinds = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
-        self.device = torch.cuda.current_device
-        # the stream's handle without the object around it
+        self.i32, self.f32, self.empty = torch.int32, torch.float32, torch.empty
+        # the current device and the stream's handle, without what torch wraps around them
+        self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -787,11 +788,14 @@ def _runtime():
 
 
 def _heads(x, name):
-    """Shape and row stride of x [N, H, d], whose rows have no gaps inside."""
-    shape, s = x.shape, x.stride()
+    """Shape and row stride (0: no gap) of x [N, H, d], whose rows have no gaps inside."""
+    shape = x.shape
     if len(shape) != 3:
         raise ValueError(f"{name} must be [rows, heads, d]")
     n, h, d = shape
+    if x.is_contiguous():
+        return n, h, d, 0
+    s = x.stride()
     if n > 0 and (s[2] != 1 or h > 1 and s[1] != d):
         raise ValueError(f"the rows of {name} must have no gaps inside")
     if n <= 1:
@@ -826,7 +830,7 @@ class RopeTable:
         import torch
         if freq.dtype != torch.float64 or freq.dim() != 1 or freq.numel() < 1 or not freq.is_contiguous():
             raise TypeError("freq must be a contiguous float64 vector")
-        self.freq = freq if freq.is_cuda else freq.to(device)
+        self.freq, self.lib = freq if freq.is_cuda else freq.to(device), load()
         t = binding.RopeTable()
         t.freq, t.n_pairs, t.interleaved, t.scale = self.freq.data_ptr(), self.freq.numel(), int(bool(interleaved)), float(scale)
         self.cstruct, self.ref, self.index, self.rot_dim = t, C.byref(t), self.freq.get_device(), 2 * self.freq.numel()
@@ -838,20 +842,21 @@ def rope(x, pos, table: RopeTable, inverse: bool = False, out=None):
     same table that is the gradient with respect to x.  out: like x, of any of those
     types (x itself: in place); returns it."""
     rt = _runtime_ or _runtime()
-    kinds, i32 = rt.kinds, rt.torch.int32
-    if x.dtype not in kinds:
+    kinds, kind = rt.kinds, x.dtype
+    if kind not in kinds:
         raise TypeError("x must be float16, bfloat16 or float32")
     N, H, d, xs = _heads(x, "x")
-    if pos.dtype != i32 or pos.numel() != N or not pos.is_contiguous():
+    if pos.dtype != rt.i32 or pos.numel() != N or not pos.is_contiguous():
         raise TypeError("pos must be contiguous int32 [N]")
     if out is None:
-        out = rt.torch.empty((N, H, d), dtype=x.dtype, device=x.device)
+        out, os = rt.empty((N, H, d), dtype=kind, device=x.device), 0
     elif out.dtype not in kinds or out.shape != x.shape:
         raise TypeError("out must be float16, bfloat16 or float32 of x's shape")
-    os = _heads(out, "out")[3]
+    else:
+        os = _heads(out, "out")[3]
     if not _all_on(table.index, x, pos, out):
         raise ValueError("every tensor must be on the table's device")
-    rt.call(table.index, "dwkv_rope", load().dwkv_rope, N, H, d, table.ref, 1 if inverse else 0, x.data_ptr(), kinds[x.dtype], xs,
+    rt.call(table.index, "dwkv_rope", table.lib.dwkv_rope, N, H, d, table.ref, 1 if inverse else 0, x.data_ptr(), kinds[kind], xs,
             pos.data_ptr(), out.data_ptr(), kinds[out.dtype], os)
     return out
 
@@ -882,7 +887,7 @@ class PagedCache:
         self.index = k.get_device()
         if not _all_on(self.index, k, v, page_table, seq_len):
             raise ValueError("every tensor must be on one GPU")
-        self.k, self.v, self.page_table, self.seq_len, self.device = k, v, page_table, seq_len, k.device
+        self.k, self.v, self.page_table, self.seq_len, self.device, self.dtype = k, v, page_table, seq_len, k.device, k.dtype
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, n, H, 16 * p16, 8 * d8
         self.batch, self.n_q_heads, self.shape = B, int(n_q_heads), (B, int(n_q_heads), 8 * d8)
         c = binding.Pages()
@@ -914,7 +919,7 @@ class PagedCache:
         queries q [N, H, d], at pos int32 [N] or at the tokens' places.  Returns q_out
         [N, H, d] of the cache's type, or None without q."""
         rt = _runtime_ or _runtime()
-        kinds, i32, kind = rt.kinds, rt.torch.int32, k.dtype
+        kinds, i32, kind = rt.kinds, rt.i32, k.dtype
         if kind not in kinds or v.dtype != kind or q is not None and q.dtype != kind:
             raise TypeError("k, v and q must be float16, bfloat16 or float32, of one type")
         N, H, d, ks = _heads(k, "k")
@@ -928,8 +933,8 @@ class PagedCache:
             if n != N or dq != d:
                 raise ValueError("q must be [N, H, d]")
             if q_out is None:
-                q_out = rt.torch.empty((N, nq, d), dtype=self.k.dtype, device=self.device)
-            elif q_out.dtype != self.k.dtype or q_out.shape != q.shape or not q_out.is_contiguous():
+                q_out = rt.empty((N, nq, d), dtype=self.dtype, device=self.device)
+            elif q_out.dtype != self.dtype or q_out.shape != q.shape or not q_out.is_contiguous():
                 raise TypeError("q_out must be contiguous [N, H, d] of the cache's type")
         elif q_out is not None:
             raise ValueError("q_out without q")
@@ -959,14 +964,14 @@ class PagedCache:
         [B, Hq, d].  Without a workspace the cache's own is used: give one to calls
         that may overlap."""
         rt = _runtime_ or _runtime()
-        if q.dtype != self.k.dtype:
+        if q.dtype != self.dtype:
             raise TypeError("q must have the cache's type")
-        B, Hq, d, qs = _heads(q, "q")
-        if (B, Hq, d) != self.shape:
+        qs = _heads(q, "q")[3]
+        if q.shape != self.shape:
             raise ValueError("q must be [B, Hq, d]")
         if out is None:
-            out = rt.torch.empty(self.shape, dtype=rt.torch.float32, device=self.device)
-        elif out.dtype != rt.torch.float32 or out.shape != self.shape or not out.is_contiguous():
+            out = rt.empty(self.shape, dtype=rt.f32, device=self.device)
+        elif out.dtype != rt.f32 or out.shape != self.shape or not out.is_contiguous():
             raise TypeError("out must be contiguous float32 [B, Hq, d]")
         if workspace is None:
             if self._ws is None:
@@ -974,7 +979,7 @@ class PagedCache:
             workspace = self._ws
         if not _all_on(self.index, q, out, workspace):
             raise ValueError("every tensor must be on the cache's device")
-        rt.call(self.index, "dwkv_page_decode", self.lib.dwkv_page_decode, self.ref, int(layer), q.data_ptr(), qs, Hq,
+        rt.call(self.index, "dwkv_page_decode", self.lib.dwkv_page_decode, self.ref, int(layer), q.data_ptr(), qs, self.n_q_heads,
                 float(sm_scale or 0.0), int(window), out.data_ptr(), workspace.data_ptr(), _nbytes(workspace))
         return out
 
@@ -1060,7 +1065,7 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     tokens (token int32 [N]) behind its sequence's history.  out [N, vocab], by default
     float32 with probs, else the logits' type; logits itself: in place."""
     rt = _runtime_ or _runtime()
-    kinds, i32 = rt.kinds, rt.torch.int32
+    kinds, i32 = rt.kinds, rt.i32
     if logits.dtype not in kinds or logits.dim() != 2 or logits.numel() and logits.stride(1) != 1:
         raise TypeError("logits must be [N, vocab] of float32, float16 or bfloat16")
     N, V = logits.shape
@@ -1081,7 +1086,7 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     if rules.mask is not None and (rules.mask.shape[0] != N or rules.mask.shape[1] < (V + 31) // 32):
         raise ValueError("mask must have a row of (vocab + 31) / 32 words for each row")
     if out is None:
-        out = rt.torch.empty((N, V), dtype=rt.torch.float32 if probs else logits.dtype, device=logits.device)
+        out = rt.empty((N, V), dtype=rt.f32 if probs else logits.dtype, device=logits.device)
     elif out.dtype not in kinds or out.shape != logits.shape or not out.is_contiguous():
         raise TypeError("out must be contiguous [N, vocab] of float32, float16 or bfloat16")
     index = logits.get_device()

@@ -487,6 +487,7 @@ struct PageArgs {
   int32_t batch, n_kv_heads, group, n_rb;    // n_rb: blocks of 16 heads of a group
   int32_t rows;                // min(group, 16)
   int32_t n_pages, max_pages, page_shift, window;
+  int32_t longest_first;       // workgroups in the order of their lengths (launch_page_decode)
   float qscale;                // sm_scale * log2(e)
 };
 hipError_t launch_page_decode(const PageArgs& a, int d, int type, hipStream_t s);

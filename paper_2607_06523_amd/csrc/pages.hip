@@ -109,6 +109,15 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
   };
   if constexpr (SINGLE) {
     b = blockIdx.y;
+    if (a.longest_first) {               // the order in which workgroups start: short ones fill the end
+      const int t = lane < a.batch ? tiles_of(span_of(a, lane)) : -1;
+      int before = 0;
+      for (int i = 0; i < a.batch; ++i) {
+        const int o = __builtin_amdgcn_readlane(t, i);
+        before += o > t || (o == t && i < lane);
+      }
+      b = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(lane < a.batch && before == (int)blockIdx.y)));
+    }
     wgp = blockIdx.x;
     const int p = ((wv * kPageTile) >> (a.page_shift + 4)) + lane;
     if (p < a.max_pages) early = a.table[(int64_t)b * a.max_pages + p];
@@ -512,7 +521,7 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
 bool one_workgroup_each(int64_t tiles, int64_t pairs) { return tiles <= 32 || (tiles <= 128 && pairs >= 2 * kPageWG); }
 
 template <int D, int TY>
-hipError_t launch_t(const PageArgs& a, hipStream_t s) {
+hipError_t launch_t(PageArgs a, hipStream_t s) {
   const int64_t room = (((int64_t)a.max_pages << (a.page_shift + 4)) + kPageTile - 1) / kPageTile;
   const int64_t most = a.window > 0 ? std::min<int64_t>(room, (a.window + kPageTile - 2) / kPageTile + 1) : room;
   const bool single = one_workgroup_each(most, (int64_t)a.n_kv_heads * a.n_rb * a.batch);
@@ -523,6 +532,8 @@ hipError_t launch_t(const PageArgs& a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (single) {
+    // where not all start at once, and a wave holds the lengths
+    a.longest_first = a.batch <= 64 && (int64_t)a.n_kv_heads * a.n_rb * a.batch > kPageWG;
     hipLaunchKernelGGL((page_split_kernel<D, TY, true>), dim3(a.n_kv_heads * a.n_rb, a.batch), dim3(kPT), lds, s, a);
   } else {
     hipLaunchKernelGGL((page_split_kernel<D, TY, false>), dim3(kPageWG), dim3(kPT), lds, s, a);
