@@ -766,16 +766,6 @@ class _Runtime:
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
 
-    def call(self, index, where, f, *args):
-        """f(*args, stream) on GPU index, its status checked."""
-        if self.device() == index:
-            st = f(*args, self.stream(index))
-        else:
-            with _on(self.torch, index):
-                st = f(*args, self.stream(index))
-        if st != 0:
-            raise DwkvError(st, where)
-
 
 _runtime_ = None
 
@@ -850,14 +840,20 @@ def rope(x, pos, table: RopeTable, inverse: bool = False, out=None):
         raise TypeError("pos must be contiguous int32 [N]")
     if out is None:
         out, os = rt.empty((N, H, d), dtype=kind, device=x.device), 0
-    elif out.dtype not in kinds or out.shape != x.shape:
-        raise TypeError("out must be float16, bfloat16 or float32 of x's shape")
     else:
-        os = _heads(out, "out")[3]
-    if not _all_on(table.index, x, pos, out):
+        n, h, c, os = _heads(out, "out")
+        if out.dtype not in kinds or n != N or h != H or c != d:
+            raise TypeError("out must be float16, bfloat16 or float32 of x's shape")
+    index = table.index
+    if not _all_on(index, x, pos, out):
         raise ValueError("every tensor must be on the table's device")
-    rt.call(table.index, "dwkv_rope", table.lib.dwkv_rope, N, H, d, table.ref, 1 if inverse else 0, x.data_ptr(), kinds[kind], xs,
-            pos.data_ptr(), out.data_ptr(), kinds[out.dtype], os)
+    if rt.device() != index:
+        with _on(rt.torch, index):
+            return rope(x, pos, table, inverse, out)
+    st = table.lib.dwkv_rope(N, H, d, table.ref, 1 if inverse else 0, x.data_ptr(), kinds[kind], xs, pos.data_ptr(), out.data_ptr(),
+                             kinds[out.dtype], os, rt.stream(index))
+    if st:
+        raise DwkvError(st, "dwkv_rope")
     return out
 
 
@@ -934,7 +930,7 @@ class PagedCache:
                 raise ValueError("q must be [N, H, d]")
             if q_out is None:
                 q_out = rt.empty((N, nq, d), dtype=self.dtype, device=self.device)
-            elif q_out.dtype != self.dtype or q_out.shape != q.shape or not q_out.is_contiguous():
+            elif q_out.dtype != self.dtype or _heads(q_out, "q_out") != (N, nq, d, 0):
                 raise TypeError("q_out must be contiguous [N, H, d] of the cache's type")
         elif q_out is not None:
             raise ValueError("q_out without q")
@@ -945,12 +941,18 @@ class PagedCache:
             raise TypeError("cu_new must be contiguous int32 [B+1]")
         if pos is not None and (pos.dtype != i32 or pos.numel() != N or not pos.is_contiguous()):
             raise TypeError("pos must be contiguous int32 [N]")
-        if not _all_on(self.index, k, v, q, q_out, cu_new, pos) or rope is not None and rope.index != self.index:
+        index = self.index
+        if not _all_on(index, k, v, q, q_out, cu_new, pos) or rope is not None and rope.index != index:
             raise ValueError("every tensor must be on the cache's device")
-        rt.call(self.index, "dwkv_page_append", self.lib.dwkv_page_append, self.ref, int(layer), N,
-                None if cu_new is None else cu_new.data_ptr(), k.data_ptr(), v.data_ptr(), kinds[kind], ks,
-                None if q is None else q.data_ptr(), qs, nq, None if rope is None else rope.ref,
-                None if pos is None else pos.data_ptr(), None if q is None else q_out.data_ptr())
+        if rt.device() != index:
+            with _on(rt.torch, index):
+                return self.append(layer, k, v, cu_new, q, rope, pos, q_out)
+        st = self.lib.dwkv_page_append(self.ref, int(layer), N, None if cu_new is None else cu_new.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                       kinds[kind], ks, None if q is None else q.data_ptr(), qs, nq,
+                                       None if rope is None else rope.ref, None if pos is None else pos.data_ptr(),
+                                       None if q is None else q_out.data_ptr(), rt.stream(index))
+        if st:
+            raise DwkvError(st, "dwkv_page_append")
         return q_out
 
     def workspace(self):
@@ -966,21 +968,27 @@ class PagedCache:
         rt = _runtime_ or _runtime()
         if q.dtype != self.dtype:
             raise TypeError("q must have the cache's type")
-        qs = _heads(q, "q")[3]
-        if q.shape != self.shape:
+        B, Hq, d, qs = _heads(q, "q")
+        if B != self.batch or Hq != self.n_q_heads or d != self.head_dim:
             raise ValueError("q must be [B, Hq, d]")
         if out is None:
             out = rt.empty(self.shape, dtype=rt.f32, device=self.device)
-        elif out.dtype != rt.f32 or out.shape != self.shape or not out.is_contiguous():
+        elif out.dtype != rt.f32 or _heads(out, "out") != (B, Hq, d, 0):
             raise TypeError("out must be contiguous float32 [B, Hq, d]")
         if workspace is None:
             if self._ws is None:
                 self._ws = self.workspace()
             workspace = self._ws
-        if not _all_on(self.index, q, out, workspace):
+        index = self.index
+        if not _all_on(index, q, out, workspace):
             raise ValueError("every tensor must be on the cache's device")
-        rt.call(self.index, "dwkv_page_decode", self.lib.dwkv_page_decode, self.ref, int(layer), q.data_ptr(), qs, self.n_q_heads,
-                float(sm_scale or 0.0), int(window), out.data_ptr(), workspace.data_ptr(), _nbytes(workspace))
+        if rt.device() != index:
+            with _on(rt.torch, index):
+                return self.decode(layer, q, sm_scale, window, out, workspace)
+        st = self.lib.dwkv_page_decode(self.ref, int(layer), q.data_ptr(), qs, Hq, sm_scale or 0.0, int(window), out.data_ptr(),
+                                       workspace.data_ptr(), _nbytes(workspace), rt.stream(index))
+        if st:
+            raise DwkvError(st, "dwkv_page_decode")
         return out
 
 
@@ -1028,7 +1036,7 @@ class LogitsRules:
             raise ValueError("the rules are of different numbers of sequences")
         self.n_seq = S.pop() if S else None
         self.keep = [x for x in (params, history, history_len, prompt_len, mask) + tuple(bias or ()) if x is not None]
-        self.mask = mask
+        self.mask_rows, self.mask_words = (None, 0) if mask is None else mask.shape
         self.index = self.keep[0].get_device() if self.keep else None
         if self.keep and not _all_on(self.index, *self.keep):
             raise ValueError("every tensor must be on one GPU")
@@ -1045,7 +1053,7 @@ class LogitsRules:
             r.cu_bias, r.bias_id, r.bias, r.n_bias = ptr(bias[0]), ptr(bias[1]), ptr(bias[2]), bias[1].numel()
         if mask is not None:
             r.mask_stride = mask.stride(0) if mask.shape[0] > 1 else mask.shape[1]
-        self.cstruct, self.ref = r, C.byref(r)
+        self.cstruct, self.ref, self.lib = r, C.byref(r), load()
 
 
 def adjust_logits_workspace(logits):
@@ -1066,12 +1074,18 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     float32 with probs, else the logits' type; logits itself: in place."""
     rt = _runtime_ or _runtime()
     kinds, i32 = rt.kinds, rt.i32
-    if logits.dtype not in kinds or logits.dim() != 2 or logits.numel() and logits.stride(1) != 1:
+    shape = logits.shape
+    if logits.dtype not in kinds or len(shape) != 2:
         raise TypeError("logits must be [N, vocab] of float32, float16 or bfloat16")
-    N, V = logits.shape
-    ls = logits.stride(0) if N > 1 else 0
-    if N > 1 and ls < V:
-        raise ValueError("the rows of logits must not overlap")
+    N, V = shape
+    ls = 0
+    if not logits.is_contiguous():
+        ls, one = logits.stride()
+        if one != 1 and V > 1:
+            raise TypeError("the rows of logits must have no gaps inside")
+        if N > 1 and ls < V:
+            raise ValueError("the rows of logits must not overlap")
+        ls = ls if N > 1 else 0
     S = N
     if tree is not None:
         S = tree.batch
@@ -1083,11 +1097,11 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
         raise ValueError("token without a tree")
     if rules.n_seq is not None and rules.n_seq != S:
         raise ValueError("the rules are of another number of sequences")
-    if rules.mask is not None and (rules.mask.shape[0] != N or rules.mask.shape[1] < (V + 31) // 32):
+    if rules.mask_rows is not None and (rules.mask_rows != N or rules.mask_words < (V + 31) // 32):
         raise ValueError("mask must have a row of (vocab + 31) / 32 words for each row")
     if out is None:
         out = rt.empty((N, V), dtype=rt.f32 if probs else logits.dtype, device=logits.device)
-    elif out.dtype not in kinds or out.shape != logits.shape or not out.is_contiguous():
+    elif out.dtype not in kinds or out.shape != shape or not out.is_contiguous():
         raise TypeError("out must be contiguous [N, vocab] of float32, float16 or bfloat16")
     index = logits.get_device()
     if rules.index not in (None, index) or tree is not None and tree.index != index or not _all_on(index, logits, token, out, workspace):
@@ -1095,7 +1109,12 @@ def adjust_logits(logits, rules: LogitsRules, tree: DraftTree | None = None, tok
     if N == 0:
         return out
     ws = workspace if workspace is not None or not probs else adjust_logits_workspace(logits)
-    rt.call(index, "dwkv_logits", load().dwkv_logits, S, None if tree is None else tree.ref, None if token is None else token.data_ptr(),
-            V, logits.data_ptr(), kinds[logits.dtype], ls, rules.ref, 1 if probs else 0, out.data_ptr(), kinds[out.dtype],
-            None if ws is None else ws.data_ptr(), 0 if ws is None else _nbytes(ws))
+    if rt.device() != index:
+        with _on(rt.torch, index):
+            return adjust_logits(logits, rules, tree, token, probs, out, ws)
+    st = rules.lib.dwkv_logits(S, None if tree is None else tree.ref, None if token is None else token.data_ptr(), V, logits.data_ptr(),
+                               kinds[logits.dtype], ls, rules.ref, 1 if probs else 0, out.data_ptr(), kinds[out.dtype],
+                               None if ws is None else ws.data_ptr(), 0 if ws is None else _nbytes(ws), rt.stream(index))
+    if st:
+        raise DwkvError(st, "dwkv_logits")
     return out
