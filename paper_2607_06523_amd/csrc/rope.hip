@@ -280,9 +280,10 @@ __device__ __forceinline__ void find_rows(const AppendArgs& a, int r0, int rows,
     for (int j = 0; j < rows; ++j) {
       const unsigned long long after = __ballot(lane < a.batch && c1 > r0 + j);
       const int k = after ? __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(after)) : 0;
+      const int at = __builtin_amdgcn_readlane(len, k) - (__builtin_amdgcn_readlane(c1, k) - (r0 + j));
       if (threadIdx.x == 0) {
         in[j] = after != 0;
-        place[j] = __builtin_amdgcn_readlane(len, k) - (__builtin_amdgcn_readlane(c1, k) - (r0 + j));
+        place[j] = at;
       }
     }
   } else {                               // sequences that end before the row
