@@ -68,7 +68,7 @@ __device__ __forceinline__ void fetch_ids(const int32_t* h, int base, int n, int
   const __amdgpu_buffer_rsrc_t list = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(h), 0, 4 * n, 0x00020000);
 #pragma unroll
   for (int j = 0; j < kIds / 4; ++j)
-    id[j] = __builtin_bit_cast(int4_t, __builtin_amdgcn_raw_buffer_load_b128(list, 16 * ((int)threadIdx.x + j * NT), 4 * base, 0));
+    id[j] = __builtin_bit_cast(int4_t, __builtin_amdgcn_raw_buffer_load_b128(list, (int)(16u * (threadIdx.x + j * NT) + 4u * (uint32_t)base), 0, 0));
 }
 template <int NT>
 __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
@@ -84,7 +84,7 @@ __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
     x.token = a.token[at.first + lane];
   }
   x.n = (int)min((int64_t)max(x.n, 0), a.history_stride);
-  x.e0 = max(x.e0, 0);
+  x.e0 = min(max(x.e0, 0), a.n_bias);
   x.e1 = min(x.e1, a.n_bias);
   const int32_t* h = a.history + b * a.history_stride;
   fetch_ids<NT>(h, 0, x.n, x.hist);
@@ -274,7 +274,11 @@ __device__ __forceinline__ void put8(const LogitsArgs& a, int row, int v, float8
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
-__device__ __forceinline__ float scale_of(const Rules& r) { return r.temp > 0.f ? kLog2e / r.temp : 0.f; }
+// Neither infinite nor 0, so that 0 and -inf times it stay what they are: a temperature
+// of +inf makes what is allowed even, the smallest one leaves the largest entries.
+__device__ __forceinline__ float scale_of(const Rules& r) {
+  return r.temp > 0.f ? fminf(fmaxf(kLog2e / r.temp, 0x1p-126f), 0x1.fffffep127f) : 0.f;
+}
 __device__ __forceinline__ float wave_max(float v) {
   for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;

@@ -120,6 +120,25 @@ def test_greedy_rows():
     assert torch.equal(out, want)
 
 
+@pytest.mark.parametrize("V", [900, 30000])
+def test_temperatures_at_the_ends(V):
+    """+inf makes what is allowed even; the smallest ones, whose inverse is no float32, leave the largest entries."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import LogitsRules, adjust_logits
+    announce(f"temperatures at the ends {V}")
+    l = torch.randn((3, V), generator=torch.Generator().manual_seed(1)).cuda()
+    l[:, [5, V - 1]] = 9.0
+    l[:, 7] = float("-inf")
+    params = torch.tensor([[1.0, 0.0, 0.0, t] for t in (float("inf"), 1e-38, 1e-45)], device="cuda")
+    out = adjust_logits(l, LogitsRules(params=params)).double()
+    even = torch.full((V,), 1 / (V - 1), dtype=torch.float64, device="cuda")
+    even[7] = 0
+    # a sum of V ones is exact, its inverse and the product rounded
+    assert ((out[0] - even).abs() <= 2 ** -22 * even).all()
+    assert (out[1:, [5, V - 1]] == 0.5).all() and (out[1:].sum(1) == 1).all()
+
+
 def test_rows_that_are_not_numbers():
     """Masked NaN and infinities count for nothing; one that is not masked makes its row NaN and no other."""
     torch = torch_gpu()
