@@ -714,13 +714,15 @@ typedef struct dwkv_pages {
  * turned at its position, its value as it is, both rounded once to the cache's
  * type.  Its queries are turned too, into q_out.
  *   n_rows:  N rows of q, k and v
- *   cu_new:  DEVICE [B+1] packed starts of the new rows, or NULL: N = B, one row for
- *            each sequence.  Rows from cu_new[B] on are left out, q_out's too
+ *   cu_new:  DEVICE [B+1] packed starts of the new rows (the first 0), or NULL: N = B,
+ *            one row for each sequence.  Rows from cu_new[B] on are left out, q_out's
+ *            too
  *   k, v:    rows of [Hkv][d] in x_type (DWKV_F16, DWKV_BF16 or DWKV_F32), kv_stride
  *            elements apart;  q: NULL, or rows of [n_q_heads][d], q_stride apart
  *   table:   NULL: nothing turns;  pos: DEVICE int32 [N] positions, NULL: the
  *            tokens' places in their sequences
- *   q_out:   [N][n_q_heads][d] in the cache's type, no overlap with the inputs
+ *   q_out:   [N][n_q_heads][d] in the cache's type.  It may be q when types agree and
+ *            rows have no gap; no other overlap
  * A row whose place lies before the sequence's start (a sequence of length 0 in a
  * padded batch), past its table or in no page is not stored.  A place in one page
  * that two sequences share must not be written by both.  Strides are multiples of
@@ -746,8 +748,11 @@ size_t dwkv_page_workspace_bytes(const dwkv_pages* pages, int32_t n_q_heads);
  *   workspace:>= dwkv_page_workspace_bytes bytes, no initial contents
  * Scores and sums are float32; probabilities have 22 bits (24 in bfloat16 caches)
  * down to 2^-12 of a row's largest.  n_q_heads is a multiple of Hkv, any group.
- * q, out, pages and workspace are 16-byte aligned.  Two launches.
- * DWKV_E_UNSUPPORTED for lists of 2^31 or more tiles of 32 tokens. */
+ * q, out, pages and workspace are 16-byte aligned.  One launch where the table or the
+ * window spans 32 tiles of 32 tokens at most (128 with 512 or more KV heads over the
+ * batch), else two.  Groups of more than 16 heads read a KV head's tokens once for every 16.
+ * DWKV_E_UNSUPPORTED for lists of 2^31 or more tiles of 32 tokens, and for more than
+ * 2^22 rows of out. */
 dwkv_status dwkv_page_decode(const dwkv_pages* pages, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,
                              float sm_scale, int32_t window, float* out, void* workspace, size_t ws_bytes, void* stream);
 
@@ -775,12 +780,12 @@ size_t dwkv_logits_workspace_bytes(int32_t n_rows, int32_t vocab);
 /* Rows of logits made ready to draw from, or to verify drafts against
  * (dwkv_tree_verify's target or draft).  For entry t of a row, in this order, each
  * step in float32:
- *   z = l;   t in the history: z = z > 0 ? z / repetition : z repetition
- *   t said c > 0 times:        z = z - frequency c - presence
+ *   z = l;   t in the history: z = z > 0 ? z (1 / repetition) : z repetition
+ *   t said c > 0 times:        z = z - (frequency c + presence)
  *   z = z + bias (one listed twice adds twice);   not allowed: z = -inf
  * and out = z, or with probs != 0
- *   out = softmax(z / temperature);  temperature <= 0 or NaN: 1 at the first largest
- *         z that is not -inf or NaN, else 0
+ *   out = softmax(z / temperature), at +inf its limit;  temperature <= 0 or NaN: 1 at
+ *         the first largest z that is not -inf or NaN, else 0
  * A row of nothing but -inf has probabilities 0, one with a NaN or +inf NaN. "Said"
  * are the history's ids from prompt_len on and, with a tree, the tokens on the
  * path from node 0 to the row's node, node 0's not (it is the history's last).
@@ -795,8 +800,8 @@ size_t dwkv_logits_workspace_bytes(int32_t n_rows, int32_t vocab);
  *   workspace: with probs, >= dwkv_logits_workspace_bytes(N, vocab), no initial
  *            contents, 16-byte aligned; else unused
  * Pointers are aligned to their type.  N up to 65535, vocab up to 2^30, history_stride
- * under 2^29.  One launch,
- * with probs two (none for no rows). */
+ * under 2^29.  One launch; with probs and rows of more than 8192 entries up to two
+ * (none for no rows). */
 dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, const void* logits,
                         int32_t l_type, int64_t l_stride, const dwkv_logits_rules* rules, int32_t probs, void* out,
                         int32_t out_type, void* workspace, size_t ws_bytes, void* stream);

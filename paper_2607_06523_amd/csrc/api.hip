@@ -1610,7 +1610,8 @@ int64_t page_layer(const dwkv_pages* p) { return (int64_t)p->n_pages * p->n_kv_h
 
 dwkv_status check_page_heads(const dwkv_pages* p, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads % p->n_kv_heads != 0) return DWKV_E_DIMS;
-  if (n_q_heads > 65535) return DWKV_E_UNSUPPORTED;
+  // a workgroup for each row of the output
+  if (n_q_heads > 65535 || (int64_t)n_q_heads * p->batch > 1 << 22) return DWKV_E_UNSUPPORTED;
   // the list of tiles of every sequence, KV head and block of 16 heads
   const int64_t group = n_q_heads / p->n_kv_heads, tiles = ((int64_t)p->max_pages * p->page_size + kPageTile - 1) / kPageTile + 1;
   const double list = (double)p->batch * tiles * p->n_kv_heads * (double)((group + 15) / 16);
@@ -1705,6 +1706,7 @@ dwkv_status dwkv_page_append(const dwkv_pages* p, int32_t layer, int32_t n_rows,
   if (n_rows == 0) return DWKV_OK;
   if (!k || !v || (q && !q_out)) return DWKV_E_NULL;
   if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out) || !aligned4(cu_new) || !aligned4(pos)) return DWKV_E_ALIGN;
+  if (q && q == q_out && (x_type != p->type || q_stride != (int64_t)n_q_heads * p->head_dim)) return DWKV_E_DIMS;
   AppendArgs a;
   std::memset(&a, 0, sizeof(a));
   a.t = rope_spec(table, false);

@@ -133,6 +133,24 @@ def test_append_leaves_out_what_has_no_place():
             assert (V[p, :, o] == (V0[p, :, o] if r is None else rows[r, 3 * H:].cpu().numpy())).all(), (p, o)
 
 
+@pytest.mark.parametrize("rot", [64, 42])
+def test_append_turns_queries_in_place(rot):
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache, RopeTable, rope_freqs
+    announce(f"append in place {rot}")
+    lens = [40, 3, 17]
+    table, n_pages = deal(lens, 16)
+    cache = PagedCache(*pool(torch, "f16", n_pages, 2, 16, 64), i32(torch, table), i32(torch, lens), n_q_heads=6)
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn((24, h, 64), generator=g).half().cuda() for h in (6, 2, 2))
+    cu, t = i32(torch, [0, 20, 20, 23]), RopeTable(rope_freqs(rot))
+    want = cache.append(0, k, v, cu_new=cu, q=q, rope=t)
+    want[23:] = q[23:]                                        # behind the last start
+    assert cache.append(0, k, v, cu_new=cu, q=q, rope=t, q_out=q) is q
+    assert torch.equal(q, want)
+
+
 def test_append_at_given_positions():
     torch = torch_gpu()
     lib_ready()

@@ -157,7 +157,8 @@ def test_append_refused(lib):
                      (dict(table=T(pairs=0)), 2), (dict(table=T(pairs=33)), 2), (dict(table=T(freq=None)), 1), (dict(table=T(freq=FAKE + 4)), 7),
                      (dict(k=None), 1), (dict(v=None), 1), (dict(q_out=None), 1), (dict(n=(1 << 24) + 1, cu=FAKE), 3),
                      (dict(k=FAKE + 8), 7), (dict(v=FAKE + 8), 7), (dict(q=FAKE + 8), 7), (dict(q_out=FAKE + 8), 7),
-                     (dict(cu=FAKE + 2), 7), (dict(pos=FAKE + 2), 7)]:
+                     (dict(cu=FAKE + 2), 7), (dict(pos=FAKE + 2), 7),
+                     (dict(xt=1), 2), (dict(xt=2), 2), (dict(qs=264), 2)]:           # q_out over q: of another type, with gaps
         assert append_status(lib, **kw) == want, kw
 
 
@@ -168,6 +169,8 @@ def test_page_decode_refused(lib):
                      (dict(qs=258), 2), (dict(q=None), 1), (dict(out=None), 1), (dict(ws=None), 1), (dict(ws_bytes=need - 1), 4),
                      (dict(q=FAKE + 2), 7), (dict(out=FAKE + 4), 7), (dict(ws=FAKE + 8), 7)]:
         assert decode_status(lib, **kw) == want, kw
+    p = pages(batch=4096)
+    assert decode_status(lib, p, nq=2048) == 3 and decode_status(lib, p, nq=1026) == 3 and decode_status(lib, p, nq=65536) == 3
     # a list of tiles past 2^31
     p = pages(batch=4096, max_pages=1 << 23, n_kv_heads=2)
     assert decode_status(lib, p) == 3 and lib.dwkv_page_workspace_bytes(C.byref(p), 4) == 0
