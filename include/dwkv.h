@@ -748,9 +748,8 @@ size_t dwkv_page_workspace_bytes(const dwkv_pages* pages, int32_t n_q_heads);
  *   workspace:>= dwkv_page_workspace_bytes bytes, no initial contents
  * Scores and sums are float32; probabilities have 22 bits (24 in bfloat16 caches)
  * down to 2^-12 of a row's largest.  n_q_heads is a multiple of Hkv, any group.
- * q, out, pages and workspace are 16-byte aligned.  One launch where the table or the
- * window spans 32 tiles of 32 tokens at most (128 with 512 or more KV heads over the
- * batch), else two.  Groups of more than 16 heads read a KV head's tokens once for every 16.
+ * q, out, pages and workspace are 16-byte aligned.  One launch where
+ * the table or the window allows few tokens, else two.  Groups of more than 16 heads read a KV head's tokens once for every 16.
  * DWKV_E_UNSUPPORTED for lists of 2^31 or more tiles of 32 tokens, and for more than
  * 2^22 rows of out. */
 dwkv_status dwkv_page_decode(const dwkv_pages* pages, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,

@@ -7,7 +7,9 @@
 // about keeping loads in flight.
 //  * Lengths and page tables are device data (a captured graph follows them), so
 //    the work is shared out on the device: tiles of 32 tokens of every (sequence,
-//    KV head, block of 16 heads) in one list, an equal run of it for each wave.
+//    KV head, block of 16 heads) in one list, an equal run of it for each wave.  Where
+//    one workgroup can read a pair's tokens in the time that the second launch takes, each
+//    pair has one, and the longest sequences come first.
 //  * Keys lie in tiles of 16 tokens x 8 channels and values in blocks of 8 tokens, as
 //    the factorized cache's coefficients do: each wave load covers whole 128-byte lines
 //    and is an operand as it stands.  Scores come out with a lane's head down its
@@ -28,6 +30,8 @@ namespace dwkv {
 namespace {
 
 constexpr int kPT = 64 * kPageWaves;
+constexpr int kSingleTiles = 128, kSingleBits = 8;    // most tiles of a pair that one workgroup takes, and their bits
+constexpr int kRanked = 256;             // sequences that are taken longest first
 constexpr float kNoRef = -1.7e38f;       // reference of a row without scores
 constexpr float kRefTop = 9.f, kRefMove = 15.5f;
 
@@ -74,8 +78,65 @@ __device__ __forceinline__ Span span_of(const PageArgs& a, int b) {
 }
 __device__ __forceinline__ int tiles_of(Span s) { return (s.len + kPageTile - 1) / kPageTile - s.start / kPageTile; }
 
+// How the list of `total` tiles is shared out: runs of `wg` for each workgroup and of `per` for
+// each of its waves.  Lists of less than a tile a wave go to all workgroups evenly, as
+// what one compute unit can read at a time is the limit there.
+struct Share {
+  int wg, per;
+};
+__device__ __forceinline__ Share share_of(int total) {
+  Share s;
+  s.per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
+  s.wg = s.per > 1 ? s.per * kPageWaves : max(1, (total + kPageWG - 1) / kPageWG);
+  return s;
+}
+
 // Slot of the partial that run [x, ...) of wave w writes for the pair that begins at p0.
 __device__ __forceinline__ int slot_of(int w, int x, int p0) { return 2 * w + (x > p0 ? 0 : 1); }
+
+// The sequence with `rank` ones before it in the order from the longest to the shortest, equal ones as
+// they come: up to kRanked sequences, up to 2^kSingleBits - 1 tiles.  A bit at a time: those with it
+// come before those without.
+__device__ __forceinline__ int of_rank(const PageArgs& a, int rank, int lane) {
+  constexpr int N = kRanked / 64;
+  int t[N];
+  unsigned long long left[N];            // those that share the bits so far
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    const int i = 64 * c + lane;
+    t[c] = 0;
+    left[c] = 0;
+    if (64 * c < a.batch) {
+      left[c] = __ballot(i < a.batch);
+      if (i < a.batch) t[c] = tiles_of(span_of(a, i));
+    }
+  }
+#pragma unroll
+  for (int bit = kSingleBits - 1; bit >= 0; --bit) {
+    unsigned long long set[N];
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+      set[c] = 0;
+      if (64 * c < a.batch) set[c] = __ballot((t[c] >> bit) & 1) & left[c];
+      n += (int)__popcll(set[c]);
+    }
+    const bool in = rank < n;
+    if (!in) rank -= n;
+#pragma unroll
+    for (int c = 0; c < N; ++c) left[c] = in ? set[c] : left[c] & ~set[c];
+  }
+  int b = 0;
+#pragma unroll
+  for (int c = 0; c < N; ++c) {
+    const int n = (int)__popcll(left[c]);
+    const int below = __builtin_amdgcn_mbcnt_hi((uint32_t)(left[c] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)left[c], 0));
+    const unsigned long long it = __ballot((left[c] >> lane & 1) && below == rank);
+    if (it) b = 64 * c + (int)__builtin_ctzll(it);
+    rank = rank < n ? -1 : rank - n;
+  }
+  return __builtin_amdgcn_readfirstlane(b);
+}
 
 // SINGLE: grid (KV heads x blocks of 16 heads, B), a workgroup for each pair, the output
 // written at once.  Else kPageWG workgroups, and a merge after it.
@@ -110,13 +171,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
   if constexpr (SINGLE) {
     b = blockIdx.y;
     if (a.longest_first) {               // the order in which workgroups start: short ones fill the end
-      const int t = lane < a.batch ? tiles_of(span_of(a, lane)) : -1;
-      int before = 0;
-      for (int i = 0; i < a.batch; ++i) {
-        const int o = __builtin_amdgcn_readlane(t, i);
-        before += o > t || (o == t && i < lane);
-      }
-      b = __builtin_amdgcn_readfirstlane((int)__builtin_ctzll(__ballot(lane < a.batch && before == (int)blockIdx.y)));
+      b = of_rank(a, blockIdx.y, lane);
     }
     wgp = blockIdx.x;
     const int p = ((wv * kPageTile) >> (a.page_shift + 4)) + lane;
@@ -166,12 +221,12 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
       __syncthreads();
     }
     total *= pairs;
-    const int per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
-    wg0 = min(total, (int)blockIdx.x * kPageWaves * per);
-    wg1 = min(total, wg0 + kPageWaves * per);
+    const Share s = share_of(total);
+    wg0 = min(total, (int)blockIdx.x * s.wg);
+    wg1 = min(total, wg0 + s.wg);
     if (wg0 >= wg1) return;
-    x = min(total, w * per);
-    end = min(total, x + per);
+    x = min(wg1, wg0 + wv * s.per);
+    end = min(wg1, x + s.per);
     b = seq_at(wg0);
     wgT = before(b + 1) - before(b);
     wgp = (wg0 - before(b) * pairs) / wgT;
@@ -438,18 +493,18 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
     if (threadIdx.x < D) out[threadIdx.x] = 0.f;
     return;
   }
-  const int per = max(1, (total + kPageWG * kPageWaves - 1) / (kPageWG * kPageWaves));
+  const Share s = share_of(total);
   const int p0 = pb * pairs + (h * a.n_rb + r / 16) * T, p1 = p0 + T;
-  const int w0 = p0 / per, w1 = (p1 - 1) / per;
+  const int g0 = p0 / s.wg, g1 = (p1 - 1) / s.wg;
+  const int w0 = g0 * kPageWaves + (p0 - g0 * s.wg) / s.per, w1 = g1 * kPageWaves + (p1 - 1 - g1 * s.wg) / s.per;
   if (w0 == w1) return;                                      // written by its wave
-  const int g0 = w0 / kPageWaves, g1 = w1 / kPageWaves;
   const auto joined = [&](int g) {
-    const int x = g * kPageWaves * per;
-    return x >= p0 && min(total, x + kPageWaves * per) <= p1;
+    const int x = g * s.wg;
+    return x >= p0 && min(total, x + s.wg) <= p1;
   };
   const bool j0 = joined(g0), j1 = joined(g1);
   if (g0 == g1 && j0) return;                                // written by its workgroup
-  const int n0 = j0 ? 1 : min(w1, g0 * kPageWaves + kPageWaves - 1) - w0 + 1, mid = max(0, g1 - g0 - 1);
+  const int n0 = j0 ? 1 : min(w1, g0 * kPageWaves + (s.wg - 1) / s.per) - w0 + 1, mid = max(0, g1 - g0 - 1);
   const int n = n0 + mid + (g1 == g0 ? 0 : j1 ? 1 : w1 - g1 * kPageWaves + 1);
   const auto partial = [&](int i) -> const float* {
     int slot;
@@ -465,17 +520,17 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
   if (k < NG)
     for (int i0 = k; i0 < n; i0 += kAt * NG) {
       float4_t v[kAt];
-      float2 s[kAt];
+      float2 of[kAt];
 #pragma unroll
       for (int j = 0; j < kAt; ++j) {
         const float* p = partial(min(i0 + j * NG, n - 1));
         v[j] = *reinterpret_cast<const float4_t*>(p + 4 * c);
-        s[j] = *reinterpret_cast<const float2*>(p + D);
+        of[j] = *reinterpret_cast<const float2*>(p + D);
       }
       float to = top;
 #pragma unroll
       for (int j = 0; j < kAt; ++j)
-        if (i0 + j * NG < n) to = fmaxf(to, s[j].x);
+        if (i0 + j * NG < n) to = fmaxf(to, of[j].x);
       const float f = __builtin_amdgcn_exp2f(top - to);
       sum *= f;
       all *= f;
@@ -483,9 +538,9 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
 #pragma unroll
       for (int j = 0; j < kAt; ++j)
         if (i0 + j * NG < n) {
-          const float e = __builtin_amdgcn_exp2f(s[j].x - to);
+          const float e = __builtin_amdgcn_exp2f(of[j].x - to);
           sum += v[j] * e;
-          all += s[j].y * e;
+          all += of[j].y * e;
         }
     }
   if (k < NG) {
@@ -511,20 +566,25 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
 }
 
 // Whether every pair gets one workgroup: by the longest span that the table or the
-// window allows (lengths are the device's).  A launch and the merge are saved: with 8
-// heads and up to 1000 tokens, 1, 8, 32 and 64 sequences take 7.3, 9.9, 18 and 34 us
-// against 8.7, 9.8, 23 and 40; at 2000 tokens 1 and 8 sequences take 11 and 18 against
-// 8.5 and 14.  With two workgroups per compute unit and more, up to 4096 tokens,
-// the even end of the list is not missed: 64 x 4096 tokens 160 us against 170, 64
-// ragged sequences 91 against 91, 256 of up to 1500 135 against 163 (33 of 2000 to
-// 4096, one workgroup per compute unit and a few: 84 against 76).
-bool one_workgroup_each(int64_t tiles, int64_t pairs) { return tiles <= 32 || (tiles <= 128 && pairs >= 2 * kPageWG); }
+// window allows (lengths are the device's).  A launch and the merge are saved, about 3 us;
+// but one compute unit reads no more than 60 GB/s, so long spans of few pairs are better
+// shared out.  With heads of 128, nothing in the caches: 2 pairs of 256, 512 and 1000 tokens
+// take 4.7, 7.4 and 11.6 us against 7.2, 7.5 and 7.8; 128 pairs 6.7, 9.7 and 16.6 against
+// 10.3, 12.9 and 18.4; 256 of 1000 and 2000 tokens 26 and 49 against 29 and 56.  Then by
+// how full the last round of workgroups is: 272 of 512 and 1000 tokens 20 and 34 against
+// 22 and 33, 512 of 1000 48 against 53.  From two full rounds on it wins or ties up to 4096
+// tokens: 512 pairs 187 against 194, with lengths spread evenly 102 against 107.
+bool one_workgroup_each(int64_t tiles, int64_t pairs, int d) {
+  if (tiles > kSingleTiles) return false;
+  const int64_t rounds = (pairs + kPageWG - 1) / kPageWG;
+  return pairs >= 2 * kPageWG || tiles * d <= std::max<int64_t>(2048, 8192 * pairs / (kPageWG * rounds));
+}
 
 template <int D, int TY>
 hipError_t launch_t(PageArgs a, hipStream_t s) {
   const int64_t room = (((int64_t)a.max_pages << (a.page_shift + 4)) + kPageTile - 1) / kPageTile;
   const int64_t most = a.window > 0 ? std::min<int64_t>(room, (a.window + kPageTile - 2) / kPageTile + 1) : room;
-  const bool single = one_workgroup_each(most, (int64_t)a.n_kv_heads * a.n_rb * a.batch);
+  const bool single = one_workgroup_each(most, (int64_t)a.n_kv_heads * a.n_rb * a.batch, D);
   const size_t lds = ((size_t)kPageWaves * a.rows * (D + 4) + (single ? 0 : a.batch + 1)) * sizeof(float);
   if (lds > 64 * 1024) {
     const void* k = single ? (const void*)page_split_kernel<D, TY, true> : (const void*)page_split_kernel<D, TY, false>;
@@ -532,8 +592,9 @@ hipError_t launch_t(PageArgs a, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   if (single) {
-    // where not all start at once, and a wave holds the lengths
-    a.longest_first = a.batch <= 64 && (int64_t)a.n_kv_heads * a.n_rb * a.batch > kPageWG;
+    // where not all start at once, and are long enough to matter: 1024 pairs with lengths spread
+    // up to 4096 take 196 us, 228 as they come; up to 1000 it would cost 56 against 53
+    a.longest_first = a.batch <= kRanked && most * D >= 6144 && (int64_t)a.n_kv_heads * a.n_rb * a.batch > kPageWG;
     hipLaunchKernelGGL((page_split_kernel<D, TY, true>), dim3(a.n_kv_heads * a.n_rb, a.batch), dim3(kPT), lds, s, a);
   } else {
     hipLaunchKernelGGL((page_split_kernel<D, TY, false>), dim3(kPageWG), dim3(kPT), lds, s, a);

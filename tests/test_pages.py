@@ -306,6 +306,23 @@ def test_decode_of_many_sequences(B, top, H, G, d, spare):
     check(out.cpu().numpy(), want, tol, "many")
 
 
+@pytest.mark.parametrize("B,H", [(64, 8), (65, 8), (130, 4), (256, 2), (257, 2)])
+def test_decode_longest_first(B, H):
+    """A few long sequences among many short ones, of equal lengths some of them, in one launch."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce(f"page decode longest first {B} {H}")
+    rng = np.random.default_rng(B)
+    lens = np.where(rng.random(B) < 0.05, rng.integers(500, 768, B), rng.integers(0, 70, B))
+    lens[B // 2] = lens[B - 1] = 768
+    case = (lens.tolist(), H, 1, 256, 16, "f16", 0, [])
+    table, k, v, q = decode_case(torch, case, spare=0)
+    out = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=H).decode(0, q)
+    want, tol = reference(case, table, k, v, q)
+    check(out.cpu().numpy(), want, tol, "longest first")
+
+
 def test_decode_lengths_and_queries_as_they_come():
     """Lengths below 0 and past the table are held to it; queries inside wider rows; the last of several layers."""
     torch = torch_gpu()
