@@ -10,9 +10,13 @@
 // into its run in LDS (integers: the order does not matter), so no array of counts as
 // wide as the vocabulary is kept, cleared or read; the price is that every run reads
 // the whole history, so runs are as long as still give the chip two workgroups per
-// compute unit.  Probabilities take a second launch that works z out again: reading
-// the logits twice (2 to 4 bytes, from the last-level cache) is less than writing z and
-// reading it.
+// compute unit.  Probabilities of short rows are made in one launch, a workgroup with its
+// row in registers.  Else they take a second one that works z out again: reading the
+// logits twice (2 to 4 bytes, from the last-level cache) is less than writing z and reading
+// it.  For float32 outputs it is told the counts, a byte an entry; others count again.
+// 64 rows of 131072 float32 entries behind 16000 tokens take 16 and 15 us: the first by
+// its arithmetic (30 instructions an entry, 6 us) after its loads, as all workgroups start
+// together; the second moves 75 MB, 4.9 TB/s.
 #include <algorithm>
 
 #include "entry.h"
@@ -26,7 +30,7 @@ constexpr int kRunThreads = 512;         // of a workgroup with a run of a row
 constexpr int kRowThreads = 1024;        // with a whole row
 constexpr int kStep = 8 * kRunThreads;   // entries of a run's round
 constexpr int kMostWhole = 32 * kRowThreads;     // entries of a row that one workgroup takes (128 KB of LDS)
-constexpr uint32_t kInPrompt = 1u << 31;
+constexpr int kNowhere = 64;             // words of LDS behind a run's: what lies in another run counts there, a lane apart
 constexpr int kIds = 16;                 // ids of the history that a thread has under way
 
 struct Rules {                           // of a row; less = 1 / rep
@@ -94,7 +98,7 @@ __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
 }
 
 // How often the row's history holds each entry of [v0, v0 + a.run), and the bias of
-// each: LDS words, kInPrompt set for a token of the prompt.
+// each: LDS words, twice the times that it was said, and bit 0 for a token of the prompt.
 template <int NT>
 __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int v0, Lists& x, uint32_t* seen, float* bias) {
   const int run = min(a.run, a.vocab - v0), b = at.seq, tid = threadIdx.x;
@@ -128,18 +132,29 @@ __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int 
     x.val = e + tid < x.e1 ? a.bias[e + tid] : 0.f;
   }
   const int32_t* h = a.history + b * a.history_stride;
+  const uint32_t nowhere = a.run + (tid & 63);
   for (int base = 0; base < x.n;) {
 #pragma unroll
     for (int j = 0; j < kIds / 4; ++j) {
       const int lo = base + 4 * NT * j, hi = lo + 4 * NT, at = lo + 4 * tid;
+      uint32_t i[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t i = (uint32_t)x.hist[j][k] - (uint32_t)v0;      // ids below 0 lie past every run
-        if (hi > x.n) i = at + k < x.n ? i : ~0u;
-        if (i < (uint32_t)run) {
-          if (hi <= x.m || (lo < x.m && at + k < x.m)) atomicOr(&seen[i], kInPrompt);
-          else atomicAdd(&seen[i], 1u);
-        }
+      for (int k = 0; k < 4; ++k) i[k] = (uint32_t)x.hist[j][k] - (uint32_t)v0;      // ids below 0 lie past every run
+#pragma unroll
+      for (int k = 0; k < 4; ++k) i[k] = i[k] < (uint32_t)run ? i[k] : nowhere;
+      if (hi <= min(x.m, x.n)) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) atomicOr(&seen[i[k]], 1u);
+      } else if (lo >= x.m && hi <= x.n) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) atomicAdd(&seen[i[k]], 2u);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (at + k < x.n) {
+            if (at + k < x.m) atomicOr(&seen[i[k]], 1u);
+            else atomicAdd(&seen[i[k]], 2u);
+          }
       }
     }
     base += kIds * NT;
@@ -155,7 +170,7 @@ __device__ __forceinline__ void count(const LogitsArgs& a, int row, Row at, int 
     }
     if ((path >> tid) & 1) {
       const uint32_t i = (uint32_t)x.token - (uint32_t)v0;
-      if (i < (uint32_t)run) atomicAdd(&seen[i], 1u);
+      if (i < (uint32_t)run) atomicAdd(&seen[i], 2u);
     }
   }
   __syncthreads();
@@ -181,39 +196,58 @@ struct Mine {
   float8_t z[R];
   uint32_t ok[R];
 };
+// The same as it comes from memory.  Nothing waits for it before open(): one past the row's last eight
+// entries has those.
+template <int T, int R>
+struct Raw {
+  typename AnyPlace<T>::eight l[R];
+  uint32_t ok[R];
+};
 template <int T, int NT, int R>
-__device__ __forceinline__ void load(const LogitsArgs& a, int row, int v0, Mine<R>& x) {
+__device__ __forceinline__ void load(const LogitsArgs& a, int row, int v0, Raw<T, R>& x) {
   const row_t<T>* l = static_cast<const row_t<T>*>(a.logits) + row * a.stride;
   const uint8_t* mask = reinterpret_cast<const uint8_t*>(a.mask + row * a.mask_stride);
   const int first = v0 + 8 * (int)threadIdx.x;
-  if (v0 + 8 * NT * R <= a.vocab) {      // a run inside the row
+  if (a.vocab >= 8) {
 #pragma unroll
-    for (int j = 0; j < R; ++j) x.z[j] = load8_any<T>(l + first + 8 * j * NT);
-    if (a.mask) {
-#pragma unroll
-      for (int j = 0; j < R; ++j) x.ok[j] = mask[(first >> 3) + j * NT];
-    }
-    return;
+    for (int j = 0; j < R; ++j) x.l[j] = *reinterpret_cast<const typename AnyPlace<T>::eight*>(l + min(first + 8 * j * NT, a.vocab - 8));
   }
+  if (a.mask) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) x.ok[j] = mask[min(first + 8 * j * NT, a.vocab - 1) >> 3];
+  }
+}
+template <int T, int NT, int R>
+__device__ __forceinline__ void open(const LogitsArgs& a, int row, int v0, const Raw<T, R>& x, Mine<R>& z) {
+  const row_t<T>* l = static_cast<const row_t<T>*>(a.logits) + row * a.stride;
 #pragma unroll
   for (int j = 0; j < R; ++j) {
-    const int v = first + 8 * j * NT;
-    x.z[j] = load8_near<T>(l, v, a.vocab);
-    x.ok[j] = a.mask && v < a.vocab ? mask[v >> 3] : 0xff;
+    z.ok[j] = x.ok[j];
+    z.z[j] = __builtin_convertvector(x.l[j], float8_t);
+  }
+  if (v0 + 8 * NT * R <= a.vocab) return;                // a run inside the row
+#pragma unroll
+  for (int j = 0; j < R; ++j) {
+    const int v = v0 + 8 * ((int)threadIdx.x + j * NT);
+    if (v + 8 > a.vocab) z.z[j] = load8_near<T>(l, v, a.vocab);
   }
 }
 
-// l of an entry that the history holds, said so often (0: in the prompt only).
-__device__ __forceinline__ float changed(float l, bool seen, float said, const Rules& r) {
-  const float m = seen ? (l > 0.f ? r.less : r.rep) : 1.f;
-  const float off = said > 0.f ? __builtin_fmaf(r.freq, said, r.pres) : 0.f;
+// l of an entry with the count c, as count() leaves it.
+__device__ __forceinline__ float changed(float l, uint32_t c, const Rules& r) {
+  const float m = c != 0 ? (l > 0.f ? r.less : r.rep) : 1.f;
+  const float off = c > 1 ? __builtin_fmaf(r.freq, (float)(c >> 1), r.pres) : 0.f;
   return __builtin_fmaf(l, m, -off);
 }
 
+// The low bytes of four words.
+__device__ __forceinline__ uint32_t bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u), 0x05040100u);
+}
+
 // l into z.  What the lists made of eight entries goes to the second launch as a byte
-// of each: how often it was said, up to 126, and kSeen if it is in the prompt; all
-// ones: a bias or a larger count among them, their z are in the output.
-constexpr uint32_t kSeen = 0x80;
+// of each, its count up to 253; all ones: a bias or a larger count among them, their z are
+// in the output.
 template <bool TELL, int NT, int R>
 __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const uint32_t* seen, const float* bias, Mine<R>& x,
                                       uint2 (&code)[R]) {
@@ -221,7 +255,6 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
   for (int j = 0; j < R; ++j) {
     const int at = 8 * ((int)threadIdx.x + j * NT);
     bool tell = false;
-    uint32_t most = 0;
     code[j] = make_uint2(0, 0);
     if (seen) {
       uint32_t c[8];
@@ -229,14 +262,11 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
       *reinterpret_cast<uint4*>(c + 4) = *reinterpret_cast<const uint4*>(seen + at + 4);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (__any(c[i] != 0)) {          // few entries are in a list: mostly a wave has none of its 64
-          const uint32_t said = c[i] & ~kInPrompt;
-          x.z[j][i] = changed(x.z[j][i], c[i] != 0, (float)said, r);
-          if constexpr (TELL) {
-            (i < 4 ? code[j].x : code[j].y) |= ((c[i] & 127) | (c[i] >> 24 & kSeen)) << (8 * (i & 3));
-            most = max(most, said);
-          }
-        }
+        x.z[j][i] = changed(x.z[j][i], c[i], r);
+      if constexpr (TELL) {
+        code[j] = make_uint2(bytes(c[0], c[1], c[2], c[3]), bytes(c[4], c[5], c[6], c[7]));
+        tell = max(max(max(c[0], c[1]), max(c[2], c[3])), max(max(c[4], c[5]), max(c[6], c[7]))) > 253;
+      }
     }
     if (a.bias) {
       const float8_t d = *reinterpret_cast<const float8_t*>(bias + at);
@@ -246,7 +276,7 @@ __device__ __forceinline__ void shape(const LogitsArgs& a, const Rules& r, const
       tell |= any != 0;
       x.z[j] += d;
     }
-    if (tell || most > 126) code[j] = make_uint2(0xffffffffu, 0xffffffffu);
+    if (tell) code[j] = make_uint2(0xffffffffu, 0xffffffffu);
   }
 }
 
@@ -256,8 +286,10 @@ __device__ __forceinline__ void hide(const LogitsArgs& a, Mine<R>& x) {     // w
 #pragma unroll
   for (int j = 0; j < R; ++j)
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (!((x.ok[j] >> i) & 1)) x.z[j][i] = -__builtin_inff();
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t keep = (uint32_t)((int32_t)(x.ok[j] << (31 - i)) >> 31);
+      x.z[j][i] = __builtin_bit_cast(float, (__builtin_bit_cast(uint32_t, (float)x.z[j][i]) & keep) | (0xff800000u & ~keep));
+    }
 }
 
 // Eight entries of the output from v on.
@@ -324,15 +356,19 @@ __global__ __launch_bounds__(M == WHOLE ? kRowThreads : kRunThreads) void logits
   extern __shared__ __align__(16) uint32_t lds[];
   __shared__ LogitsPart parts[NW];
   const int row = blockIdx.y, v0 = blockIdx.x * a.run, tid = threadIdx.x;
+  Raw<T, R> raw;
+  Mine<R> x;
+  load<T, NT>(a, row, v0, raw);          // on its way while the lists are found and counted
   const Row at = row_of(a, row);
   const Rules r = rules_of(a, at.seq);
   const bool counts = a.history || a.cu_nodes;
-  float* bias = reinterpret_cast<float*>(lds + a.run);
-  Mine<R> x;
+  float* bias = reinterpret_cast<float*>(lds + a.run + kNowhere);
   if (counts || a.bias) {
     Lists w = fetch<NT>(a, at);
-    load<T, NT>(a, row, v0, x);
     count<NT>(a, row, at, v0, w, lds, bias);
+  }
+  open<T, NT>(a, row, v0, raw, x);
+  if (counts || a.bias) {
     uint2 code[R];
     shape<M == PART && kept<TO>, NT>(a, r, counts ? lds : nullptr, bias, x, code);
     if constexpr (M == PART && kept<TO>) {
@@ -345,8 +381,6 @@ __global__ __launch_bounds__(M == WHOLE ? kRowThreads : kRunThreads) void logits
         }
       }
     }
-  } else {
-    load<T, NT>(a, row, v0, x);
   }
   hide(a, x);
   if constexpr (M == LOGITS) {
@@ -434,6 +468,7 @@ __global__ __launch_bounds__(kRunThreads) void probs_kernel(const LogitsArgs a) 
     }
     return;
   }
+  Raw<T, R> raw;
   Mine<R> x;
   Lists w;
   uint2 code[R];
@@ -448,13 +483,15 @@ __global__ __launch_bounds__(kRunThreads) void probs_kernel(const LogitsArgs a) 
       w = fetch<NT>(a, at);
     }
   }
-  load<T, NT>(a, row, v0, x);
+  load<T, NT>(a, row, v0, raw);
   float top = -__builtin_inff(), sum = 0.f;
   for (int i = lane; i < a.n_run; i += 64) top = fmaxf(top, part[i].top);
   top = wave_max(top);
   const float ref = top == -__builtin_inff() ? 0.f : top;
   for (int i = lane; i < a.n_run; i += 64) sum += part[i].sum * __builtin_amdgcn_exp2f((part[i].top - ref) * scale);
   sum = wave_sum(sum);
+  if (!kept<TO> && lists) count<NT>(a, row, at, v0, w, lds, reinterpret_cast<float*>(lds + a.run + kNowhere));
+  open<T, NT>(a, row, v0, raw, x);
   if (lists) {
     if constexpr (kept<TO>) {
 #pragma unroll
@@ -465,14 +502,12 @@ __global__ __launch_bounds__(kRunThreads) void probs_kernel(const LogitsArgs a) 
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const uint32_t c = ((i < 4 ? code[j].x : code[j].y) >> (8 * (i & 3))) & 255;
-            if (__any(c != 0)) x.z[j][i] = changed(x.z[j][i], c != 0, (float)(c & 127), r);
+            if (__any(c != 0)) x.z[j][i] = changed(x.z[j][i], c, r);
           }
         }
       }
     } else {
-      float* bias = reinterpret_cast<float*>(lds + a.run);
-      count<NT>(a, row, at, v0, w, lds, bias);
-      shape<false, NT>(a, r, counts ? lds : nullptr, bias, x, code);
+      shape<false, NT>(a, r, counts ? lds : nullptr, reinterpret_cast<const float*>(lds + a.run + kNowhere), x, code);
     }
   }
   hide(a, x);
@@ -538,7 +573,7 @@ hipError_t launch_logits(LogitsArgs a, int from, int to, bool probs, hipStream_t
     while (a.run < (a.bias ? 2 : 4) * kStep && (int64_t)a.n_rows * ((a.vocab + 2 * a.run - 1) / (2 * a.run)) >= 512) a.run *= 2;
   }
   a.n_run = (a.vocab + a.run - 1) / a.run;
-  const size_t lds = (size_t)4 * words * a.run;
+  const size_t lds = words ? (size_t)4 * (words * a.run + kNowhere) : 0;
   switch (from) {
     case DWKV_F32: return launch_from<DWKV_F32>(a, to, probs, lds, s);
     case DWKV_F16: return launch_from<DWKV_F16>(a, to, probs, lds, s);
