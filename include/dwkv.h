@@ -799,7 +799,7 @@ size_t dwkv_logits_workspace_bytes(int32_t n_rows, int32_t vocab);
  *   workspace: with probs, >= dwkv_logits_workspace_bytes(N, vocab), no initial
  *            contents, 16-byte aligned; else unused
  * Pointers are aligned to their type.  N up to 65535, vocab up to 2^30, history_stride
- * under 2^29.  One launch; with probs and rows of more than 8192 entries up to two
+ * under 2^29.  One launch; with probs and rows of more than 16384 entries up to two
  * (none for no rows). */
 dwkv_status dwkv_logits(int32_t batch, const dwkv_tree* tree, const int32_t* token, int32_t vocab, const void* logits,
                         int32_t l_type, int64_t l_stride, const dwkv_logits_rules* rules, int32_t probs, void* out,

@@ -512,6 +512,7 @@ struct LogitsArgs {
   int64_t stride, history_stride, mask_stride;
   int32_t batch, n_rows, vocab, n_bias;
   int32_t run, n_run, whole;   // entries of a workgroup; whether that is a row (launch_logits)
+  int32_t tell;                // whether the first launch writes `code` for the second
 };
 int64_t logits_most_runs(int64_t vocab);
 hipError_t launch_logits(LogitsArgs a, int from, int to, bool probs, hipStream_t s);

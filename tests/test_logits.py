@@ -19,6 +19,11 @@ CASES = [
     (2, 40000, 9000, "f32", "f32", True, "phbm"),
     (70, 66000, 40, "bf16", "bf16", True, "phbm"),         # the longer runs
     (300, 20000, 64, "f16", "f32", True, "ph"),
+    (70, 66000, 40, "f16", "f32", True, "phb"),
+    (128, 66000, 300, "bf16", "f32", True, "phbm"),          # the longest, whose second launch counts again
+    (110, 78001, 17000, "f32", "f32", True, "ph"),           # or does not
+    (128, 66003, 100, "f32", "bf16", True, "b"),
+    (300, 16500, 90, "f32", "f32", True, "pbm"),            # 128 KB of counts
     (6, 500, 30, "f32", "f32", True, ""),
     (6, 500, 30, "f32", "bf16", False, "m"),
 ]
