@@ -23,7 +23,7 @@ constexpr int kRT = 256;                 // threads of a workgroup
 constexpr int kRows = 2;                 // rows of a workgroup, at most
 constexpr int kSlots = 16;               // slots of a workgroup that fills pages
 
-enum Pairs { HALF = 0, HALF_ODD = 1, NEXT = 2 };   // (i, n + i), n a multiple of 8 or not; (2i, 2i + 1)
+enum Pairs { HALF = 0, PART = 1, NEXT = 2 };   // (i, n + i) of all channels, of some; (2i, 2i + 1)
 
 // sin and cos of x.  x - n pi/2 in two steps (n pi/2's upper part is exact in the
 // fused product), then Taylor: to x^13 and x^14 in float64 (below 2^-45 on
@@ -70,14 +70,25 @@ __device__ __forceinline__ void sin_cos(double x, double& s, double& c) {
   c = (k + 1) & 2 ? -v : v;
 }
 
-// (cos, sin) of row r's pair i at cs[r * n_pairs + i], already scaled.
-template <int TO>
+// (cos, sin) of row r's pair i at cs[r * entries + i], already scaled.  PART: an entry for each
+// of a pair's channels, (cos, -sin) for the first.
+template <int P>
+__device__ __forceinline__ int entries(int np) {
+  return P == PART ? 2 * np : np;
+}
+template <int P, int TO>
 __device__ __forceinline__ void fill_table(float2* cs, const RopeSpec& t, const int* pos, int rows) {
   for (int u = threadIdx.x; u < rows * t.n_pairs; u += kRT) {
     const int r = u / t.n_pairs, i = u - r * t.n_pairs;
     double s, c;
     sin_cos<TO == DWKV_F32>((double)pos[r] * t.freq[i], s, c);
-    cs[u] = make_float2((float)(c * t.scale), (float)(s * (t.inverse ? -(double)t.scale : (double)t.scale)));
+    const float2 of = make_float2((float)(c * t.scale), (float)(s * (t.inverse ? -(double)t.scale : (double)t.scale)));
+    if constexpr (P == PART) {
+      cs[u + r * t.n_pairs] = make_float2(of.x, -of.y);
+      cs[u + (r + 1) * t.n_pairs] = of;
+    } else {
+      cs[u] = of;
+    }
   }
 }
 
@@ -87,18 +98,20 @@ __device__ __forceinline__ void turn(float& a, float& b, float2 cs) {
   b = __builtin_fmaf(y, cs.x, x * cs.y);
 }
 
-// A head falls into pieces of eight pairs, or of eight channels that are copied.
-// Neighbouring pairs: eight channels a piece.  Halves: eight pairs a piece (16
-// channels), then the rest eight channels a piece.
+// A head falls into pieces of eight channels; halves of whole heads into pieces of eight pairs.
 template <int P>
-__device__ __forceinline__ int pieces(int d, int np) {
-  return P == NEXT ? d / 8 : (np + 7) / 8 + (d - 2 * np + 7) / 8;
+__device__ __forceinline__ int pieces(int d) {
+  return P == HALF ? d / 16 : d / 8;
 }
 
-// Piece a of a head: its channels from x, turned, to put(channel, eight numbers)
-// (16-byte pieces) or put1(channel, number).
-template <int P, int TI, class Put, class Put1>
-__device__ __forceinline__ void turn_piece(const row_t<TI>* x, int a, int d, int np, const float2* cs, Put put, Put1 put1) {
+// Piece a of a head, turned, to put(channel, eight numbers), in 16-byte pieces.  Where the
+// halves end within the head, a piece has its channels and reads what they pair with once
+// more, as the stores of a wave then cover whole lines: 16384 rows of 40 heads of 128,
+// the first 48 or 42 channels turned, take 66 and 75 us; in pieces of pairs 105 and 282.
+// edge: the first or the last head of all, where eight numbers from within the head may
+// reach past the rows' memory.
+template <int P, int TI, class Put>
+__device__ __forceinline__ void turn_piece(const row_t<TI>* x, int a, int np, bool edge, const float2* cs, Put put) {
   if constexpr (P == NEXT) {
     float8_t v = load8<TI>(x + 8 * a);
 #pragma unroll
@@ -111,32 +124,71 @@ __device__ __forceinline__ void turn_piece(const row_t<TI>* x, int a, int d, int
       }
     put(8 * a, v);
   } else if constexpr (P == HALF) {
-    if (8 * a < np) {
-      float8_t lo = load8<TI>(x + 8 * a), hi = load8<TI>(x + np + 8 * a);
+    float8_t lo = load8<TI>(x + 8 * a), hi = load8<TI>(x + np + 8 * a);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float u = lo[i], v = hi[i];
-        turn(u, v, cs[8 * a + i]);
-        lo[i] = u;
-        hi[i] = v;
-      }
-      put(8 * a, lo);
-      put(np + 8 * a, hi);
-    } else {
-      const int c = 8 * a + np;
-      put(c, load8<TI>(x + c));
+    for (int i = 0; i < 8; ++i) {
+      float u = lo[i], v = hi[i];
+      turn(u, v, cs[8 * a + i]);
+      lo[i] = u;
+      hi[i] = v;
     }
-  } else {                               // channels one at a time
-    const int turned = (np + 7) / 8;
-    if (a < turned) {
-      for (int i = 8 * a; i < np && i < 8 * a + 8; ++i) {
-        float u = (float)x[i], v = (float)x[np + i];
-        turn(u, v, cs[i]);
-        put1(i, u);
-        put1(np + i, v);
+    put(8 * a, lo);
+    put(np + 8 * a, hi);
+  } else {
+    typedef typename AnyPlace<TI>::eight any8;
+    const int c = 8 * a;
+    const bool low = c < np, cross = low && c + 8 > np, alone = cross && edge;    // cross: in both halves
+    // both loads on their way before anything waits for one
+    const row8_t<TI> own = *reinterpret_cast<const row8_t<TI>*>(x + c);
+    const any8 first = *reinterpret_cast<const any8*>(x + (alone || c >= 2 * np ? c : low ? c + np : c - np));
+    any8 back = first;
+    if (cross) {
+      if (alone) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) back[i] = x[c + i < np ? c + i + np : c + i < 2 * np ? c + i - np : 0];
+      } else {
+        back = *reinterpret_cast<const any8*>(x + c - np);
       }
+    }
+    float8_t v = __builtin_convertvector(own, float8_t);
+    if (c < 2 * np) {
+      const float8_t f = __builtin_convertvector(first, float8_t), b = __builtin_convertvector(back, float8_t);
+      const float2* t = cs + c;
+      const int turns = alone ? 0 : low ? np - c : 8;            // numbers of `first` that count
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (c + i < 2 * np) v[i] = __builtin_fmaf(v[i], t[i].x, (i < turns ? f[i] : b[i]) * t[i].y);
+    }
+    put(c, v);
+  }
+}
+
+// Pieces of heads that a workgroup has at a time.  PART in place: whole heads, which are all read
+// before any is stored.
+template <int P>
+__device__ __forceinline__ int pieces_at_once(int A, bool in_place) {
+  return P == PART && in_place ? kRT / A * A : kRT;
+}
+
+// The pieces of `rows` rows, `per` in each: from(row, head) to to(row, head, channel, eight numbers).
+template <int P, int TI, class From, class Edge, class To>
+__device__ __forceinline__ void turn_rows(int rows, int per, int A, int np, bool in_place, const float2* cs, From from, Edge edge, To to) {
+  const int step = pieces_at_once<P>(A, in_place);
+  for (int u0 = 0; u0 < rows * per; u0 += step) {
+    const int u = u0 + (int)threadIdx.x, r = u / per, w = u - r * per, h = w / A, p = w - h * A;
+    const bool mine = (int)threadIdx.x < step && u < rows * per;
+    if constexpr (P == PART) {
+      int at = 0;
+      float8_t v;
+      if (mine)
+        turn_piece<P, TI>(from(r, h), p, np, edge(r, h), cs + r * entries<P>(np), [&](int c, float8_t z) {
+          at = c;
+          v = z;
+        });
+      if (in_place) __syncthreads();
+      if (mine) to(r, h, at, v);
     } else {
-      for (int c = 2 * np + 8 * (a - turned); c < d && c < 2 * np + 8 * (a - turned) + 8; ++c) put1(c, (float)x[c]);
+      if (mine) turn_piece<P, TI>(from(r, h), p, np, false, cs + r * entries<P>(np), [&](int c, float8_t z) { to(r, h, c, z); });
     }
   }
 }
@@ -151,18 +203,15 @@ __global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
   const int h0 = blockIdx.y * a.chunk, nh = min(a.chunk, a.n_heads - h0);
   if (threadIdx.x < rows) pos[threadIdx.x] = a.pos[r0 + threadIdx.x];
   __syncthreads();
-  fill_table<TO>(cs, a.t, pos, rows);
+  fill_table<P, TO>(cs, a.t, pos, rows);
   __syncthreads();
-  const int np = a.t.n_pairs, A = pieces<P>(a.d, np), per = A * nh;
+  const int np = a.t.n_pairs, A = pieces<P>(a.d), per = A * nh;
   const row_t<TI>* x = static_cast<const row_t<TI>*>(a.x);
   row_t<TO>* out = static_cast<row_t<TO>*>(a.out);
-  for (int u = threadIdx.x; u < rows * per; u += kRT) {
-    const int r = u / per, w = u - r * per, h = w / A, p = w - h * A;
-    row_t<TO>* y = out + (r0 + r) * a.out_stride + (int64_t)(h0 + h) * a.d;
-    turn_piece<P, TI>(
-        x + (r0 + r) * a.x_stride + (int64_t)(h0 + h) * a.d, p, a.d, np, cs + r * np,
-        [&](int c, float8_t v) { store8<TO, PAST>(y + c, v); }, [&](int c, float v) { y[c] = (row_t<TO>)v; });
-  }
+  turn_rows<P, TI>(
+      rows, per, A, np, a.x == a.out, cs, [&](int r, int h) { return x + (r0 + r) * a.x_stride + (int64_t)(h0 + h) * a.d; },
+      [&](int r, int h) { return (r0 + r == 0 && h0 + h == 0) || (r0 + r == a.n_rows - 1 && h0 + h == a.n_heads - 1); },
+      [&](int r, int h, int c, float8_t v) { store8<TO, PAST>(out + (r0 + r) * a.out_stride + (int64_t)(h0 + h) * a.d + c, v); });
 }
 
 template <int P, int TI, int TO>
@@ -318,20 +367,18 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, int w, float
   if (a.pos && threadIdx.x < rows) pos[threadIdx.x] = a.pos[r0 + threadIdx.x];
   __syncthreads();
   if (np > 0) {
-    fill_table<TC>(cs, a.t, pos, rows);
+    fill_table<P, TC>(cs, a.t, pos, rows);
     __syncthreads();
   }
-  const int A = pieces<P>(d, np), per = A * nh;
+  const int A = pieces<P>(d), per = A * nh;
   const row_t<TI>* x = static_cast<const row_t<TI>*>(a.q) + r0 * a.q_stride + (int64_t)c0 * d;
   row_t<TC>* out = static_cast<row_t<TC>*>(a.q_out) + ((int64_t)r0 * a.n_q_heads + c0) * d;
-  for (int u = threadIdx.x; u < rows * per; u += kRT) {
-    const int r = u / per, v = u - r * per, h = v / A, p = v - h * A;
-    if (!in[r]) continue;
-    row_t<TC>* y = out + ((int64_t)r * a.n_q_heads + h) * d;
-    turn_piece<P, TI>(
-        x + r * a.q_stride + (int64_t)h * d, p, d, np, cs + r * np, [&](int c, float8_t z) { store8<TC, PAST>(y + c, z); },
-        [&](int c, float z) { y[c] = (row_t<TC>)z; });
-  }
+  turn_rows<P, TI>(
+      rows, per, A, np, a.q == a.q_out, cs, [&](int r, int h) { return x + r * a.q_stride + (int64_t)h * d; },
+      [&](int r, int h) { return (r0 + r == 0 && c0 + h == 0) || (r0 + r == a.n_rows - 1 && c0 + h == a.n_q_heads - 1); },
+      [&](int r, int h, int c, float8_t z) {
+        if (in[r]) store8<TC, PAST>(out + ((int64_t)r * a.n_q_heads + h) * d + c, z);
+      });
 }
 
 template <int P, int TI, int TC, bool PAST>
@@ -367,11 +414,11 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
   if (np > 0) {
     if (threadIdx.x < rows) pos[threadIdx.x] = a.pos ? a.pos[r0 + threadIdx.x] : slot0 + (int)threadIdx.x;
     __syncthreads();
-    fill_table<TC>(cs, a.t, pos, rows);
+    fill_table<P, TC>(cs, a.t, pos, rows);
   }
   __syncthreads();
   const int hk = a.n_kv_heads, c0 = ((int)blockIdx.x - w * a.kv_chunks) * a.kv_chunk, c1 = min(c0 + a.kv_chunk, 2 * hk);
-  const int A = pieces<P>(d, np);
+  const int A = pieces<P>(d);
   if (id < 0 || id >= a.n_pages) return;
   const int t0 = slot0 & (page - 1) & ~15;                 // the group's place in its page
   const int64_t at = ((int64_t)id * hk * page + t0) * d;     // of KV head 0
@@ -383,9 +430,9 @@ __global__ __launch_bounds__(kRT) void append_kernel(const AppendArgs a) {
       const int h = u / per + k0, w = u % per, p = w / rows, r = w - p * rows;
       row_t<TC>* y = tile + (int64_t)h * page * d + (off + r) * 8;
       turn_piece<P, TI>(
-          x + (int64_t)(r0 + r) * a.kv_stride + (int64_t)h * d, p, d, np, cs + r * np,
-          [&](int c, float8_t v) { store8<TC, PAST>(y + c * 16, v); },
-          [&](int c, float v) { y[(c >> 3) * 128 + (c & 7)] = (row_t<TC>)v; });
+          x + (int64_t)(r0 + r) * a.kv_stride + (int64_t)h * d, p, np,
+          (r0 + r == 0 && h == 0) || (r0 + r == a.n_rows - 1 && h == hk - 1), cs + r * entries<P>(np),
+          [&](int c, float8_t v) { store8<TC, PAST>(y + c * 16, v); });
     }
   }
   if (c1 > hk) {                         // values: two blocks of [d][8], eight channels of eight tokens a piece
@@ -469,10 +516,10 @@ hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s) {
   a.chunk = head_chunk(groups, a.rows, a.n_heads, a.d);
   const bool past = past_caches(a.n_rows, a.n_heads, a.d, to);
   const dim3 g((unsigned)groups, (a.n_heads + a.chunk - 1) / a.chunk);
-  const size_t lds = (size_t)a.rows * a.t.n_pairs * sizeof(float2);
+  const size_t lds = (size_t)a.rows * 2 * a.t.n_pairs * sizeof(float2);
   if (a.t.interleaved) rope_in<NEXT>(a, from, to, past, g, lds, s);
-  else if (a.t.n_pairs % 8 == 0) rope_in<HALF>(a, from, to, past, g, lds, s);
-  else rope_in<HALF_ODD>(a, from, to, past, g, lds, s);
+  else if (a.t.n_pairs % 8 == 0 && 2 * a.t.n_pairs == a.d) rope_in<HALF>(a, from, to, past, g, lds, s);
+  else rope_in<PART>(a, from, to, past, g, lds, s);
   return hipGetLastError();
 }
 
@@ -492,10 +539,10 @@ hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s) {
   a.n_fill = (int)(groups * a.kv_chunks);
   const bool past = past_caches(a.n_rows, a.n_q_heads + 2 * a.n_kv_heads, a.d, to);
   const dim3 g((unsigned)(a.n_fill + q_groups * a.q_chunks));
-  const size_t lds = (size_t)std::max(slots, a.rows) * a.t.n_pairs * sizeof(float2);
+  const size_t lds = (size_t)std::max(slots, a.rows) * 2 * a.t.n_pairs * sizeof(float2);
   if (a.t.interleaved) append_in<NEXT>(a, from, to, past, g, lds, s);
-  else if (a.t.n_pairs % 8 == 0) append_in<HALF>(a, from, to, past, g, lds, s);
-  else append_in<HALF_ODD>(a, from, to, past, g, lds, s);
+  else if (a.t.n_pairs % 8 == 0 && 2 * a.t.n_pairs == a.d) append_in<HALF>(a, from, to, past, g, lds, s);
+  else append_in<PART>(a, from, to, past, g, lds, s);
   return hipGetLastError();
 }
 

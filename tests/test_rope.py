@@ -12,7 +12,7 @@ CASES = [
     (1, 1, 8, 2, False, "f32", "f32", 0, {}),
     (1, 40, 128, 128, False, "bf16", "bf16", 1024, {}),
     (17, 5, 128, 128, True, "f16", "f16", 0, dict(scaling="linear", factor=4.0)),
-    (33, 3, 64, 10, False, "f32", "f32", 8, {}),            # pairs off 8: one number at a time
+    (33, 3, 64, 10, False, "f32", "f32", 8, {}),            # pairs off 8
     (33, 3, 64, 10, True, "f32", "f32", 8, {}),
     (16, 2, 96, 42, False, "bf16", "f16", 0, dict(scaling="base", factor=8.0)),
     (15, 7, 256, 64, False, "f16", "bf16", 0, dict(scaling="ramp", factor=8.0, context=8192)),
@@ -67,6 +67,39 @@ def test_rope_in_place(kind, rot, inter):
     want = rope(x, pos, table)
     assert rope(x, pos, table, out=x) is x
     assert torch.equal(x, want)
+
+
+@pytest.mark.parametrize("N,H,d,rot", [(1, 1, 8, 6), (1, 1, 64, 2), (1, 2, 128, 126), (3, 1, 16, 14), (7, 40, 96, 30), (2100, 21, 96, 90),
+                                       (2051, 5, 512, 500), (2200, 9, 128, 120), (40, 3, 256, 48), (9, 70, 32, 18)])
+@pytest.mark.parametrize("kind", ["f16", "f32"])
+def test_rope_of_some_channels(N, H, d, rot, kind):
+    """Halves that end within the heads, within eight channels: against 64 bits, and the same in place."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import RopeTable, rope, rope_freqs
+    announce(f"rope of some channels {N} {H} {d} {rot} {kind}")
+    x, pos = rows_of(torch, N, H, d, kind, 0), positions(torch, N)
+    freq = rope_freqs(rot)
+    table = RopeTable(freq, scale=0.5)
+    out = rope(x, torch.from_numpy(pos).cuda(), table)
+    want, tol = rotate(x.double().cpu().numpy(), pos, freq.numpy(), False, 0.5, False)
+    check(out.double().cpu().numpy(), want, tol + rounding(np.abs(want) + tol, kind), "some channels")
+    assert torch.equal(out[:, :, rot:], x[:, :, rot:])
+    assert rope(x, torch.from_numpy(pos).cuda(), table, out=x) is x
+    assert torch.equal(x, out)
+
+
+def test_rope_reads_only_its_rows():
+    """NaN around the rows, in the gaps between them too, reaches nothing."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import RopeTable, rope, rope_freqs
+    announce("rope between gaps")
+    table, pos = RopeTable(rope_freqs(42)), torch.arange(20, dtype=torch.int32, device="cuda")
+    wide = torch.full((22, 3 * 64 + 16), float("nan"), device="cuda")
+    x = wide[1:21, 8:200].unflatten(1, (3, 64))
+    x.copy_(torch.randn((20, 3, 64), generator=torch.Generator().manual_seed(2)))
+    assert torch.equal(rope(x, pos, table), rope(x.contiguous(), pos, table))
 
 
 @pytest.mark.parametrize("rot,inter", [(64, False), (64, True), (22, False)])
