@@ -216,8 +216,13 @@ __global__ __launch_bounds__(kRT) void rope_kernel(const RopeArgs a) {
 
 template <int P, int TI, int TO>
 void rope_past(const RopeArgs& a, bool past, dim3 g, size_t lds, hipStream_t s) {
-  if (past) hipLaunchKernelGGL((rope_kernel<P, TI, TO, true>), g, dim3(kRT), lds, s, a);
-  else hipLaunchKernelGGL((rope_kernel<P, TI, TO, false>), g, dim3(kRT), lds, s, a);
+  if constexpr (TO != DWKV_F32) {
+    if (past) {
+      hipLaunchKernelGGL((rope_kernel<P, TI, TO, true>), g, dim3(kRT), lds, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((rope_kernel<P, TI, TO, false>), g, dim3(kRT), lds, s, a);
 }
 
 template <int P, int TI>
@@ -505,8 +510,10 @@ int head_chunk(int64_t groups, int rows, int heads, int d) {
 // with 4, 8 and 16.
 int rows_of(int64_t n_rows) { return n_rows >= 2048 ? kRows : 1; }
 
-// Whether what is written goes past the caches: more than the eight L2s hold.
-bool past_caches(int64_t rows, int heads, int d, int type) { return rows * heads * d * (type == DWKV_F32 ? 4 : 2) > (32 << 20); }
+// Whether 16-bit numbers are written past the caches: more than the eight L2s hold.  (float32
+// ones leave in two stores of half lines: 8192 rows of 40 heads of 128 take 67 us through the
+// caches and 72 past them, of 256 in neighbouring pairs 143 and 192, of 64 37 and 32.)
+bool past_caches(int64_t rows, int heads, int d) { return rows * heads * d * 2 > (32 << 20); }
 
 }  // namespace
 
@@ -514,7 +521,7 @@ hipError_t launch_rope(RopeArgs a, int from, int to, hipStream_t s) {
   a.rows = rows_of(a.n_rows);
   const int64_t groups = (a.n_rows + a.rows - 1) / a.rows;
   a.chunk = head_chunk(groups, a.rows, a.n_heads, a.d);
-  const bool past = past_caches(a.n_rows, a.n_heads, a.d, to);
+  const bool past = past_caches(a.n_rows, a.n_heads, a.d);
   const dim3 g((unsigned)groups, (a.n_heads + a.chunk - 1) / a.chunk);
   const size_t lds = (size_t)a.rows * 2 * a.t.n_pairs * sizeof(float2);
   if (a.t.interleaved) rope_in<NEXT>(a, from, to, past, g, lds, s);
@@ -537,7 +544,7 @@ hipError_t launch_append(AppendArgs a, int from, int to, hipStream_t s) {
     a.q_chunks = (a.n_q_heads + a.q_chunk - 1) / a.q_chunk;
   }
   a.n_fill = (int)(groups * a.kv_chunks);
-  const bool past = past_caches(a.n_rows, a.n_q_heads + 2 * a.n_kv_heads, a.d, to);
+  const bool past = past_caches(a.n_rows, a.n_q_heads + 2 * a.n_kv_heads, a.d);
   const dim3 g((unsigned)(a.n_fill + q_groups * a.q_chunks));
   const size_t lds = (size_t)std::max(slots, a.rows) * 2 * a.t.n_pairs * sizeof(float2);
   if (a.t.interleaved) append_in<NEXT>(a, from, to, past, g, lds, s);
