@@ -331,17 +331,33 @@ constexpr float kLog2e = 1.44269504088896340736f;
 __device__ __forceinline__ float scale_of(const Rules& r) {
   return r.temp > 0.f ? fminf(fmaxf(kLog2e / r.temp, 0x1p-126f), 0x1.fffffep127f) : 0.f;
 }
-__device__ __forceinline__ float wave_max(float v) {
-  for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
+// op over a wave's lanes, which all get it: within rows of 16 by rotation, then rows and halves
+// against each other.  Both sides of each step are the same two numbers: one order in every lane.
+template <int N>
+__device__ __forceinline__ int rotated(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true);
 }
-__device__ __forceinline__ float wave_sum(float v) {       // the same order in every lane
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+template <class V, class Op>
+__device__ __forceinline__ V wave_all(V v, Op op) {
+  const auto bits = [](V x) { return __builtin_bit_cast(int, x); };
+  const auto from = [](int x) { return __builtin_bit_cast(V, x); };
+  v = op(v, from(rotated<8>(bits(v))));
+  v = op(v, from(rotated<4>(bits(v))));
+  v = op(v, from(rotated<2>(bits(v))));
+  v = op(v, from(rotated<1>(bits(v))));
+  const auto rows = __builtin_amdgcn_permlane16_swap((uint32_t)bits(v), (uint32_t)bits(v), false, false);
+  v = op(from((int)rows[0]), from((int)rows[1]));
+  const auto halves = __builtin_amdgcn_permlane32_swap((uint32_t)bits(v), (uint32_t)bits(v), false, false);
+  return op(from((int)halves[0]), from((int)halves[1]));
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_all(v, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+  return wave_all(v, [](float a, float b) { return a + b; });
 }
 __device__ __forceinline__ int wave_min(int v) {
-  for (int d = 1; d < 64; d <<= 1) v = min(v, __shfl_xor(v, d));
-  return v;
+  return wave_all(v, [](int a, int b) { return min(a, b); });
 }
 
 // Whether the second launch may be told what the lists made of the entries, which it

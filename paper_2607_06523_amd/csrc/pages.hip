@@ -184,11 +184,11 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     int total = 0;
     if (few) {
       inc = lane < a.batch ? tiles_of(span_of(a, lane)) : 0;
-      for (int d = 1; d < 64; d <<= 1) {
+      for (int d = 1; d < a.batch; d <<= 1) {
         const int o = __shfl_up(inc, d);
         if (lane >= d) inc += o;
       }
-      total = __builtin_amdgcn_readlane(inc, 63);
+      total = __builtin_amdgcn_readlane(inc, a.batch - 1);
       if (blockIdx.x == 0 && wv == 0) {
         if (lane < a.batch) a.plan[lane + 1] = inc;
         if (lane == 0) a.plan[0] = 0;
