@@ -72,7 +72,8 @@ __device__ __forceinline__ void fetch_ids(const int32_t* h, int base, int n, int
   const __amdgpu_buffer_rsrc_t list = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(h), 0, 4 * n, 0x00020000);
 #pragma unroll
   for (int j = 0; j < kIds / 4; ++j)
-    id[j] = __builtin_bit_cast(int4_t, __builtin_amdgcn_raw_buffer_load_b128(list, (int)(16u * (threadIdx.x + j * NT) + 4u * (uint32_t)base), 0, 0));
+    id[j] = __builtin_bit_cast(
+        int4_t, __builtin_amdgcn_raw_buffer_load_b128(list, (int)(16u * (threadIdx.x + j * NT) + 4u * (uint32_t)base), 0, 0));
 }
 template <int NT>
 __device__ __forceinline__ Lists fetch(const LogitsArgs& a, Row at) {
