@@ -740,16 +740,20 @@ size_t dwkv_page_workspace_bytes(const dwkv_pages* pages, int32_t n_q_heads);
  * over the tokens t of sequence b that lie in a page, with window > 0 the last
  * `window` tokens of it only; KV head hq / (n_q_heads / Hkv).  A sequence
  * with none of them gets zeros, and so does a row whose scores are all -inf.
- * What a token does not see changes nothing, infinities and NaN included.
+ * What a token does not see changes nothing, infinities and NaN included.  Where one of
+ * the values that it sees is infinite, that channel is, however small the weight (any finite
+ * score has one); infinities of both signs, or a NaN, make it NaN.
  *   q:        [B] rows of [n_q_heads][d] in the cache's type, q_stride elements
  *             apart (a multiple of 8; 0 = rows without a gap)
  *   sm_scale: <= 0 selects 1/sqrt(d)
  *   out:      fp32 [B][n_q_heads][d], written
  *   workspace:>= dwkv_page_workspace_bytes bytes, no initial contents
  * Scores and sums are float32; probabilities have 22 bits (24 in bfloat16 caches)
- * down to 2^-12 of a row's largest.  n_q_heads is a multiple of Hkv, any group.
- * q, out, pages and workspace are 16-byte aligned.  One launch where
- * the table or the window allows few tokens, else two.  Groups of more than 16 heads read a KV head's tokens once for every 16.
+ * down to 2^-12 of a row's largest.  They are held up to 2^15.5 times larger than they
+ * are: values of T tokens past 2^112 / T, which bfloat16 has, may add up to infinity.
+ * n_q_heads is a multiple of Hkv, any group.  q, out, pages and workspace are 16-byte
+ * aligned.  One launch where the table or the window allows few tokens, else two.  Groups
+ * of more than 16 heads read a KV head's tokens once for every 16.
  * DWKV_E_UNSUPPORTED for lists of 2^31 or more tiles of 32 tokens, and for more than
  * 2^22 rows of out. */
 dwkv_status dwkv_page_decode(const dwkv_pages* pages, int32_t layer, const void* q, int64_t q_stride, int32_t n_q_heads,

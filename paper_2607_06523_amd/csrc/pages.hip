@@ -18,7 +18,8 @@
 //  * Probabilities: the reference leaves a row's largest at 2^9 and moves when one
 //    passes 2^15.5, as 2^9 leaves small ones room in fp16's range.  They enter the
 //    product as two fp16 or three bf16 terms (22 and 24 bits): the values' type has 11
-//    or 8, which would be the output's error.
+//    or 8, which would be the output's error.  Only what is finite can be multiplied like
+//    that: where a sum is not, its infinities are added up by themselves.
 //  * A wave writes what it has of a pair that it shares with others as a partial, and
 //    a pair of its own as output; the waves of a workgroup that all work on one
 //    pair join in LDS first.  page_merge_kernel joins the partials.
@@ -33,6 +34,7 @@ constexpr int kPT = 64 * kPageWaves;
 constexpr int kSingleTiles = 128, kSingleBits = 8;    // most tiles of a pair that one workgroup takes, and their bits
 constexpr int kRanked = 256;             // sequences that are taken longest first
 constexpr float kNoRef = -1.7e38f;       // reference of a row without scores
+constexpr float kFar = 0x1.fffffep127f;
 constexpr float kRefTop = 9.f, kRefMove = 15.5f;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -65,6 +67,16 @@ __device__ __forceinline__ uint32_t take(float& a, float& b) {
     return __builtin_bit_cast(uint32_t, p);
   }
 }
+
+// The halves of a pair that are infinite or NaN; 0 for others.
+template <int TY>
+__device__ __forceinline__ uint32_t not_finite(uint32_t v) {
+  constexpr uint32_t lo = TY == DWKV_F16 ? 0x7c00u : 0x7f80u, hi = lo << 16;
+  return ((v & lo) == lo ? v & 0xffffu : 0u) | ((v & hi) == hi ? v & 0xffff0000u : 0u);
+}
+
+// sum + x f of a partial's x and its weight f, which is 0 below float32's range: an infinite x counts all the same.
+__device__ __forceinline__ float plus(float sum, float x, float f) { return f != 0.f ? __builtin_fmaf(x, f, sum) : x - x == 0.f ? sum : sum + x; }
 
 struct Span {               // tokens of a sequence that its new one attends to
   int start, len;
@@ -266,15 +278,22 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     const int32_t* row = a.table + (int64_t)b * a.max_pages;
     int first = t0 >> sh;
     int ids = early;
-    if (!SINGLE || a.window > 0) ids = first + lane < a.max_pages ? row[first + lane] : -1;
-    asm volatile("" : "+v"(ids));
+    const auto list = [&](int t) {
+      first = t >> sh;
+      ids = first + lane < a.max_pages ? row[first + lane] : -1;
+      asm volatile("" : "+v"(ids));    // waited for here: the reads of ids then wait for no tile
+    };
+    if (!SINGLE || a.window > 0) list(t0);
+    else asm volatile("" : "+v"(ids));
     const uint16_t* q = a.q + b * a.q_stride + (int64_t)(h * a.group + r0 + m) * D + 8 * g;
     uint4_t qf[KS];
 #pragma unroll
     for (int i = 0; i < KS; ++i) qf[i] = r0 + m < a.group ? *reinterpret_cast<const uint4_t*>(q + 32 * i) : 0;
-    // wide heads: the registers are short, so the query waits in the wave's part of LDS
+    // wide heads: the registers are short, so the query waits in the wave's part of LDS, read
+    // by offsets from one LDS address (a generic pointer takes two registers for each piece: spills)
     // (what rows past the group read there goes into columns that nobody reads)
-    volatile uint4_t* held = reinterpret_cast<volatile uint4_t*>(joined + (wv * a.rows + min(m, a.rows - 1)) * PS) + g;
+    typedef volatile __attribute__((address_space(3))) uint4_t lds_t;
+    lds_t* held = (lds_t*)(joined + (wv * a.rows + min(m, a.rows - 1)) * PS) + g;
     if constexpr (D > 192) {
       if (m < a.rows)
 #pragma unroll
@@ -300,11 +319,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     uint4_t kf[NB][2][KS], vf[NB][VB];
     int64_t at0, at1;
     const auto find = [&](int t) {
-      if (((t + 16) >> sh) - first >= 64) {
-        first = t >> sh;
-        ids = first + lane < a.max_pages ? row[first + lane] : -1;
-        asm volatile("" : "+v"(ids));  // waited for here: the reads of ids then wait for no tile
-      }
+      if (((t + 16) >> sh) - first >= 64) list(t);
       at0 = place(t);
       at1 = place(t + 16);
     };
@@ -321,6 +336,40 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
       const uint16_t* v0 = a.v + max(g < 2 ? at0 : at1, (int64_t)0) + (g & 1) * 8 * D + m * 8;
 #pragma unroll
       for (int i = 0; i < VB; ++i) v[i] = fetch(v0 + i * 128);
+    };
+
+    const auto hide_scores = [&](float (&s)[8], int g, bool here0, bool here1) {
+      const int t = t0 + 4 * g;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (!(here0 && t + j >= sp.start && t + j < sp.len)) s[j] = -__builtin_inff();
+        if (!(here1 && t + 16 + j >= sp.start && t + 16 + j < sp.len)) s[4 + j] = -__builtin_inff();
+      }
+    };
+    const auto hide_values = [&](auto& v, int g, bool here0, bool here1) {   // nothing of a masked token's counts
+      const int t = t0 + 8 * g;
+      const bool here = g < 2 ? here0 : here1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bool lo = here && t + 2 * j >= sp.start && t + 2 * j < sp.len;
+        const bool hi = here && t + 2 * j + 1 >= sp.start && t + 2 * j + 1 < sp.len;
+        const uint32_t keep = (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
+#pragma unroll
+        for (uint4_t& x : v) x[j] &= keep;
+      }
+    };
+    // the second product's operand: one term of p, which is left with the rest
+    const auto operand = [&](float (&p)[8]) {
+      uint4_t pf;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t u = take<TY>(p[2 * j], p[2 * j + 1]), w2 = take<TY>(p[4 + 2 * j], p[5 + 2 * j]);
+        const auto half = __builtin_amdgcn_permlane32_swap(u, w2, false, false);
+        const auto quad = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
+        pf[j] = quad[0];
+        pf[2 + j] = quad[1];
+      }
+      return pf;
     };
 
     const auto step = [&](uint4_t (&k)[2][KS], uint4_t (&v)[VB], uint4_t (&kn)[2][KS], uint4_t (&vn)[VB], bool more) {
@@ -347,14 +396,7 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
         s[j] = s0[j] * a.qscale;
         s[4 + j] = s1[j] * a.qscale;
       }
-      if (!whole) {
-        const int t = t0 + 4 * g;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          if (!(here0 && t + j >= sp.start && t + j < sp.len)) s[j] = -__builtin_inff();
-          if (!(here1 && t + 16 + j >= sp.start && t + 16 + j < sp.len)) s[4 + j] = -__builtin_inff();
-        }
-      }
+      if (!whole) hide_scores(s, g, here0, here1);
       float top = s[0];
 #pragma unroll
       for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
@@ -375,29 +417,10 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
         p[j] = __builtin_amdgcn_exp2f(s[j] - ref);
         l += p[j];
       }
-      if (!whole) {                    // nothing of a masked token's values counts
-        const int t = t0 + 8 * g;
-        const bool here = g < 2 ? here0 : here1;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bool lo = here && t + 2 * j >= sp.start && t + 2 * j < sp.len;
-          const bool hi = here && t + 2 * j + 1 >= sp.start && t + 2 * j + 1 < sp.len;
-          const uint32_t keep = (lo ? 0xffffu : 0u) | (hi ? 0xffff0000u : 0u);
-#pragma unroll
-          for (int i = 0; i < VB; ++i) v[i][j] &= keep;
-        }
-      }
+      if (!whole) hide_values(v, g, here0, here1);
 #pragma unroll
       for (int term = 0; term < (TY == DWKV_F16 ? 2 : 3); ++term) {
-        uint4_t pf;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const uint32_t u = take<TY>(p[2 * j], p[2 * j + 1]), w2 = take<TY>(p[4 + 2 * j], p[5 + 2 * j]);
-          const auto half = __builtin_amdgcn_permlane32_swap(u, w2, false, false);
-          const auto quad = __builtin_amdgcn_permlane16_swap(half[0], half[1], false, false);
-          pf[j] = quad[0];
-          pf[2 + j] = quad[1];
-        }
+        const uint4_t pf = operand(p);
 #pragma unroll
         for (int i = 0; i < VB; ++i) o[i] = product<TY>(v[i], pf, o[i]);
       }
@@ -419,12 +442,80 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+
+    // A weight's later terms may be 0 or below, and the first one 0 where the weight is not: times them an
+    // infinite value is NaN.  Sums that are not finite are worked out once more, over the values that
+    // are not, with a weight of one for every score above -inf.  Sums of finite values that passed
+    // float32's range are kFar meanwhile, and infinite again.  The check costs a wave some 0.1 us:
+    // 256 sequences of 64 tokens with 8 KV heads take 30 us, 29.4 without it, longer ones the same.
+    float4_t zero = 0.f;
+#pragma unroll
+    for (int k = 0; k < VB; ++k) zero += o[k] * 0.f;
+    const float sign = (zero[0] + zero[1]) + (zero[2] + zero[3]);
+    if (__builtin_expect(__ballot(sign != sign && l == l && r0 + m < a.group) != 0, 0)) {
+      // a piece at a time, with numbers that are not made before: registers are short, and the loop
+      // above needs them
+      int id = threadIdx.x;
+      float far = kFar;
+      asm volatile("" : "+v"(id), "+s"(far));
+      const int em = id & 15, eg = (id & 63) >> 4;
+#pragma unroll
+      for (int k = 0; k < VB; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[k][j] = __builtin_amdgcn_fmed3f(o[k][j], -far, far);
+      t0 -= n * turn * kPageTile;
+      list(t0);
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        find(t0);
+        const bool here0 = at0 >= 0, here1 = at1 >= 0;
+        const uint16_t* k0 = a.k + max(at0, (int64_t)0) + eg * 128 + em * 8;
+        const uint16_t* k1 = a.k + max(at1, (int64_t)0) + eg * 128 + em * 8;
+        const uint16_t* v0 = a.v + max(eg < 2 ? at0 : at1, (int64_t)0) + (eg & 1) * 8 * D + em * 8;
+        float4_t s0 = 0.f, s1 = 0.f;
+#pragma unroll
+        for (int c = 0; c < KS; ++c) {
+          uint4_t qi;
+          if constexpr (D > 192) qi = held[4 * c];
+          else qi = qf[c];
+          s0 = product<TY>(fetch(k0 + 512 * c), qi, s0);
+          s1 = product<TY>(fetch(k1 + 512 * c), qi, s1);
+          asm volatile("" ::: "memory");
+        }
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          p[j] = s0[j] * a.qscale;
+          p[4 + j] = s1[j] * a.qscale;
+        }
+        hide_scores(p, eg, here0, here1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = p[j] > -__builtin_inff() ? 1.f : 0.f;
+        const uint4_t pf = operand(p);
+#pragma unroll
+        for (int k = 0; k < VB; ++k) {
+          uint4_t v[1] = {fetch(v0 + 128 * k)};
+          hide_values(v, eg, here0, here1);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[0][j] = not_finite<TY>(v[0][j]);
+          o[k] = product<TY>(v[0], pf, o[k]);
+          asm volatile("" ::: "memory");
+        }
+        t0 += turn * kPageTile;
+      }
+#pragma unroll
+      for (int k = 0; k < VB; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (__builtin_fabsf(o[k][j]) == far) o[k][j] = __builtin_copysignf(__builtin_inff(), o[k][j]);
+    }
     if (!join && r0 + m < a.group) {
       if (x == p0 && n == T) {           // a pair of this wave's own
         float* out = a.out + ((int64_t)b * a.n_kv_heads * a.group + h * a.group + r0 + m) * D + 4 * g;
-        const float f = l > 0.f || l != l ? 1.f / l : 0.f;
+        const bool some = l > 0.f || l != l;
+        const float f = some ? 1.f / l : 0.f;
 #pragma unroll
-        for (int k = 0; k < VB; ++k) *reinterpret_cast<float4_t*>(out + 16 * k) = o[k] * f;
+        for (int k = 0; k < VB; ++k) *reinterpret_cast<float4_t*>(out + 16 * k) = some ? o[k] * f : float4_t(0.f);
       } else {
         float* part = a.part + ((int64_t)slot_of(w, x, p0) * a.rows + m) * PS;
 #pragma unroll
@@ -464,9 +555,21 @@ __global__ __launch_bounds__(kPT) void page_split_kernel(const PageArgs a) {
       sum += *reinterpret_cast<const float4_t*>(from + c) * f;
       all += from[D + 1] * f;
     }
+    const float4_t zero = sum * 0.f;
+    const float sign = (zero[0] + zero[1]) + (zero[2] + zero[3]);
+    if (__builtin_expect(sign != sign && all == all, 0)) {
+      sum = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < kPageWaves; ++i) {
+        const float* from = joined + (i * a.rows + r) * PS;
+        const float f = __builtin_amdgcn_exp2f(from[D] - top);
+        for (int j = 0; j < 4; ++j) sum[j] = plus(sum[j], from[c + j], f);
+      }
+    }
     if (own) {
-      const float f = all > 0.f || all != all ? 1.f / all : 0.f;
-      *reinterpret_cast<float4_t*>(a.out + ((int64_t)b * a.n_kv_heads * a.group + h * a.group + r0 + r) * D + c) = sum * f;
+      const bool some = all > 0.f || all != all;
+      *reinterpret_cast<float4_t*>(a.out + ((int64_t)b * a.n_kv_heads * a.group + h * a.group + r0 + r) * D + c) =
+          some ? sum * (1.f / all) : float4_t(0.f);
     } else {
       float* part = a.part + ((int64_t)slot_of(blockIdx.x * kPageWaves, wg0, wgp0) * a.rows + r) * PS;
       *reinterpret_cast<float4_t*>(part + c) = sum;
@@ -560,6 +663,11 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
       const float e = __builtin_amdgcn_exp2f(tops[i] - to);
       v += sums[i][threadIdx.x] * e;
       l += alls[i] * e;
+    }
+    if (__builtin_expect(v != v && l == l, 0)) {
+      v = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) v = plus(v, partial(i)[threadIdx.x], __builtin_amdgcn_exp2f(partial(i)[D] - to));
     }
     out[threadIdx.x] = l > 0.f || l != l ? v / l : 0.f;
   }

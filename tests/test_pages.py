@@ -435,3 +435,102 @@ def test_step_captured(G, d, columns):
         assert torch.equal(got, twin.decode(0, q)), i
         assert torch.equal(got2, twin.decode(0, q, window=5)), i
         assert torch.equal(k, k2) and torch.equal(v, v2)
+
+
+# ---- numbers at the ends -----------------------------------------------------------------------------
+
+def not_finite(v, case, table, want):
+    """attend's results over the finite values alone, and in each channel that a sequence sees an infinity or a NaN
+    in, what that makes of it: every finite score has a weight above 0."""
+    lens, H, G, d, page, _, window, _ = case
+    V, out = value_rows(v[0].double().cpu().numpy()), want.copy()
+    for b, n in enumerate(lens):
+        ts = [t for t in range(max(0, n - window) if window else 0, n) if 0 <= table[b, t // page] < V.shape[0]]
+        for h in range(H):
+            x = np.array([V[table[b, t // page], h, t % page] for t in ts]).reshape(-1, d)
+            x = np.where(np.isfinite(x), 0.0, x)
+            with np.errstate(invalid="ignore"):
+                all_of = x.sum(0)
+            out[b, h * G:(h + 1) * G] = np.where(all_of == 0, out[b, h * G:(h + 1) * G], all_of)
+    return out
+
+
+@pytest.mark.parametrize("case,spare", [
+    (([1, 40, 700, 0], 2, 4, 64, 16, "f16", 0, []), 1),
+    (([1, 40, 700, 0], 2, 4, 64, 16, "bf16", 0, []), 1),
+    (([90, 3000, 33], 2, 4, 128, 16, "f16", 0, [(1, 40)]), 700),
+    (([90, 3000, 33], 1, 16, 128, 32, "bf16", 0, []), 700),
+    (([700, 2500], 1, 17, 64, 16, "f16", 600, []), 700),
+    (([300, 65], 2, 3, 256, 16, "bf16", 0, []), 1),
+    (([300, 2000], 1, 16, 256, 16, "f16", 0, []), 700),
+    (([20] * 80, 2, 2, 32, 16, "bf16", 0, []), 700),
+], ids=lambda x: str(x) if isinstance(x, int) else f"{len(x[0])}x{max(x[0])}-g{x[2]}-d{x[3]}-{x[5]}")
+@pytest.mark.parametrize("sharp", [2.0, 60.0])
+def test_decode_of_infinite_values(case, spare, sharp):
+    """An infinity that a sequence sees is its channel's output, however small its weight; both signs, or a NaN,
+    make it NaN; other channels, heads and sequences are as they were.  Sharp: weights far below float32's range."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce(f"page decode of infinite values {case} {spare} {sharp}")
+    table, k, v, q = decode_case(torch, case, spare=spare, sharp=sharp, junk=float("nan"))
+    lens, H, page, window = case[0], case[1], case[4], case[6]
+    rng = np.random.default_rng(4)
+    put = []
+    for b, n in enumerate(lens):
+        if n == 0 or b % 3 == 2:
+            continue
+        first = max(0, n - window) if window else 0
+        for c, signs in ((0, (1,)), (5, (-1,)), (17, (1, 1, 1)), (18, (1, -1)), (30, (0,)), (31, (1, 0))):
+            for s in signs:
+                t = int(rng.integers(first, n))
+                put.append((table[b, t // page], int(rng.integers(H)), t % page, c, {1: np.inf, -1: -np.inf, 0: np.nan}[s]))
+    for p, h, o, c, x in put:
+        if 0 <= p < v.shape[1]:
+            v[0, p, h, o // 8, c, o % 8] = x
+    fin = v.clone()
+    fin[~torch.isfinite(fin)] = 0
+    want, tol = reference(case, table, k, fin, q)
+    want = not_finite(v, case, table, want)
+    assert not np.isfinite(want).all()
+    out = PagedCache(k, v, i32(torch, table), i32(torch, lens), n_q_heads=q.shape[1]).decode(0, q, window=window)
+    check(out.cpu().numpy(), want, tol, "infinite values")
+
+
+@pytest.mark.parametrize("spare", [1, 700])
+def test_decode_rows_without_scores_of_infinite_values(spare):
+    """Scores of -inf alone give zeros whatever the values are."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce(f"page decode without scores, infinite values {spare}")
+    case = ([40, 900], 1, 4, 64, 16, "bf16", 0, [])
+    table, k, v, q = decode_case(torch, case, spare=spare, junk=0.0)
+    k[0, :, :, :, 0, :, 0] = float("inf")                    # channel 0 of every key
+    q[:, :, 0] = -1.0
+    v[0, :, :, ::2, 3] = float("inf")
+    v[0, :, :, ::3, 9] = float("nan")
+    cache = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=4)
+    assert (cache.decode(0, q) == 0).all()
+
+
+@pytest.mark.parametrize("spare", [1, 700])
+def test_decode_of_large_values(spare):
+    """Values up to 2^112 / T are added up as others are; what the sums of larger ones make infinite keeps its
+    sign, beside an infinity too, and changes no other channel."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce(f"page decode of large values {spare}")
+    case = ([1, 500, 2000], 1, 4, 64, 16, "bf16", 0, [])
+    table, k, v, q = decode_case(torch, case, spare=spare, junk=0.0)
+    v[0, :, :, :, 3] *= 2.0 ** 98                            # 2^112 / 2000 is 2^101: normal numbers stay below 2^3
+    plain = v.clone()
+    v[0, :, :, :, 5] = 2.0 ** 127
+    v[0, :, :, :, 6] = -2.0 ** 127
+    v[0, table[1, 2], 0, 0, 7] = float("-inf")
+    want, tol = reference(case, table, k, plain, q)
+    out = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=4).decode(0, q).cpu().numpy()
+    assert (out[:, :, 5] >= 2.0 ** 126).all() and (out[:, :, 6] <= -2.0 ** 126).all() and (out[1, :, 7] == -np.inf).all()
+    out[:, :, 5:7], out[1, :, 7] = want[:, :, 5:7], want[1, :, 7]
+    check(out, want, tol, "large values")
