@@ -33,8 +33,8 @@ namespace {
 constexpr int kPT = 64 * kPageWaves;
 constexpr int kSingleTiles = 128, kSingleBits = 8;    // most tiles of a pair that one workgroup takes, and their bits
 constexpr int kRanked = 256;             // sequences that are taken longest first
-constexpr float kNoRef = -1.7e38f;       // reference of a row without scores
 constexpr float kFar = 0x1.fffffep127f;
+constexpr float kNoRef = -kFar;          // reference of a row without scores: below every other number
 constexpr float kRefTop = 9.f, kRefMove = 15.5f;
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));

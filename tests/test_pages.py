@@ -534,3 +534,29 @@ def test_decode_of_large_values(spare):
     assert (out[:, :, 5] >= 2.0 ** 126).all() and (out[:, :, 6] <= -2.0 ** 126).all() and (out[1, :, 7] == -np.inf).all()
     out[:, :, 5:7], out[1, :, 7] = want[:, :, 5:7], want[1, :, 7]
     check(out, want, tol, "large values")
+
+
+@pytest.mark.parametrize("spare", [1, 700])
+def test_decode_of_the_lowest_scores(spare):
+    """Finite scores near float32's lowest number have their softmax as others do: of the keys that score
+    highest, all alike here, the mean of the values.  Weights are exact, l and the sums add up
+    to T / 32 + 64 numbers, the values' products are exact: (T / 32 + 64) U and a division."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce(f"page decode of the lowest scores {spare}")
+    case = ([70, 3000], 1, 2, 64, 16, "bf16", 0, [])
+    table, k, v, q = decode_case(torch, case, spare=spare, junk=0.0)
+    k[0], q[:] = 0.0, 0.0
+    # times log2(e): -1.84e38, and -1.85e38 for every third token
+    k[0, :, :, :, 0, :, 0] = 2.0 ** 63
+    k[0, :, :, :, 0, ::3, 0] = 2.0 ** 63 * 1.0078125
+    q[:, 0, 0] = -1.5 * 2.0 ** 63
+    q[:, 1, 0] = 0.0                                          # and a row of even scores
+    out = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=2).decode(0, q, sm_scale=1.0).cpu().numpy()
+    V = value_rows(v[0].double().cpu().numpy())
+    for b, n in enumerate(case[0]):
+        x = np.array([V[table[b, t // 16], 0, t % 16] for t in range(n)])
+        for r, of in ((0, [t for t in range(n) if t % 16 % 3]), (1, list(range(n)))):
+            tol = (2 * (n / 32 + 64) + 2) * 2.0 ** -24 * np.abs(x[of]).mean(0)
+            check(out[b, r], x[of].mean(0), tol, f"lowest scores {b} {r}")
