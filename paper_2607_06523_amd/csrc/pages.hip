@@ -691,7 +691,7 @@ bool one_workgroup_each(int64_t tiles, int64_t pairs, int d) {
 template <int D, int TY>
 hipError_t launch_t(PageArgs a, hipStream_t s) {
   const int64_t room = (((int64_t)a.max_pages << (a.page_shift + 4)) + kPageTile - 1) / kPageTile;
-  const int64_t most = a.window > 0 ? std::min<int64_t>(room, (a.window + kPageTile - 2) / kPageTile + 1) : room;
+  const int64_t most = a.window > 0 ? std::min<int64_t>(room, ((int64_t)a.window + kPageTile - 2) / kPageTile + 1) : room;
   const bool single = one_workgroup_each(most, (int64_t)a.n_kv_heads * a.n_rb * a.batch, D);
   const size_t lds = ((size_t)kPageWaves * a.rows * (D + 4) + (single ? 0 : a.batch + 1)) * sizeof(float);
   if (lds > 64 * 1024) {

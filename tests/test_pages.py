@@ -560,3 +560,17 @@ def test_decode_of_the_lowest_scores(spare):
         for r, of in ((0, [t for t in range(n) if t % 16 % 3]), (1, list(range(n)))):
             tol = (2 * (n / 32 + 64) + 2) * 2.0 ** -24 * np.abs(x[of]).mean(0)
             check(out[b, r], x[of].mean(0), tol, f"lowest scores {b} {r}")
+
+
+def test_decode_window_without_end():
+    """The largest window is none: the same kernels, so the same bits."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce("page decode window without end")
+    for case, spare in ((([20000, 700], 1, 4, 128, 16, "bf16", 0, []), 1), (([600, 5], 2, 4, 128, 16, "f16", 0, []), 1),
+                        (([300] * 40, 8, 1, 128, 16, "f16", 0, []), 400)):
+        table, k, v, q = decode_case(torch, case, spare=spare)
+        cache = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=q.shape[1])
+        for window in (2 ** 31 - 1, 2 ** 31 - 31, 2 ** 31 - 30, 2 ** 30):
+            assert torch.equal(cache.decode(0, q, window=window), cache.decode(0, q)), (case, window)
