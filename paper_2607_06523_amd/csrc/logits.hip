@@ -327,10 +327,16 @@ __device__ __forceinline__ void put8(const LogitsArgs& a, int row, int v, float8
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
-// Neither infinite nor 0, so that 0 and -inf times it stay what they are: a temperature
-// of +inf makes what is allowed even, the smallest one leaves the largest entries.
+// Entries are weighed by exp2 of half their distance to the largest (two finite ones may lie further
+// apart than float32 reaches) times twice the inverse of the temperature.  That is neither infinite
+// nor 0, so that 0 and -inf times it stay what they are: a temperature of +inf makes what is
+// allowed even (off by 2^-21 between float32's lowest and highest numbers), the smallest one leaves the
+// largest entries.
 __device__ __forceinline__ float scale_of(const Rules& r) {
-  return r.temp > 0.f ? fminf(fmaxf(kLog2e / r.temp, 0x1p-126f), 0x1.fffffep127f) : 0.f;
+  return r.temp > 0.f ? fminf(fmaxf(2.f * kLog2e / r.temp, 0x1p-149f), 0x1.fffffep127f) : 0.f;
+}
+__device__ __forceinline__ float weight(float z, float half_ref, float scale) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(z, 0.5f, -half_ref) * scale);
 }
 // op over a wave's lanes, which all get it: within rows of 16 by rotation, then rows and halves
 // against each other.  Both sides of each step are the same two numbers: one order in every lane.
@@ -371,16 +377,16 @@ constexpr bool tells = TO == DWKV_F32;
 // first); or, where a run is a whole row, its probabilities.
 enum Makes { LOGITS, PART, WHOLE };
 
-// exp2((z - top) scale) of this thread's entries, and their sum.
+// The weights of this thread's entries, and their sum.
 template <int R>
 __device__ __forceinline__ float weights(const Mine<R>& x, float top, float scale, float8_t (&e)[R]) {
-  const float ref = top == -__builtin_inff() ? 0.f : top;
+  const float ref = top == -__builtin_inff() ? 0.f : 0.5f * top;
   float sum = 0.f;
 #pragma unroll
   for (int j = 0; j < R; ++j)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      e[j][i] = __builtin_amdgcn_exp2f((x.z[j][i] - ref) * scale);
+      e[j][i] = weight(x.z[j][i], ref, scale);
       sum += e[j][i];
     }
   return sum;
@@ -520,8 +526,8 @@ __global__ __launch_bounds__(kRunThreads) void probs_kernel(const LogitsArgs a) 
   float top = -__builtin_inff(), sum = 0.f;
   for (int i = lane; i < a.n_run; i += 64) top = fmaxf(top, part[i].top);
   top = wave_max(top);
-  const float ref = top == -__builtin_inff() ? 0.f : top;
-  for (int i = lane; i < a.n_run; i += 64) sum += part[i].sum * __builtin_amdgcn_exp2f((part[i].top - ref) * scale);
+  const float ref = top == -__builtin_inff() ? 0.f : 0.5f * top;
+  for (int i = lane; i < a.n_run; i += 64) sum += part[i].sum * weight(part[i].top, ref, scale);
   sum = wave_sum(sum);
   if (!told && counts) count<NT, R>(a, row, at, v0, w, lds);
   open<T, NT>(a, row, v0, raw, x);

@@ -204,3 +204,29 @@ def test_logits_captured():
         got = out.clone()
         torch.cuda.synchronize()
         assert torch.equal(got, adjust_logits(l, rules)), i
+
+
+@pytest.mark.parametrize("V", [900, 30000])
+def test_temperatures_over_the_whole_range(V):
+    """Rows that hold float32's lowest and highest numbers, at temperatures as large: +inf makes them even too.
+    There an exponent is at most 2^128 halved, times twice the smallest number, 2^-149: off by 2^-21, and
+    the sum as much."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import LogitsRules, adjust_logits
+    announce(f"temperatures over the whole range {V}")
+    temps = [float("inf"), 3.4e38, 3e38, 1e38, 1.2e38, 2e37, 1e30]
+    big = torch.finfo(torch.float32).max
+    l = torch.randn((len(temps), V), generator=torch.Generator().manual_seed(2)).cuda()
+    l[:, ::5] = -big
+    l[:, 3::7] = big
+    l[:, 6::11] = big / 3
+    l[:, 8] = float("-inf")
+    params = torch.tensor([[1.0, 0.0, 0.0, t] for t in temps], dtype=torch.float32, device="cuda")
+    out = adjust_logits(l, LogitsRules(params=params)).cpu().numpy()
+    host, par = l.double().cpu().numpy(), params.cpu().numpy()
+    want, tol = shape_logits(host[1:], par[1:], probs=True)
+    even = np.full((1, V), 1 / (V - 1))
+    even[0, 8] = 0
+    check(out[:1], even, 2.0 ** -20 * even, "temperature inf")
+    check(out[1:], want, tol, "large temperatures")
