@@ -894,7 +894,6 @@ class PagedCache:
         self._bytes = int(self.lib.dwkv_page_workspace_bytes(self.ref, self.n_q_heads))
         if self._bytes == 0:
             raise DwkvError(3, "dwkv_page_workspace_bytes")
-        self._ws = None
 
     @classmethod
     def empty(cls, page_table, seq_len, *, n_pages: int, page_size: int, n_kv_heads: int, n_q_heads: int, head_dim: int = 128,
@@ -963,8 +962,7 @@ class PagedCache:
         """dwkv_page_decode: attention of one new token per sequence, q [B, Hq, d] of
         the cache's type (rows may be slices of wider ones), over the tokens that
         seq_len counts (window > 0: the last of them only).  Returns out fp32
-        [B, Hq, d].  Without a workspace the cache's own is used: give one to calls
-        that may overlap."""
+        [B, Hq, d].  Without a workspace the call takes one of its own."""
         rt = _runtime_ or _runtime()
         if q.dtype != self.dtype:
             raise TypeError("q must have the cache's type")
@@ -975,16 +973,14 @@ class PagedCache:
             out = rt.empty(self.shape, dtype=rt.f32, device=self.device)
         elif out.dtype != rt.f32 or _heads(out, "out") != (B, Hq, d, 0):
             raise TypeError("out must be contiguous float32 [B, Hq, d]")
-        if workspace is None:
-            if self._ws is None:
-                self._ws = self.workspace()
-            workspace = self._ws
         index = self.index
         if not _all_on(index, q, out, workspace):
             raise ValueError("every tensor must be on the cache's device")
         if rt.device() != index:
             with _on(rt.torch, index):
                 return self.decode(layer, q, sm_scale, window, out, workspace)
+        if workspace is None:
+            workspace = self.workspace()
         st = self.lib.dwkv_page_decode(self.ref, int(layer), q.data_ptr(), qs, Hq, sm_scale or 0.0, int(window), out.data_ptr(),
                                        workspace.data_ptr(), _nbytes(workspace), rt.stream(index))
         if st:

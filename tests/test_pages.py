@@ -574,3 +574,50 @@ def test_decode_window_without_end():
         cache = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=q.shape[1])
         for window in (2 ** 31 - 1, 2 ** 31 - 31, 2 ** 31 - 30, 2 ** 30):
             assert torch.equal(cache.decode(0, q, window=window), cache.decode(0, q)), (case, window)
+
+
+def test_decode_on_two_streams_without_workspaces():
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce("page decode on two streams without workspaces")
+    case = ([3000, 50, 700], 2, 4, 128, 16, "bf16", 0, [])
+    table, k, v, q = decode_case(torch, case)
+    cache = PagedCache(k, v, i32(torch, table), i32(torch, case[0]), n_q_heads=8)
+    args = [(q, 0), ((q * 0.5).to(q.dtype), 40)]                # another window: another plan
+    wants = [cache.decode(0, x, window=w) for x, w in args]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(6):
+        for i in (0, 1):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(cache.decode(0, args[i][0], window=args[i][1]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(o, wants[i]) for o in outs[i])
+
+
+def test_decode_captured_without_a_workspace():
+    """Two graphs with workspaces of their own, replayed with eager calls between them."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import PagedCache
+    announce("page decode captured without a workspace")
+    case = ([3000, 50, 700], 2, 4, 128, 16, "f16", 0, [])
+    table, k, v, q = decode_case(torch, case)
+    lens = i32(torch, case[0])
+    cache = PagedCache(k, v, i32(torch, table), lens, n_q_heads=8)
+    outs, graphs = [torch.empty(cache.shape, device="cuda") for _ in range(2)], []
+    for o, window in zip(outs, (0, 100)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            cache.decode(0, q, window=window, out=o)
+    for i in range(4):
+        lens -= 1
+        for g in graphs:
+            g.replay()
+        got = [o.clone() for o in outs]
+        torch.cuda.synchronize()
+        for o, window in zip(got, (0, 100)):
+            assert torch.equal(o, cache.decode(0, q, window=window)), i

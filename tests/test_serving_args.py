@@ -192,6 +192,35 @@ def test_paged_cache_in_python_refused(lib):
         PagedCache.empty(table, lens, n_pages=4, page_size=24, n_kv_heads=2, n_q_heads=4)
 
 
+def test_decodes_that_overlap_share_no_workspace(lib, monkeypatch):
+    """A call without a workspace, made while another one's two launches are under way (here between its
+    arguments and its return), works in memory of its own."""
+    import paper_2607_06523_amd as fw
+    monkeypatch.setattr(fw, "_all_on", lambda index, *tensors: True)
+    z = lambda *s: torch.zeros(s, dtype=torch.float16)
+    cache = fw.PagedCache(z(1, 4, 2, 1, 8, 16, 8), z(1, 4, 2, 2, 64, 8), torch.zeros((2, 3), dtype=torch.int32),
+                          torch.zeros(2, dtype=torch.int32), n_q_heads=4)
+    q, seen = z(2, 4, 64), []
+
+    class Lib:                                              # records the calls and enqueues nothing
+        @staticmethod
+        def dwkv_page_decode(*args):
+            seen.append((args[8], args[9]))
+            if len(seen) < 3:
+                cache.decode(0, q)
+            return 0
+    cache.lib = Lib
+    rt = fw._runtime()
+    monkeypatch.setattr(rt, "device", lambda: cache.index)
+    monkeypatch.setattr(rt, "stream", lambda index: 0)
+    cache.decode(0, q)
+    seen.sort()
+    assert len(seen) == 3 and all(a + n <= b for (a, n), (b, _) in zip(seen, seen[1:])), seen
+    given = cache.workspace()
+    cache.decode(0, q, workspace=given)
+    assert seen[-1] == (given.data_ptr(), given.nbytes)
+
+
 # ---- logits ----------------------------------------------------------------------------------------
 
 def logits_status(lib, batch=2, tree=None, token=None, vocab=100, l=FAKE, lt=2, ls=0, rules="yes", probs=1, out=2 * FAKE, ot=2, ws=FAKE,
