@@ -19,7 +19,8 @@ Several drafted tokens per sequence:
     new = cache.empty_like(seqlens, res_stride)   # then the tokens that stay, with room for the kept ones
     new.repack_from(cache, src_token, src_seq, new_code=codes)
 
-Between a model's projections and those calls, and the dense cache in pages:
+Between a model's projections and those calls, and the dense cache in pages
+(``rope`` has a gradient; what the other calls return carries none):
 
     table = RopeTable(rope_freqs(128, base=5e5), interleaved=False)   # .to the GPU by itself
     qk = rope(rows[:, :Hq + Hkv], pos, table)     # [N, heads, d], or in place with out=
@@ -765,6 +766,36 @@ class _Runtime:
         self.device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
             lambda index: torch.cuda.current_stream(index).cuda_stream)
+        self.grads = torch.is_grad_enabled
+        self.rope = _rope_function(torch)
+
+
+def _rope_function(torch):
+    class Rope(torch.autograd.Function):
+        """rope for tensors that require grad: gradients are turned back.  What is written
+        comes first: autograd takes the first input of a call that changes a view for it."""
+
+        @staticmethod
+        def forward(ctx, first, x, pos, table, inverse):
+            in_place = x is None
+            if first is not None:
+                ctx.mark_dirty(first)
+            ctx.save_for_backward(pos, table.freq)
+            ctx.table, ctx.inverse, ctx.in_place, ctx.type = table, inverse, in_place, (first if in_place else x).dtype
+            return rope(first if in_place else x, pos, table, inverse, first)
+
+        @staticmethod
+        def backward(ctx, g):
+            pos, _ = ctx.saved_tensors                      # unchanged since, or this raises
+            if not g.is_contiguous() or g.data_ptr() % 16:
+                g = g.clone(memory_format=torch.contiguous_format)
+            out = None if g.dtype == ctx.type else torch.empty(g.shape, dtype=ctx.type, device=g.device)
+            x = rope(g, pos, ctx.table, not ctx.inverse, out)
+            if ctx.in_place:
+                return x, None, None, None, None
+            # what was in out counts for nothing: zeros, as None would take the gradient of all around it too
+            return torch.zeros_like(g) if ctx.needs_input_grad[0] else None, x, None, None, None
+    return Rope
 
 
 _runtime_ = None
@@ -829,9 +860,14 @@ class RopeTable:
 def rope(x, pos, table: RopeTable, inverse: bool = False, out=None):
     """dwkv_rope: the heads of x [N, H, d] (float16, bfloat16 or float32; rows may be
     slices of wider ones) turned at pos int32 [N].  inverse turns back: with the
-    same table that is the gradient with respect to x.  out: like x, of any of those
-    types (x itself: in place); returns it."""
+    same table that is the gradient with respect to x, and the one that flows through
+    autograd where x requires grad.  out: like x, of any of those types (x itself: in
+    place); returns it."""
     rt = _runtime_ or _runtime()
+    if (x.requires_grad or out is not None and out.requires_grad) and rt.grads():
+        if out is not None and out.requires_grad and (out.is_leaf or out._is_view() and out._base.is_leaf):
+            raise ValueError("out is, or lies in, a leaf that requires grad")
+        return rt.rope.apply(x, None, pos, table, inverse) if out is x else rt.rope.apply(out, x, pos, table, inverse)
     kinds, kind = rt.kinds, x.dtype
     if kind not in kinds:
         raise TypeError("x must be float16, bfloat16 or float32")

@@ -161,3 +161,61 @@ def test_rope_without_rows():
     announce("rope without rows")
     z = torch.zeros((0, 4, 64), device="cuda")
     assert rope(z, torch.zeros(0, dtype=torch.int32, device="cuda"), RopeTable(rope_freqs(64))).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("kind,to,rot,inter", [("f32", "f32", 64, False), ("bf16", "bf16", 64, True), ("f16", "f32", 22, False), ("f32", "bf16", 64, False)])
+def test_rope_gradient_through_autograd(kind, to, rot, inter):
+    """The gradient that autograd takes is the formula's: against 64 bits, and bit for bit what inverse gives."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import RopeTable, rope, rope_freqs
+    announce(f"rope through autograd {kind} {to} {rot} {inter}")
+    N, H, d = 50, 6, 64
+    pos, freq = positions(torch, N), rope_freqs(rot, base=500000.0)
+    at, table = torch.from_numpy(pos).cuda(), RopeTable(freq, interleaved=inter, scale=1.25)
+    x, w = rows_of(torch, N, H, d, kind, 0).requires_grad_(), rows_of(torch, N, H, d, to, 0, seed=9)
+    y = rope(x, at, table, out=torch.empty((N, H, d), dtype=torch_type(to), device="cuda"))
+    with torch.no_grad():
+        assert torch.equal(y, rope(x, at, table, out=torch.empty_like(y)))
+        back = rope(w, at, table, inverse=True, out=torch.empty_like(x))
+    y.backward(w)
+    assert x.grad.dtype == x.dtype and torch.equal(x.grad, back)
+    want, tol = rotate(w.double().cpu().numpy(), pos, freq.numpy(), inter, 1.25, True)
+    check(x.grad.double().cpu().numpy(), want, tol + rounding(np.abs(want) + tol, kind), "gradient")
+    # a fused projection's slice in place
+    base = rows_of(torch, N, H + 4, d, kind, 0, seed=3).requires_grad_()
+    rows = base * 1.0
+    rope(rows[:, 2:8], at, table, out=rows[:, 2:8])
+    g = rows_of(torch, N, H + 4, d, kind, 0, seed=4)
+    rows.backward(g)
+    want = g.clone()
+    rope(want[:, 2:8], at, table, inverse=True, out=want[:, 2:8])
+    assert torch.equal(base.grad, want)
+
+
+def test_rope_gradient_captured():
+    """Forward and backward in one graph, replayed against eager passes."""
+    torch = torch_gpu()
+    lib_ready()
+    from paper_2607_06523_amd import RopeTable, rope, rope_freqs
+    announce("rope gradient captured")
+    x = rows_of(torch, 40, 4, 128, "bf16", 0).requires_grad_()
+    w = rows_of(torch, 40, 4, 128, "bf16", 0, seed=5)
+    pos, table = torch.arange(40, dtype=torch.int32, device="cuda"), RopeTable(rope_freqs(128))
+    both = lambda: torch.autograd.grad(rope(x, pos, table), x, w)[0]
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both()
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = both()
+    for k in range(4):
+        pos += 1000 * k
+        w.mul_(0.5)
+        g.replay()
+        mine = got.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(mine, rope(w, pos, table, inverse=True)), k
+        assert torch.equal(mine, both()), k

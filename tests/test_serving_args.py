@@ -112,6 +112,96 @@ def test_rope_in_python_refused(lib):
         rope(x[:1].expand(4, 2, 64), pos, Table())
 
 
+@pytest.fixture
+def doubling(monkeypatch):
+    """The call as a host function that doubles its rows, and halves them where it turns back, so that it and autograd
+    around it run without a GPU: (a table for it, the calls' `inverse`)."""
+    import paper_2607_06523_amd as fw
+    monkeypatch.setattr(fw, "_all_on", lambda index, *tensors: True)
+    rt, calls = fw._runtime(), []
+    monkeypatch.setattr(rt, "device", lambda: -1)
+    monkeypatch.setattr(rt, "stream", lambda index: 0)
+
+    class Lib:
+        @staticmethod
+        def dwkv_rope(N, H, d, table, inverse, x, x_type, xs, pos, out, out_type, os, stream):
+            calls.append(inverse)
+            rows = lambda p, r, s, t: np.ctypeslib.as_array(C.cast(p + r * (s or H * d) * (4 if t == 2 else 2), C.POINTER(
+                C.c_float if t == 2 else C.c_uint16)), (H * d,)).view(np.float32 if t == 2 else np.float16)
+            for r in range(N):
+                rows(out, r, os, out_type)[:] = rows(x, r, xs, x_type) * (0.5 if inverse else 2.0)
+            return 0
+
+    class Table:
+        index, ref, lib, freq = -1, None, Lib, torch.ones(4, dtype=torch.float64)
+    return Table(), calls
+
+
+def test_rope_gradient_flows(doubling):
+    from paper_2607_06523_amd import rope
+    table, calls = doubling
+    pos = torch.arange(4, dtype=torch.int32)
+    leaf = torch.randn(4, 3, 8, requires_grad=True)
+    y = rope(leaf, pos, table)
+    assert torch.equal(y, 2 * leaf)
+    y.sum().backward()                                       # a gradient without strides of its own
+    assert calls == [0, 1] and torch.equal(leaf.grad, torch.full_like(leaf, 0.5))
+    # the inverse's gradient, and a gradient's gradient
+    g, = torch.autograd.grad(rope(leaf, pos, table, inverse=True).pow(2).sum(), leaf, create_graph=True)
+    assert torch.equal(g, leaf.detach() * 2)                 # d (x / 2)^2: 2 (x / 2), turned by 2
+    h, = torch.autograd.grad(g.sum(), leaf)                  # ones through the doubling that made g, the square, the halving
+    assert torch.equal(h, torch.full_like(leaf, 0.5 * 2 * 2))
+    # another type out, and back into the input's
+    half = torch.empty(4, 3, 8, dtype=torch.float16)
+    y = rope(leaf, pos, table, out=half)
+    assert y is half and y.requires_grad and torch.equal(y, (2 * leaf).half())
+    g, = torch.autograd.grad(y.float().sum(), leaf)
+    assert g.dtype == torch.float32 and torch.equal(g, torch.full_like(leaf, 0.5))
+    # nothing to do with gradients
+    with torch.no_grad():
+        assert not rope(leaf, pos, table).requires_grad
+    assert not rope(leaf.detach(), pos, table).requires_grad
+
+
+def test_rope_gradient_in_place(doubling):
+    """Slices of a fused projection turned in place, through one name for them and through two."""
+    from paper_2607_06523_amd import rope
+    table, _ = doubling
+    pos = torch.arange(4, dtype=torch.int32)
+    for two in (False, True):
+        w = torch.randn(4, 6, 8, requires_grad=True)
+        rows = w * 1.0
+        qk = rows[:, 1:4]
+        assert rope(qk, pos, table, out=rows[:, 1:4] if two else qk) is not None
+        want = torch.ones(4, 6, 8)
+        want[:, 1:4] = 2.0
+        assert torch.equal(rows, w * want)
+        weights = torch.randn(4, 6, 8)
+        g, = torch.autograd.grad((rows * weights).sum(), w)
+        back = torch.ones(4, 6, 8)
+        back[:, 1:4] = 0.5
+        assert torch.equal(g, weights * back)
+    # the result into a slice of something else that has a gradient
+    a, w = torch.randn(4, 6, 8, requires_grad=True), torch.randn(4, 2, 8, requires_grad=True)
+    rows = a * 1.0
+    rope(w, pos, table, out=rows[:, 2:4])
+    weights = torch.randn(4, 6, 8)
+    ga, gw = torch.autograd.grad((rows * weights).sum(), (a, w))
+    assert torch.equal(gw, 0.5 * weights[:, 2:4])
+    weights[:, 2:4] = 0
+    assert torch.equal(ga, weights)
+    before = a.detach().clone()
+    for out in (a, a[:, :3]):                                # leaves stay as they are
+        with pytest.raises(ValueError):
+            rope(out, pos, table, out=out)
+    assert torch.equal(a, before)
+    # positions that change before the gradient is taken
+    y = rope(w, pos, table)
+    pos += 1
+    with pytest.raises(RuntimeError):
+        y.sum().backward()
+
+
 # ---- pages -----------------------------------------------------------------------------------------
 
 def pages(**kw):
