@@ -481,7 +481,7 @@ struct PageArgs {
   const int32_t *table, *len;
   const uint16_t* q;
   float* out;
-  float* part;                 // [2 * waves][rows][d + 2]
+  float* part;                 // [2 * waves][rows][d + 4]: d sums, their reference, the sum of weights, two unused
   int32_t* plan;               // [B+1] tiles before each sequence
   int64_t q_stride;
   int32_t batch, n_kv_heads, group, n_rb;    // n_rb: blocks of 16 heads of a group

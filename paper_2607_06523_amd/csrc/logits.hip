@@ -19,7 +19,6 @@
 // together; the second the same and a write of 34 MB.
 #include <algorithm>
 
-#include "entry.h"
 #include "internal.h"
 #include "rows_dev.h"
 
@@ -615,8 +614,10 @@ hipError_t launch_logits(LogitsArgs a, int from, int to, bool probs, hipStream_t
   a.n_run = (a.vocab + a.run - 1) / a.run;
   // A byte an entry written and read, or the lists counted again: 1 row of 131072, 16 of
   // 131072 and 48 of 131072 (runs of 4096 and 8192) 8.1, 11.4 and 22.2 us told, 9.5, 12.9 and
-  // 22.9 not; 64 of 131072 behind 8000 tokens, in the longest runs, 27.3 and 25.2, behind
-  // 16000 the same.
+  // 22.9 not.  In the longest runs 64 of 131072 behind 8000 tokens 28.6 and 27.1, behind 16000, 32000 and
+  // 64000 32.7, 37.4 and 44.3 told, 35.5, 44.9 and 59.4 not.  The host knows the lists' room, not
+  // their lengths: 500 tokens where there is room for 32768 take 25.0 told and 24.8 not, 256 such
+  // rows 80 and 78.
   a.tell = probs && !a.whole && lists && to == DWKV_F32 && (a.run < 4 * kStep || a.history_stride > a.run);
   const size_t lds = lists ? (size_t)4 * (a.run + kNowhere) : 0;
   switch (from) {

@@ -674,14 +674,19 @@ __global__ __launch_bounds__(256) void page_merge_kernel(const PageArgs a) {
 }
 
 // Whether every pair gets one workgroup: by the longest span that the table or the
-// window allows (lengths are the device's).  A launch and the merge are saved, about 3 us;
+// window allows (lengths are the device's: a table with room for more than 4096 tokens takes
+// the list whatever the lengths are).  A launch and the merge are saved, about 3 us;
 // but one compute unit reads no more than 60 GB/s, so long spans of few pairs are better
 // shared out.  With heads of 128, nothing in the caches: 2 pairs of 256, 512 and 1000 tokens
 // take 4.7, 7.4 and 11.6 us against 7.2, 7.5 and 7.8; 128 pairs 6.7, 9.7 and 16.6 against
 // 10.3, 12.9 and 18.4; 256 of 1000 and 2000 tokens 26 and 49 against 29 and 56.  Then by
 // how full the last round of workgroups is: 272 of 512 and 1000 tokens 20 and 34 against
-// 22 and 33, 512 of 1000 48 against 53.  From two full rounds on it wins or ties up to 4096
-// tokens: 512 pairs 187 against 194, with lengths spread evenly 102 against 107.
+// 22 and 33, 512 of 1000 48 against 53.  From two full rounds on, up to 4096 tokens: 512 pairs 187
+// against 194, with lengths spread evenly 102 against 107.  With short spans the list wins
+// where pairs are many: of 1, 64, 256 and 512 tokens 512 pairs take 8.6, 9.1, 16.3 and 25.4
+// against 9.5, 13.5, 22.3 and 31.9, 1024 pairs 15.4, 16.0, 30.1 and 50.3 against 13.8, 21.7, 36.4
+// and 58.5, 2048 pairs 29.1, 29.0, 55.1 and 92.2 against 20.6, 26.0, 56.9 and 96.2; with heads of
+// 256 2048 pairs 42, 49, 108 and 182 against 26, 39, 103 and 179.
 bool one_workgroup_each(int64_t tiles, int64_t pairs, int d) {
   if (tiles > kSingleTiles) return false;
   const int64_t rounds = (pairs + kPageWG - 1) / kPageWG;

@@ -9,7 +9,7 @@
 // float32 outputs, float32 for outputs of 16 bits (off by 2^-23 where those have 2^-11).
 // Then its threads stream pieces of 16 bytes.  Bound by HBM: what a call of many rows
 // writes goes past the caches (16384 rows of 40 heads of 128 turned in 60 us, 5.6 TB/s,
-// against 64 with plain stores; appended with 8 heads of values 81 against 83, 8100 rows of
+// against 64 with plain stores; a copy of them past the caches takes 59; appended with 8 heads of values 81 against 83, 8100 rows of
 // seven prompts 43 against 45).
 #include <algorithm>
 

@@ -23,12 +23,7 @@ template <int T>
 __device__ __forceinline__ float8_t load8(const row_t<T>* p) {
   return __builtin_convertvector(*reinterpret_cast<const row8_t<T>*>(p), float8_t);
 }
-// Rounded to nearest even.
-template <int T>
-__device__ __forceinline__ void store8(row_t<T>* p, float8_t x) {
-  *reinterpret_cast<row8_t<T>*>(p) = __builtin_convertvector(x, row8_t<T>);
-}
-// The same, PAST: past the caches.
+// Rounded to nearest even; PAST: past the caches.
 template <int T, bool PAST>
 __device__ __forceinline__ void store8(row_t<T>* p, float8_t x) {
   const row8_t<T> v = __builtin_convertvector(x, row8_t<T>);
