@@ -1017,7 +1017,8 @@ class PagedCache:
                 return self.decode(layer, q, sm_scale, window, out, workspace)
         if workspace is None:
             workspace = self.workspace()
-        st = self.lib.dwkv_page_decode(self.ref, int(layer), q.data_ptr(), qs, Hq, sm_scale or 0.0, int(window), out.data_ptr(),
+        window = min(max(int(window), -1), 0x7fffffff)       # of 32 bits in the call
+        st = self.lib.dwkv_page_decode(self.ref, int(layer), q.data_ptr(), qs, Hq, sm_scale or 0.0, window, out.data_ptr(),
                                        workspace.data_ptr(), _nbytes(workspace), rt.stream(index))
         if st:
             raise DwkvError(st, "dwkv_page_decode")

@@ -311,6 +311,30 @@ def test_decodes_that_overlap_share_no_workspace(lib, monkeypatch):
     assert seen[-1] == (given.data_ptr(), given.nbytes)
 
 
+def test_windows_past_32_bits_are_none(lib, monkeypatch):
+    """They are not cut off to their low bits."""
+    import paper_2607_06523_amd as fw
+    monkeypatch.setattr(fw, "_all_on", lambda index, *tensors: True)
+    z = lambda *s: torch.zeros(s, dtype=torch.float16)
+    cache = fw.PagedCache(z(1, 4, 2, 1, 8, 16, 8), z(1, 4, 2, 2, 64, 8), torch.zeros((2, 3), dtype=torch.int32),
+                          torch.zeros(2, dtype=torch.int32), n_q_heads=4)
+    seen = []
+
+    class Lib:
+        @staticmethod
+        def dwkv_page_decode(*args):
+            seen.append(C.c_int32(args[6]).value)           # as the call gets it
+            return 0
+    cache.lib = Lib
+    monkeypatch.setattr(fw._runtime(), "device", lambda: cache.index)
+    monkeypatch.setattr(fw._runtime(), "stream", lambda index: 0)
+    for window in (0, 7, 2 ** 31 - 1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 63 - 1):
+        cache.decode(0, z(2, 4, 64), window=window)
+    assert seen == [0, 7] + [2 ** 31 - 1] * 5
+    cache.decode(0, z(2, 4, 64), window=-2 ** 32 + 9)        # and stay below 0, which the call refuses
+    assert seen[-1] < 0
+
+
 # ---- logits ----------------------------------------------------------------------------------------
 
 def logits_status(lib, batch=2, tree=None, token=None, vocab=100, l=FAKE, lt=2, ls=0, rules="yes", probs=1, out=2 * FAKE, ot=2, ws=FAKE,
