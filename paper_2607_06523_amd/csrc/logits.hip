@@ -15,7 +15,7 @@
 // logits twice (2 to 4 bytes, from the last-level cache) is less than writing z and reading
 // it.  It counts again too, or is told the counts, a byte an entry.
 // 64 rows of 131072 float32 entries behind 16000 tokens take 14 and 17 us: the first by
-// its arithmetic (30 instructions an entry, 6 us) after its loads, as all workgroups start
+// its arithmetic (28 instructions an entry, 6 us) after its loads, as all workgroups start
 // together; the second the same and a write of 34 MB.
 #include <algorithm>
 

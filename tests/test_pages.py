@@ -464,6 +464,10 @@ def not_finite(v, case, table, want):
     (([300, 65], 2, 3, 256, 16, "bf16", 0, []), 1),
     (([300, 2000], 1, 16, 256, 16, "f16", 0, []), 700),
     (([20] * 80, 2, 2, 32, 16, "bf16", 0, []), 700),
+    (([200, 64, 70], 2, 4, 128, 16, "bf16", 90, [(0, 8)]), 1),
+    (([130] * 40, 8, 1, 192, 64, "f16", 0, []), 0),
+    (([4000, 90], 2, 5, 224, 16, "f16", 0, []), 700),
+    (([1500], 1, 33, 160, 256, "bf16", 1200, []), 30),
 ], ids=lambda x: str(x) if isinstance(x, int) else f"{len(x[0])}x{max(x[0])}-g{x[2]}-d{x[3]}-{x[5]}")
 @pytest.mark.parametrize("sharp", [2.0, 60.0])
 def test_decode_of_infinite_values(case, spare, sharp):
